@@ -276,6 +276,94 @@ int sta_window_tokens_to_tiles(const int window_tokens[3], const int tile[3],
 double sta_kept_flops(int B, int H, int D, const int grid[3], const int tile[3],
                       const int *window_tiles);
 
+/*
+ * Rows of heads around the attention.  One row is the D channels of one head of one token, adjacent in memory; row
+ * (batch b, token n, head h) starts at data + b * batch + n * token + h * head, the strides counted in elements.  So one
+ * description covers the heads inside the output of a fused projection ([B, N, Hq + 2 Hkv, D]) and the [B, H, N, D] tensors of the
+ * attention.  dtype: sta_dtype.  Strides of tensors that are read may be 0 (broadcast); rows that are written must not overlap.
+ */
+typedef struct {
+    void *data;                 /* device */
+    int64_t batch, token, head;
+    int heads;
+    int dtype;
+} sta_head_rows;
+
+/*
+ * Rotary positions.  The first `channels` channels of a row form channels / 2 pairs: neighbours (2i, 2i + 1) where interleaved is
+ * not 0, else (i, i + channels / 2).  Pair i belongs to one of three axes: the first pairs[0] to axis 0, the next pairs[1] to axis 1,
+ * the last pairs[2] to axis 2 (text: pairs = {channels / 2, 0, 0}; video: time, height, width).  A token at position x of the
+ * pair's axis has the pair (a, b) turned into
+ *     magnitude * (a cos t - b sin t, a sin t + b cos t),   t = 2 pi frac(x * steps[i] / 2^64).
+ * Steps in units of 2^-64 turns make the reduction to one turn the overflow of an integer product: exact at every position, where
+ * x * frequency in 32-bit floating point is off by whole radians beyond a million.  sta_rope_steps computes them.
+ * positions: device int32; token n of batch b has its positions at positions[b * position_batch + n * position_token + axis]
+ * (position_batch 0: the same for every batch entry).  NULL: with a grid, the token's (t, h, w) in it; without, n on axis 0.
+ */
+typedef struct {
+    const int64_t *steps;       /* device, channels / 2 entries */
+    const int32_t *positions;
+    int64_t position_batch, position_token;
+    int channels;
+    int pairs[3];
+    int interleaved;
+    float magnitude;            /* 0 stands for 1 */
+} sta_rotary;
+
+/*
+ * How frequencies follow from theta for `channels` channels of one axis: pair i turns by f = theta^(-2i / channels) radians per
+ * position, and with a factor s >= 1 by which the context has grown
+ *   STA_ROPE_NONE    f, s is not looked at
+ *   STA_ROPE_LINEAR  f / s
+ *   STA_ROPE_NTK     theta * s^(channels / (channels - 2)) in place of theta
+ *   STA_ROPE_YARN    f (1 - k) / s + f k, k = clamp((L f / 2 pi - 1) / (32 - 1), 0, 1) with L = original_positions, and
+ *                    magnitude 0.1 ln s + 1 (arXiv 2309.00071)
+ * Host only.  steps: host int64 [channels / 2]; magnitude: host, may be NULL.
+ */
+typedef enum { STA_ROPE_NONE = 0, STA_ROPE_LINEAR = 1, STA_ROPE_NTK = 2, STA_ROPE_YARN = 3 } sta_rope_scaling;
+int sta_rope_steps(int channels, double theta, int scaling, double factor, double original_positions, int64_t *steps,
+                   float *magnitude);
+
+/*
+ * Rotation of rows: n_tensors (1 to 3) tensors of B x N tokens, out[i] <- rotation of in[i], all in one launch.  inverse not 0 turns the other way
+ * (times the same magnitude), which is the gradient.  Channels beyond rotary->channels are copied.  out[i] may be in[i] itself;
+ * other overlaps of outputs with inputs or each other are STA_ERR_ALIAS.  Arithmetic in fp32, rounded once.
+ * D: even, 2 .. 256.  Rows that start at multiples of 16 bytes, D a multiple of 16 and rotary->channels a multiple of 16 (of 8
+ * where interleaved) take the fast kernel; others one that reads single elements.  B or N of 0: nothing to do.
+ */
+int sta_rope(const sta_head_rows *in, const sta_head_rows *out, int n_tensors, int B, int N, int D, const sta_rotary *rotary,
+             int inverse, void *hip_stream);
+
+/*
+ * What stands between the projections of a layer and its attention, in one pass: every query and key row divided by its root mean
+ * square and multiplied by a weight, then rotated; value rows are moved along.  y = rotation(w o x / sqrt(mean(x^2) + eps)).
+ * q, k and their outputs: B x N tokens, any numbers of heads; v and v_out both NULL: no values.  q_weight, k_weight: device [D], type
+ * weight_dt, NULL for ones.  rotary NULL: no rotation.
+ * tile NULL: token n goes to place n of the outputs.  Otherwise the tokens are those of grid (N = its product) in raster order and
+ * go to tiled order, so that [B, H, N, D] outputs are what sta_forward reads.
+ * Arithmetic in fp32, rounded once.  D, alignment and overlaps as sta_rope; with a tile no output may overlap an input.
+ */
+int sta_qk_norm_rope(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *q_out,
+                     const sta_head_rows *k_out, const sta_head_rows *v_out, const void *q_weight, const void *k_weight,
+                     int weight_dt, float eps, const sta_rotary *rotary, int B, int N, int D, const int grid[3],
+                     const int tile[3], void *hip_stream);
+
+/*
+ * Its gradients.  q, k: the rows that went in; d_*_out: gradients with respect to the outputs, laid out (and ordered) like them; d_q, d_k, d_v:
+ * written, laid out like the inputs.  d_q_weight, d_k_weight: device float32 [D], written, or NULL.  With g the
+ * gradient turned back and r = 1 / sqrt(mean(x^2) + eps): d_weight = sum over rows of g x r, d_x = r (g w - x r^2 mean(g w x)).
+ * d_v_out and d_v both NULL: no values.  Sums in fp32 in a fixed order, no atomics: repeated calls give identical bits.
+ * workspace: device, 16-byte aligned, at least sta_qk_norm_rope_workspace_bytes(D) bytes, else STA_ERR_WORKSPACE; not needed where both
+ * weight gradients are NULL.
+ */
+size_t sta_qk_norm_rope_workspace_bytes(int D);
+int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *d_q_out,
+                              const sta_head_rows *d_k_out, const sta_head_rows *d_v_out, const sta_head_rows *d_q,
+                              const sta_head_rows *d_k, const sta_head_rows *d_v, const void *q_weight, const void *k_weight,
+                              int weight_dt, float *d_q_weight, float *d_k_weight, float eps, const sta_rotary *rotary, int B,
+                              int N, int D, const int grid[3], const int tile[3], void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
 const char *sta_strerror(int status);
 int sta_version(void);
 

@@ -26,6 +26,8 @@ EXPORTED_SYMBOLS = (
     "sta_dump_key_tiles", "sta_window_tokens_to_tiles", "sta_kept_flops", "sta_strerror", "sta_version",
     "sta_head_mse_workspace_bytes", "sta_head_mse", "sta_mask_search", "sta_attention_recall", "sta_block_census", "sta_forward_general",
     "sta_backward_workspace_bytes", "sta_backward", "sta_query_tile_box", "sta_head_mse_static",
+    # bound in layer_ops
+    "sta_rope_steps", "sta_rope", "sta_qk_norm_rope", "sta_qk_norm_rope_workspace_bytes", "sta_qk_norm_rope_backward",
 )
 
 

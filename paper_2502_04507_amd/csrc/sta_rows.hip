@@ -1,0 +1,859 @@
+// Rows of heads between a layer's projections and its attention: RMS norm and rotary positions of query and key rows and the move of
+// queries, keys and values into the attention's order, in one pass; its gradients; the rotation alone.
+//
+// A row is the D channels of one head of one token.  Mathematics, per row x with weight w, root mean square factor
+// r = 1 / sqrt(mean(x^2) + eps) and a rotation R (orthogonal times a magnitude m) that the token's position gives:
+//   forward   y = R (w o x r)
+//   backward  g = R^T dy;  dw += g o x r;  dx = r (g o w - x r mean(g o w o x r))
+// All of it is a few dozen fp32 operations per 16 bytes, so HBM bounds it: every row is read once and written once, and what a
+// token needs beyond its rows (position, cosines and sines) is computed once for all of its heads.
+//
+// Fast path: L lanes share a row and a lane holds two chunks of 8 channels, chosen so that both members of a pair are in one lane (half
+// layout: channels 8c.. and rot/2 + 8c..): no exchange between lanes but for the two sums over a row.  A wave holds 64 / L
+// tokens side by side and walks over heads; the four waves of a workgroup take its tokens' heads in turn.  Tokens go in the order of
+// the outputs' places, so that a wave writes whole runs of a head (2 KB at D = 128), and the workgroup reads its tokens' heads from
+// end to end.
+// General path: a wave per row, two pairs a lane, single elements from any address.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/sta.h"
+#include "sta_internal.h"
+
+namespace {
+
+using sta::fast_div;
+using sta::fast_div_of;
+using sta::FastDiv;
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kHalf = 0, kInterleaved = 1, kGeneral = 2;      // paths
+
+// Rows of one tensor as a kernel walks them; strides in bytes.
+struct Rows {
+    char *data;
+    int64_t batch, token, head;
+};
+struct Tensor {
+    Rows x, dy, out;            // input rows; gradients of the outputs (backward); what is written
+    const void *weight;         // [D] or null: ones
+    uint32_t heads;
+    uint32_t norm, rotate;
+};
+struct Params {
+    Tensor t[3];
+    uint32_t n_tensors;
+    uint32_t tokens;            // B * N
+    uint32_t D, rot;            // channels, rotated channels
+    uint32_t weight_f32;
+    uint32_t interleaved;       // of the general path
+    float inv_D, eps;
+    // rotation
+    const int64_t *steps;
+    const int32_t *positions;
+    int64_t position_batch, position_token;
+    uint32_t axis1, axis2;      // first pairs of axes 1 and 2
+    float magnitude, sign;      // sign: -1 turns back
+    uint32_t turns;             // there is a rotation
+    // places
+    FastDiv by_N, by_P, by_nw, by_nh, by_Tw, by_Th, by_gw, by_gh;
+    uint32_t N, tiled, has_grid, T_t, T_h, T_w, g_h, g_w;
+    // backward
+    float *partial;             // [workgroups][2][D] sums of the weight gradients, or null
+};
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    bf16x2 v;
+    v[0] = static_cast<__bf16>(a);   // round to nearest even
+    v[1] = static_cast<__bf16>(b);
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// The raw bits of a lane's channels of one row.
+template <int PATH, bool F32>
+struct Raw {
+    u32x4 w[F32 ? 4 : 2];       // chunks of 8 channels
+};
+template <bool F32>
+struct Raw<kGeneral, F32> {
+    uint32_t w[4];              // two pairs of channels
+};
+
+// Which channels of a row a lane holds.
+struct Place {
+    uint32_t a, b;              // fast paths: first channels of the two chunks
+    bool turn_a, turn_b;        // ... and whether they are rotated
+    uint32_t e[4];              // general path: the channels of two pairs
+    bool in, in2;               // the lane (general path: its pairs) are inside the row
+};
+template <int PATH, int L>
+__device__ __forceinline__ Place place_of(uint32_t c, const Params &p)
+{
+    Place at = {};
+    if constexpr (PATH == kHalf) {
+        at.in = 16 * c < p.D;
+        at.turn_a = at.turn_b = 16 * c < p.rot;
+        at.a = at.turn_a ? 8 * c : 16 * c;
+        at.b = at.turn_a ? p.rot / 2 + 8 * c : 16 * c + 8;
+    } else if constexpr (PATH == kInterleaved) {
+        at.in = 16 * c < p.D;
+        at.a = 8 * c;
+        at.b = p.D / 2 + 8 * c;
+        at.turn_a = at.a < p.rot;
+        at.turn_b = at.b < p.rot;
+    } else {
+        const uint32_t pairs = p.rot / 2;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t i = c + 64 * j;
+            const bool turned = i < pairs;
+            at.e[2 * j] = turned && !p.interleaved ? i : 2 * i;           // unrotated pairs are neighbours behind the rotated ones
+            at.e[2 * j + 1] = turned && !p.interleaved ? i + pairs : 2 * i + 1;
+            (j ? at.turn_b : at.turn_a) = turned;
+        }
+        at.in = 2 * c < p.D;
+        at.in2 = 2 * (c + 64) < p.D;
+    }
+    return at;
+}
+
+template <int PATH, bool F32>
+__device__ __forceinline__ Raw<PATH, F32> load_row(const char *row, const Place &at, bool on)
+{
+    Raw<PATH, F32> r;
+    constexpr int S = F32 ? 4 : 2;
+    if constexpr (PATH == kGeneral) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            r.w[j] = 0;
+            if (on && (j < 2 ? at.in : at.in2)) {
+                if constexpr (F32) r.w[j] = *reinterpret_cast<const uint32_t *>(row + at.e[j] * S);
+                else r.w[j] = (uint32_t)*reinterpret_cast<const uint16_t *>(row + at.e[j] * S) << 16;
+            }
+        }
+    } else {
+#pragma unroll
+        for (auto &w : r.w) w = u32x4{0, 0, 0, 0};
+        if (on && at.in) {
+            const u32x4 *a = reinterpret_cast<const u32x4 *>(row + at.a * S), *b = reinterpret_cast<const u32x4 *>(row + at.b * S);
+            if constexpr (F32) {
+                r.w[0] = a[0]; r.w[1] = a[1]; r.w[2] = b[0]; r.w[3] = b[1];
+            } else {
+                r.w[0] = a[0]; r.w[1] = b[0];
+            }
+        }
+    }
+    return r;
+}
+
+constexpr int pairs_of(int path) { return path == kGeneral ? 2 : 8; }
+
+// The 16 (general path: 4) channels as pairs (x0[i], x1[i]).
+template <int PATH, bool F32>
+__device__ __forceinline__ void unpack(const Raw<PATH, F32> &r, float (&x0)[pairs_of(PATH)], float (&x1)[pairs_of(PATH)])
+{
+    if constexpr (PATH == kGeneral) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            x0[j] = __uint_as_float(r.w[2 * j]);
+            x1[j] = __uint_as_float(r.w[2 * j + 1]);
+        }
+    } else {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if constexpr (F32) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
+            else v[i] = i & 1 ? high_half(r.w[i / 8][(i % 8) / 2]) : low_half(r.w[i / 8][(i % 8) / 2]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x0[i] = PATH == kHalf ? v[i] : v[2 * i];
+            x1[i] = PATH == kHalf ? v[8 + i] : v[2 * i + 1];
+        }
+    }
+}
+
+// 16-byte stores that leave no dirty line in L2, like those of the permutation: the next kernel reads these rows.
+template <int PATH, bool F32>
+__device__ __forceinline__ void store_row(char *row, const Place &at, bool on, const float (&x0)[pairs_of(PATH)], const float (&x1)[pairs_of(PATH)])
+{
+    constexpr int S = F32 ? 4 : 2;
+    if (!on) return;
+    if constexpr (PATH == kGeneral) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float v = j & 1 ? x1[j / 2] : x0[j / 2];
+            if (j < 2 ? at.in : at.in2) {
+                if constexpr (F32) *reinterpret_cast<float *>(row + at.e[j] * S) = v;
+                else *reinterpret_cast<__bf16 *>(row + at.e[j] * S) = static_cast<__bf16>(v);
+            }
+        }
+    } else if (at.in) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[PATH == kHalf ? i : 2 * i] = x0[i];
+            v[PATH == kHalf ? 8 + i : 2 * i + 1] = x1[i];
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            u32x4 *to = reinterpret_cast<u32x4 *>(row + (half ? at.b : at.a) * S);
+            const float *x = v + 8 * half;
+            if constexpr (F32) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    __builtin_nontemporal_store(u32x4{__float_as_uint(x[4 * q]), __float_as_uint(x[4 * q + 1]), __float_as_uint(x[4 * q + 2]),
+                                                      __float_as_uint(x[4 * q + 3])}, to + q);
+            } else {
+                __builtin_nontemporal_store(u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}, to);
+            }
+        }
+    }
+}
+
+// Sum over the L lanes of a row.
+template <int L>
+__device__ __forceinline__ float row_sum(float x)
+{
+#pragma unroll
+    for (int m = L / 2; m > 0; m /= 2) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+// Cosine and sine of x * step / 2^64 turns.  The upper 32 bits of the product are the angle to 2^-32 turns; the nearest quarter
+// turn is taken off exactly and what is left, at most an eighth of a turn, goes into the Taylor polynomials (terms left out: below
+// 2e-9 and 3e-8).
+__device__ __forceinline__ void turn_of(int32_t x, int64_t step, float magnitude, float sign, float &c, float &s)
+{
+    const uint32_t lo = (uint32_t)step, hi = (uint32_t)((uint64_t)step >> 32), n = (uint32_t)x;
+    const uint32_t turns = __umulhi(n, lo) + n * hi - (x < 0 ? lo : 0u);
+    const uint32_t quarter = (turns + 0x20000000u) >> 30;
+    const float a = (float)(int32_t)(turns - (quarter << 30)) * 1.4629180792671596e-9f;       // 2 pi / 2^32
+    const float a2 = a * a;
+    const float sn = fmaf(fmaf(fmaf(fmaf(2.7557319e-6f, a2, -1.9841270e-4f), a2, 8.3333333e-3f), a2, -1.6666667e-1f), a2 * a, a);
+    const float cs = fmaf(fmaf(fmaf(fmaf(2.4801587e-5f, a2, -1.3888889e-3f), a2, 4.1666667e-2f), a2, -0.5f), a2, 1.0f);
+    const bool odd = quarter & 1;
+    const float c0 = odd ? sn : cs, s0 = odd ? cs : sn;
+    c = ((quarter + 1) & 2 ? -c0 : c0) * magnitude;
+    s = (quarter & 2 ? -s0 : s0) * (magnitude * sign);
+}
+
+// The token of a place: where its rows lie and where it is on the axes.
+struct Token {
+    uint32_t b, n, place;       // batch, index in the inputs' order, index in the outputs' order
+    int32_t at[3];
+};
+__device__ __forceinline__ Token token_of(uint32_t id, const Params &p)
+{
+    Token t;
+    t.b = fast_div(id, p.by_N);
+    t.place = id - t.b * p.N;
+    t.n = t.place;
+    t.at[0] = (int32_t)t.n;
+    t.at[1] = t.at[2] = 0;
+    if (p.tiled) {
+        const uint32_t tile = fast_div(t.place, p.by_P), in = t.place - tile * p.by_P.d;
+        const uint32_t row = fast_div(tile, p.by_nw), tw = tile - row * p.by_nw.d;
+        const uint32_t tt = fast_div(row, p.by_nh), th = row - tt * p.by_nh.d;
+        const uint32_t line = fast_div(in, p.by_Tw), iw = in - line * p.by_Tw.d;
+        const uint32_t it = fast_div(line, p.by_Th), ih = line - it * p.by_Th.d;
+        t.at[0] = (int32_t)(tt * p.T_t + it);
+        t.at[1] = (int32_t)(th * p.T_h + ih);
+        t.at[2] = (int32_t)(tw * p.T_w + iw);
+        t.n = ((uint32_t)t.at[0] * p.g_h + (uint32_t)t.at[1]) * p.g_w + (uint32_t)t.at[2];
+    } else if (p.has_grid) {
+        const uint32_t line = fast_div(t.n, p.by_gw);
+        t.at[2] = (int32_t)(t.n - line * p.g_w);
+        const uint32_t plane = fast_div(line, p.by_gh);
+        t.at[1] = (int32_t)(line - plane * p.g_h);
+        t.at[0] = (int32_t)plane;
+    }
+    if (p.positions) {
+        const int32_t *x = p.positions + (int64_t)t.b * p.position_batch + (int64_t)t.n * p.position_token;
+        t.at[0] = x[0];
+        if (p.axis1 < p.rot / 2) t.at[1] = x[1];
+        if (p.axis2 < p.rot / 2) t.at[2] = x[2];
+    }
+    return t;
+}
+
+// Cosines and sines of a lane's pairs (1 and 0 where they are not rotated; not looked at there).
+template <int PATH>
+__device__ __forceinline__ void turns_of(const Token &t, uint32_t lane_in_row, const Place &at, const Params &p, float (&c)[pairs_of(PATH)],
+                                         float (&s)[pairs_of(PATH)])
+{
+#pragma unroll
+    for (int i = 0; i < pairs_of(PATH); ++i) {
+        c[i] = 1.f;
+        s[i] = 0.f;
+        const bool second = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
+        if (!p.turns || !(second ? at.turn_b : at.turn_a)) continue;
+        const uint32_t pair = PATH == kHalf ? at.a + i : PATH == kGeneral ? lane_in_row + 64 * i : second ? at.b / 2 + i - 4 : at.a / 2 + i;
+        const int32_t x = pair < p.axis1 ? t.at[0] : pair < p.axis2 ? t.at[1] : t.at[2];
+        turn_of(x, p.steps[pair], p.magnitude, p.sign, c[i], s[i]);
+    }
+}
+
+template <int PATH>
+__device__ __forceinline__ void rotate(float (&x0)[pairs_of(PATH)], float (&x1)[pairs_of(PATH)], const float (&c)[pairs_of(PATH)],
+                                       const float (&s)[pairs_of(PATH)], const Place &at, float turn_back)
+{
+#pragma unroll
+    for (int i = 0; i < pairs_of(PATH); ++i) {
+        const bool second = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
+        if (second ? at.turn_b : at.turn_a) {
+            const float a = x0[i], b = x1[i], sn = s[i] * turn_back;
+            x0[i] = a * c[i] - b * sn;
+            x1[i] = a * sn + b * c[i];
+        }
+    }
+}
+
+template <int PATH>
+__device__ __forceinline__ void load_weights(const void *weight, const Params &p, const Place &at, float (&w0)[pairs_of(PATH)],
+                                             float (&w1)[pairs_of(PATH)])
+{
+    auto one = [&](uint32_t e) {
+        return p.weight_f32 ? static_cast<const float *>(weight)[e] : __uint_as_float((uint32_t)static_cast<const uint16_t *>(weight)[e] << 16);
+    };
+#pragma unroll
+    for (int i = 0; i < pairs_of(PATH); ++i) {
+        w0[i] = w1[i] = 1.f;
+        const bool in = PATH == kGeneral && i ? at.in2 : at.in;
+        if (!weight || !in) continue;
+        if constexpr (PATH == kGeneral) {
+            w0[i] = one(at.e[2 * i]);
+            w1[i] = one(at.e[2 * i + 1]);
+        } else if constexpr (PATH == kHalf) {
+            w0[i] = one(at.a + i);
+            w1[i] = one(at.b + i);
+        } else {
+            const uint32_t e = i < 4 ? at.a + 2 * i : at.b + 2 * (i - 4);
+            w0[i] = one(e);
+            w1[i] = one(e + 1);
+        }
+    }
+}
+
+__device__ __forceinline__ const char *row_at(const Rows &r, uint32_t b, uint32_t token) { return r.data + (int64_t)b * r.batch + (int64_t)token * r.token; }
+
+// Workgroup (x, y): tokens 64 / L * x .., heads y * kWaves + wave and every gridDim.y * kWaves after that.
+template <int PATH, int L, bool SRC_F32, bool DST_F32>
+__global__ __launch_bounds__(kThreads) void sta_rows_forward_kernel(Params p)
+{
+    constexpr int NP = pairs_of(PATH);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t c = lane % L, id = blockIdx.x * (64 / L) + lane / L;
+    const bool on = id < p.tokens;
+    const Token t = token_of(on ? id : 0, p);
+    const Place at = place_of<PATH, L>(c, p);
+    float cs[NP], sn[NP];
+    turns_of<PATH>(t, c, at, p, cs, sn);
+    const uint32_t stride = gridDim.y * kWaves;
+    uint32_t h = blockIdx.y * kWaves + wave;
+    for (uint32_t i = 0; i < p.n_tensors; ++i) {
+        const Tensor &T = p.t[i];
+        if (h < T.heads) {
+            const char *x = row_at(T.x, t.b, t.n);
+            char *out = const_cast<char *>(row_at(T.out, t.b, t.place));
+            float w0[NP], w1[NP];
+            if (T.norm) load_weights<PATH>(T.weight, p, at, w0, w1);
+            Raw<PATH, SRC_F32> next = load_row<PATH, SRC_F32>(x + (int64_t)h * T.x.head, at, on);
+            for (; h < T.heads; h += stride) {
+                const Raw<PATH, SRC_F32> raw = next;
+                if (h + stride < T.heads) next = load_row<PATH, SRC_F32>(x + (int64_t)(h + stride) * T.x.head, at, on);
+                float x0[NP], x1[NP];
+                unpack<PATH, SRC_F32>(raw, x0, x1);
+                if (T.norm) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
+                    const float r = rsqrtf(fmaf(row_sum<L>(sum), p.inv_D, p.eps));
+#pragma unroll
+                    for (int j = 0; j < NP; ++j) {
+                        x0[j] *= r * w0[j];
+                        x1[j] *= r * w1[j];
+                    }
+                }
+                if (T.rotate) rotate<PATH>(x0, x1, cs, sn, at, 1.f);
+                store_row<PATH, DST_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
+            }
+        }
+        h -= T.heads;           // the first head of the next tensor that is this wave's
+    }
+}
+
+// Workgroups take groups of tokens in turn; the first two tensors' weight gradients are summed in registers, then over the
+// workgroup, and left in `partial`.
+template <int PATH, int L, bool SRC_F32, bool DST_F32>
+__global__ __launch_bounds__(kThreads) void sta_rows_backward_kernel(Params p)
+{
+    constexpr int NP = pairs_of(PATH);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t c = lane % L;
+    const Place at = place_of<PATH, L>(c, p);
+    float dw0[2][NP], dw1[2][NP];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) dw0[i][j] = dw1[i][j] = 0.f;
+    const uint32_t stride = gridDim.y * kWaves, groups = (p.tokens + 64 / L - 1) / (64 / L);
+    for (uint32_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const uint32_t id = group * (64 / L) + lane / L;
+        const bool on = id < p.tokens;
+        const Token t = token_of(on ? id : 0, p);
+        float cs[NP], sn[NP];
+        turns_of<PATH>(t, c, at, p, cs, sn);
+        uint32_t h = blockIdx.y * kWaves + wave;
+        auto tensor = [&](const Tensor &T, float(&sum0)[NP], float(&sum1)[NP]) __attribute__((always_inline)) {
+            if (h < T.heads) {
+                const char *x = row_at(T.x, t.b, t.n), *dy = row_at(T.dy, t.b, t.place);
+                char *out = const_cast<char *>(row_at(T.out, t.b, t.n));
+                float w0[NP], w1[NP];
+                load_weights<PATH>(T.weight, p, at, w0, w1);
+                for (; h < T.heads; h += stride) {
+                    const Raw<PATH, SRC_F32> raw_x = load_row<PATH, SRC_F32>(x + (int64_t)h * T.x.head, at, on);
+                    const Raw<PATH, DST_F32> raw_g = load_row<PATH, DST_F32>(dy + (int64_t)h * T.dy.head, at, on);
+                    float x0[NP], x1[NP], g0[NP], g1[NP];
+                    unpack<PATH, SRC_F32>(raw_x, x0, x1);
+                    unpack<PATH, DST_F32>(raw_g, g0, g1);
+                    rotate<PATH>(g0, g1, cs, sn, at, -1.f);
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
+                    const float r = rsqrtf(fmaf(row_sum<L>(sum), p.inv_D, p.eps));
+                    float dot = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NP; ++j) {
+                        x0[j] *= r;
+                        x1[j] *= r;
+                        sum0[j] = fmaf(g0[j], x0[j], sum0[j]);
+                        sum1[j] = fmaf(g1[j], x1[j], sum1[j]);
+                        g0[j] *= w0[j];
+                        g1[j] *= w1[j];
+                        dot = fmaf(g0[j], x0[j], fmaf(g1[j], x1[j], dot));
+                    }
+                    dot = row_sum<L>(dot) * p.inv_D;
+#pragma unroll
+                    for (int j = 0; j < NP; ++j) {
+                        x0[j] = r * fmaf(-dot, x0[j], g0[j]);
+                        x1[j] = r * fmaf(-dot, x1[j], g1[j]);
+                    }
+                    store_row<PATH, SRC_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
+                }
+            }
+            h -= T.heads;
+        };
+        tensor(p.t[0], dw0[0], dw1[0]);
+        tensor(p.t[1], dw0[1], dw1[1]);
+        if (p.n_tensors > 2 && h < p.t[2].heads) {              // values: moved back
+            const Tensor &T = p.t[2];
+            const char *dy = row_at(T.dy, t.b, t.place);
+            char *out = const_cast<char *>(row_at(T.out, t.b, t.n));
+            for (; h < T.heads; h += stride) {
+                float x0[NP], x1[NP];
+                unpack<PATH, DST_F32>(load_row<PATH, DST_F32>(dy + (int64_t)h * T.dy.head, at, on), x0, x1);
+                store_row<PATH, SRC_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
+            }
+        }
+    }
+    if (!p.partial) return;
+    // over the tokens of a wave, then over the waves; channels in their places
+    __shared__ float sums[kWaves][2][256];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            float a = dw0[i][j], b = dw1[i][j];
+#pragma unroll
+            for (int m = L; m < 64; m *= 2) {
+                a += __shfl_xor(a, m, 64);
+                b += __shfl_xor(b, m, 64);
+            }
+            if (lane < L && (PATH == kGeneral && j ? at.in2 : at.in)) {
+                uint32_t ea, eb;
+                if constexpr (PATH == kGeneral) { ea = at.e[2 * j]; eb = at.e[2 * j + 1]; }
+                else if constexpr (PATH == kHalf) { ea = at.a + j; eb = at.b + j; }
+                else { ea = j < 4 ? at.a + 2 * j : at.b + 2 * (j - 4); eb = ea + 1; }
+                sums[wave][i][ea] = a;
+                sums[wave][i][eb] = b;
+            }
+        }
+    __syncthreads();
+    float *to = p.partial + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.D;
+    for (uint32_t e = threadIdx.x; e < 2 * p.D; e += kThreads) {
+        const uint32_t i = e >= p.D, ch = e - i * p.D;
+        to[e] = (sums[0][i][ch] + sums[1][i][ch]) + (sums[2][i][ch] + sums[3][i][ch]);
+    }
+}
+
+// d_weight = sum of the workgroups' sums: 16 columns a workgroup, 16 slices of the rows, then the slices in order.
+__global__ __launch_bounds__(256) void sta_rows_weights_kernel(const float *partial, uint32_t rows, uint32_t D, float *d_q, float *d_k)
+{
+    __shared__ float sums[16][17];
+    const uint32_t col = threadIdx.x & 15, slice = threadIdx.x >> 4, e = blockIdx.x * 16 + col;
+    float sum = 0.f;
+    if (e < 2 * D)
+        for (uint32_t r = slice; r < rows; r += 16) sum += partial[(size_t)r * 2 * D + e];
+    sums[slice][col] = sum;
+    __syncthreads();
+    if (slice == 0 && e < 2 * D) {
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += sums[i][col];
+        float *to = e < D ? d_q : d_k;
+        if (to) to[e < D ? e : e - D] = sum;
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------------
+bool valid_type(int dt) { return dt == STA_BF16 || dt == STA_F32; }
+int64_t size_of(int dt) { return dt == STA_F32 ? 4 : 2; }
+
+constexpr int64_t kMostStride = (int64_t)1 << 40;           // elements; products with 2^31 tokens or heads stay in 64 bits with room
+constexpr int kMostD = 256;
+
+int check_rows(const sta_head_rows *r, bool written, int B, int N, int D)
+{
+    if (!r || !r->data) return STA_ERR_NULL;
+    if (r->heads < 1 || r->heads > 65536) return STA_ERR_SHAPE;
+    if (!valid_type(r->dtype)) return STA_ERR_UNSUPPORTED;
+    if ((uintptr_t)r->data % size_of(r->dtype)) return STA_ERR_SHAPE;
+    int64_t stride[3] = {r->batch, r->token, r->head}, count[3] = {B, N, r->heads};
+    long double last = D;
+    for (int i = 0; i < 3; ++i) {
+        if (stride[i] < 0 || stride[i] > kMostStride) return STA_ERR_SHAPE;
+        last += (long double)(count[i] - 1) * stride[i];
+    }
+    if (last > 4.0e18L / 4) return STA_ERR_SHAPE;
+    if (written) {                                          // from the smallest stride up: no row inside another
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2 - i; ++j)
+                if (stride[j] > stride[j + 1]) {
+                    const int64_t s = stride[j], c = count[j];
+                    stride[j] = stride[j + 1]; count[j] = count[j + 1];
+                    stride[j + 1] = s; count[j + 1] = c;
+                }
+        int64_t extent = D;
+        for (int i = 0; i < 3; ++i) {
+            if (count[i] == 1) continue;
+            if (stride[i] < extent) return STA_ERR_SHAPE;
+            extent += (count[i] - 1) * stride[i];
+        }
+    }
+    return STA_OK;
+}
+
+// Bytes from the first to behind the last element.
+uint64_t extent_of(const sta_head_rows &r, int B, int N, int D)
+{
+    return (uint64_t)((B - 1) * r.batch + (N - 1) * r.token + (r.heads - 1) * r.head + D) * size_of(r.dtype);
+}
+
+// Whether an element of a may lie in b.  Heads of one fused tensor interleave: same strides, other heads.
+bool rows_overlap(const sta_head_rows &a, const sta_head_rows &b, int B, int N, int D)
+{
+    const uintptr_t a0 = (uintptr_t)a.data, b0 = (uintptr_t)b.data;
+    if (a0 + extent_of(a, B, N, D) <= b0 || b0 + extent_of(b, B, N, D) <= a0) return false;
+    if (a.dtype != b.dtype || a.token != b.token || a.batch != b.batch || a.token <= 0) return true;
+    const int64_t size = size_of(a.dtype), period = a.token * size;
+    if (B > 1 && a.batch % a.token) return true;
+    const int64_t wide_a = ((a.heads - 1) * a.head + D) * size, wide_b = ((b.heads - 1) * b.head + D) * size;
+    if (wide_a > period || wide_b > period) return true;
+    const int64_t off = (int64_t)(((int64_t)(b0 - a0) % period + period) % period);        // where b's rows of a token begin
+    return off < wide_a || off + wide_b > period;
+}
+
+bool same_rows(const sta_head_rows &a, const sta_head_rows &b)
+{
+    return a.data == b.data && a.batch == b.batch && a.token == b.token && a.head == b.head && a.heads == b.heads && a.dtype == b.dtype;
+}
+
+Rows rows_of(const sta_head_rows &r)
+{
+    const int64_t s = size_of(r.dtype);
+    return {static_cast<char *>(r.data), r.batch * s, r.token * s, r.head * s};
+}
+
+bool chunked(const Rows &r) { return (((uintptr_t)r.data | (uintptr_t)r.batch | (uintptr_t)r.token | (uintptr_t)r.head) & 15) == 0; }
+
+// What does not depend on the tensors.
+int fill_params(Params *p, const sta_rotary *rotary, int B, int N, int D, const int *grid, const int *tile, float eps, int inverse)
+{
+    if (B < 0 || N < 0) return STA_ERR_SHAPE;
+    if (D < 2 || D > kMostD || D % 2) return STA_ERR_UNSUPPORTED;
+    if ((int64_t)B * N > 0x7fffffff) return STA_ERR_SHAPE;
+    if (tile && !grid) return STA_ERR_NULL;
+    p->tokens = (uint32_t)((int64_t)B * N);
+    p->D = D;
+    p->inv_D = 1.f / (float)D;
+    p->eps = eps;
+    p->N = N > 0 ? N : 1;
+    p->by_N = fast_div_of(p->N);
+    if (grid) {
+        int64_t n = 1;
+        for (int a = 0; a < 3; ++a) {
+            if (grid[a] <= 0 || (tile && (tile[a] <= 0 || grid[a] % tile[a] != 0))) return STA_ERR_SHAPE;
+            n *= grid[a];
+            if (n > 0x7fffffff) return STA_ERR_SHAPE;
+        }
+        if (n != N) return STA_ERR_SHAPE;
+        p->has_grid = 1;
+        p->g_h = grid[1];
+        p->g_w = grid[2];
+        p->by_gw = fast_div_of(grid[2]);
+        p->by_gh = fast_div_of(grid[1]);
+        if (tile) {
+            p->tiled = 1;
+            p->T_t = tile[0]; p->T_h = tile[1]; p->T_w = tile[2];
+            p->by_P = fast_div_of((uint32_t)(tile[0] * tile[1] * tile[2]));
+            p->by_nw = fast_div_of(grid[2] / tile[2]);
+            p->by_nh = fast_div_of(grid[1] / tile[1]);
+            p->by_Tw = fast_div_of(tile[2]);
+            p->by_Th = fast_div_of(tile[1]);
+        }
+    }
+    p->sign = inverse ? -1.f : 1.f;
+    if (rotary) {
+        const int pairs = rotary->channels / 2;
+        if (rotary->channels < 0 || rotary->channels % 2 || rotary->channels > D) return STA_ERR_SHAPE;
+        int64_t sum = 0;
+        for (int a = 0; a < 3; ++a) {
+            if (rotary->pairs[a] < 0) return STA_ERR_SHAPE;
+            sum += rotary->pairs[a];
+        }
+        if (sum != pairs) return STA_ERR_SHAPE;
+        if (!rotary->positions && !grid && rotary->pairs[0] != pairs) return STA_ERR_SHAPE;        // a token index has one axis
+        if (pairs > 0 && !rotary->steps) return STA_ERR_NULL;
+        if (((uintptr_t)rotary->steps & 7) || ((uintptr_t)rotary->positions & 3)) return STA_ERR_SHAPE;
+        if (rotary->position_batch < 0 || rotary->position_token < 0 || rotary->position_batch > kMostStride || rotary->position_token > kMostStride)
+            return STA_ERR_SHAPE;
+        p->rot = rotary->channels;
+        p->steps = rotary->steps;
+        p->positions = pairs > 0 ? rotary->positions : nullptr;
+        p->position_batch = rotary->position_batch;
+        p->position_token = rotary->position_token;
+        p->axis1 = rotary->pairs[0];
+        p->axis2 = rotary->pairs[0] + rotary->pairs[1];
+        p->magnitude = rotary->magnitude == 0.f ? 1.f : rotary->magnitude;
+        p->interleaved = rotary->interleaved != 0;
+        p->turns = pairs > 0;
+    }
+    return STA_OK;
+}
+
+// Which kernel: the general one where a chunk of 8 channels is not 16 aligned bytes or would be split by the rotation.
+int path_of(const Params &p)
+{
+    if (p.D % 16 || p.rot % (p.interleaved ? 8 : 16)) return kGeneral;
+    for (uint32_t i = 0; i < p.n_tensors; ++i)
+        if (!chunked(p.t[i].x) || !chunked(p.t[i].out) || !chunked(p.t[i].dy)) return kGeneral;
+    return p.interleaved ? kInterleaved : kHalf;
+}
+
+constexpr uint32_t kWantBlocks = 1024;          // four workgroups a CU
+constexpr uint32_t kMostPartials = 1024;
+
+// Heads are dealt to gridDim.y workgroups where the tokens alone do not make enough of them.
+uint32_t split_of(uint32_t groups, uint32_t heads)
+{
+    const uint32_t most = (heads + kWaves - 1) / kWaves, want = (kWantBlocks + groups - 1) / groups;
+    return want < 1 ? 1 : want < most ? want : most;
+}
+
+template <int PATH, int L, bool SRC_F32, bool DST_F32>
+hipError_t launch(const Params &p, bool backward, uint32_t *rows, hipStream_t stream)
+{
+    const uint32_t per = 64 / L, groups = (p.tokens + per - 1) / per;
+    uint32_t heads = 0;
+    for (uint32_t i = 0; i < p.n_tensors; ++i) heads += p.t[i].heads;
+    const uint32_t y = split_of(groups, heads);
+    if (!backward) return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, y), dim3(kThreads), stream, p);
+    const uint32_t x = groups * (uint64_t)y > kMostPartials ? kMostPartials / y : groups;
+    *rows = x * y;
+    return sta::launch_kernel(sta_rows_backward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(x, y), dim3(kThreads), stream, p);
+}
+
+template <int PATH, int L>
+hipError_t launch_types(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+{
+    if (src_f32) return dst_f32 ? launch<PATH, L, true, true>(p, backward, rows, stream) : launch<PATH, L, true, false>(p, backward, rows, stream);
+    return dst_f32 ? launch<PATH, L, false, true>(p, backward, rows, stream) : launch<PATH, L, false, false>(p, backward, rows, stream);
+}
+
+template <int PATH>
+hipError_t launch_lanes(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+{
+    if (p.D <= 64) return launch_types<PATH, 4>(p, src_f32, dst_f32, backward, rows, stream);
+    if (p.D <= 128) return launch_types<PATH, 8>(p, src_f32, dst_f32, backward, rows, stream);
+    return launch_types<PATH, 16>(p, src_f32, dst_f32, backward, rows, stream);
+}
+
+hipError_t launch_rows(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+{
+    switch (path_of(p)) {
+    case kHalf: return launch_lanes<kHalf>(p, src_f32, dst_f32, backward, rows, stream);
+    case kInterleaved: return launch_lanes<kInterleaved>(p, src_f32, dst_f32, backward, rows, stream);
+    default: return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, rows, stream);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int sta_rope_steps(int channels, double theta, int scaling, double factor, double original_positions, int64_t *steps, float *magnitude)
+{
+    if (!steps) return STA_ERR_NULL;
+    if (channels < 2 || channels % 2 || channels > kMostD) return STA_ERR_SHAPE;
+    if (scaling < STA_ROPE_NONE || scaling > STA_ROPE_YARN) return STA_ERR_UNSUPPORTED;
+    if (!(theta >= 1.0) || !(theta <= 1e300)) return STA_ERR_SHAPE;
+    if (scaling != STA_ROPE_NONE && (!(factor >= 1.0) || !(factor <= 1e9))) return STA_ERR_SHAPE;
+    if (scaling == STA_ROPE_YARN && !(original_positions >= 1.0)) return STA_ERR_SHAPE;
+    const long double two_pi = 6.283185307179586476925286766559L;
+    const int pairs = channels / 2;
+    long double base = theta;
+    if (scaling == STA_ROPE_NTK && pairs > 1) base *= powl((long double)factor, (long double)channels / (channels - 2));
+    for (int i = 0; i < pairs; ++i) {
+        long double f = powl(base, -(long double)i / pairs);
+        if (scaling == STA_ROPE_LINEAR) f /= factor;
+        if (scaling == STA_ROPE_YARN) {
+            long double keep = (original_positions * f / two_pi - 1.0L) / 31.0L;
+            keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+            f = f * keep + f / factor * (1 - keep);
+        }
+        steps[i] = (int64_t)roundl(f / two_pi * 18446744073709551616.0L);          // f <= 1: below 2^62
+    }
+    if (magnitude) *magnitude = scaling == STA_ROPE_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+    return STA_OK;
+}
+
+int sta_rope(const sta_head_rows *in, const sta_head_rows *out, int n_tensors, int B, int N, int D, const sta_rotary *rotary, int inverse,
+             void *hip_stream)
+{
+    if (!in || !out || !rotary) return STA_ERR_NULL;
+    if (n_tensors < 1 || n_tensors > 3) return STA_ERR_SHAPE;
+    Params p = {};
+    if (int rc = fill_params(&p, rotary, B, N, D, nullptr, nullptr, 0.f, inverse)) return rc;
+    if (p.tokens == 0) return STA_OK;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (int rc = check_rows(in + i, false, B, N, D)) return rc;
+        if (int rc = check_rows(out + i, true, B, N, D)) return rc;
+        if (in[i].heads != out[i].heads) return STA_ERR_SHAPE;
+        if (in[i].dtype != in[0].dtype || out[i].dtype != out[0].dtype) return STA_ERR_UNSUPPORTED;
+    }
+    for (int i = 0; i < n_tensors; ++i)
+        for (int j = 0; j < n_tensors; ++j) {
+            if (!(i == j && same_rows(in[i], out[j])) && rows_overlap(in[i], out[j], B, N, D)) return STA_ERR_ALIAS;
+            if (i < j && rows_overlap(out[i], out[j], B, N, D)) return STA_ERR_ALIAS;
+        }
+    p.n_tensors = n_tensors;
+    for (int i = 0; i < n_tensors; ++i) {
+        p.t[i].x = rows_of(in[i]);
+        p.t[i].out = rows_of(out[i]);
+        p.t[i].heads = in[i].heads;
+        p.t[i].rotate = p.turns;
+    }
+    const hipError_t e = launch_rows(p, in[0].dtype == STA_F32, out[0].dtype == STA_F32, false, nullptr, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? STA_OK : STA_ERR_HIP;
+}
+
+int sta_qk_norm_rope(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *q_out,
+                     const sta_head_rows *k_out, const sta_head_rows *v_out, const void *q_weight, const void *k_weight, int weight_dt,
+                     float eps, const sta_rotary *rotary, int B, int N, int D, const int grid[3], const int tile[3], void *hip_stream)
+{
+    if (!q || !k || !q_out || !k_out || (v == nullptr) != (v_out == nullptr)) return STA_ERR_NULL;
+    if (!valid_type(weight_dt)) return STA_ERR_UNSUPPORTED;
+    Params p = {};
+    if (int rc = fill_params(&p, rotary, B, N, D, grid, tile, eps, 0)) return rc;
+    if (p.tokens == 0) return STA_OK;
+    const sta_head_rows *in[3] = {q, k, v}, *out[3] = {q_out, k_out, v_out};
+    p.n_tensors = v ? 3 : 2;
+    p.weight_f32 = weight_dt == STA_F32;
+    for (uint32_t i = 0; i < p.n_tensors; ++i) {
+        if (int rc = check_rows(in[i], false, B, N, D)) return rc;
+        if (int rc = check_rows(out[i], true, B, N, D)) return rc;
+        if (in[i]->heads != out[i]->heads) return STA_ERR_SHAPE;
+        if (in[i]->dtype != q->dtype || out[i]->dtype != q_out->dtype) return STA_ERR_UNSUPPORTED;
+        p.t[i].x = rows_of(*in[i]);
+        p.t[i].out = rows_of(*out[i]);
+        p.t[i].heads = in[i]->heads;
+        p.t[i].norm = i < 2;
+        p.t[i].rotate = i < 2 && p.turns;
+        p.t[i].weight = i == 0 ? q_weight : i == 1 ? k_weight : nullptr;
+        if ((uintptr_t)p.t[i].weight % size_of(weight_dt)) return STA_ERR_SHAPE;
+    }
+    for (uint32_t i = 0; i < p.n_tensors; ++i)
+        for (uint32_t j = 0; j < p.n_tensors; ++j) {
+            if (!(i == j && !tile && same_rows(*in[i], *out[j])) && rows_overlap(*in[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
+            if (i < j && rows_overlap(*out[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
+        }
+    const hipError_t e = launch_rows(p, q->dtype == STA_F32, q_out->dtype == STA_F32, false, nullptr, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? STA_OK : STA_ERR_HIP;
+}
+
+size_t sta_qk_norm_rope_workspace_bytes(int D)
+{
+    return D < 2 || D > kMostD || D % 2 ? 0 : (size_t)kMostPartials * 2 * D * sizeof(float);
+}
+
+int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *d_q_out, const sta_head_rows *d_k_out,
+                              const sta_head_rows *d_v_out, const sta_head_rows *d_q, const sta_head_rows *d_k, const sta_head_rows *d_v,
+                              const void *q_weight, const void *k_weight, int weight_dt, float *d_q_weight, float *d_k_weight, float eps,
+                              const sta_rotary *rotary, int B, int N, int D, const int grid[3], const int tile[3], void *workspace,
+                              size_t workspace_bytes, void *hip_stream)
+{
+    if (!q || !k || !d_q_out || !d_k_out || !d_q || !d_k || (d_v_out == nullptr) != (d_v == nullptr)) return STA_ERR_NULL;
+    if (!valid_type(weight_dt)) return STA_ERR_UNSUPPORTED;
+    Params p = {};
+    if (int rc = fill_params(&p, rotary, B, N, D, grid, tile, eps, 0)) return rc;
+    const bool sums = d_q_weight || d_k_weight;
+    if (sums && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sta_qk_norm_rope_workspace_bytes(D))) return STA_ERR_WORKSPACE;
+    if (((uintptr_t)d_q_weight | (uintptr_t)d_k_weight) & 3) return STA_ERR_SHAPE;
+    const sta_head_rows *x[3] = {q, k, nullptr}, *dy[3] = {d_q_out, d_k_out, d_v_out}, *dx[3] = {d_q, d_k, d_v};
+    p.n_tensors = d_v ? 3 : 2;
+    p.weight_f32 = weight_dt == STA_F32;
+    p.partial = sums ? static_cast<float *>(workspace) : nullptr;
+    uint32_t rows = 0;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (p.tokens != 0) {
+        for (uint32_t i = 0; i < p.n_tensors; ++i) {
+            if (x[i])
+                if (int rc = check_rows(x[i], false, B, N, D)) return rc;
+            if (int rc = check_rows(dy[i], false, B, N, D)) return rc;
+            if (int rc = check_rows(dx[i], true, B, N, D)) return rc;
+            if (dy[i]->heads != dx[i]->heads || (x[i] && x[i]->heads != dx[i]->heads)) return STA_ERR_SHAPE;
+            if (dx[i]->dtype != q->dtype || (x[i] && x[i]->dtype != q->dtype) || dy[i]->dtype != d_q_out->dtype) return STA_ERR_UNSUPPORTED;
+            p.t[i].dy = rows_of(*dy[i]);
+            p.t[i].out = rows_of(*dx[i]);
+            if (x[i]) p.t[i].x = rows_of(*x[i]);
+            p.t[i].heads = dx[i]->heads;
+            p.t[i].norm = i < 2;
+            p.t[i].rotate = i < 2 && p.turns;
+            p.t[i].weight = i == 0 ? q_weight : i == 1 ? k_weight : nullptr;
+            if ((uintptr_t)p.t[i].weight % size_of(weight_dt)) return STA_ERR_SHAPE;
+        }
+        const uintptr_t w0 = (uintptr_t)workspace, w1 = w0 + (sums ? sta_qk_norm_rope_workspace_bytes(D) : 0);
+        for (uint32_t i = 0; i < p.n_tensors; ++i)
+            for (uint32_t j = 0; j < p.n_tensors; ++j) {
+                if ((x[i] && rows_overlap(*x[i], *dx[j], B, N, D)) || rows_overlap(*dy[i], *dx[j], B, N, D)) return STA_ERR_ALIAS;
+                if (i < j && rows_overlap(*dx[i], *dx[j], B, N, D)) return STA_ERR_ALIAS;
+                for (const sta_head_rows *r : {x[i], dy[i], dx[i]})
+                    if (sums && r && w0 < (uintptr_t)r->data + extent_of(*r, B, N, D) && (uintptr_t)r->data < w1) return STA_ERR_ALIAS;
+            }
+        if (launch_rows(p, q->dtype == STA_F32, d_q_out->dtype == STA_F32, true, &rows, stream) != hipSuccess) return STA_ERR_HIP;
+    }
+    if (sums && sta::launch_kernel(sta_rows_weights_kernel, dim3((2 * D + 15) / 16), dim3(256), stream, p.partial, rows, p.D, d_q_weight, d_k_weight) != hipSuccess)
+        return STA_ERR_HIP;
+    return STA_OK;
+}
+
+}  // extern "C"
