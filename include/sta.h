@@ -364,6 +364,42 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
                               int N, int D, const int grid[3], const int tile[3], void *workspace, size_t workspace_bytes,
                               void *hip_stream);
 
+/*
+ * Softmax attention over S packed sequences of different lengths: prompts, single tokens against a cache, cross attention.
+ * q, o: [tokens_q, Hq, D]; k, v: [tokens_k, Hkv, D], Hq a multiple of Hkv: query heads g n .. g n + g - 1, g = Hq / Hkv, read key head
+ * n.  Strides as sta_head_rows says (batch is not looked at); all bf16.  Sequence s has the query tokens cu_q[s] .. cu_q[s + 1] - 1 and the
+ * key tokens cu_k[s] .. cu_k[s + 1] - 1, of which, with k_used (NULL: all), the first k_used[s]: a cache with room to grow is cu_k at its
+ * slots' bounds and k_used the lengths.  cu_q, cu_k, k_used: device int32 of S + 1, S + 1 and S entries; entries that leave the tensors or do
+ * not ascend are cut to what is there.  max_q, max_k: host, upper bounds of the sequences' lengths (rows beyond may stay unwritten).
+ * With the sequence's lq query and lk key tokens, query token i sees, if causal is not 0, the keys j <= i + lk - lq (the last token sees
+ * all), else all.  A row that sees no key: o = 0, lse = -infinity.  A length may be 0.  Query tokens that no sequence has keep what o
+ * and lse hold.  Keys that a row does not see take no part in it, whatever they hold, infinities and NaN in V included.
+ * lse: NULL, or device float32 [Hq, tokens_q], ln of each row's softmax denominator.  scale <= 0 selects 1 / sqrt(D).
+ * Arithmetic as sta_forward (with lse, the sum is taken before the probabilities are rounded).
+ * workspace: as sta_forward, of at least sta_packed_workspace_bytes(...) bytes: launches that would not fill the chip are cut along the keys.
+ * NULL: no parts.  Results are repeatable bit for bit.
+ * Supported: D in {64, 128}; rows at multiples of 16 bytes (else STA_ERR_SHAPE).  o must not overlap what is read.
+ */
+size_t sta_packed_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k);
+int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o, float *lse,
+                       int64_t tokens_q, int64_t tokens_k, const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_used, int S,
+                       int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes,
+                       void *hip_stream);
+
+/*
+ * Gradients of sta_packed_forward (of all keys: no k_used), o and lse as it returned them for the same q, k, v, bounds, causal and scale.
+ * d_q: like q; d_k, d_v: like k and v, summed over the query heads of a group.  Written for every token of a sequence (0 where no
+ * row saw it).  P is recomputed from the scores and lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are
+ * rounded once.  No atomics: repeated calls give identical bits.
+ * workspace: device, 16-byte aligned, at least sta_packed_backward_workspace_bytes(Hq, tokens_q) bytes, else STA_ERR_WORKSPACE.
+ */
+size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q);
+int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o,
+                        const sta_head_rows *d_o, const float *lse, const sta_head_rows *d_q, const sta_head_rows *d_k,
+                        const sta_head_rows *d_v, int64_t tokens_q, int64_t tokens_k, const int32_t *cu_q, const int32_t *cu_k, int S,
+                        int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
 const char *sta_strerror(int status);
 int sta_version(void);
 

@@ -12,6 +12,7 @@ from .binding import (  # noqa: F401
     sta_backward, sta_backward_workspace_bytes, sta_query_tile_box, sta_head_mse_static, sta_forward_general,
 )
 from .layer_ops import (  # noqa: F401
-    STA_ROPE_LINEAR, STA_ROPE_NONE, STA_ROPE_NTK, STA_ROPE_YARN, StaRotary, sta_qk_norm_rope, sta_qk_norm_rope_backward,
+    STA_ROPE_LINEAR, STA_ROPE_NONE, STA_ROPE_NTK, STA_ROPE_YARN, StaRotary, sta_packed_backward,
+    sta_packed_backward_workspace_bytes, sta_packed_forward, sta_packed_workspace_bytes, sta_qk_norm_rope, sta_qk_norm_rope_backward,
     sta_qk_norm_rope_workspace_bytes, sta_rope, sta_rope_steps,
 )

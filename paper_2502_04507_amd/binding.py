@@ -28,6 +28,7 @@ EXPORTED_SYMBOLS = (
     "sta_backward_workspace_bytes", "sta_backward", "sta_query_tile_box", "sta_head_mse_static",
     # bound in layer_ops
     "sta_rope_steps", "sta_rope", "sta_qk_norm_rope", "sta_qk_norm_rope_workspace_bytes", "sta_qk_norm_rope_backward",
+    "sta_packed_workspace_bytes", "sta_packed_forward", "sta_packed_backward_workspace_bytes", "sta_packed_backward",
 )
 
 

@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsta.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["sta_api.hip", "sta_permute.hip", "sta_attention.hip", "sta_reduce.hip", "sta_backward.hip", "sta_rows.hip"]
+SOURCES = ["sta_api.hip", "sta_permute.hip", "sta_attention.hip", "sta_reduce.hip", "sta_backward.hip", "sta_rows.hip", "sta_packed.hip", "sta_packed_backward.hip"]
 PROBE_SOURCE = "bench_mfma_probe.hip"
 PROBE_OUT = os.path.join(HERE, "libsta_mfma_probe.so")
 

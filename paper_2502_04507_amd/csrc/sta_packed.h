@@ -1,0 +1,160 @@
+// Attention over packed sequences: what the forward and gradient kernels share.  Sequence s has the query tokens cu_q[s] .. cu_q[s + 1]
+// and the key tokens from cu_k[s] on; query heads g n .. g n + g - 1 (a group) read key head n.
+//
+// The rows of one sequence and key head are its (token, head of the group) pairs, token after token: row R = token * g + head.  So a
+// tile of rows shares its keys whatever g is, a single token fills g of its rows, and along a tile the keys that a causal row sees
+// never shrink.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sta.h"
+#include "sta_device_util.h"
+#include "sta_internal.h"
+#include "sta_staged.h"
+
+namespace sta {
+
+// Whether a [tokens, heads, D] tensor can be read (written) 16 bytes at a time; heads_of: heads it must have, 0: any.
+int packed_check(const sta_head_rows *r, int64_t tokens, int heads_of, int D, bool written);
+
+}  // namespace sta
+
+namespace {
+
+// Strides in bytes.
+struct PackedRows {
+    char *data;
+    int64_t token, head;
+};
+
+struct PackedParams {
+    PackedRows q, k, v, o;
+    float *lse;                     // [Hq, tokens_q] or null
+    const int32_t *cu_q, *cu_k, *k_used;
+    uint32_t S, tokens_q, tokens_k;
+    uint32_t Hkv, g;                // key heads, query heads of each
+    sta::FastDiv by_g, by_Hkv, by_parts;
+    uint32_t causal;
+    float scale_log2e, scale;
+    // tiles of rows cut along the keys: part j takes the sub-blocks part_subs * j .. ; a tile of more than one part leaves partial sums
+    // in ws
+    uint32_t part_subs, parts;
+    float *ws;
+};
+
+// One sequence; every wave finds it for itself, so all members are the same in all lanes.
+struct PackedSeq {
+    int32_t q0, lq, k0, lk;         // first query and key token, and how many
+    // keys that a row of query token t sees: the first keys_of(t)
+    __device__ __forceinline__ int keys_of(int t, const PackedParams &p) const
+    {
+        if (!p.causal) return lk;
+        const int n = t + 1 + lk - lq;
+        return n < 0 ? 0 : n < lk ? n : lk;
+    }
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Bounds that do not follow each other, or leave the tensors, are cut to what is there: no access depends on the arrays being right.
+__device__ __forceinline__ int bound_of(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+__device__ __forceinline__ PackedSeq seq_of(uint32_t s, const PackedParams &p)
+{
+    PackedSeq q;
+    q.q0 = bound_of(p.cu_q[s], 0, (int)p.tokens_q);
+    q.lq = bound_of(p.cu_q[s + 1], q.q0, (int)p.tokens_q) - q.q0;
+    q.k0 = bound_of(p.cu_k[s], 0, (int)p.tokens_k);
+    q.lk = bound_of(p.cu_k[s + 1], q.k0, (int)p.tokens_k) - q.k0;
+    if (p.k_used) q.lk = bound_of(p.k_used[s], 0, q.lk);
+    return q;
+}
+
+// Sum over the lanes up to and including this one.
+__device__ __forceinline__ uint32_t scan64(uint32_t x, int lane)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint32_t y = __shfl_up(x, m, 64);
+        if (lane >= m) x += y;
+    }
+    return x;
+}
+
+// The tile that is number `rank` from the end of all sequences' tiles (the last tiles of a causal sequence are its longest), and its
+// sequence.  TILE rows a tile of query rows; KEYS: tiles of TILE keys instead.  The number of tiles is known on the device only: launches have an upper
+// bound of them, and false is returned for ranks beyond.
+struct PackedTile {
+    PackedSeq seq;
+    uint32_t index;                 // of the tile in its sequence
+    uint32_t slot;                  // of the tile among all sequences' tiles
+};
+template <int TILE, bool KEYS>
+__device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, int lane, PackedTile *out)
+{
+    auto tiles_of = [&](uint32_t s) {
+        if (s >= p.S) return 0u;
+        const PackedSeq q = seq_of(s, p);
+        return ((KEYS ? (uint32_t)q.lk : (uint32_t)q.lq * p.g) + TILE - 1) / TILE;
+    };
+    uint32_t total = 0, last = 0;
+    for (uint32_t s0 = 0; s0 < p.S; s0 += 64) {
+        last = scan64(tiles_of(s0 + lane), lane);
+        total += __builtin_amdgcn_readlane(last, 63);
+    }
+    if (rank >= total) return false;
+    const uint32_t idx = KEYS ? rank : total - 1 - rank;     // (the first keys of a causal sequence are seen by the most rows)
+    uint32_t before = 0;
+    for (uint32_t s0 = 0; s0 < p.S; s0 += 64) {
+        const uint32_t own = tiles_of(s0 + lane);
+        const uint32_t upto = p.S <= 64 ? last : scan64(own, lane);
+        const uint32_t all = __builtin_amdgcn_readlane(upto, 63);
+        if (idx < before + all) {
+            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > idx));
+            out->slot = idx;
+            out->index = idx - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
+            out->seq = seq_of(s0 + at, p);
+            out->seq.q0 = uniform(out->seq.q0);
+            out->seq.lq = uniform(out->seq.lq);
+            out->seq.k0 = uniform(out->seq.k0);
+            out->seq.lk = uniform(out->seq.lk);
+            return true;
+        }
+        before += all;
+    }
+    return false;
+}
+
+// DMA of rows into LDS: where a lane's 16 bytes of a group of rows come from, and the rows beyond the last one read as the last one.
+template <int D, bool ROWS_ONLY>
+struct PackedDma {
+    static constexpr int LPR = D / 8;                               // lanes per row
+    static constexpr int GroupRows = Staged<D>::GroupRows;
+    int r;                                                          // row inside a group
+    uint32_t chunk;                                                 // byte offset inside the row
+    uint32_t off;                                                   // ... from the group's first row
+    __device__ __forceinline__ void start(int lane, int64_t token)
+    {
+        r = lane / LPR;
+        const int pos = lane % LPR;
+        if constexpr (ROWS_ONLY) chunk = (uint32_t)((pos ^ StagedRows<D>::turn(r)) << 4);
+        else chunk = (uint32_t)(D == 128 ? (pos ^ (r << 2)) << 4 : (pos ^ (((r >> 1) & 3) << 1)) << 4);
+        off = (uint32_t)(r * (int)token) + chunk;
+    }
+    // Rows `first` .. of base (already at the sequence's first row), of which `rows` exist, to LDS address dst.
+    __device__ __forceinline__ void bring(const char *base, int64_t token, int first, int rows, char *dst) const
+    {
+        const char *src;
+        if (first + GroupRows <= rows) {
+            uint32_t o = off;
+            asm volatile("" : "+v"(o));                             // a 32-bit lane offset next to a scalar base
+            src = base + (int64_t)first * token + o;
+        } else {
+            const int row = first + r < rows ? first + r : rows - 1;
+            src = base + (int64_t)row * token + chunk;
+        }
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, STA_LDS_PTR(dst), 16, 0, 0);
+    }
+};
+
+}  // namespace

@@ -1,0 +1,717 @@
+// Softmax attention over packed sequences of different lengths, causal or not, grouped heads: forward.
+//
+// O = softmax(scale Q K^T) V for every sequence, row of a query token and head by itself; the running maximum and sum of the softmax
+// make it one pass over the keys.  Formulation as in the tile attention: S^T = K Q^T on v_mfma_f32_16x16x32_bf16, so that a lane owns a
+// column (a row of queries) and its softmax needs exchanges only among four lanes; P, rounded to bf16, goes from the accumulators
+// straight into O^T += V^T P^T.
+//
+// sta_packed_tile_kernel   four waves of 32 rows share the staged keys and values: prompts.  Bound by the matrix pipe.
+// sta_packed_few_kernel    at most 16 or 32 rows per sequence and key head (single tokens and a few more): four waves take sub-blocks of
+//                          32 keys in turn, each with LDS of its own and no barrier, and merge at the end.  Bound by reading the keys and values.
+// sta_packed_merge_kernel  joins the parts of tiles that were cut along the keys to fill the chip.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/sta.h"
+#include "sta_packed.h"
+#include "sta_rows_check.h"
+
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kTile = 128;                                  // rows of a workgroup of the tile kernel
+
+// Running softmax of a wave's columns: offsets in the units of the scores, sums, accumulators [channel block][column block] of O^T.
+template <int D, int NC, bool LSE>
+struct Softmax {
+    static constexpr int CB = D / 16;
+    floatx4 acc[CB][NC];
+    float m[NC];                    // -infinity until a key is seen
+    bool far;                       // an offset is so large (masks of the type's lowest number) that its product with the scale is too coarse
+    floatx4 l[NC];                  // LSE: [0] is this lane's share of the sum; otherwise all four are the whole sum of the rounded probabilities
+    __device__ __forceinline__ void start()
+    {
+        far = false;
+#pragma unroll
+        for (int col = 0; col < NC; ++col) {
+            m[col] = -INFINITY;
+            l[col] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) acc[cb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // The sum of a column (over the lanes that share it).
+    __device__ __forceinline__ float sum(int col) const { return LSE ? quad_lane_sum(l[col][0]) : l[col][0]; }
+};
+
+// Whether a staged sub-block of V holds an infinity or a NaN; the same in all lanes.
+template <int D>
+__device__ __forceinline__ bool holds_no_numbers(const char *v, int lane)
+{
+    uint32_t seen = 0;                                      // 0x7f80 is the exponent of both: one more carries into bit 15
+#pragma unroll
+    for (int group = 0; group < Staged<D>::Groups; ++group) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(v + group * Staged<D>::Group + lane * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) seen |= (w[i] & 0x7f807f80u) + 0x00800080u;
+    }
+    return __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
+}
+
+// O^T += V^T P^T for a sub-block whose V holds infinities or NaN and of which some column does not see all keys: a probability of 0
+// times one of those is no 0.  Numbers go through the product as ever; how many infinities of either sign and NaN a column sees is three
+// products more with ones in their places, and a column that sees one gets it.  The first operands of pv are on their way.
+template <int D, int NC, int V_OFF>
+__device__ __forceinline__ void product_without_unseen(StagedTransposedProduct<D, V_OFF> &pv, const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC],
+                                                       const bf16x8 (&P)[NC], const int (&lim)[NC], int first, int g4)
+{
+    using Product = StagedTransposedProduct<D, V_OFF>;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    bf16x8 sees[NC];
+#pragma unroll
+    for (int col = 0; col < NC; ++col)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sees[col][i] = static_cast<__bf16>(first + 4 * g4 + (i < 4 ? i : 12 + i) < lim[col] ? 1.0f : 0.0f);
+    static_for<0, Product::NG>([&](auto gc) {
+        constexpr int g = decltype(gc)::value;
+        if constexpr (g > 0) pv.template issue<g>(v_addr);
+        pv_wait<0>(pv.frag[g]);
+        static_for<0, 4>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, cb = 4 * g + i;
+            const u32x4 x = __builtin_bit_cast(u32x4, __builtin_shufflevector(pv.frag[g][i][0], pv.frag[g][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+            u32x4 odd, nan;                                 // bit 15 of every half: no number; NaN
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                odd[w] = ((x[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                nan[w] = (((x[w] & 0x007f007fu) + 0x007f007fu) << 8) & odd[w];
+            }
+            static_for<0, 4>([&](auto kc) {
+                constexpr int kind = decltype(kc)::value;   // numbers, +infinity, -infinity, NaN
+                u32x4 a;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if constexpr (kind == 0) {
+                        a[w] = x[w] & ~(odd[w] | (odd[w] - (odd[w] >> 15)));
+                    } else {
+                        const uint32_t sign = x[w] & 0x80008000u, inf = odd[w] & ~nan[w];
+                        const uint32_t at = kind == 1 ? inf & ~sign : kind == 2 ? inf & sign : nan[w];
+                        a[w] = (at >> 1) - (at >> 8);       // 1.0
+                    }
+                }
+#pragma unroll
+                for (int col = 0; col < NC; ++col) {
+                    if constexpr (kind == 0) {
+                        acc[cb][col] = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), P[col], acc[cb][col]);
+                    } else {
+                        const floatx4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), sees[col], floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            // on the bits: floating-point sums of infinities may be folded by the compiler
+                            const uint32_t o = __float_as_uint(acc[cb][col][r]), inf = kind == 2 ? 0xff800000u : 0x7f800000u;
+                            const bool against = (o & 0x7fffffffu) > 0x7f800000u || o == (inf ^ 0x80000000u);      // NaN, the other infinity
+                            const uint32_t with = kind == 3 || against ? 0x7fc00000u : inf;
+                            acc[cb][col][r] = __uint_as_float(n[r] > 0.f ? with : o);
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    });
+}
+
+// One sub-block of 32 keys: K at LDS offset K_OFF of k_addr in the layout StagedRows, V at V_OFF of v_addr in the layout Staged.  lim: how many
+// keys a column sees; first: the sub-block's first key.  MASKED: some column may not see all of them (v: where V is staged).
+template <int D, int NC, bool LSE, bool MASKED, int K_OFF, int V_OFF>
+__device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint32_t k_addr, const uint32_t (&v_addr)[4],
+                                                  const bf16x8 (&Q)[NC][D / 32], float c, float grow_above, int first,
+                                                  const int (&lim)[NC], const char *v, int lane)
+{
+    const int g4 = lane >> 4;
+    bool odd = false;               // not only numbers, and not for all columns
+    floatx4 S[2][NC];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int col = 0; col < NC; ++col) S[kb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
+    rows_times_resident<D, K_OFF, NC>(k_addr, Q, S);
+    if constexpr (MASKED) {                                 // a select, whatever the score is
+        odd = holds_no_numbers<D>(v, lane);
+#pragma unroll
+        for (int col = 0; col < NC; ++col) {
+            const int left = lim[col] - first - 4 * g4;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[kb][col][r] = 16 * kb + r < left ? S[kb][col][r] : -INFINITY;
+        }
+    }
+    // The offset only moves when a score exceeds it by more than 2^8 in the exponent.
+    float mx[NC];
+    bool grown = false;
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        mx[col] = max3(S[0][col][0], S[0][col][1], S[0][col][2]);
+        mx[col] = max3(mx[col], S[0][col][3], S[1][col][0]);
+        mx[col] = max3(mx[col], S[1][col][1], S[1][col][2]);
+        mx[col] = quad_lane_max(fmaxf(mx[col], S[1][col][3]));
+        grown = grown || mx[col] > st.m[col] + grow_above;
+    }
+    if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+        bool far = false;
+#pragma unroll
+        for (int col = 0; col < NC; ++col) {
+            const bool up = mx[col] > st.m[col] + grow_above;
+            const float alpha = up ? __builtin_amdgcn_exp2f((st.m[col] - mx[col]) * c) : 1.f;
+            st.m[col] = up ? mx[col] : st.m[col];
+            st.l[col] *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) st.acc[cb][col] *= alpha;
+            far = far || (fabsf(st.m[col] * c) > 1024.f && st.m[col] != -INFINITY);
+        }
+        st.far = __builtin_amdgcn_ballot_w64(far) != 0;
+    }
+    StagedTransposedProduct<D, V_OFF> pv;
+    pv.prefetch(v_addr);
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 P[NC];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const float m = st.m[col] == -INFINITY ? 0.f : st.m[col], mc = st.far ? 0.f : m * c;
+        if (__builtin_expect(st.far, 0)) {                  // the difference first, which is exact
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[kb][col][r] -= m;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(S[kb][col][r], c, -mc));
+                if constexpr (LSE) sum += e;
+                P[col][4 * kb + r] = static_cast<__bf16>(e);
+            }
+        if constexpr (LSE) st.l[col][0] += sum;
+    }
+    if constexpr (!LSE) {
+        bf16x8 ones;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
+#pragma unroll
+        for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[col], st.l[col]);
+    }
+    if (MASKED && __builtin_expect(odd, 0)) product_without_unseen<D, NC>(pv, v_addr, st.acc, P, lim, first, g4);
+    else pv.template run<NC>(v_addr, P, st.acc);
+}
+
+// Where a column's row lies.
+struct RowAt {
+    int token, head;                // inside the sequence and the group
+    bool on;
+};
+__device__ __forceinline__ RowAt row_at(uint32_t row, uint32_t rows, const PackedParams &p)
+{
+    const bool on = row < rows;
+    const uint32_t r = on ? row : rows - 1;
+    const uint32_t t = sta::fast_div(r, p.by_g);
+    return {(int)t, (int)(r - t * p.g), on};
+}
+
+template <int D, int NC>
+__device__ __forceinline__ void load_queries(const PackedParams &p, const PackedSeq &seq, uint32_t kv, const RowAt (&at)[NC], int g4, bf16x8 (&Q)[NC][D / 32])
+{
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const char *row = p.q.data + (int64_t)(seq.q0 + at[col].token) * p.q.token + (int64_t)(kv * p.g + at[col].head) * p.q.head;
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) Q[col][ks] = *reinterpret_cast<const bf16x8 *>(row + 64 * ks + 16 * g4);
+    }
+}
+
+// Partial sums of a tile's part: accumulators [R][D], then offsets (base-2 units) and sums of the rows.
+template <int D, int R>
+constexpr size_t part_floats() { return (size_t)R * D + 2 * R; }
+
+// How many parts a walk of n sub-blocks has, and where one ends: the last one takes what is left.
+__device__ __forceinline__ int parts_of(int n, const PackedParams &p)
+{
+    const int want = (n + (int)p.part_subs - 1) / (int)p.part_subs;
+    return want < (int)p.parts ? want : (int)p.parts;
+}
+__device__ __forceinline__ int part_end(uint32_t part, int n, const PackedParams &p)
+{
+    const int end = (int)((part + 1) * p.part_subs);
+    return part + 1 == p.parts || end > n ? n : end;
+}
+
+__device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, uint32_t kv, uint32_t part, size_t floats)
+{
+    return p.ws + ((slot * p.Hkv + kv) * p.parts + part) * floats;
+}
+
+template <int D, bool LSE>
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(PackedParams p)
+{
+    constexpr int NC = 2, CB = D / 16;
+    using LK = StagedRows<D>;
+    using LV = Staged<D>;
+    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, PER_WAVE = LV::Groups / 4;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    const uint32_t rank = sta::fast_div(item, p.by_parts), part = item - rank * p.parts;
+    PackedTile tile;
+    if (!find_tile<kTile, false>(rank, p, lane, &tile)) return;
+    const PackedSeq seq = tile.seq;
+    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * kTile;
+    const uint32_t last_row = row0 + kTile < rows ? row0 + kTile - 1 : rows - 1;
+    const int n_keys = uniform(seq.keys_of((int)sta::fast_div(last_row, p.by_g), p));
+    const int n_all = (n_keys + kSub - 1) / kSub;
+    const int sub0 = (int)(part * p.part_subs);
+    const int sub1 = part_end(part, n_all, p);
+    if (part > 0 && sub0 >= n_all) return;                  // the first part of a tile without keys writes its zeros
+
+    const uint32_t wave_row = row0 + 32 * wave;
+    const bool idle = wave_row >= rows;
+    RowAt at[NC];
+    int lim[NC];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        at[col] = row_at(wave_row + 16 * col + c16, rows, p);
+        lim[col] = seq.keys_of(at[col].token, p);
+    }
+    const uint32_t wave_last = wave_row + 31 < rows ? wave_row + 31 : rows - 1;
+    const int n_whole = uniform(seq.keys_of((int)sta::fast_div(row0, p.by_g), p));          // keys that all rows see
+    const int lim_hi = idle ? 0 : uniform(seq.keys_of((int)sta::fast_div(wave_last, p.by_g), p));
+
+    const char *kh = p.k.data + (int64_t)seq.k0 * p.k.token + (int64_t)kv * p.k.head;
+    const char *vh = p.v.data + (int64_t)seq.k0 * p.v.token + (int64_t)kv * p.v.head;
+    PackedDma<D, true> k_dma;
+    PackedDma<D, false> v_dma;
+    k_dma.start(lane, p.k.token);
+    v_dma.start(lane, p.v.token);
+    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
+        if (sub >= sub1) return;
+        char *to = smem + stage * STAGE;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int group = PER_WAVE * wave + i, first = sub * kSub + group * LV::GroupRows;
+            k_dma.bring(kh, p.k.token, first, seq.lk, to + group * LK::Group);
+            v_dma.bring(vh, p.v.token, first, seq.lk, to + V_AT + group * LV::Group);
+        }
+    };
+    issue(0, sub0);
+
+    bf16x8 Q[NC][D / 32];
+    load_queries<D, NC>(p, seq, kv, at, g4, Q);
+    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    const uint32_t k_addr = LK::address(base, lane);
+    uint32_t v_addr[4];
+    LV::transposed_addresses(base, lane, v_addr);
+    Softmax<D, NC, LSE> st;
+    st.start();
+    const float c = p.scale_log2e, grow_above = 8.0f / c;
+    auto step = [&](auto stage_c, auto masked_c, int sub) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage_c)::value;
+        constexpr bool MASKED = decltype(masked_c)::value;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's part of the stage has landed
+        __syncthreads();                                    // ... and everyone's, and nobody reads the other stage any more
+        issue(ST ^ 1, sub + 1);
+        const int first = sub * kSub;
+        if (!MASKED || first < lim_hi)
+            softmax_sub_block<D, NC, LSE, MASKED, ST * STAGE, ST * STAGE + V_AT>(st, k_addr, v_addr, Q, c, grow_above, first, lim, smem + ST * STAGE + V_AT,
+                                                                                 lane);
+    };
+    using Stage0 = std::integral_constant<int, 0>;
+    using Stage1 = std::integral_constant<int, 1>;
+    // pairs of sub-blocks that every row of the tile sees all of, then the others
+    int sub = sub0;
+#pragma unroll 1
+    for (; sub + 1 < sub1 && (sub + 2) * kSub <= n_whole; sub += 2) {
+        step(Stage0{}, std::false_type{}, sub);
+        step(Stage1{}, std::false_type{}, sub + 1);
+    }
+#pragma unroll 1
+    for (; sub < sub1; sub += 2) {
+        step(Stage0{}, std::true_type{}, sub);
+        if (sub + 1 < sub1) step(Stage1{}, std::true_type{}, sub + 1);
+    }
+
+    const bool whole = parts_of(n_all, p) <= 1;
+    if (!whole) {
+        float *ws = part_at(p, tile.slot, kv, part, part_floats<D, kTile>());
+#pragma unroll
+        for (int col = 0; col < NC; ++col) {
+            const int r = 32 * wave + 16 * col + c16;
+            const float l = st.sum(col);
+            if (idle) continue;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<floatx4 *>(ws + (size_t)r * D + 16 * cb + 4 * g4) = st.acc[cb][col];
+            if (g4 == 0) {
+                ws[(size_t)kTile * D + r] = st.m[col] * c;
+                ws[(size_t)kTile * D + kTile + r] = l;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const float l = st.sum(col), inv = l > 0.f ? 1.f / l : 0.f;
+        if (!at[col].on) continue;
+        const int64_t token = seq.q0 + at[col].token, head = kv * p.g + at[col].head;
+        char *row = p.o.data + token * p.o.token + head * p.o.head;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            bf16x4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(st.acc[cb][col][r] * inv);
+            *reinterpret_cast<bf16x4 *>(row + 32 * cb + 8 * g4) = v;
+        }
+        if (LSE && p.lse && g4 == 0) p.lse[head * p.tokens_q + token] = l > 0.f ? st.m[col] * c * kLn2 + __logf(l) : -INFINITY;
+    }
+}
+
+// Rows of one sequence and key head: at most 16 * NC.  Workgroup (part, key head, sequence).
+template <int D, int NC, bool LSE>
+__global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
+{
+    constexpr int CB = D / 16, R = 16 * NC;
+    using LK = StagedRows<D>;
+    using LV = Staged<D>;
+    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, OPS = LK::Groups + LV::Groups;
+    constexpr int WAVE = 2 * STAGE, MERGE = CB * NC * 1024;         // a wave's LDS; its accumulators at the end
+    static_assert(MERGE <= WAVE, "LDS");
+    __shared__ __attribute__((aligned(1024))) char smem[4 * WAVE];
+    __shared__ float2 stats[4][R];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    const uint32_t s = sta::fast_div(item, p.by_parts), part = item - s * p.parts;
+    PackedSeq seq = seq_of(s, p);
+    const uint32_t all_rows = (uint32_t)seq.lq * p.g, rows = all_rows < R ? all_rows : R;
+    if (rows == 0) return;
+    const int n_keys = uniform(seq.keys_of((int)sta::fast_div(rows - 1, p.by_g), p));
+    const int n_all = (n_keys + kSub - 1) / kSub;
+    const int sub0 = (int)(part * p.part_subs);
+    const int sub1 = part_end(part, n_all, p);
+    if (part > 0 && sub0 >= n_all) return;
+
+    RowAt at[NC];
+    int lim[NC];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        at[col] = row_at(16 * col + c16, rows, p);
+        lim[col] = seq.keys_of(at[col].token, p);
+    }
+    const int n_whole = uniform(seq.keys_of(0, p));         // keys that all rows see
+
+    const char *kh = p.k.data + (int64_t)seq.k0 * p.k.token + (int64_t)kv * p.k.head;
+    const char *vh = p.v.data + (int64_t)seq.k0 * p.v.token + (int64_t)kv * p.v.head;
+    PackedDma<D, true> k_dma;
+    PackedDma<D, false> v_dma;
+    k_dma.start(lane, p.k.token);
+    v_dma.start(lane, p.v.token);
+    char *own = smem + wave * WAVE;
+    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
+        char *to = own + stage * STAGE;
+#pragma unroll
+        for (int group = 0; group < LK::Groups; ++group) k_dma.bring(kh, p.k.token, sub * kSub + group * LV::GroupRows, seq.lk, to + group * LK::Group);
+#pragma unroll
+        for (int group = 0; group < LV::Groups; ++group) v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, to + V_AT + group * LV::Group);
+    };
+    int sub = sub0 + wave;
+    bf16x8 Q[NC][D / 32];
+    load_queries<D, NC>(p, seq, kv, at, g4, Q);
+    if (sub < sub1) issue(0, sub);
+    const uint32_t base = (uint32_t)(uintptr_t)own;
+    const uint32_t k_addr = LK::address(base, lane);
+    uint32_t v_addr[4];
+    LV::transposed_addresses(base, lane, v_addr);
+    Softmax<D, NC, LSE> st;
+    st.start();
+    const float c = p.scale_log2e, grow_above = 8.0f / c;
+    auto step = [&](auto stage_c, auto masked_c, int sub) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage_c)::value;
+        __builtin_amdgcn_sched_barrier(0);                  // reads of the other stage are done: their values have been used
+        if (sub + 4 < sub1) {
+            issue(ST ^ 1, sub + 4);
+            wait_dma<OPS>();
+        } else {
+            wait_dma<0>();
+        }
+        const int first = sub * kSub;
+        softmax_sub_block<D, NC, LSE, decltype(masked_c)::value, ST * STAGE, ST * STAGE + V_AT>(st, k_addr, v_addr, Q, c, grow_above, first, lim,
+                                                                                               own + ST * STAGE + V_AT, lane);
+    };
+    using Stage0 = std::integral_constant<int, 0>;
+    using Stage1 = std::integral_constant<int, 1>;
+#pragma unroll 1
+    for (; sub + 4 < sub1 && (sub + 5) * kSub <= n_whole; sub += 8) {
+        step(Stage0{}, std::false_type{}, sub);
+        step(Stage1{}, std::false_type{}, sub + 4);
+    }
+#pragma unroll 1
+    for (; sub < sub1; sub += 8) {
+        step(Stage0{}, std::true_type{}, sub);
+        if (sub + 4 < sub1) step(Stage1{}, std::true_type{}, sub + 4);
+    }
+
+    // ---- merge of the four waves: every wave sums the parts of its channel blocks, in ascending order
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int col = 0; col < NC; ++col) *reinterpret_cast<floatx4 *>(own + (cb * NC + col) * 1024 + lane * 16) = st.acc[cb][col];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const float l = st.sum(col);
+        if (g4 == 0) stats[wave][16 * col + c16] = make_float2(st.m[col] * c, l);
+    }
+    __syncthreads();
+    const bool whole = parts_of(n_all, p) <= 1;
+    float *ws = whole ? nullptr : part_at(p, s, kv, part, part_floats<D, R>());
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        float m = -INFINITY, l = 0.f, weight[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[w][16 * col + c16].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 x = stats[w][16 * col + c16];
+            weight[w] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+            l += x.y * weight[w];
+        }
+        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+        const int64_t token = seq.q0 + at[col].token, head = kv * p.g + at[col].head;
+#pragma unroll
+        for (int j = 0; j < CB / 4; ++j) {
+            const int cb = wave * (CB / 4) + j;
+            floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const floatx4 x = *reinterpret_cast<const floatx4 *>(smem + w * WAVE + (cb * NC + col) * 1024 + lane * 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] = fmaf(x[r], weight[w], sum[r]);
+            }
+            if (!at[col].on) continue;
+            if (whole) {
+                bf16x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(sum[r] * inv);
+                *reinterpret_cast<bf16x4 *>(p.o.data + token * p.o.token + head * p.o.head + 32 * cb + 8 * g4) = v;
+            } else {
+                *reinterpret_cast<floatx4 *>(ws + (size_t)(16 * col + c16) * D + 16 * cb + 4 * g4) = sum;
+            }
+        }
+        if (wave == 0 && g4 == 0 && at[col].on) {
+            if (!whole) {
+                ws[(size_t)R * D + 16 * col + c16] = m;
+                ws[(size_t)R * D + R + 16 * col + c16] = l;
+            } else if (LSE && p.lse) {
+                p.lse[head * p.tokens_q + token] = l > 0.f ? m * kLn2 + __logf(l) : -INFINITY;
+            }
+        }
+    }
+}
+
+// Joins the parts of the rows of a tile: O = sum_j 2^(m_j - m) O_j / sum_j 2^(m_j - m) l_j, in ascending order.  D / 4 lanes a row, four
+// channels a lane.
+template <int D, int R, bool TILES>
+__global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
+{
+    constexpr int LPR = D / 4, ROWS = 256 / LPR;
+    const int lane = threadIdx.x & 63;
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    PackedTile tile;
+    if constexpr (TILES) {
+        if (!find_tile<R, false>(item, p, lane, &tile)) return;
+    } else {
+        tile.seq = seq_of(item, p);
+        tile.index = 0;
+        tile.slot = item;
+    }
+    const PackedSeq seq = tile.seq;
+    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * R;
+    const uint32_t in_tile = rows - row0 < (uint32_t)R ? rows - row0 : (uint32_t)R;
+    if (rows == 0) return;
+    const uint32_t r = blockIdx.y * ROWS + threadIdx.x / LPR;
+    const int n_all = (seq.keys_of((int)sta::fast_div(row0 + in_tile - 1, p.by_g), p) + kSub - 1) / kSub;
+    const int n = parts_of(n_all, p), ch = 4 * (threadIdx.x % LPR);
+    if (r >= in_tile || n <= 1) return;
+    const size_t floats = part_floats<D, R>();
+    const float *ws = part_at(p, tile.slot, kv, 0, floats);
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < n; ++j) m = fmaxf(m, ws[j * floats + (size_t)R * D + r]);
+    floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < n; ++j) {
+        const float *part = ws + j * floats;
+        const float mj = part[(size_t)R * D + r], w = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - m);
+        l = fmaf(part[(size_t)R * D + R + r], w, l);
+        const floatx4 x = *reinterpret_cast<const floatx4 *>(part + (size_t)r * D + ch);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(x[i], w, sum[i]);
+    }
+    const RowAt at = row_at(row0 + r, rows, p);
+    const int64_t token = seq.q0 + at.token, head = kv * p.g + at.head;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    bf16x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>(sum[i] * inv);
+    *reinterpret_cast<bf16x4 *>(p.o.data + token * p.o.token + head * p.o.head + 2 * ch) = v;
+    if (p.lse && ch == 0) p.lse[head * p.tokens_q + token] = l > 0.f ? m * kLn2 + __logf(l) : -INFINITY;
+}
+
+}  // namespace
+
+namespace {
+
+PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(r.data), r.token * 2, r.head * 2}; }
+
+// How a launch is cut.  Rows of one sequence and key head that fit 16 or 32 columns take the kernel for few rows.
+struct PackedPlan {
+    int few;                        // 0: tiles of 128 rows; 1, 2: blocks of 16 columns
+    uint32_t slots;                 // tiles (few: sequences), an upper bound
+    uint32_t parts, part_subs;
+    size_t floats;                  // of one part
+    size_t workspace() const { return parts > 1 ? floats : 0; }
+};
+
+constexpr uint32_t kNoParts = 1u << 30;
+
+bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
+{
+    const int64_t g = Hq / Hkv, rows = g * max_q;
+    plan->few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+    const int R = plan->few ? 16 * plan->few : kTile;
+    int64_t slots = S;
+    if (!plan->few) {
+        const int64_t by_tokens = tokens_q * g / kTile + S, by_longest = (rows + kTile - 1) / kTile * S;
+        slots = by_tokens < by_longest ? by_tokens : by_longest;
+    }
+    plan->parts = 1;
+    plan->part_subs = kNoParts;
+    const int64_t items = slots * Hkv, subs = ((int64_t)max_k + kSub - 1) / kSub;
+    if (items > 0x7fffffff) return false;
+    plan->slots = (uint32_t)slots;
+    const int64_t cus = sta::compute_units(), want = cut ? (plan->few ? 4 : 6) * cus : 0;
+    if (items > 0 && items < want / 2) {
+        int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
+        if (each < 16) each = 16;
+        parts = (subs + each - 1) / each;
+        if (parts > 1 && items * parts <= 0x7fffffff) {
+            plan->parts = (uint32_t)parts;
+            plan->part_subs = (uint32_t)each;
+        }
+    }
+    plan->floats = (size_t)items * plan->parts * ((size_t)R * D + 2 * R);
+    return true;
+}
+
+template <int D, bool LSE>
+hipError_t launch_packed(const PackedParams &p, const PackedPlan &plan, hipStream_t stream)
+{
+    const dim3 grid(plan.slots * p.Hkv * plan.parts), block(256);
+    hipError_t e;
+    if (plan.few == 1) e = sta::launch_kernel(sta_packed_few_kernel<D, 1, LSE>, grid, block, stream, p);
+    else if (plan.few == 2) e = sta::launch_kernel(sta_packed_few_kernel<D, 2, LSE>, grid, block, stream, p);
+    else e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE>, grid, block, stream, p);
+    if (e != hipSuccess || plan.parts == 1) return e;
+    constexpr int ROWS = 1024 / D;
+    const uint32_t items = plan.slots * p.Hkv;
+    if (plan.few == 1) return sta::launch_kernel(sta_packed_merge_kernel<D, 16, false>, dim3(items, 16 / ROWS), block, stream, p);
+    if (plan.few == 2) return sta::launch_kernel(sta_packed_merge_kernel<D, 32, false>, dim3(items, 32 / ROWS), block, stream, p);
+    return sta::launch_kernel(sta_packed_merge_kernel<D, kTile, true>, dim3(items, kTile / ROWS), block, stream, p);
+}
+
+}  // namespace
+
+namespace sta {
+
+int packed_check(const sta_head_rows *r, int64_t tokens, int heads_of, int D, bool written)
+{
+    if (int rc = check_rows(r, written, 1, tokens > 0 ? tokens : 1, D)) return rc;
+    if (r->dtype != STA_BF16) return STA_ERR_UNSUPPORTED;
+    if (heads_of && r->heads != heads_of) return STA_ERR_SHAPE;
+    if (((uintptr_t)r->data & 15) || r->token % 8 || r->head % 8 || r->token >= (int64_t)1 << 26) return STA_ERR_SHAPE;
+    return STA_OK;
+}
+
+}  // namespace sta
+
+extern "C" {
+
+size_t sta_packed_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
+{
+    if (Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128) || S < 0 || tokens_q < 0 || max_q < 0 || max_k < 0) return 0;
+    PackedPlan plan;
+    return plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, true, &plan) ? plan.workspace() * sizeof(float) : 0;
+}
+
+int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o, float *lse,
+                       int64_t tokens_q, int64_t tokens_k, const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_used, int S, int max_q,
+                       int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!q || !k || !v || !o) return STA_ERR_NULL;
+    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > 0x7fffffff || tokens_k > 0x7fffffff) return STA_ERR_SHAPE;
+    if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
+    if (int rc = sta::packed_check(q, tokens_q, 0, D, false)) return rc;
+    if (int rc = sta::packed_check(k, tokens_k, 0, D, false)) return rc;
+    if (int rc = sta::packed_check(v, tokens_k, k->heads, D, false)) return rc;
+    if (int rc = sta::packed_check(o, tokens_q, q->heads, D, true)) return rc;
+    if (q->heads % k->heads || tokens_q * q->heads > 0x7fffffff) return STA_ERR_SHAPE;
+    if (S == 0 || tokens_q == 0 || max_q == 0) return STA_OK;
+    if (!cu_q || !cu_k) return STA_ERR_NULL;
+    if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)k_used | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
+    const int64_t nk = tokens_k > 0 ? tokens_k : 1;
+    if (rows_overlap(*o, tokens_q, *q, tokens_q, 1, D) || rows_overlap(*o, tokens_q, *k, nk, 1, D) || rows_overlap(*o, tokens_q, *v, nk, 1, D))
+        return STA_ERR_ALIAS;
+    PackedPlan plan;
+    if (!plan_of(q->heads, k->heads, D, S, tokens_q, max_q, max_k, workspace != nullptr, &plan)) return STA_ERR_SHAPE;
+    const struct { const sta_head_rows *r; int64_t n; } tensors[4] = {{q, tokens_q}, {k, nk}, {v, nk}, {o, tokens_q}};
+    if (workspace) {
+        if (((uintptr_t)workspace & 15) || workspace_bytes < plan.workspace() * sizeof(float)) return STA_ERR_WORKSPACE;
+        for (const auto &t : tensors)
+            if ((uintptr_t)workspace < (uintptr_t)t.r->data + extent_of(*t.r, 1, t.n, D) && (uintptr_t)t.r->data < (uintptr_t)workspace + workspace_bytes)
+                return STA_ERR_ALIAS;
+    }
+    if (lse) {
+        const uintptr_t l0 = (uintptr_t)lse, l1 = l0 + (size_t)tokens_q * q->heads * sizeof(float);
+        for (const auto &t : tensors)
+            if (l0 < (uintptr_t)t.r->data + extent_of(*t.r, 1, t.n, D) && (uintptr_t)t.r->data < l1) return STA_ERR_ALIAS;
+        if (workspace && l0 < (uintptr_t)workspace + workspace_bytes && (uintptr_t)workspace < l1) return STA_ERR_ALIAS;
+    }
+    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
+    PackedParams p = {};
+    p.q = packed_rows_of(*q);
+    p.k = packed_rows_of(*k);
+    p.v = packed_rows_of(*v);
+    p.o = packed_rows_of(*o);
+    p.lse = lse;
+    p.cu_q = cu_q;
+    p.cu_k = cu_k;
+    p.k_used = k_used;
+    p.S = S;
+    p.tokens_q = (uint32_t)tokens_q;
+    p.tokens_k = (uint32_t)tokens_k;
+    p.Hkv = k->heads;
+    p.g = q->heads / k->heads;
+    p.by_g = sta::fast_div_of(p.g);
+    p.by_Hkv = sta::fast_div_of(p.Hkv);
+    p.by_parts = sta::fast_div_of(plan.parts);
+    p.causal = causal != 0;
+    p.scale = scale;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.parts = plan.parts;
+    p.part_subs = plan.part_subs;
+    p.ws = static_cast<float *>(workspace);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    hipError_t e;
+    if (D == 64) e = lse ? launch_packed<64, true>(p, plan, stream) : launch_packed<64, false>(p, plan, stream);
+    else e = lse ? launch_packed<128, true>(p, plan, stream) : launch_packed<128, false>(p, plan, stream);
+    return e == hipSuccess ? STA_OK : STA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,476 @@
+// Gradients of the attention over packed sequences.
+//
+//   P_ij = exp(S_ij - lse_i),  dV_j = sum_i P_ij dO_i,  dP_ij = dO_i . V_j,  dS_ij = P_ij (dP_ij - delta_i),  delta_i = dO_i . O_i
+//   dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i       (i: the rows of all heads of a group)
+//
+// Three kernels, no atomics:
+//   sta_packed_stats_kernel   -delta_i and -lse_i / scale of every row, in the order of the rows;
+//   sta_packed_dq_kernel      four waves of 32 rows walk the keys they see: three products per block;
+//   sta_packed_dkv_kernel     four waves of 32 keys walk the rows that see them: four products per block.
+// The heads of a group are rows like any others, so their gradients of K and V are summed in the accumulators.  Matrix pipe bound.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <utility>
+
+#include "../../include/sta.h"
+#include "sta_packed.h"
+#include "sta_rows_check.h"
+
+namespace {
+
+constexpr int kTile = 128;          // rows or keys of a workgroup
+
+struct BackwardParams {
+    PackedParams p;                 // q, k, v, o and the bounds
+    PackedRows d_o, d_q, d_k, d_v;
+    const float *lse;               // [Hq, tokens_q]
+    float *neg_lse, *neg_delta;     // [Hkv, tokens_q, g], in raw scores
+    float inv_scale;
+};
+
+// ---- statistics: D / 8 lanes a row
+template <int D>
+__global__ __launch_bounds__(256) void sta_packed_stats_kernel(BackwardParams b)
+{
+    constexpr int LPR = D / 8;
+    const PackedParams &p = b.p;
+    const uint32_t row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;      // token * g + head of the group
+    const uint32_t kv = blockIdx.y;
+    const bool on = row < p.tokens_q * p.g;
+    const uint32_t r = on ? row : 0, t = sta::fast_div(r, p.by_g);
+    const int64_t head = (int64_t)kv * p.g + (r - t * p.g);
+    const bf16x8 o = *reinterpret_cast<const bf16x8 *>(p.o.data + (int64_t)t * p.o.token + head * p.o.head + 16 * c);
+    const bf16x8 g = *reinterpret_cast<const bf16x8 *>(b.d_o.data + (int64_t)t * b.d_o.token + head * b.d_o.head + 16 * c);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = fmaf((float)o[i], (float)g[i], sum);
+#pragma unroll
+    for (int m = LPR / 2; m > 0; m /= 2) sum += __shfl_xor(sum, m, 64);
+    if (on && c == 0) {
+        const size_t at = (size_t)kv * p.tokens_q * p.g + row;
+        b.neg_delta[at] = -sum;
+        b.neg_lse[at] = -b.lse[head * p.tokens_q + t] * b.inv_scale;
+    }
+}
+
+// Columns of a wave out of their accumulators: [channel block][column block] of the transposed result.
+template <int D, int NC>
+__device__ __forceinline__ void store_column(const floatx4 (&acc)[D / 16][NC], int col, float factor, char *row, int g4)
+{
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) {
+        bf16x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(acc[cb][col][r] * factor);
+        *reinterpret_cast<bf16x4 *>(row + 32 * cb + 8 * g4) = v;
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
+{
+    const PackedParams &p = b.p;
+    constexpr int NC = 2, KS = D / 32, CB = D / 16;
+    using LK = Staged<D>;
+    using LV = StagedRows<D>;
+    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, PER_WAVE = LK::Groups / 4;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
+    PackedTile tile;
+    if (!find_tile<kTile, false>(rank, p, lane, &tile)) return;
+    const PackedSeq seq = tile.seq;
+    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * kTile;
+    const uint32_t last_row = row0 + kTile < rows ? row0 + kTile - 1 : rows - 1;
+    const int n_keys = uniform(seq.keys_of((int)sta::fast_div(last_row, p.by_g), p));
+    const int n_sub = (n_keys + kSub - 1) / kSub;
+
+    const uint32_t wave_row = row0 + 32 * wave;
+    const bool idle = wave_row >= rows;
+    int token[NC], lim[NC];
+    int64_t head[NC];
+    bool on[NC];
+    float neg_lse[NC], neg_delta[NC];
+    bf16x8 Q[NC][KS], G[NC][KS];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const uint32_t row = wave_row + 16 * col + c16;
+        on[col] = row < rows;
+        const uint32_t r = on[col] ? row : rows - 1, t = sta::fast_div(r, p.by_g);
+        token[col] = (int)t;
+        head[col] = (int64_t)kv * p.g + (r - t * p.g);
+        lim[col] = seq.keys_of((int)t, p);
+        const size_t stat = ((size_t)kv * p.tokens_q + seq.q0) * p.g + r;
+        neg_lse[col] = b.neg_lse[stat];
+        neg_delta[col] = b.neg_delta[stat];
+        const char *q = p.q.data + (int64_t)(seq.q0 + token[col]) * p.q.token + head[col] * p.q.head;
+        const char *g = b.d_o.data + (int64_t)(seq.q0 + token[col]) * b.d_o.token + head[col] * b.d_o.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Q[col][ks] = *reinterpret_cast<const bf16x8 *>(q + 64 * ks + 16 * g4);
+            G[col][ks] = *reinterpret_cast<const bf16x8 *>(g + 64 * ks + 16 * g4);
+        }
+    }
+    const uint32_t wave_last = wave_row + 31 < rows ? wave_row + 31 : rows - 1;
+    const int lim_lo = idle ? 0 : uniform(seq.keys_of((int)sta::fast_div(wave_row, p.by_g), p));
+    const int lim_hi = idle ? 0 : uniform(seq.keys_of((int)sta::fast_div(wave_last, p.by_g), p));
+
+    const char *kh = p.k.data + (int64_t)seq.k0 * p.k.token + (int64_t)kv * p.k.head;
+    const char *vh = p.v.data + (int64_t)seq.k0 * p.v.token + (int64_t)kv * p.v.head;
+    PackedDma<D, false> k_dma;
+    PackedDma<D, true> v_dma;
+    k_dma.start(lane, p.k.token);
+    v_dma.start(lane, p.v.token);
+    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
+        if (sub >= n_sub) return;
+        char *to = smem + stage * STAGE;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int group = PER_WAVE * wave + i, first = sub * kSub + group * LK::GroupRows;
+            k_dma.bring(kh, p.k.token, first, seq.lk, to + group * LK::Group);
+            v_dma.bring(vh, p.v.token, first, seq.lk, to + V_AT + group * LV::Group);
+        }
+    };
+    issue(0, 0);
+    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    uint32_t k_addr[KS], k_tr[4];
+    LK::addresses(base, lane, k_addr, k_tr);
+    const uint32_t v_addr = LV::address(base + V_AT, lane);
+    floatx4 acc[CB][NC];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int col = 0; col < NC; ++col) acc[cb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const float c = p.scale_log2e;
+    auto step = [&](auto stage_c, int sub) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage_c)::value * STAGE;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        issue(decltype(stage_c)::value ^ 1, sub + 1);
+        const int first = sub * kSub;
+        if (first >= lim_hi) return;
+        floatx4 S[2][NC], dP[2][NC];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    S[kb][col][r] = neg_lse[col];
+                    dP[kb][col][r] = neg_delta[col];
+                }
+        staged_rows_times_resident<D, ST, NC>(k_addr, Q, S);                        // K Q^T - lse / scale
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[kb][col][r] = __builtin_amdgcn_exp2f(S[kb][col][r] * c);
+        rows_times_resident<D, ST, NC>(v_addr, G, dP);                              // V dO^T - delta
+        StagedTransposedProduct<D, ST> product;
+        product.prefetch(k_tr);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[kb][col][r] *= dP[kb][col][r];
+        if (first + kSub > lim_lo) {                                                // a select, whatever the product is
+#pragma unroll
+            for (int col = 0; col < NC; ++col) {
+                const int left = lim[col] - first - 4 * g4;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[kb][col][r] = 16 * kb + r < left ? S[kb][col][r] : 0.f;
+            }
+        }
+        bf16x8 dS[NC];
+#pragma unroll
+        for (int col = 0; col < NC; ++col)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dS[col][4 * kb + r] = static_cast<__bf16>(S[kb][col][r]);
+        product.template run<NC>(k_tr, dS, acc);                                    // dQ^T += K^T dS^T
+    };
+#pragma unroll 1
+    for (int sub = 0; sub < n_sub; sub += 2) {
+        step(std::integral_constant<int, 0>{}, sub);
+        if (sub + 1 < n_sub) step(std::integral_constant<int, 1>{}, sub + 1);
+    }
+#pragma unroll
+    for (int col = 0; col < NC; ++col)
+        if (on[col]) store_column<D, NC>(acc, col, p.scale, b.d_q.data + (int64_t)(seq.q0 + token[col]) * b.d_q.token + head[col] * b.d_q.head, g4);
+}
+
+template <int D>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void sta_packed_dkv_kernel(BackwardParams b)
+{
+    const PackedParams &p = b.p;
+    constexpr int NC = 2, KS = D / 32, CB = D / 16;
+    using L = Staged<D>;
+    constexpr int STATS = 2 * L::Tile, STAGE = STATS + 1024, G_AT = L::Tile, PER_WAVE = L::Groups / 4, LPR = D / 8;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
+    PackedTile tile;
+    if (!find_tile<kTile, true>(rank, p, lane, &tile)) return;
+    const PackedSeq seq = tile.seq;
+    const int rows = seq.lq * (int)p.g, key0 = (int)tile.index * kTile, ahead = seq.lk - seq.lq;
+    // key j is seen by the rows from first_row(j) on
+    auto first_row = [&](int j) {
+        const int t = j - ahead;
+        return !p.causal || t <= 0 ? 0 : t < seq.lq ? t * (int)p.g : rows;
+    };
+    const int sub0 = uniform(first_row(key0) / kSub), n_sub = (rows + kSub - 1) / kSub;
+    const int wave_key = key0 + 32 * wave;
+    const int see_lo = uniform(first_row(wave_key)), see_hi = uniform(first_row(wave_key + 31));        // of the wave's first and last key
+    int from[NC];
+    bf16x8 K[NC][KS], V[NC][KS];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const int key = wave_key + 16 * col + c16, j = key < seq.lk ? key : seq.lk - 1;
+        from[col] = first_row(key);
+        const char *k = p.k.data + (int64_t)(seq.k0 + j) * p.k.token + (int64_t)kv * p.k.head;
+        const char *v = p.v.data + (int64_t)(seq.k0 + j) * p.v.token + (int64_t)kv * p.v.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            K[col][ks] = *reinterpret_cast<const bf16x8 *>(k + 64 * ks + 16 * g4);
+            V[col][ks] = *reinterpret_cast<const bf16x8 *>(v + 64 * ks + 16 * g4);
+        }
+    }
+    // DMA: row -> (token, head); its 16-byte chunk at this lane's place
+    const int r_in = lane / LPR, pos = lane % LPR;
+    const uint32_t chunk = (uint32_t)(D == 128 ? (pos ^ (r_in << 2)) << 4 : (pos ^ (((r_in >> 1) & 3) << 1)) << 4);
+    const char *qh = p.q.data + (int64_t)seq.q0 * p.q.token + (int64_t)kv * p.g * p.q.head + chunk;
+    const char *gh = b.d_o.data + (int64_t)seq.q0 * b.d_o.token + (int64_t)kv * p.g * b.d_o.head + chunk;
+    const float *stats = (lane < kSub ? b.neg_lse : b.neg_delta) + ((size_t)kv * p.tokens_q + seq.q0) * p.g;
+    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
+        if (sub >= n_sub) return;
+        char *to = smem + stage * STAGE;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int group = PER_WAVE * wave + i, row = sub * kSub + group * L::GroupRows + r_in;
+            const uint32_t r = (uint32_t)(row < rows ? row : rows - 1), t = sta::fast_div(r, p.by_g), h = r - t * p.g;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(qh + (int64_t)t * p.q.token + (int64_t)h * p.q.head),
+                                             STA_LDS_PTR(to + group * L::Group), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + (int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head),
+                                             STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
+        }
+        if (wave == 3) {
+            const int row = sub * kSub + (lane & (kSub - 1));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(stats + (row < rows ? row : rows - 1)),
+                                             STA_LDS_PTR(to + STATS), 4, 0, 0);
+        }
+    };
+    issue(0, sub0);
+    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    uint32_t row_addr[KS], tr_addr[4];
+    L::addresses(base, lane, row_addr, tr_addr);
+    const uint32_t stat_addr = base + STATS + 16 * g4;
+    floatx4 dK[CB][NC], dV[CB][NC];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int col = 0; col < NC; ++col) dK[cb][col] = dV[cb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const float c = p.scale_log2e;
+    auto step = [&](auto stage_c, int sub) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage_c)::value * STAGE;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        issue(decltype(stage_c)::value ^ 1, sub + 1);
+        const int first = sub * kSub;
+        if (first + kSub <= see_lo || wave_key >= seq.lk) return;
+        auto start = [&](auto off_c) {                      // four rows' statistics for every register of a row block
+            floatx4 x[2];
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            u32x4 a, d;
+            asm volatile("ds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(a), "=&v"(d)
+                         : "v"(stat_addr), "n"(ST + decltype(off_c)::value), "n"(ST + decltype(off_c)::value + 64));
+            x[0] = __builtin_bit_cast(floatx4, a);
+            x[1] = __builtin_bit_cast(floatx4, d);
+            return std::pair<floatx4, floatx4>(x[0], x[1]);
+        };
+        floatx4 S[2][NC];
+        {
+            const auto x = start(std::integral_constant<int, 0>{});
+#pragma unroll
+            for (int col = 0; col < NC; ++col) { S[0][col] = x.first; S[1][col] = x.second; }
+        }
+        staged_rows_times_resident<D, ST, NC>(row_addr, K, S);                      // Q K^T - lse / scale
+        StagedTransposedProduct<D, ST + G_AT> for_v;
+        for_v.prefetch(tr_addr);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[qb][col][r] = __builtin_amdgcn_exp2f(S[qb][col][r] * c);
+        if (first < see_hi || first + kSub > rows) {
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = first + 16 * qb + 4 * g4 + r;
+                        S[qb][col][r] = row >= from[col] && row < rows ? S[qb][col][r] : 0.f;
+                    }
+        }
+        bf16x8 packed[NC];
+        auto pack = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) packed[col][4 * qb + r] = static_cast<__bf16>(S[qb][col][r]);
+        };
+        pack();
+        for_v.template run<NC>(tr_addr, packed, dV);                                // dV^T += dO^T P
+        floatx4 dP[2][NC];
+        {
+            const auto x = start(std::integral_constant<int, kSub * 4>{});
+#pragma unroll
+            for (int col = 0; col < NC; ++col) { dP[0][col] = x.first; dP[1][col] = x.second; }
+        }
+        staged_rows_times_resident<D, ST + G_AT, NC>(row_addr, V, dP);              // dO V^T - delta
+        StagedTransposedProduct<D, ST> for_k;
+        for_k.prefetch(tr_addr);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[qb][col][r] *= dP[qb][col][r];
+        pack();
+        for_k.template run<NC>(tr_addr, packed, dK);                                // dK^T += Q^T dS
+    };
+#pragma unroll 1
+    for (int sub = sub0; sub < n_sub; sub += 2) {
+        step(std::integral_constant<int, 0>{}, sub);
+        if (sub + 1 < n_sub) step(std::integral_constant<int, 1>{}, sub + 1);
+    }
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const int key = wave_key + 16 * col + c16;
+        if (key >= seq.lk) continue;
+        store_column<D, NC>(dV, col, 1.0f, b.d_v.data + (int64_t)(seq.k0 + key) * b.d_v.token + (int64_t)kv * b.d_v.head, g4);
+        store_column<D, NC>(dK, col, p.scale, b.d_k.data + (int64_t)(seq.k0 + key) * b.d_k.token + (int64_t)kv * b.d_k.head, g4);
+    }
+}
+
+template <int D>
+hipError_t launch_gradients(const BackwardParams &b, uint32_t row_tiles, uint32_t key_tiles, hipStream_t stream)
+{
+    const PackedParams &p = b.p;
+    constexpr uint32_t PER = 256 / (D / 8);
+    hipError_t e = hipSuccess;
+    if (p.tokens_q > 0) {
+        e = sta::launch_kernel(sta_packed_stats_kernel<D>, dim3((p.tokens_q * p.g + PER - 1) / PER, p.Hkv), dim3(256), stream, b);
+        if (e == hipSuccess) e = sta::launch_kernel(sta_packed_dq_kernel<D>, dim3(row_tiles * p.Hkv), dim3(256), stream, b);
+    }
+    if (e == hipSuccess && key_tiles > 0) e = sta::launch_kernel(sta_packed_dkv_kernel<D>, dim3(key_tiles * p.Hkv), dim3(256), stream, b);
+    return e;
+}
+
+// Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than max_length x g.
+int64_t tiles_of(int64_t tokens, int64_t g, int S, int64_t max_length)
+{
+    const int64_t by_tokens = tokens * g / kTile + S, by_longest = (max_length * g + kTile - 1) / kTile * S;
+    return by_tokens < by_longest ? by_tokens : by_longest;
+}
+
+constexpr size_t kStatPad = 64;     // floats behind either array
+
+}  // namespace
+
+extern "C" {
+
+size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q)
+{
+    if (Hq < 1 || tokens_q < 0 || tokens_q > 0x7fffffff) return 0;
+    return 2 * ((size_t)Hq * tokens_q + kStatPad) * sizeof(float);
+}
+
+int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o, const sta_head_rows *d_o,
+                        const float *lse, const sta_head_rows *d_q, const sta_head_rows *d_k, const sta_head_rows *d_v, int64_t tokens_q,
+                        int64_t tokens_k, const int32_t *cu_q, const int32_t *cu_k, int S, int max_q, int max_k, int D, int causal, float scale,
+                        void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!q || !k || !v || !o || !d_o || !lse || !d_q || !d_k || !d_v) return STA_ERR_NULL;
+    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > 0x7fffffff || tokens_k > 0x7fffffff) return STA_ERR_SHAPE;
+    if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
+    const sta_head_rows *in[5] = {q, k, v, o, d_o}, *out[3] = {d_q, d_k, d_v};
+    const int64_t nq = tokens_q > 0 ? tokens_q : 1, nk = tokens_k > 0 ? tokens_k : 1;
+    const int64_t n_in[5] = {nq, nk, nk, nq, nq}, n_out[3] = {nq, nk, nk};
+    for (int i = 0; i < 5; ++i)
+        if (int rc = sta::packed_check(in[i], n_in[i], i == 0 || i == 1 ? 0 : i == 2 ? k->heads : q->heads, D, false)) return rc;
+    for (int i = 0; i < 3; ++i)
+        if (int rc = sta::packed_check(out[i], n_out[i], i == 0 ? q->heads : k->heads, D, true)) return rc;
+    if (q->heads % k->heads || tokens_q * q->heads > 0x7fffffff) return STA_ERR_SHAPE;
+    if (S == 0 || (tokens_q == 0 && tokens_k == 0)) return STA_OK;
+    if (!cu_q || !cu_k) return STA_ERR_NULL;
+    if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sta_packed_backward_workspace_bytes(q->heads, tokens_q)) return STA_ERR_WORKSPACE;
+    const uintptr_t w0 = (uintptr_t)workspace, w1 = w0 + sta_packed_backward_workspace_bytes(q->heads, tokens_q);
+    const uintptr_t l0 = (uintptr_t)lse, l1 = l0 + (size_t)tokens_q * q->heads * sizeof(float);
+    auto meets = [&](const sta_head_rows &r, int64_t n, uintptr_t a0, uintptr_t a1) {
+        return a0 < (uintptr_t)r.data + extent_of(r, 1, n, D) && (uintptr_t)r.data < a1;
+    };
+    if (w0 < l1 && l0 < w1) return STA_ERR_ALIAS;
+    for (int j = 0; j < 3; ++j) {
+        for (int i = 0; i < 5; ++i)
+            if (rows_overlap(*in[i], n_in[i], *out[j], n_out[j], 1, D)) return STA_ERR_ALIAS;
+        for (int i = 0; i < j; ++i)
+            if (rows_overlap(*out[i], n_out[i], *out[j], n_out[j], 1, D)) return STA_ERR_ALIAS;
+        if (meets(*out[j], n_out[j], w0, w1) || meets(*out[j], n_out[j], l0, l1)) return STA_ERR_ALIAS;
+    }
+    for (int i = 0; i < 5; ++i)
+        if (meets(*in[i], n_in[i], w0, w1)) return STA_ERR_ALIAS;
+    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
+    BackwardParams b = {};
+    PackedParams &p = b.p;
+    auto rows = [](const sta_head_rows &r) { return PackedRows{static_cast<char *>(r.data), r.token * 2, r.head * 2}; };
+    p.q = rows(*q);
+    p.k = rows(*k);
+    p.v = rows(*v);
+    p.o = rows(*o);
+    b.d_o = rows(*d_o);
+    b.d_q = rows(*d_q);
+    b.d_k = rows(*d_k);
+    b.d_v = rows(*d_v);
+    p.cu_q = cu_q;
+    p.cu_k = cu_k;
+    p.S = S;
+    p.tokens_q = (uint32_t)tokens_q;
+    p.tokens_k = (uint32_t)tokens_k;
+    p.Hkv = k->heads;
+    p.g = q->heads / k->heads;
+    p.by_g = sta::fast_div_of(p.g);
+    p.by_Hkv = sta::fast_div_of(p.Hkv);
+    p.by_parts = sta::fast_div_of(1);
+    p.causal = causal != 0;
+    p.scale = scale;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.parts = 1;
+    b.lse = lse;
+    b.neg_lse = static_cast<float *>(workspace);
+    b.neg_delta = b.neg_lse + (size_t)q->heads * tokens_q + kStatPad;
+    b.inv_scale = 1.0f / scale;
+    const int64_t row_tiles = tiles_of(tokens_q, p.g, S, max_q), key_tiles = tiles_of(tokens_k, 1, S, max_k);
+    if (row_tiles * p.Hkv > 0x7fffffff || key_tiles * p.Hkv > 0x7fffffff || p.Hkv > 65535) return STA_ERR_SHAPE;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = D == 64 ? launch_gradients<64>(b, (uint32_t)row_tiles, (uint32_t)key_tiles, stream)
+                                 : launch_gradients<128>(b, (uint32_t)row_tiles, (uint32_t)key_tiles, stream);
+    return e == hipSuccess ? STA_OK : STA_ERR_HIP;
+}
+
+}  // extern "C"

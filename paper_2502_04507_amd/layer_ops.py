@@ -35,6 +35,13 @@ def _bind(lib):
     lib.sta_qk_norm_rope_workspace_bytes.argtypes = [ci]
     lib.sta_qk_norm_rope_workspace_bytes.restype = sz
     lib.sta_qk_norm_rope_backward.argtypes = [rows] * 8 + [vp, vp, ci, vp, vp, cf, ctypes.POINTER(_Rotary), ci, ci, ci, i3, i3, vp, sz, vp]
+    i64 = ctypes.c_int64
+    lib.sta_packed_workspace_bytes.argtypes = [ci, ci, ci, ci, i64, ci, ci]
+    lib.sta_packed_workspace_bytes.restype = sz
+    lib.sta_packed_forward.argtypes = [rows] * 4 + [vp, i64, i64, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, sz, vp]
+    lib.sta_packed_backward_workspace_bytes.argtypes = [ci, i64]
+    lib.sta_packed_backward_workspace_bytes.restype = sz
+    lib.sta_packed_backward.argtypes = [rows] * 5 + [vp] + [rows] * 3 + [i64, i64, vp, vp, ci, ci, ci, ci, ci, cf, vp, sz, vp]
     lib._layer_ops_bound = True
     return lib
 
@@ -193,4 +200,81 @@ def sta_qk_norm_rope_backward(q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_
     ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
     _check(_lib().sta_qk_norm_rope_backward(*rows, wq, wk, dtype, *dw, eps, None if rotary is None else rotary._struct(B, N), B, N, D, g, t, ws,
                                             nbytes, _stream_ptr(stream)))
+    return d_q, d_k, d_v
+
+
+def _packed_rows(t, name, tokens, heads, D):
+    """One [tokens, H, D] tensor, its channels adjacent."""
+    if t.dim() != 3 or t.shape != (tokens, heads, D):
+        raise ValueError("%s must be [tokens, heads, D] like the others" % name)
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be bfloat16" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must live in device memory" % name)
+    token, head, channel = t.stride()
+    if channel != 1:
+        raise ValueError("the channels of %s must be adjacent" % name)
+    return _HeadRows(t.data_ptr() or 16, 0, token, head, heads, STA_BF16)
+
+
+def _bounds(t, name, n):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != (n,):
+        raise ValueError("%s must be int32 [%d]" % (name, n))
+    return _dev(t, name)
+
+
+def _packed_shapes(q, k):
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("expect [tokens, heads, D] tensors")
+    (tq, Hq, D), (tk, Hkv, _) = q.shape, k.shape
+    return tq, Hq, D, tk, Hkv
+
+
+def _lse_ptr(lse, Hq, tq):
+    if lse is None:
+        return None
+    if lse.dtype != torch.float32 or lse.shape != (Hq, tq):
+        raise ValueError("lse must be float32 [Hq, tokens]")
+    return _dev(lse, "lse") or 16
+
+
+def sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k) -> int:
+    return int(_lib().sta_packed_workspace_bytes(int(Hq), int(Hkv), int(D), int(S), int(tokens_q), int(max_q), int(max_k)))
+
+
+def sta_packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal=True, scale=0.0, lse=None, k_used=None, workspace=None, stream=None):
+    """Attention over packed sequences: q, o bf16 [tokens, Hq, D], k, v bf16 [key tokens, Hkv, D] (strided views with adjacent channels); cu_q, cu_k
+    int32 [S + 1] where the sequences begin, k_used int32 [S] or None; lse float32 [Hq, tokens] or None; max_q, max_k upper bounds of the lengths."""
+    tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
+    S = cu_q.numel() - 1
+    if S < 0:
+        raise ValueError("cu_q needs an entry more than there are sequences")
+    ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
+    _check(_lib().sta_packed_forward(_packed_rows(q, "q", tq, Hq, D), _packed_rows(k, "k", tk, Hkv, D), _packed_rows(v, "v", tk, Hkv, D),
+                                     _packed_rows(o, "o", tq, Hq, D), _lse_ptr(lse, Hq, tq), tq, tk, _bounds(cu_q, "cu_q", S + 1),
+                                     _bounds(cu_k, "cu_k", S + 1), _bounds(k_used, "k_used", S), S, max_q, max_k, D, int(bool(causal)), scale, ws,
+                                     nbytes, _stream_ptr(stream)))
+    return o
+
+
+def sta_packed_backward_workspace_bytes(Hq, tokens_q) -> int:
+    return int(_lib().sta_packed_backward_workspace_bytes(int(Hq), int(tokens_q)))
+
+
+def sta_packed_backward(q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, max_k, workspace, causal=True, scale=0.0, stream=None):
+    """Gradients of sta_packed_forward; tensors as there, workspace: device bytes, at least sta_packed_backward_workspace_bytes(Hq, tokens)."""
+    tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
+    S = cu_q.numel() - 1
+    if S < 0:
+        raise ValueError("cu_q needs an entry more than there are sequences")
+    if lse is None:
+        raise ValueError("lse is needed")
+    _check(_lib().sta_packed_backward(_packed_rows(q, "q", tq, Hq, D), _packed_rows(k, "k", tk, Hkv, D), _packed_rows(v, "v", tk, Hkv, D),
+                                      _packed_rows(o, "o", tq, Hq, D), _packed_rows(d_o, "d_o", tq, Hq, D), _lse_ptr(lse, Hq, tq),
+                                      _packed_rows(d_q, "d_q", tq, Hq, D), _packed_rows(d_k, "d_k", tk, Hkv, D),
+                                      _packed_rows(d_v, "d_v", tk, Hkv, D), tq, tk, _bounds(cu_q, "cu_q", S + 1), _bounds(cu_k, "cu_k", S + 1), S,
+                                      max_q, max_k, D, int(bool(causal)), scale, _dev(workspace, "workspace"),
+                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
     return d_q, d_k, d_v
