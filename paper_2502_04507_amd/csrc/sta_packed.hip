@@ -62,13 +62,14 @@ __device__ __forceinline__ bool holds_no_numbers(const char *v, int lane)
 
 // O^T += V^T P^T for a sub-block whose V holds infinities or NaN and of which some column does not see all keys: a probability of 0
 // times one of those is no 0.  Numbers go through the product as ever; how many infinities of either sign and NaN a column sees is three
-// products more with ones in their places, and a column that sees one gets it.  The first operands of pv are on their way.
+// products more with ones in their places, and a column that sees one gets it.
 template <int D, int NC, int V_OFF>
-__device__ __forceinline__ void product_without_unseen(StagedTransposedProduct<D, V_OFF> &pv, const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC],
+__device__ __forceinline__ void product_without_unseen(const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC],
                                                        const bf16x8 (&P)[NC], const int (&lim)[NC], int first, int g4)
 {
     using Product = StagedTransposedProduct<D, V_OFF>;
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    Product pv;
     bf16x8 sees[NC];
 #pragma unroll
     for (int col = 0; col < NC; ++col)
@@ -76,7 +77,7 @@ __device__ __forceinline__ void product_without_unseen(StagedTransposedProduct<D
         for (int i = 0; i < 8; ++i) sees[col][i] = static_cast<__bf16>(first + 4 * g4 + (i < 4 ? i : 12 + i) < lim[col] ? 1.0f : 0.0f);
     static_for<0, Product::NG>([&](auto gc) {
         constexpr int g = decltype(gc)::value;
-        if constexpr (g > 0) pv.template issue<g>(v_addr);
+        pv.template issue<g>(v_addr);
         pv_wait<0>(pv.frag[g]);
         static_for<0, 4>([&](auto ic) {
             constexpr int i = decltype(ic)::value, cb = 4 * g + i;
@@ -173,19 +174,24 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
         }
         st.far = __builtin_amdgcn_ballot_w64(far) != 0;
     }
-    StagedTransposedProduct<D, V_OFF> pv;
-    pv.prefetch(v_addr);
-    __builtin_amdgcn_sched_barrier(0);
-    bf16x8 P[NC];
+    if (__builtin_expect(st.far, 0)) {                      // the difference first, which is exact
 #pragma unroll
-    for (int col = 0; col < NC; ++col) {
-        const float m = st.m[col] == -INFINITY ? 0.f : st.m[col], mc = st.far ? 0.f : m * c;
-        if (__builtin_expect(st.far, 0)) {                  // the difference first, which is exact
+        for (int col = 0; col < NC; ++col)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[kb][col][r] -= m;
-        }
+                for (int r = 0; r < 4; ++r) S[kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
+    }
+    // Reads on their way are not carried over a branch: the compiler, which does not know that they are, may move their registers there.
+    StagedTransposedProduct<D, V_OFF> pv;
+    if constexpr (!MASKED) {
+        pv.prefetch(v_addr);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    bf16x8 P[NC];
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const float mc = st.far || st.m[col] == -INFINITY ? 0.f : st.m[col] * c;
         float sum = 0.f;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -204,8 +210,14 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
 #pragma unroll
         for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[col], st.l[col]);
     }
-    if (MASKED && __builtin_expect(odd, 0)) product_without_unseen<D, NC>(pv, v_addr, st.acc, P, lim, first, g4);
-    else pv.template run<NC>(v_addr, P, st.acc);
+    if constexpr (MASKED) {
+        if (__builtin_expect(odd, 0)) {
+            product_without_unseen<D, NC, V_OFF>(v_addr, st.acc, P, lim, first, g4);
+            return;
+        }
+        pv.prefetch(v_addr);
+    }
+    pv.template run<NC>(v_addr, P, st.acc);
 }
 
 // Where a column's row lies.
