@@ -125,22 +125,27 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
     return false;
 }
 
+// The lane, found again: what is worked out from it behind a loop is not kept in registers through it.
+__device__ __forceinline__ int fresh_lane()
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // DMA of rows into LDS: where a lane's 16 bytes of a group of rows come from, and the rows beyond the last one read as the last one.
 template <int D, bool ROWS_ONLY>
 struct PackedDma {
     static constexpr int LPR = D / 8;                               // lanes per row
     static constexpr int GroupRows = Staged<D>::GroupRows;
-    int r;                                                          // row inside a group
-    uint32_t chunk;                                                 // byte offset inside the row
-    uint32_t off;                                                   // ... from the group's first row
-    __device__ __forceinline__ void start(int lane, int64_t token)
+    uint32_t off;                                                   // from the group's first row
+    static __device__ __forceinline__ uint32_t chunk_of(int lane)
     {
-        r = lane / LPR;
-        const int pos = lane % LPR;
-        if constexpr (ROWS_ONLY) chunk = (uint32_t)((pos ^ StagedRows<D>::turn(r)) << 4);
-        else chunk = (uint32_t)(D == 128 ? (pos ^ (r << 2)) << 4 : (pos ^ (((r >> 1) & 3) << 1)) << 4);
-        off = (uint32_t)(r * (int)token) + chunk;
+        const int r = lane / LPR, pos = lane % LPR;
+        if constexpr (ROWS_ONLY) return (uint32_t)((pos ^ StagedRows<D>::turn(r)) << 4);
+        else return (uint32_t)(D == 128 ? (pos ^ (r << 2)) << 4 : (pos ^ (((r >> 1) & 3) << 1)) << 4);
     }
+    __device__ __forceinline__ void start(int lane, int64_t token) { off = (uint32_t)((lane / LPR) * (int)token) + chunk_of(lane); }
     // Rows `first` .. of base (already at the sequence's first row), of which `rows` exist, to LDS address dst.
     __device__ __forceinline__ void bring(const char *base, int64_t token, int first, int rows, char *dst) const
     {
@@ -150,8 +155,8 @@ struct PackedDma {
             asm volatile("" : "+v"(o));                             // a 32-bit lane offset next to a scalar base
             src = base + (int64_t)first * token + o;
         } else {
-            const int row = first + r < rows ? first + r : rows - 1;
-            src = base + (int64_t)row * token + chunk;
+            const int lane = fresh_lane(), row = first + lane / LPR;
+            src = base + (int64_t)(row < rows ? row : rows - 1) * token + chunk_of(lane);
         }
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, STA_LDS_PTR(dst), 16, 0, 0);
     }

@@ -29,46 +29,74 @@ struct Softmax {
     floatx4 acc[CB][NC];
     float m[NC];                    // -infinity until a key is seen
     bool far;                       // an offset is so large (masks of the type's lowest number) that its product with the scale is too coarse
-    floatx4 l[NC];                  // LSE: [0] is this lane's share of the sum; otherwise all four are the whole sum of the rounded probabilities
+    uint32_t odd;                   // not 0: a masked sub-block of V held more than numbers
+    using Sum = std::conditional_t<LSE, float, floatx4>;
+    Sum l[NC];                      // LSE: this lane's share of the sum; otherwise all four are the whole sum of the rounded probabilities
     __device__ __forceinline__ void start()
     {
         far = false;
+        odd = 0;
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
             m[col] = -INFINITY;
-            l[col] = floatx4{0.f, 0.f, 0.f, 0.f};
+            l[col] = Sum{};
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) acc[cb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
     }
     // The sum of a column (over the lanes that share it).
-    __device__ __forceinline__ float sum(int col) const { return LSE ? quad_lane_sum(l[col][0]) : l[col][0]; }
+    __device__ __forceinline__ float sum(int col) const
+    {
+        if constexpr (LSE) return quad_lane_sum(l[col]);
+        else return l[col][0];
+    }
 };
 
-// Whether a staged sub-block of V holds an infinity or a NaN; the same in all lanes.
-template <int D>
-__device__ __forceinline__ bool holds_no_numbers(const char *v, int lane)
-{
-    uint32_t seen = 0;                                      // 0x7f80 is the exponent of both: one more carries into bit 15
-#pragma unroll
-    for (int group = 0; group < Staged<D>::Groups; ++group) {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(v + group * Staged<D>::Group + lane * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) seen |= (w[i] & 0x7f807f80u) + 0x00800080u;
-    }
-    return __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
-}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// O^T += V^T P^T for a sub-block whose V holds infinities or NaN and of which some column does not see all keys: a probability of 0
-// times one of those is no 0.  Numbers go through the product as ever; how many infinities of either sign and NaN a column sees is three
-// products more with ones in their places, and a column that sees one gets it.
+// Bit 15 of every half of the words of eight bf16 values: set where the value is an infinity or a NaN (the exponent of both is 0x7f80, and one
+// more carries into that bit); and NaN alone.
+__device__ __forceinline__ uint32_t no_numbers(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t nans(uint32_t x) { return (((x & 0x007f007fu) + 0x007f007fu) << 8) & no_numbers(x); }
+
+// O^T += V^T P^T with a zero in the place of every value of V that is no number: where a column does not see a key, its probability is 0, and 0
+// times one of those would be no 0.  odd: whether there were any.  What columns get that see them, add_no_numbers adds.
 template <int D, int NC, int V_OFF>
-__device__ __forceinline__ void product_without_unseen(const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC],
-                                                       const bf16x8 (&P)[NC], const int (&lim)[NC], int first, int g4)
+__device__ __forceinline__ void product_of_numbers(const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC], const bf16x8 (&P)[NC], uint32_t &odd)
 {
     using Product = StagedTransposedProduct<D, V_OFF>;
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    Product pv;
+    pv.template issue<0>(v_addr);
+    static_for<0, Product::NG>([&](auto gc) {
+        constexpr int g = decltype(gc)::value;
+        if constexpr (g + 1 < Product::NG) {
+            pv.template issue<g + 1>(v_addr);
+            pv_wait<8>(pv.frag[g]);
+        } else {
+            pv_wait<0>(pv.frag[g]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x4 x = __builtin_bit_cast(u32x4, __builtin_shufflevector(pv.frag[g][i][0], pv.frag[g][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t at = no_numbers(x[w]);
+                odd |= at;
+                x[w] &= ~(at | (at - (at >> 15)));
+            }
+#pragma unroll
+            for (int col = 0; col < NC; ++col) acc[4 * g + i][col] = mfma_16x16x32(__builtin_bit_cast(bf16x8, x), P[col], acc[4 * g + i][col]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
+
+// How many infinities of either sign and NaN of a sub-block of V a column sees, a product each with ones in their places; a column that
+// sees one gets it.  This runs behind the walk, and only where there are any.
+template <int D, int NC>
+__device__ __forceinline__ void add_no_numbers(const uint32_t (&v_addr)[4], floatx4 (&acc)[D / 16][NC], const int (&lim)[NC], int first, int g4)
+{
+    using Product = StagedTransposedProduct<D, 0>;
     Product pv;
     bf16x8 sees[NC];
 #pragma unroll
@@ -79,59 +107,38 @@ __device__ __forceinline__ void product_without_unseen(const uint32_t (&v_addr)[
         constexpr int g = decltype(gc)::value;
         pv.template issue<g>(v_addr);
         pv_wait<0>(pv.frag[g]);
-        static_for<0, 4>([&](auto ic) {
-            constexpr int i = decltype(ic)::value, cb = 4 * g + i;
-            const u32x4 x = __builtin_bit_cast(u32x4, __builtin_shufflevector(pv.frag[g][i][0], pv.frag[g][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
-            u32x4 odd, nan;                                 // bit 15 of every half: no number; NaN
+        static_for<0, 12>([&](auto ic) {
+            constexpr int i = decltype(ic)::value / 3, cb = 4 * g + i, kind = decltype(ic)::value % 3;       // +infinity, -infinity, NaN
+            u32x4 x = __builtin_bit_cast(u32x4, __builtin_shufflevector(pv.frag[g][i][0], pv.frag[g][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                odd[w] = ((x[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                nan[w] = (((x[w] & 0x007f007fu) + 0x007f007fu) << 8) & odd[w];
+                const uint32_t sign = x[w] & 0x80008000u, nan = nans(x[w]), inf = no_numbers(x[w]) & ~nan;
+                const uint32_t at = kind == 0 ? inf & ~sign : kind == 1 ? inf & sign : nan;
+                x[w] = (at >> 1) - (at >> 8);       // 1.0
             }
-            static_for<0, 4>([&](auto kc) {
-                constexpr int kind = decltype(kc)::value;   // numbers, +infinity, -infinity, NaN
-                u32x4 a;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    if constexpr (kind == 0) {
-                        a[w] = x[w] & ~(odd[w] | (odd[w] - (odd[w] >> 15)));
-                    } else {
-                        const uint32_t sign = x[w] & 0x80008000u, inf = odd[w] & ~nan[w];
-                        const uint32_t at = kind == 1 ? inf & ~sign : kind == 2 ? inf & sign : nan[w];
-                        a[w] = (at >> 1) - (at >> 8);       // 1.0
-                    }
+            for (int col = 0; col < NC; ++col) {
+                const floatx4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, x), sees[col], floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    // on the bits: floating-point sums of infinities may be folded by the compiler
+                    const uint32_t o = __float_as_uint(acc[cb][col][r]), add = kind == 1 ? 0xff800000u : 0x7f800000u;
+                    const bool against = (o & 0x7fffffffu) > 0x7f800000u || o == (add ^ 0x80000000u);       // NaN, the other infinity
+                    acc[cb][col][r] = __uint_as_float(n[r] > 0.f ? (kind == 2 || against ? 0x7fc00000u : add) : o);
                 }
-#pragma unroll
-                for (int col = 0; col < NC; ++col) {
-                    if constexpr (kind == 0) {
-                        acc[cb][col] = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), P[col], acc[cb][col]);
-                    } else {
-                        const floatx4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), sees[col], floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            // on the bits: floating-point sums of infinities may be folded by the compiler
-                            const uint32_t o = __float_as_uint(acc[cb][col][r]), inf = kind == 2 ? 0xff800000u : 0x7f800000u;
-                            const bool against = (o & 0x7fffffffu) > 0x7f800000u || o == (inf ^ 0x80000000u);      // NaN, the other infinity
-                            const uint32_t with = kind == 3 || against ? 0x7fc00000u : inf;
-                            acc[cb][col][r] = __uint_as_float(n[r] > 0.f ? with : o);
-                        }
-                    }
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
+            }
+            __builtin_amdgcn_sched_barrier(0);
         });
     });
 }
 
 // One sub-block of 32 keys: K at LDS offset K_OFF of k_addr in the layout StagedRows, V at V_OFF of v_addr in the layout Staged.  lim: how many
-// keys a column sees; first: the sub-block's first key.  MASKED: some column may not see all of them (v: where V is staged).
+// keys a column sees; first: the sub-block's first key.  MASKED: some column may not see all of them.
 template <int D, int NC, bool LSE, bool MASKED, int K_OFF, int V_OFF>
 __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint32_t k_addr, const uint32_t (&v_addr)[4],
                                                   const bf16x8 (&Q)[NC][D / 32], float c, float grow_above, int first,
-                                                  const int (&lim)[NC], const char *v, int lane)
+                                                  const int (&lim)[NC], int g4)
 {
-    const int g4 = lane >> 4;
-    bool odd = false;               // not only numbers, and not for all columns
     floatx4 S[2][NC];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -139,7 +146,6 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
         for (int col = 0; col < NC; ++col) S[kb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
     rows_times_resident<D, K_OFF, NC>(k_addr, Q, S);
     if constexpr (MASKED) {                                 // a select, whatever the score is
-        odd = holds_no_numbers<D>(v, lane);
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
             const int left = lim[col] - first - 4 * g4;
@@ -182,7 +188,6 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
     }
-    // Reads on their way are not carried over a branch: the compiler, which does not know that they are, may move their registers there.
     StagedTransposedProduct<D, V_OFF> pv;
     if constexpr (!MASKED) {
         pv.prefetch(v_addr);
@@ -201,7 +206,7 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
                 if constexpr (LSE) sum += e;
                 P[col][4 * kb + r] = static_cast<__bf16>(e);
             }
-        if constexpr (LSE) st.l[col][0] += sum;
+        if constexpr (LSE) st.l[col] += sum;
     }
     if constexpr (!LSE) {
         bf16x8 ones;
@@ -210,14 +215,8 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
 #pragma unroll
         for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[col], st.l[col]);
     }
-    if constexpr (MASKED) {
-        if (__builtin_expect(odd, 0)) {
-            product_without_unseen<D, NC, V_OFF>(v_addr, st.acc, P, lim, first, g4);
-            return;
-        }
-        pv.prefetch(v_addr);
-    }
-    pv.template run<NC>(v_addr, P, st.acc);
+    if constexpr (MASKED) product_of_numbers<D, NC, V_OFF>(v_addr, st.acc, P, st.odd);
+    else pv.template run<NC>(v_addr, P, st.acc);
 }
 
 // Where a column's row lies.
@@ -234,14 +233,23 @@ __device__ __forceinline__ RowAt row_at(uint32_t row, uint32_t rows, const Packe
 }
 
 template <int D, int NC>
-__device__ __forceinline__ void load_queries(const PackedParams &p, const PackedSeq &seq, uint32_t kv, const RowAt (&at)[NC], int g4, bf16x8 (&Q)[NC][D / 32])
+__device__ __forceinline__ void load_queries(const PackedParams &p, const PackedSeq &seq, uint32_t kv, uint32_t row0, uint32_t rows, int lane, bf16x8 (&Q)[NC][D / 32])
 {
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
-        const char *row = p.q.data + (int64_t)(seq.q0 + at[col].token) * p.q.token + (int64_t)(kv * p.g + at[col].head) * p.q.head;
+        const RowAt at = row_at(row0 + 16 * col + (lane & 15), rows, p);
+        const char *row = p.q.data + (int64_t)(seq.q0 + at.token) * p.q.token + (int64_t)(kv * p.g + at.head) * p.q.head;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) Q[col][ks] = *reinterpret_cast<const bf16x8 *>(row + 64 * ks + 16 * g4);
+        for (int ks = 0; ks < D / 32; ++ks) Q[col][ks] = *reinterpret_cast<const bf16x8 *>(row + 64 * ks + 16 * (lane >> 4));
     }
+}
+
+// How many keys the columns of a wave see.
+template <int NC>
+__device__ __forceinline__ void limits_of(const PackedParams &p, const PackedSeq &seq, uint32_t row0, uint32_t rows, int lane, int (&lim)[NC])
+{
+#pragma unroll
+    for (int col = 0; col < NC; ++col) lim[col] = seq.keys_of(row_at(row0 + 16 * col + (lane & 15), rows, p).token, p);
 }
 
 // Partial sums of a tile's part: accumulators [R][D], then offsets (base-2 units) and sums of the rows.
@@ -290,13 +298,6 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
 
     const uint32_t wave_row = row0 + 32 * wave;
     const bool idle = wave_row >= rows;
-    RowAt at[NC];
-    int lim[NC];
-#pragma unroll
-    for (int col = 0; col < NC; ++col) {
-        at[col] = row_at(wave_row + 16 * col + c16, rows, p);
-        lim[col] = seq.keys_of(at[col].token, p);
-    }
     const uint32_t wave_last = wave_row + 31 < rows ? wave_row + 31 : rows - 1;
     const int n_whole = uniform(seq.keys_of((int)sta::fast_div(row0, p.by_g), p));          // keys that all rows see
     const int lim_hi = idle ? 0 : uniform(seq.keys_of((int)sta::fast_div(wave_last, p.by_g), p));
@@ -307,27 +308,34 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
     PackedDma<D, false> v_dma;
     k_dma.start(lane, p.k.token);
     v_dma.start(lane, p.v.token);
-    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        if (sub >= sub1) return;
-        char *to = smem + stage * STAGE;
+    auto issue_v = [&](int stage, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i, first = sub * kSub + group * LV::GroupRows;
-            k_dma.bring(kh, p.k.token, first, seq.lk, to + group * LK::Group);
-            v_dma.bring(vh, p.v.token, first, seq.lk, to + V_AT + group * LV::Group);
+            const int group = PER_WAVE * wave + i;
+            v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, smem + stage * STAGE + V_AT + group * LV::Group);
         }
+    };
+    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
+        if (sub >= sub1) return;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int group = PER_WAVE * wave + i;
+            k_dma.bring(kh, p.k.token, sub * kSub + group * LV::GroupRows, seq.lk, smem + stage * STAGE + group * LK::Group);
+        }
+        issue_v(stage, sub);
     };
     issue(0, sub0);
 
     bf16x8 Q[NC][D / 32];
-    load_queries<D, NC>(p, seq, kv, at, g4, Q);
+    load_queries<D, NC>(p, seq, kv, wave_row, rows, lane, Q);
     const uint32_t base = (uint32_t)(uintptr_t)smem;
     const uint32_t k_addr = LK::address(base, lane);
     uint32_t v_addr[4];
-    LV::transposed_addresses(base, lane, v_addr);
+    LV::transposed_addresses(base + V_AT, lane, v_addr);
     Softmax<D, NC, LSE> st;
     st.start();
     const float c = p.scale_log2e, grow_above = 8.0f / c;
+    int lim[NC] = {};                                       // found where the tail begins
     auto step = [&](auto stage_c, auto masked_c, int sub) __attribute__((always_inline)) {
         constexpr int ST = decltype(stage_c)::value;
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -336,8 +344,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
         issue(ST ^ 1, sub + 1);
         const int first = sub * kSub;
         if (!MASKED || first < lim_hi)
-            softmax_sub_block<D, NC, LSE, MASKED, ST * STAGE, ST * STAGE + V_AT>(st, k_addr, v_addr, Q, c, grow_above, first, lim, smem + ST * STAGE + V_AT,
-                                                                                 lane);
+            softmax_sub_block<D, NC, LSE, MASKED, ST * STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
@@ -348,10 +355,22 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
         step(Stage0{}, std::false_type{}, sub);
         step(Stage1{}, std::false_type{}, sub + 1);
     }
+    const int tail = sub;
+    limits_of<NC>(p, seq, wave_row, rows, fresh_lane(), lim);
 #pragma unroll 1
     for (; sub < sub1; sub += 2) {
         step(Stage0{}, std::true_type{}, sub);
         if (sub + 1 < sub1) step(Stage1{}, std::true_type{}, sub + 1);
+    }
+    if (__builtin_expect(__syncthreads_or(st.odd != 0), 0)) {
+#pragma unroll 1
+        for (sub = tail; sub < sub1; ++sub) {
+            issue_v(0, sub);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (sub * kSub < lim_hi) add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
+            __syncthreads();
+        }
     }
 
     const bool whole = parts_of(n_all, p) <= 1;
@@ -371,11 +390,13 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
         }
         return;
     }
+    const int last_lane = fresh_lane();
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
         const float l = st.sum(col), inv = l > 0.f ? 1.f / l : 0.f;
-        if (!at[col].on) continue;
-        const int64_t token = seq.q0 + at[col].token, head = kv * p.g + at[col].head;
+        const RowAt at = row_at(wave_row + 16 * col + (last_lane & 15), rows, p);
+        if (!at.on) continue;
+        const int64_t token = seq.q0 + at.token, head = kv * p.g + at.head;
         char *row = p.o.data + token * p.o.token + head * p.o.head;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -412,13 +433,8 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
     const int sub1 = part_end(part, n_all, p);
     if (part > 0 && sub0 >= n_all) return;
 
-    RowAt at[NC];
     int lim[NC];
-#pragma unroll
-    for (int col = 0; col < NC; ++col) {
-        at[col] = row_at(16 * col + c16, rows, p);
-        lim[col] = seq.keys_of(at[col].token, p);
-    }
+    limits_of<NC>(p, seq, 0, rows, lane, lim);
     const int n_whole = uniform(seq.keys_of(0, p));         // keys that all rows see
 
     const char *kh = p.k.data + (int64_t)seq.k0 * p.k.token + (int64_t)kv * p.k.head;
@@ -437,12 +453,12 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
     };
     int sub = sub0 + wave;
     bf16x8 Q[NC][D / 32];
-    load_queries<D, NC>(p, seq, kv, at, g4, Q);
+    load_queries<D, NC>(p, seq, kv, 0, rows, lane, Q);
     if (sub < sub1) issue(0, sub);
     const uint32_t base = (uint32_t)(uintptr_t)own;
     const uint32_t k_addr = LK::address(base, lane);
     uint32_t v_addr[4];
-    LV::transposed_addresses(base, lane, v_addr);
+    LV::transposed_addresses(base + V_AT, lane, v_addr);
     Softmax<D, NC, LSE> st;
     st.start();
     const float c = p.scale_log2e, grow_above = 8.0f / c;
@@ -456,8 +472,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
             wait_dma<0>();
         }
         const int first = sub * kSub;
-        softmax_sub_block<D, NC, LSE, decltype(masked_c)::value, ST * STAGE, ST * STAGE + V_AT>(st, k_addr, v_addr, Q, c, grow_above, first, lim,
-                                                                                               own + ST * STAGE + V_AT, lane);
+        softmax_sub_block<D, NC, LSE, decltype(masked_c)::value, ST * STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
@@ -466,10 +481,20 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
         step(Stage0{}, std::false_type{}, sub);
         step(Stage1{}, std::false_type{}, sub + 4);
     }
+    const int tail = sub;
 #pragma unroll 1
     for (; sub < sub1; sub += 8) {
         step(Stage0{}, std::true_type{}, sub);
         if (sub + 4 < sub1) step(Stage1{}, std::true_type{}, sub + 4);
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(st.odd != 0) != 0, 0)) {
+#pragma unroll 1
+        for (sub = tail; sub < sub1; sub += 4) {
+            __builtin_amdgcn_sched_barrier(0);
+            issue(0, sub);
+            wait_dma<0>();
+            add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
+        }
     }
 
     // ---- merge of the four waves: every wave sums the parts of its channel blocks, in ascending order
@@ -497,7 +522,8 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
             l += x.y * weight[w];
         }
         const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-        const int64_t token = seq.q0 + at[col].token, head = kv * p.g + at[col].head;
+        const RowAt at = row_at(16 * col + c16, rows, p);
+        const int64_t token = seq.q0 + at.token, head = kv * p.g + at.head;
 #pragma unroll
         for (int j = 0; j < CB / 4; ++j) {
             const int cb = wave * (CB / 4) + j;
@@ -508,7 +534,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[r] = fmaf(x[r], weight[w], sum[r]);
             }
-            if (!at[col].on) continue;
+            if (!at.on) continue;
             if (whole) {
                 bf16x4 v;
 #pragma unroll
@@ -518,7 +544,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
                 *reinterpret_cast<floatx4 *>(ws + (size_t)(16 * col + c16) * D + 16 * cb + 4 * g4) = sum;
             }
         }
-        if (wave == 0 && g4 == 0 && at[col].on) {
+        if (wave == 0 && g4 == 0 && at.on) {
             if (!whole) {
                 ws[(size_t)R * D + 16 * col + c16] = m;
                 ws[(size_t)R * D + R + 16 * col + c16] = l;
