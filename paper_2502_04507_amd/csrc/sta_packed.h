@@ -70,59 +70,92 @@ __device__ __forceinline__ PackedSeq seq_of(uint32_t s, const PackedParams &p)
     return q;
 }
 
-// Sum over the lanes up to and including this one.
-__device__ __forceinline__ uint32_t scan64(uint32_t x, int lane)
+// Sum over the lanes up to and including this one: inside the rows of 16 lanes, then over the rows.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ uint32_t scan64(uint32_t x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const uint32_t y = __shfl_up(x, m, 64);
-        if (lane >= m) x += y;
-    }
+    x += from_lane<0x111, 0xf>(x);          // the lane 1, 2, 4, 8 before, of the row
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);          // the last lane of the row before: rows 1 and 3
+    x += from_lane<0x143, 0xc>(x);          // the last lane of row 1: rows 2 and 3
     return x;
 }
+__device__ __forceinline__ uint32_t sum64(uint32_t x) { return __builtin_amdgcn_readlane(scan64(x), 63); }
 
-// The tile that is number `rank` from the end of all sequences' tiles (the last tiles of a causal sequence are its longest), and its
-// sequence.  TILE rows a tile of query rows; KEYS: tiles of TILE keys instead.  The number of tiles is known on the device only: launches have an upper
-// bound of them, and false is returned for ranks beyond.
+// A tile of a sequence: TILE rows, or keys (KEYS).  Launches have an upper bound of the tiles, which only the device can count.
 struct PackedTile {
     PackedSeq seq;
     uint32_t index;                 // of the tile in its sequence
     uint32_t slot;                  // of the tile among all sequences' tiles
 };
+
+// The tile of a workgroup, the longest walks first: with up to 64 sequences, a lane each, in the order of how many tiles' walks a tile's is
+// long (rows that see more keys stand later in a causal sequence, keys that more rows see stand earlier), which a search over that number finds;
+// with more, sequence after sequence from the last.  False: there are not so many tiles.
 template <int TILE, bool KEYS>
 __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, int lane, PackedTile *out)
 {
-    auto tiles_of = [&](uint32_t s) {
+    // tiles, and by how many tiles' walks they are longer than those of a sequence without earlier keys
+    auto tiles_of = [&](uint32_t s, uint32_t *longer) {
+        *longer = 0;
         if (s >= p.S) return 0u;
         const PackedSeq q = seq_of(s, p);
+        if (!KEYS && q.lk > q.lq) {
+            const uint64_t more = (uint64_t)(q.lk - q.lq) * p.g / TILE;
+            *longer = more < (1u << 24) ? (uint32_t)more : 1u << 24;
+        }
         return ((KEYS ? (uint32_t)q.lk : (uint32_t)q.lq * p.g) + TILE - 1) / TILE;
     };
-    uint32_t total = 0, last = 0;
-    for (uint32_t s0 = 0; s0 < p.S; s0 += 64) {
-        last = scan64(tiles_of(s0 + lane), lane);
-        total += __builtin_amdgcn_readlane(last, 63);
-    }
-    if (rank >= total) return false;
-    const uint32_t idx = KEYS ? rank : total - 1 - rank;     // (the first keys of a causal sequence are seen by the most rows)
-    uint32_t before = 0;
-    for (uint32_t s0 = 0; s0 < p.S; s0 += 64) {
-        const uint32_t own = tiles_of(s0 + lane);
-        const uint32_t upto = p.S <= 64 ? last : scan64(own, lane);
-        const uint32_t all = __builtin_amdgcn_readlane(upto, 63);
-        if (idx < before + all) {
-            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > idx));
-            out->slot = idx;
-            out->index = idx - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
-            out->seq = seq_of(s0 + at, p);
-            out->seq.q0 = uniform(out->seq.q0);
-            out->seq.lq = uniform(out->seq.lq);
-            out->seq.k0 = uniform(out->seq.k0);
-            out->seq.lk = uniform(out->seq.lk);
-            return true;
+    uint32_t longer;
+    int at;                         // lane of the sequence
+    uint32_t s0 = 0;
+    if (p.S <= 64) {
+        const uint32_t own = tiles_of(lane, &longer), upto = scan64(own);
+        if (rank >= (uint32_t)__builtin_amdgcn_readlane(upto, 63)) return false;
+        // the largest level that so many tiles reach that this one is among them
+        auto reach = [&](uint32_t level) {
+            const uint32_t below = level > longer ? level - longer : 0;
+            return own > below ? own - below : 0;
+        };
+        uint32_t lo = 0;
+        for (uint32_t step = 1u << 25; step > 0; step >>= 1) {
+            // levels that no tile reaches are left out without a sum
+            if (__builtin_amdgcn_ballot_w64(reach(lo + step) != 0) == 0) continue;
+            if (sum64(reach(lo + step)) > rank) lo += step;
         }
-        before += all;
+        uint32_t left = rank - sum64(reach(lo + 1));
+        uint64_t here = __builtin_amdgcn_ballot_w64(own != 0 && longer <= lo && lo < longer + own);
+        while (left-- > 0) here &= here - 1;
+        at = __builtin_ctzll(here);
+        const uint32_t level = lo - __builtin_amdgcn_readlane(longer, at), n = __builtin_amdgcn_readlane(own, at);
+        out->index = KEYS ? n - 1 - level : level;
+        out->slot = __builtin_amdgcn_readlane(upto, at) - n + out->index;
+    } else {
+        uint32_t total = 0;
+        for (uint32_t s = 0; s < p.S; s += 64) total += sum64(tiles_of(s + lane, &longer));
+        if (rank >= total) return false;
+        const uint32_t idx = KEYS ? rank : total - 1 - rank;
+        uint32_t before = 0, own, upto;
+        for (;; s0 += 64) {
+            own = tiles_of(s0 + lane, &longer);
+            upto = scan64(own);
+            const uint32_t all = __builtin_amdgcn_readlane(upto, 63);
+            if (idx < before + all) break;                      // there is one: idx < total
+            before += all;
+        }
+        at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > idx));
+        out->slot = idx;
+        out->index = idx - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
     }
-    return false;
+    out->seq = seq_of(s0 + at, p);
+    out->seq.q0 = uniform(out->seq.q0);
+    out->seq.lq = uniform(out->seq.lq);
+    out->seq.k0 = uniform(out->seq.k0);
+    out->seq.lk = uniform(out->seq.lk);
+    return true;
 }
 
 // The lane, found again: what is worked out from it behind a loop is not kept in registers through it.

@@ -132,38 +132,46 @@ __device__ __forceinline__ void add_no_numbers(const uint32_t (&v_addr)[4], floa
     });
 }
 
-// One sub-block of 32 keys: K at LDS offset K_OFF of k_addr in the layout StagedRows, V at V_OFF of v_addr in the layout Staged.  lim: how many
-// keys a column sees; first: the sub-block's first key.  MASKED: some column may not see all of them.
-template <int D, int NC, bool LSE, bool MASKED, int K_OFF, int V_OFF>
-__device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint32_t k_addr, const uint32_t (&v_addr)[4],
-                                                  const bf16x8 (&Q)[NC][D / 32], float c, float grow_above, int first,
-                                                  const int (&lim)[NC], int g4)
+// U sub-blocks of 32 keys, SUB bytes apart in LDS: K at OFF of k_addr in the layout StagedRows, V at OFF of v_addr in the layout Staged.  lim: how
+// many keys a column sees; first: the first sub-block's first key.  MASKED: some column may not see all of them.
+template <int D, int NC, bool LSE, bool MASKED, int U, int SUB, int OFF>
+__device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint32_t k_addr, const uint32_t (&v_addr)[4],
+                                                   const bf16x8 (&Q)[NC][D / 32], float c, float grow_above, int first,
+                                                   const int (&lim)[NC], int g4)
 {
-    floatx4 S[2][NC];
+    floatx4 S[U][2][NC];
+    static_for<0, U>([&](auto uc) {
+        constexpr int u = decltype(uc)::value;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int col = 0; col < NC; ++col) S[kb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
-    rows_times_resident<D, K_OFF, NC>(k_addr, Q, S);
-    if constexpr (MASKED) {                                 // a select, whatever the score is
+            for (int col = 0; col < NC; ++col) S[u][kb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
+        rows_times_resident<D, OFF + u * SUB, NC, 4>(k_addr, Q, S[u]);
+        if constexpr (MASKED) {                             // a select, whatever the score is
 #pragma unroll
-        for (int col = 0; col < NC; ++col) {
-            const int left = lim[col] - first - 4 * g4;
+            for (int col = 0; col < NC; ++col) {
+                const int left = lim[col] - first - kSub * u - 4 * g4;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[kb][col][r] = 16 * kb + r < left ? S[kb][col][r] : -INFINITY;
+                    for (int r = 0; r < 4; ++r) S[u][kb][col][r] = 16 * kb + r < left ? S[u][kb][col][r] : -INFINITY;
+            }
         }
-    }
+    });
     // The offset only moves when a score exceeds it by more than 2^8 in the exponent.
     float mx[NC];
     bool grown = false;
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
-        mx[col] = max3(S[0][col][0], S[0][col][1], S[0][col][2]);
-        mx[col] = max3(mx[col], S[0][col][3], S[1][col][0]);
-        mx[col] = max3(mx[col], S[1][col][1], S[1][col][2]);
-        mx[col] = quad_lane_max(fmaxf(mx[col], S[1][col][3]));
+        float m = S[0][0][col][0];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            m = max3(m, S[u][0][col][0], S[u][0][col][1]);
+            m = max3(m, S[u][0][col][2], S[u][0][col][3]);
+            m = max3(m, S[u][1][col][0], S[u][1][col][1]);
+            m = max3(m, S[u][1][col][2], S[u][1][col][3]);
+        }
+        mx[col] = quad_lane_max(m);
         grown = grown || mx[col] > st.m[col] + grow_above;
     }
     if (__builtin_amdgcn_ballot_w64(grown) != 0) {
@@ -184,39 +192,56 @@ __device__ __forceinline__ void softmax_sub_block(Softmax<D, NC, LSE> &st, uint3
 #pragma unroll
         for (int col = 0; col < NC; ++col)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[u][kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
     }
-    StagedTransposedProduct<D, V_OFF> pv;
+    StagedTransposedProduct<D, OFF> pv;
     if constexpr (!MASKED) {
         pv.prefetch(v_addr);
         __builtin_amdgcn_sched_barrier(0);
     }
-    bf16x8 P[NC];
+    bf16x8 P[U][NC];
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
         const float mc = st.far || st.m[col] == -INFINITY ? 0.f : st.m[col] * c;
         float sum = 0.f;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(S[kb][col][r], c, -mc));
-                if constexpr (LSE) sum += e;
-                P[col][4 * kb + r] = static_cast<__bf16>(e);
-            }
-        if constexpr (LSE) st.l[col] += sum;
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(S[u][kb][col][r], c, -mc));
+                    if constexpr (LSE) sum += e;
+                    P[u][col][4 * kb + r] = static_cast<__bf16>(e);
+                }
+        if constexpr (LSE) {
+            st.l[col] += sum;
+            __builtin_amdgcn_sched_barrier(0);              // one column's scores at a time: fewer registers
+        }
     }
     if constexpr (!LSE) {
         bf16x8 ones;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
 #pragma unroll
-        for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[col], st.l[col]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[u][col], st.l[col]);
     }
-    if constexpr (MASKED) product_of_numbers<D, NC, V_OFF>(v_addr, st.acc, P, st.odd);
-    else pv.template run<NC>(v_addr, P, st.acc);
+    if constexpr (MASKED) {
+        static_for<0, U>([&](auto uc) { product_of_numbers<D, NC, OFF + decltype(uc)::value * SUB>(v_addr, st.acc, P[decltype(uc)::value], st.odd); });
+    } else {
+        pv.template run<NC>(v_addr, P[0], st.acc);
+        static_for<1, U>([&](auto uc) {
+            StagedTransposedProduct<D, OFF + decltype(uc)::value * SUB> more;
+            more.prefetch(v_addr);
+            more.template run<NC>(v_addr, P[decltype(uc)::value], st.acc);
+        });
+    }
 }
 
 // Where a column's row lies.
@@ -273,13 +298,13 @@ __device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, ui
     return p.ws + ((slot * p.Hkv + kv) * p.parts + part) * floats;
 }
 
-template <int D, bool LSE>
+template <int D, bool LSE, int U>
 __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(PackedParams p)
 {
     constexpr int NC = 2, CB = D / 16;
     using LK = StagedRows<D>;
     using LV = Staged<D>;
-    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, PER_WAVE = LV::Groups / 4;
+    constexpr int SUB = LK::Tile + LV::Tile, STAGE = U * SUB, V_AT = LK::Tile, PER_WAVE = LV::Groups / 4;
     __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
@@ -308,21 +333,26 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
     PackedDma<D, false> v_dma;
     k_dma.start(lane, p.k.token);
     v_dma.start(lane, p.v.token);
-    auto issue_v = [&](int stage, int sub) __attribute__((always_inline)) {
+    auto issue_v = [&](char *to, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i) {
             const int group = PER_WAVE * wave + i;
-            v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, smem + stage * STAGE + V_AT + group * LV::Group);
+            v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, to + V_AT + group * LV::Group);
         }
     };
+    // sub .. sub + U - 1; those of the last stage that nobody sees are brought as well, from the last key's row
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
         if (sub >= sub1) return;
 #pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i;
-            k_dma.bring(kh, p.k.token, sub * kSub + group * LV::GroupRows, seq.lk, smem + stage * STAGE + group * LK::Group);
+        for (int u = 0; u < U; ++u) {
+            char *to = smem + stage * STAGE + u * SUB;
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int group = PER_WAVE * wave + i;
+                k_dma.bring(kh, p.k.token, (sub + u) * kSub + group * LV::GroupRows, seq.lk, to + group * LK::Group);
+            }
+            issue_v(to, sub + u);
         }
-        issue_v(stage, sub);
     };
     issue(0, sub0);
 
@@ -341,31 +371,31 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
         constexpr bool MASKED = decltype(masked_c)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's part of the stage has landed
         __syncthreads();                                    // ... and everyone's, and nobody reads the other stage any more
-        issue(ST ^ 1, sub + 1);
+        issue(ST ^ 1, sub + U);
         const int first = sub * kSub;
         if (!MASKED || first < lim_hi)
-            softmax_sub_block<D, NC, LSE, MASKED, ST * STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
+            softmax_sub_blocks<D, NC, LSE, MASKED, U, SUB, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
-    // pairs of sub-blocks that every row of the tile sees all of, then the others
+    // pairs of stages that every row of the tile sees all of, then the others
     int sub = sub0;
 #pragma unroll 1
-    for (; sub + 1 < sub1 && (sub + 2) * kSub <= n_whole; sub += 2) {
+    for (; sub + 2 * U <= sub1 && (sub + 2 * U) * kSub <= n_whole; sub += 2 * U) {
         step(Stage0{}, std::false_type{}, sub);
-        step(Stage1{}, std::false_type{}, sub + 1);
+        step(Stage1{}, std::false_type{}, sub + U);
     }
     const int tail = sub;
     limits_of<NC>(p, seq, wave_row, rows, fresh_lane(), lim);
 #pragma unroll 1
-    for (; sub < sub1; sub += 2) {
+    for (; sub < sub1; sub += 2 * U) {
         step(Stage0{}, std::true_type{}, sub);
-        if (sub + 1 < sub1) step(Stage1{}, std::true_type{}, sub + 1);
+        if (sub + U < sub1) step(Stage1{}, std::true_type{}, sub + U);
     }
     if (__builtin_expect(__syncthreads_or(st.odd != 0), 0)) {
 #pragma unroll 1
         for (sub = tail; sub < sub1; ++sub) {
-            issue_v(0, sub);
+            issue_v(smem, sub);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (sub * kSub < lim_hi) add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
@@ -472,7 +502,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
             wait_dma<0>();
         }
         const int first = sub * kSub;
-        softmax_sub_block<D, NC, LSE, decltype(masked_c)::value, ST * STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
+        softmax_sub_blocks<D, NC, LSE, decltype(masked_c)::value, 1, STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
@@ -637,7 +667,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     const int64_t cus = sta::compute_units(), want = cut ? (plan->few ? 4 : 6) * cus : 0;
     if (items > 0 && items < want / 2) {
         int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
-        if (each < 16) each = 16;
+        each = each < 16 ? 16 : (each + 1) & ~(int64_t)1;          // stages of two sub-blocks end with a part
         parts = (subs + each - 1) / each;
         if (parts > 1 && items * parts <= 0x7fffffff) {
             plan->parts = (uint32_t)parts;
@@ -655,7 +685,7 @@ hipError_t launch_packed(const PackedParams &p, const PackedPlan &plan, hipStrea
     hipError_t e;
     if (plan.few == 1) e = sta::launch_kernel(sta_packed_few_kernel<D, 1, LSE>, grid, block, stream, p);
     else if (plan.few == 2) e = sta::launch_kernel(sta_packed_few_kernel<D, 2, LSE>, grid, block, stream, p);
-    else e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE>, grid, block, stream, p);
+    else e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE, D == 64 ? 2 : 1>, grid, block, stream, p);
     if (e != hipSuccess || plan.parts == 1) return e;
     constexpr int ROWS = 1024 / D;
     const uint32_t items = plan.slots * p.Hkv;

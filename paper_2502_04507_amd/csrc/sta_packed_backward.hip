@@ -3,10 +3,10 @@
 //   P_ij = exp(S_ij - lse_i),  dV_j = sum_i P_ij dO_i,  dP_ij = dO_i . V_j,  dS_ij = P_ij (dP_ij - delta_i),  delta_i = dO_i . O_i
 //   dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i       (i: the rows of all heads of a group)
 //
-// Three kernels, no atomics:
-//   sta_packed_stats_kernel   -delta_i and -lse_i / scale of every row, in the order of the rows;
-//   sta_packed_dq_kernel      four waves of 32 rows walk the keys they see: three products per block;
-//   sta_packed_dkv_kernel     four waves of 32 keys walk the rows that see them: four products per block.
+// Two kernels, no atomics:
+//   sta_packed_dq_kernel      four waves of 32 rows walk the keys they see: three products per block.  It also forms -delta_i and -lse_i / scale of
+//                             its rows and leaves them, in the order of the rows, for the second kernel;
+//   sta_packed_dkv_kernel     waves of 32 keys walk the rows that see them: four products per block.
 // The heads of a group are rows like any others, so their gradients of K and V are summed in the accumulators.  Matrix pipe bound.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -30,31 +30,6 @@ struct BackwardParams {
     float inv_scale;
 };
 
-// ---- statistics: D / 8 lanes a row
-template <int D>
-__global__ __launch_bounds__(256) void sta_packed_stats_kernel(BackwardParams b)
-{
-    constexpr int LPR = D / 8;
-    const PackedParams &p = b.p;
-    const uint32_t row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;      // token * g + head of the group
-    const uint32_t kv = blockIdx.y;
-    const bool on = row < p.tokens_q * p.g;
-    const uint32_t r = on ? row : 0, t = sta::fast_div(r, p.by_g);
-    const int64_t head = (int64_t)kv * p.g + (r - t * p.g);
-    const bf16x8 o = *reinterpret_cast<const bf16x8 *>(p.o.data + (int64_t)t * p.o.token + head * p.o.head + 16 * c);
-    const bf16x8 g = *reinterpret_cast<const bf16x8 *>(b.d_o.data + (int64_t)t * b.d_o.token + head * b.d_o.head + 16 * c);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fmaf((float)o[i], (float)g[i], sum);
-#pragma unroll
-    for (int m = LPR / 2; m > 0; m /= 2) sum += __shfl_xor(sum, m, 64);
-    if (on && c == 0) {
-        const size_t at = (size_t)kv * p.tokens_q * p.g + row;
-        b.neg_delta[at] = -sum;
-        b.neg_lse[at] = -b.lse[head * p.tokens_q + t] * b.inv_scale;
-    }
-}
-
 // Columns of a wave out of their accumulators: [channel block][column block] of the transposed result.
 template <int D, int NC>
 __device__ __forceinline__ void store_column(const floatx4 (&acc)[D / 16][NC], int col, float factor, char *row, int g4)
@@ -66,6 +41,30 @@ __device__ __forceinline__ void store_column(const floatx4 (&acc)[D / 16][NC], i
         for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(acc[cb][col][r] * factor);
         *reinterpret_cast<bf16x4 *>(row + 32 * cb + 8 * g4) = v;
     }
+}
+
+// The first group's accumulators += those of the others, in ascending order.
+template <int D, int KW, int G, int NC>
+__device__ __forceinline__ void join_groups(char *smem, int walk, int wave, int lane, floatx4 (&acc)[D / 16][NC])
+{
+    constexpr int WAVE = D / 16 * NC * 1024;
+    __syncthreads();                                        // the stages, or the operand before, have been read
+    if (walk > 0) {
+        char *to = smem + ((walk - 1) * KW + wave) * WAVE + lane * 16;
+#pragma unroll
+        for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col) *reinterpret_cast<floatx4 *>(to + (cb * NC + col) * 1024) = acc[cb][col];
+    }
+    __syncthreads();
+    if (walk == 0)
+#pragma unroll
+        for (int other = 0; other < G - 1; ++other)
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+                for (int col = 0; col < NC; ++col)
+                    acc[cb][col] += *reinterpret_cast<const floatx4 *>(smem + (other * KW + wave) * WAVE + (cb * NC + col) * 1024 + lane * 16);
 }
 
 template <int D>
@@ -102,15 +101,24 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
         token[col] = (int)t;
         head[col] = (int64_t)kv * p.g + (r - t * p.g);
         lim[col] = seq.keys_of((int)t, p);
-        const size_t stat = ((size_t)kv * p.tokens_q + seq.q0) * p.g + r;
-        neg_lse[col] = b.neg_lse[stat];
-        neg_delta[col] = b.neg_delta[stat];
         const char *q = p.q.data + (int64_t)(seq.q0 + token[col]) * p.q.token + head[col] * p.q.head;
         const char *g = b.d_o.data + (int64_t)(seq.q0 + token[col]) * b.d_o.token + head[col] * b.d_o.head;
+        const char *o = p.o.data + (int64_t)(seq.q0 + token[col]) * p.o.token + head[col] * p.o.head;
+        float delta = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             Q[col][ks] = *reinterpret_cast<const bf16x8 *>(q + 64 * ks + 16 * g4);
             G[col][ks] = *reinterpret_cast<const bf16x8 *>(g + 64 * ks + 16 * g4);
+            const bf16x8 O = *reinterpret_cast<const bf16x8 *>(o + 64 * ks + 16 * g4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)O[e], (float)G[col][ks][e], delta);
+        }
+        neg_delta[col] = -quad_lane_sum(delta);
+        neg_lse[col] = -b.lse[head[col] * p.tokens_q + seq.q0 + token[col]] * b.inv_scale;
+        if (on[col] && g4 == 0) {
+            const size_t stat = ((size_t)kv * p.tokens_q + seq.q0) * p.g + r;
+            b.neg_lse[stat] = neg_lse[col];
+            b.neg_delta[stat] = neg_delta[col];
         }
     }
     const uint32_t wave_last = wave_row + 31 < rows ? wave_row + 31 : rows - 1;
@@ -207,20 +215,24 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
         if (on[col]) store_column<D, NC>(acc, col, p.scale, b.d_q.data + (int64_t)(seq.q0 + token[col]) * b.d_q.token + head[col] * b.d_q.head, g4);
 }
 
-template <int D>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void sta_packed_dkv_kernel(BackwardParams b)
+// KW waves of 32 keys; G groups of them take the sub-blocks of rows in turn, each with stages of its own, and the groups' sums are joined at the end.
+template <int D, int KW, int G>
+__global__ __attribute__((amdgpu_flat_work_group_size(KW * G * 64, KW * G * 64), amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
+void sta_packed_dkv_kernel(BackwardParams b)
 {
     const PackedParams &p = b.p;
-    constexpr int NC = 2, KS = D / 32, CB = D / 16;
+    constexpr int NC = 2, KS = D / 32, CB = D / 16, TILE = 32 * KW;
     using L = Staged<D>;
-    constexpr int STATS = 2 * L::Tile, STAGE = STATS + 1024, G_AT = L::Tile, PER_WAVE = L::Groups / 4, LPR = D / 8;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    constexpr int STATS = 2 * L::Tile, STAGE = STATS + 1024, G_AT = L::Tile, PER_WAVE = L::Groups / KW, LPR = D / 8;
+    constexpr int MERGE = G > 1 ? (G - 1) * KW * CB * NC * 1024 : 0;           // accumulators of one operand, of all groups but the first
+    __shared__ __attribute__((aligned(1024))) char smem[2 * G * STAGE > MERGE ? 2 * G * STAGE : MERGE];
+    const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const int walk = all_waves / KW, wave = all_waves % KW;
     const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
     PackedTile tile;
-    if (!find_tile<kTile, true>(rank, p, lane, &tile)) return;
+    if (!find_tile<TILE, true>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
-    const int rows = seq.lq * (int)p.g, key0 = (int)tile.index * kTile, ahead = seq.lk - seq.lq;
+    const int rows = seq.lq * (int)p.g, key0 = (int)tile.index * TILE, ahead = seq.lk - seq.lq;
     // key j is seen by the rows from first_row(j) on
     auto first_row = [&](int j) {
         const int t = j - ahead;
@@ -251,7 +263,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
     const float *stats = (lane < kSub ? b.neg_lse : b.neg_delta) + ((size_t)kv * p.tokens_q + seq.q0) * p.g;
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
         if (sub >= n_sub) return;
-        char *to = smem + stage * STAGE;
+        char *to = smem + (2 * walk + stage) * STAGE;
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i) {
             const int group = PER_WAVE * wave + i, row = sub * kSub + group * L::GroupRows + r_in;
@@ -261,14 +273,14 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + (int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head),
                                              STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
         }
-        if (wave == 3) {
+        if (wave == KW - 1) {
             const int row = sub * kSub + (lane & (kSub - 1));
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(stats + (row < rows ? row : rows - 1)),
                                              STA_LDS_PTR(to + STATS), 4, 0, 0);
         }
     };
-    issue(0, sub0);
-    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    issue(0, sub0 + walk);
+    const uint32_t base = (uint32_t)(uintptr_t)smem + 2 * walk * STAGE;
     uint32_t row_addr[KS], tr_addr[4];
     L::addresses(base, lane, row_addr, tr_addr);
     const uint32_t stat_addr = base + STATS + 16 * g4;
@@ -282,9 +294,9 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
         constexpr int ST = decltype(stage_c)::value * STAGE;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        issue(decltype(stage_c)::value ^ 1, sub + 1);
+        issue(decltype(stage_c)::value ^ 1, sub + G);
         const int first = sub * kSub;
-        if (first + kSub <= see_lo || wave_key >= seq.lk) return;
+        if (sub >= n_sub || first + kSub <= see_lo || wave_key >= seq.lk) return;
         auto start = [&](auto off_c) {                      // four rows' statistics for every register of a row block
             floatx4 x[2];
             typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -354,9 +366,14 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
         for_k.template run<NC>(tr_addr, packed, dK);                                // dK^T += Q^T dS
     };
 #pragma unroll 1
-    for (int sub = sub0; sub < n_sub; sub += 2) {
-        step(std::integral_constant<int, 0>{}, sub);
-        if (sub + 1 < n_sub) step(std::integral_constant<int, 1>{}, sub + 1);
+    for (int sub = sub0; sub < n_sub; sub += 2 * G) {       // the same number of barriers for every group
+        step(std::integral_constant<int, 0>{}, sub + walk);
+        if (sub + G < n_sub) step(std::integral_constant<int, 1>{}, sub + G + walk);
+    }
+    if constexpr (G > 1) {
+        join_groups<D, KW, G>(smem, walk, wave, lane, dV);
+        join_groups<D, KW, G>(smem, walk, wave, lane, dK);
+        if (walk != 0) return;
     }
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
@@ -367,25 +384,33 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
     }
 }
 
-template <int D>
-hipError_t launch_gradients(const BackwardParams &b, uint32_t row_tiles, uint32_t key_tiles, hipStream_t stream)
+// Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than max_length x g.
+int64_t tiles_of(int64_t tokens, int64_t g, int S, int64_t max_length, int tile)
 {
-    const PackedParams &p = b.p;
-    constexpr uint32_t PER = 256 / (D / 8);
-    hipError_t e = hipSuccess;
-    if (p.tokens_q > 0) {
-        e = sta::launch_kernel(sta_packed_stats_kernel<D>, dim3((p.tokens_q * p.g + PER - 1) / PER, p.Hkv), dim3(256), stream, b);
-        if (e == hipSuccess) e = sta::launch_kernel(sta_packed_dq_kernel<D>, dim3(row_tiles * p.Hkv), dim3(256), stream, b);
-    }
-    if (e == hipSuccess && key_tiles > 0) e = sta::launch_kernel(sta_packed_dkv_kernel<D>, dim3(key_tiles * p.Hkv), dim3(256), stream, b);
-    return e;
+    const int64_t by_tokens = tokens * g / tile + S, by_longest = (max_length * g + tile - 1) / tile * S;
+    return by_tokens < by_longest ? by_tokens : by_longest;
 }
 
-// Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than max_length x g.
-int64_t tiles_of(int64_t tokens, int64_t g, int S, int64_t max_length)
+template <int D, int KW, int G>
+hipError_t launch_dkv(const BackwardParams &b, int64_t tiles, hipStream_t stream)
 {
-    const int64_t by_tokens = tokens * g / kTile + S, by_longest = (max_length * g + kTile - 1) / kTile * S;
-    return by_tokens < by_longest ? by_tokens : by_longest;
+    return sta::launch_kernel(sta_packed_dkv_kernel<D, KW, G>, dim3((uint32_t)tiles * b.p.Hkv), dim3(KW * G * 64), stream, b);
+}
+
+template <int D>
+hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipStream_t stream)
+{
+    const PackedParams &p = b.p;
+    const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, kTile), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
+                  half_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 64);
+    if (row_tiles * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
+    hipError_t e = hipSuccess;
+    if (p.tokens_q > 0 && row_tiles > 0)
+        e = sta::launch_kernel(sta_packed_dq_kernel<D>, dim3((uint32_t)row_tiles * p.Hkv), dim3(256), stream, b);
+    if (e != hipSuccess || key_tiles == 0) return e;
+    const int64_t resident = (D == 64 ? 3 : 2) * (int64_t)sta::compute_units();
+    if (key_tiles * p.Hkv >= 3 * resident) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
+    return launch_dkv<D, 2, 2>(b, half_tiles, stream);
 }
 
 constexpr size_t kStatPad = 64;     // floats behind either array
@@ -465,11 +490,9 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     b.neg_lse = static_cast<float *>(workspace);
     b.neg_delta = b.neg_lse + (size_t)q->heads * tokens_q + kStatPad;
     b.inv_scale = 1.0f / scale;
-    const int64_t row_tiles = tiles_of(tokens_q, p.g, S, max_q), key_tiles = tiles_of(tokens_k, 1, S, max_k);
-    if (row_tiles * p.Hkv > 0x7fffffff || key_tiles * p.Hkv > 0x7fffffff || p.Hkv > 65535) return STA_ERR_SHAPE;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = D == 64 ? launch_gradients<64>(b, (uint32_t)row_tiles, (uint32_t)key_tiles, stream)
-                                 : launch_gradients<128>(b, (uint32_t)row_tiles, (uint32_t)key_tiles, stream);
+    const hipError_t e = D == 64 ? launch_gradients<64>(b, max_q, max_k, stream) : launch_gradients<128>(b, max_q, max_k, stream);
+    if (e == hipErrorInvalidValue) return STA_ERR_SHAPE;
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
 

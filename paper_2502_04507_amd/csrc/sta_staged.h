@@ -207,13 +207,13 @@ struct StagedRows {
     }
 };
 
-// X[rb][col] += A B with A in the rows-only layout at byte offset OFF of the wave's one address.
-template <int D, int OFF, int NC>
+// X[rb][col] += A B with A in the rows-only layout at byte offset OFF of the wave's one address, at most MOST reads in flight.
+template <int D, int OFF, int NC, int MOST = 6>
 __device__ __forceinline__ void rows_times_resident(uint32_t addr, const bf16x8 (&resident)[NC][D / 32], floatx4 (&X)[2][NC])
 {
     constexpr int KS = D / 32;
     constexpr int N = 2 * KS;                                   // fragments: KS k-steps of two row blocks
-    constexpr int AHEAD = N < 6 ? N : 6;                        // reads in flight
+    constexpr int AHEAD = N < MOST ? N : MOST;                  // reads in flight
     bf16x8 a[N];
     auto read = [&](auto fc) {
         constexpr int f = decltype(fc)::value;
