@@ -177,9 +177,6 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[kb][col][r] = __builtin_amdgcn_exp2f(S[kb][col][r] * c);
         rows_times_resident<D, ST, NC>(v_addr, G, dP);                              // V dO^T - delta
-        StagedTransposedProduct<D, ST> product;
-        product.prefetch(k_tr);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -196,6 +193,10 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
                     for (int r = 0; r < 4; ++r) S[kb][col][r] = 16 * kb + r < left ? S[kb][col][r] : 0.f;
             }
         }
+        // (reads on their way are not carried over a branch: the compiler, which does not know that they are, may move their registers there)
+        StagedTransposedProduct<D, ST> product;
+        product.prefetch(k_tr);
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 dS[NC];
 #pragma unroll
         for (int col = 0; col < NC; ++col)
@@ -241,12 +242,10 @@ void sta_packed_dkv_kernel(BackwardParams b)
     const int sub0 = uniform(first_row(key0) / kSub), n_sub = (rows + kSub - 1) / kSub;
     const int wave_key = key0 + 32 * wave;
     const int see_lo = uniform(first_row(wave_key)), see_hi = uniform(first_row(wave_key + 31));        // of the wave's first and last key
-    int from[NC];
     bf16x8 K[NC][KS], V[NC][KS];
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
         const int key = wave_key + 16 * col + c16, j = key < seq.lk ? key : seq.lk - 1;
-        from[col] = first_row(key);
         const char *k = p.k.data + (int64_t)(seq.k0 + j) * p.k.token + (int64_t)kv * p.k.head;
         const char *v = p.v.data + (int64_t)(seq.k0 + j) * p.v.token + (int64_t)kv * p.v.head;
 #pragma unroll
@@ -255,26 +254,28 @@ void sta_packed_dkv_kernel(BackwardParams b)
             V[col][ks] = *reinterpret_cast<const bf16x8 *>(v + 64 * ks + 16 * g4);
         }
     }
-    // DMA: row -> (token, head); its 16-byte chunk at this lane's place
-    const int r_in = lane / LPR, pos = lane % LPR;
-    const uint32_t chunk = (uint32_t)(D == 128 ? (pos ^ (r_in << 2)) << 4 : (pos ^ (((r_in >> 1) & 3) << 1)) << 4);
-    const char *qh = p.q.data + (int64_t)seq.q0 * p.q.token + (int64_t)kv * p.g * p.q.head + chunk;
-    const char *gh = b.d_o.data + (int64_t)seq.q0 * b.d_o.token + (int64_t)kv * p.g * b.d_o.head + chunk;
-    const float *stats = (lane < kSub ? b.neg_lse : b.neg_delta) + ((size_t)kv * p.tokens_q + seq.q0) * p.g;
+    // DMA: row -> (token, head); its 16-byte chunk at this lane's place.  All of it is worked out again for every stage: registers that are free
+    // then are not in the loop.
+    const char *qh = p.q.data + (int64_t)seq.q0 * p.q.token + (int64_t)kv * p.g * p.q.head;
+    const char *gh = b.d_o.data + (int64_t)seq.q0 * b.d_o.token + (int64_t)kv * p.g * b.d_o.head;
+    const size_t stat0 = ((size_t)kv * p.tokens_q + seq.q0) * p.g;
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
         if (sub >= n_sub) return;
         char *to = smem + (2 * walk + stage) * STAGE;
+        const int at = fresh_lane(), r_in = at / LPR;
+        const uint32_t chunk = PackedDma<D, false>::chunk_of(at);
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i) {
             const int group = PER_WAVE * wave + i, row = sub * kSub + group * L::GroupRows + r_in;
             const uint32_t r = (uint32_t)(row < rows ? row : rows - 1), t = sta::fast_div(r, p.by_g), h = r - t * p.g;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(qh + (int64_t)t * p.q.token + (int64_t)h * p.q.head),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(qh + ((int64_t)t * p.q.token + (int64_t)h * p.q.head + chunk)),
                                              STA_LDS_PTR(to + group * L::Group), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + (int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + ((int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head + chunk)),
                                              STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
         }
         if (wave == KW - 1) {
-            const int row = sub * kSub + (lane & (kSub - 1));
+            const int row = sub * kSub + (at & (kSub - 1));
+            const float *stats = (at < kSub ? b.neg_lse : b.neg_delta) + stat0;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(stats + (row < rows ? row : rows - 1)),
                                              STA_LDS_PTR(to + STATS), 4, 0, 0);
         }
@@ -315,26 +316,29 @@ void sta_packed_dkv_kernel(BackwardParams b)
             for (int col = 0; col < NC; ++col) { S[0][col] = x.first; S[1][col] = x.second; }
         }
         staged_rows_times_resident<D, ST, NC>(row_addr, K, S);                      // Q K^T - lse / scale
-        StagedTransposedProduct<D, ST + G_AT> for_v;
-        for_v.prefetch(tr_addr);
-        __builtin_amdgcn_sched_barrier(0);
+        StagedTransposedProduct<D, ST + G_AT, D == 64 ? 4 : 2> for_v;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
             for (int col = 0; col < NC; ++col)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[qb][col][r] = __builtin_amdgcn_exp2f(S[qb][col][r] * c);
-        if (first < see_hi || first + kSub > rows) {
+        if (first < see_hi || first + kSub > rows) {        // a select, whatever the exponential is
+            const int at = fresh_lane(), row0 = first + 4 * (at >> 4);
 #pragma unroll
-            for (int col = 0; col < NC; ++col)
+            for (int col = 0; col < NC; ++col) {
+                const int from = first_row(wave_key + 16 * col + (at & 15));
 #pragma unroll
                 for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int row = first + 16 * qb + 4 * g4 + r;
-                        S[qb][col][r] = row >= from[col] && row < rows ? S[qb][col][r] : 0.f;
+                        const int row = row0 + 16 * qb + r;
+                        S[qb][col][r] = row >= from && row < rows ? S[qb][col][r] : 0.f;
                     }
+            }
         }
+        for_v.prefetch(tr_addr);
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 packed[NC];
         auto pack = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -353,7 +357,7 @@ void sta_packed_dkv_kernel(BackwardParams b)
             for (int col = 0; col < NC; ++col) { dP[0][col] = x.first; dP[1][col] = x.second; }
         }
         staged_rows_times_resident<D, ST + G_AT, NC>(row_addr, V, dP);              // dO V^T - delta
-        StagedTransposedProduct<D, ST> for_k;
+        StagedTransposedProduct<D, ST, D == 64 ? 4 : 2> for_k;
         for_k.prefetch(tr_addr);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
