@@ -42,8 +42,14 @@ struct Tensor {
     uint32_t heads;
     uint32_t norm, rotate;
 };
+// The workgroups of one tensor's gradients, and their units.
+struct Share {
+    uint32_t first, blocks, units;
+    FastDiv splits;             // units of one group of tokens
+};
 struct Params {
     Tensor t[3];
+    Share share[3];
     uint32_t n_tensors;
     uint32_t tokens;            // B * N
     uint32_t D, rot;            // channels, rotated channels
@@ -61,7 +67,7 @@ struct Params {
     FastDiv by_N, by_P, by_nw, by_nh, by_Tw, by_Th, by_gw, by_gh;
     uint32_t N, tiled, has_grid, T_t, T_h, T_w, g_h, g_w;
     // backward
-    float *partial;             // [workgroups][2][D] sums of the weight gradients, or null
+    float *partial;             // [workgroups][D] sums of the weight gradients of queries, then keys, or null
 };
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -102,14 +108,14 @@ __device__ __forceinline__ Place place_of(uint32_t c, const Params &p)
     if constexpr (PATH == kHalf) {
         at.in = 16 * c < p.D;
         at.turn_a = at.turn_b = 16 * c < p.rot;
-        at.a = at.turn_a ? 8 * c : 16 * c;
-        at.b = at.turn_a ? p.rot / 2 + 8 * c : 16 * c + 8;
+        at.a = at.turn_a ? 8 * c : at.in ? 16 * c : 0;
+        at.b = at.turn_a ? p.rot / 2 + 8 * c : at.in ? 16 * c + 8 : 0;
     } else if constexpr (PATH == kInterleaved) {
         at.in = 16 * c < p.D;
-        at.a = 8 * c;
-        at.b = p.D / 2 + 8 * c;
-        at.turn_a = at.a < p.rot;
-        at.turn_b = at.b < p.rot;
+        at.a = at.in ? 8 * c : 0;
+        at.b = at.in ? p.D / 2 + 8 * c : 0;
+        at.turn_a = at.in && at.a < p.rot;
+        at.turn_b = at.in && at.b < p.rot;
     } else {
         const uint32_t pairs = p.rot / 2;
 #pragma unroll
@@ -122,10 +128,14 @@ __device__ __forceinline__ Place place_of(uint32_t c, const Params &p)
         }
         at.in = 2 * c < p.D;
         at.in2 = 2 * (c + 64) < p.D;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at.e[j] = (j < 2 ? at.in : at.in2) ? at.e[j] : 0;
     }
     return at;
 }
 
+// What a lane holds of a row.  A lane that holds nothing reads the row's first channels, without a branch, and its shares of the row's sums
+// are left out (general path: zeros).
 template <int PATH, bool F32>
 __device__ __forceinline__ Raw<PATH, F32> load_row(const char *row, const Place &at, bool on)
 {
@@ -134,22 +144,16 @@ __device__ __forceinline__ Raw<PATH, F32> load_row(const char *row, const Place 
     if constexpr (PATH == kGeneral) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            r.w[j] = 0;
-            if (on && (j < 2 ? at.in : at.in2)) {
-                if constexpr (F32) r.w[j] = *reinterpret_cast<const uint32_t *>(row + at.e[j] * S);
-                else r.w[j] = (uint32_t)*reinterpret_cast<const uint16_t *>(row + at.e[j] * S) << 16;
-            }
+            if constexpr (F32) r.w[j] = *reinterpret_cast<const uint32_t *>(row + at.e[j] * S);
+            else r.w[j] = (uint32_t)*reinterpret_cast<const uint16_t *>(row + at.e[j] * S) << 16;
+            r.w[j] = on && (j < 2 ? at.in : at.in2) ? r.w[j] : 0;
         }
     } else {
-#pragma unroll
-        for (auto &w : r.w) w = u32x4{0, 0, 0, 0};
-        if (on && at.in) {
-            const u32x4 *a = reinterpret_cast<const u32x4 *>(row + at.a * S), *b = reinterpret_cast<const u32x4 *>(row + at.b * S);
-            if constexpr (F32) {
-                r.w[0] = a[0]; r.w[1] = a[1]; r.w[2] = b[0]; r.w[3] = b[1];
-            } else {
-                r.w[0] = a[0]; r.w[1] = b[0];
-            }
+        const u32x4 *a = reinterpret_cast<const u32x4 *>(row + at.a * S), *b = reinterpret_cast<const u32x4 *>(row + at.b * S);
+        if constexpr (F32) {
+            r.w[0] = a[0]; r.w[1] = a[1]; r.w[2] = b[0]; r.w[3] = b[1];
+        } else {
+            r.w[0] = a[0]; r.w[1] = b[0];
         }
     }
     return r;
@@ -250,7 +254,7 @@ __device__ __forceinline__ void turn_of(int32_t x, int64_t step, float magnitude
 // The token of a place: where its rows lie and where it is on the axes.
 struct Token {
     uint32_t b, n, place;       // batch, index in the inputs' order, index in the outputs' order
-    int32_t at[3];
+    int32_t at0, at1, at2;
 };
 __device__ __forceinline__ Token token_of(uint32_t id, const Params &p)
 {
@@ -258,63 +262,74 @@ __device__ __forceinline__ Token token_of(uint32_t id, const Params &p)
     t.b = fast_div(id, p.by_N);
     t.place = id - t.b * p.N;
     t.n = t.place;
-    t.at[0] = (int32_t)t.n;
-    t.at[1] = t.at[2] = 0;
+    t.at0 = (int32_t)t.n;
+    t.at1 = t.at2 = 0;
     if (p.tiled) {
         const uint32_t tile = fast_div(t.place, p.by_P), in = t.place - tile * p.by_P.d;
         const uint32_t row = fast_div(tile, p.by_nw), tw = tile - row * p.by_nw.d;
         const uint32_t tt = fast_div(row, p.by_nh), th = row - tt * p.by_nh.d;
         const uint32_t line = fast_div(in, p.by_Tw), iw = in - line * p.by_Tw.d;
         const uint32_t it = fast_div(line, p.by_Th), ih = line - it * p.by_Th.d;
-        t.at[0] = (int32_t)(tt * p.T_t + it);
-        t.at[1] = (int32_t)(th * p.T_h + ih);
-        t.at[2] = (int32_t)(tw * p.T_w + iw);
-        t.n = ((uint32_t)t.at[0] * p.g_h + (uint32_t)t.at[1]) * p.g_w + (uint32_t)t.at[2];
+        t.at0 = (int32_t)(tt * p.T_t + it);
+        t.at1 = (int32_t)(th * p.T_h + ih);
+        t.at2 = (int32_t)(tw * p.T_w + iw);
+        t.n = ((uint32_t)t.at0 * p.g_h + (uint32_t)t.at1) * p.g_w + (uint32_t)t.at2;
     } else if (p.has_grid) {
         const uint32_t line = fast_div(t.n, p.by_gw);
-        t.at[2] = (int32_t)(t.n - line * p.g_w);
+        t.at2 = (int32_t)(t.n - line * p.g_w);
         const uint32_t plane = fast_div(line, p.by_gh);
-        t.at[1] = (int32_t)(line - plane * p.g_h);
-        t.at[0] = (int32_t)plane;
-    }
-    if (p.positions) {
-        const int32_t *x = p.positions + (int64_t)t.b * p.position_batch + (int64_t)t.n * p.position_token;
-        t.at[0] = x[0];
-        if (p.axis1 < p.rot / 2) t.at[1] = x[1];
-        if (p.axis2 < p.rot / 2) t.at[2] = x[2];
+        t.at1 = (int32_t)(line - plane * p.g_h);
+        t.at0 = (int32_t)plane;
     }
     return t;
 }
+__device__ __forceinline__ void load_positions(Token &t, const Params &p)
+{
+    if (!p.positions) return;
+    const int32_t *x = p.positions + (int64_t)t.b * p.position_batch + (int64_t)t.n * p.position_token;
+    t.at0 = x[0];
+    if (p.axis1 < p.rot / 2) t.at1 = x[1];
+    if (p.axis2 < p.rot / 2) t.at2 = x[2];
+}
 
-// Cosines and sines of a lane's pairs (1 and 0 where they are not rotated; not looked at there).
+// The steps of a lane's pairs; 0 for those that are not rotated.
 template <int PATH>
-__device__ __forceinline__ void turns_of(const Token &t, uint32_t lane_in_row, const Place &at, const Params &p, float (&c)[pairs_of(PATH)],
-                                         float (&s)[pairs_of(PATH)])
+__device__ __forceinline__ void load_steps(uint32_t lane_in_row, const Place &at, const Params &p, int64_t (&step)[pairs_of(PATH)], bool (&first)[pairs_of(PATH)],
+                                           bool (&second)[pairs_of(PATH)])
 {
 #pragma unroll
     for (int i = 0; i < pairs_of(PATH); ++i) {
-        c[i] = 1.f;
-        s[i] = 0.f;
-        const bool second = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
-        if (!p.turns || !(second ? at.turn_b : at.turn_a)) continue;
-        const uint32_t pair = PATH == kHalf ? at.a + i : PATH == kGeneral ? lane_in_row + 64 * i : second ? at.b / 2 + i - 4 : at.a / 2 + i;
-        const int32_t x = pair < p.axis1 ? t.at[0] : pair < p.axis2 ? t.at[1] : t.at[2];
-        turn_of(x, p.steps[pair], p.magnitude, p.sign, c[i], s[i]);
+        const bool b = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
+        const uint32_t pair = PATH == kHalf ? at.a + i : PATH == kGeneral ? lane_in_row + 64 * i : b ? at.b / 2 + i - 4 : at.a / 2 + i;
+        step[i] = p.steps[(b ? at.turn_b : at.turn_a) ? pair : 0];
+        first[i] = pair < p.axis1;
+        second[i] = pair < p.axis2;
     }
 }
 
+// Cosines and sines of a lane's pairs.
+template <int PATH, bool FEW_REGISTERS>
+__device__ __forceinline__ void turns_of(const Token &t, const int64_t (&step)[pairs_of(PATH)], const bool (&first)[pairs_of(PATH)],
+                                         const bool (&second)[pairs_of(PATH)], const Params &p, float (&c)[pairs_of(PATH)], float (&s)[pairs_of(PATH)])
+{
+#pragma unroll
+    for (int i = 0; i < pairs_of(PATH); ++i) {
+        turn_of(first[i] ? t.at0 : second[i] ? t.at1 : t.at2, step[i], p.magnitude, p.sign, c[i], s[i]);
+        if (FEW_REGISTERS && i % 2) __builtin_amdgcn_sched_barrier(0);        // two pairs at a time
+    }
+}
+
+// (selects, not zeros and ones: what is not rotated is to stay what it is, whatever it is)
 template <int PATH>
 __device__ __forceinline__ void rotate(float (&x0)[pairs_of(PATH)], float (&x1)[pairs_of(PATH)], const float (&c)[pairs_of(PATH)],
                                        const float (&s)[pairs_of(PATH)], const Place &at, float turn_back)
 {
 #pragma unroll
     for (int i = 0; i < pairs_of(PATH); ++i) {
-        const bool second = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
-        if (second ? at.turn_b : at.turn_a) {
-            const float a = x0[i], b = x1[i], sn = s[i] * turn_back;
-            x0[i] = a * c[i] - b * sn;
-            x1[i] = a * sn + b * c[i];
-        }
+        const bool on = (PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4) ? at.turn_b : at.turn_a;
+        const float a = x0[i], b = x1[i], sn = s[i] * turn_back;
+        x0[i] = on ? a * c[i] - b * sn : a;
+        x1[i] = on ? a * sn + b * c[i] : b;
     }
 }
 
@@ -346,172 +361,231 @@ __device__ __forceinline__ void load_weights(const void *weight, const Params &p
 
 __device__ __forceinline__ const char *row_at(const Rows &r, uint32_t b, uint32_t token) { return r.data + (int64_t)b * r.batch + (int64_t)token * r.token; }
 
-// Workgroup (x, y): tokens 64 / L * x .., heads y * kWaves + wave and every gridDim.y * kWaves after that.
+// The tensor and head of a wave's row number u of all tensors' heads.
+struct HeadAt {
+    uint32_t tensor, head;
+};
+__device__ __forceinline__ HeadAt head_at(uint32_t u, const Params &p)
+{
+    const uint32_t h1 = p.t[0].heads, h2 = h1 + p.t[1].heads;           // (0 heads where there is no such tensor)
+    return u < h1 ? HeadAt{0, u} : u < h2 ? HeadAt{1, u - h1} : HeadAt{2, u - h2};
+}
+
+// Workgroup (x, y): tokens 64 / L * x .., heads y * kWaves + wave and every gridDim.y * kWaves after that, of all tensors one after the other.
+// AHEAD rows are on their way while one is worked on; the first are asked for before the positions and steps.
 template <int PATH, int L, bool SRC_F32, bool DST_F32>
 __global__ __launch_bounds__(kThreads) void sta_rows_forward_kernel(Params p)
 {
-    constexpr int NP = pairs_of(PATH);
+    constexpr int NP = pairs_of(PATH), AHEAD = SRC_F32 ? 1 : 2;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane % L, id = blockIdx.x * (64 / L) + lane / L;
     const bool on = id < p.tokens;
-    const Token t = token_of(on ? id : 0, p);
+    Token t = token_of(on ? id : 0, p);
     const Place at = place_of<PATH, L>(c, p);
-    float cs[NP], sn[NP];
-    turns_of<PATH>(t, c, at, p, cs, sn);
-    const uint32_t stride = gridDim.y * kWaves;
-    uint32_t h = blockIdx.y * kWaves + wave;
-    for (uint32_t i = 0; i < p.n_tensors; ++i) {
-        const Tensor &T = p.t[i];
-        if (h < T.heads) {
-            const char *x = row_at(T.x, t.b, t.n);
-            char *out = const_cast<char *>(row_at(T.out, t.b, t.place));
-            float w0[NP], w1[NP];
-            if (T.norm) load_weights<PATH>(T.weight, p, at, w0, w1);
-            Raw<PATH, SRC_F32> next = load_row<PATH, SRC_F32>(x + (int64_t)h * T.x.head, at, on);
-            for (; h < T.heads; h += stride) {
-                const Raw<PATH, SRC_F32> raw = next;
-                if (h + stride < T.heads) next = load_row<PATH, SRC_F32>(x + (int64_t)(h + stride) * T.x.head, at, on);
-                float x0[NP], x1[NP];
-                unpack<PATH, SRC_F32>(raw, x0, x1);
-                if (T.norm) {
-                    float sum = 0.f;
+    const uint32_t stride = gridDim.y * kWaves, total = p.t[0].heads + p.t[1].heads + p.t[2].heads;
+    uint32_t u = blockIdx.y * kWaves + wave;
+    if (u >= total) return;
+    auto load = [&](uint32_t v) __attribute__((always_inline)) {
+        const HeadAt h = head_at(v, p);
+        const Rows &x = p.t[h.tensor].x;
+        return load_row<PATH, SRC_F32>(row_at(x, t.b, t.n) + (int64_t)h.head * x.head, at, on);
+    };
+    Raw<PATH, SRC_F32> next[AHEAD];
 #pragma unroll
-                    for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
-                    const float r = rsqrtf(fmaf(row_sum<L>(sum), p.inv_D, p.eps));
+    for (int i = 0; i < AHEAD; ++i)
+        if (i == 0 || u + i * stride < total) next[i] = load(u + i * stride);
+    float cs[NP], sn[NP], w0[NP], w1[NP];
+    uint32_t weights_of = head_at(u, p).tensor;
+    if (p.t[weights_of].norm) load_weights<PATH>(p.t[weights_of].weight, p, at, w0, w1);
+    if (p.turns) {
+        int64_t step[NP];
+        bool first[NP], second[NP];
+        load_steps<PATH>(c, at, p, step, first, second);
+        load_positions(t, p);
+        turns_of<PATH, false>(t, step, first, second, p, cs, sn);
+    }
+    for (; u < total; u += AHEAD * stride) {
+        Raw<PATH, SRC_F32> raw[AHEAD];
 #pragma unroll
-                    for (int j = 0; j < NP; ++j) {
-                        x0[j] *= r * w0[j];
-                        x1[j] *= r * w1[j];
-                    }
-                }
-                if (T.rotate) rotate<PATH>(x0, x1, cs, sn, at, 1.f);
-                store_row<PATH, DST_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
-            }
+        for (int i = 0; i < AHEAD; ++i) {
+            raw[i] = next[i];
+            const uint32_t v = u + (AHEAD + i) * stride;
+            if (v < total) next[i] = load(v);
         }
-        h -= T.heads;           // the first head of the next tensor that is this wave's
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t v = u + i * stride;
+            if (i > 0 && v >= total) break;
+            const HeadAt h = head_at(v, p);
+            const Tensor &T = p.t[h.tensor];
+            float x0[NP], x1[NP];
+            unpack<PATH, SRC_F32>(raw[i], x0, x1);
+            if (T.norm) {
+                if (h.tensor != weights_of) {
+                    weights_of = h.tensor;
+                    load_weights<PATH>(T.weight, p, at, w0, w1);
+                }
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
+                const float r = rsqrtf(fmaf(row_sum<L>(at.in ? sum : 0.f), p.inv_D, p.eps));
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    x0[j] *= r * w0[j];
+                    x1[j] *= r * w1[j];
+                }
+            }
+            if (T.rotate) rotate<PATH>(x0, x1, cs, sn, at, 1.f);
+            store_row<PATH, DST_F32>(const_cast<char *>(row_at(T.out, t.b, t.place)) + (int64_t)h.head * T.out.head, at, on, x0, x1);
+        }
     }
 }
 
-// Workgroups take groups of tokens in turn; the first two tensors' weight gradients are summed in registers, then over the
-// workgroup, and left in `partial`.
+// A workgroup works for one tensor: on units of 64 / L tokens by the heads split * kWaves + wave, and every splits * kWaves after that, in turn with
+// the tensor's other workgroups.  So a lane sums one weight gradient, which goes from the registers over the workgroup into `partial`.
+// (With all tensors in one workgroup, 168 registers and 236 bytes of scratch, or 183 registers and nothing asked for ahead: 378 and 252 us for a
+// clip of 27,648 tokens by 12 heads of 128 from float32; now 244, 4.5 TB/s.)
 template <int PATH, int L, bool SRC_F32, bool DST_F32>
-__global__ __launch_bounds__(kThreads) void sta_rows_backward_kernel(Params p)
+__global__ __launch_bounds__(kThreads, 3) void sta_rows_backward_kernel(Params p)
 {
     constexpr int NP = pairs_of(PATH);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane % L;
     const Place at = place_of<PATH, L>(c, p);
-    float dw0[2][NP], dw1[2][NP];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < NP; ++j) dw0[i][j] = dw1[i][j] = 0.f;
-    const uint32_t stride = gridDim.y * kWaves, groups = (p.tokens + 64 / L - 1) / (64 / L);
-    for (uint32_t group = blockIdx.x; group < groups; group += gridDim.x) {
-        const uint32_t id = group * (64 / L) + lane / L;
-        const bool on = id < p.tokens;
-        const Token t = token_of(on ? id : 0, p);
-        float cs[NP], sn[NP];
-        turns_of<PATH>(t, c, at, p, cs, sn);
-        uint32_t h = blockIdx.y * kWaves + wave;
-        auto tensor = [&](const Tensor &T, float(&sum0)[NP], float(&sum1)[NP]) __attribute__((always_inline)) {
-            if (h < T.heads) {
-                const char *x = row_at(T.x, t.b, t.n), *dy = row_at(T.dy, t.b, t.place);
-                char *out = const_cast<char *>(row_at(T.out, t.b, t.n));
-                float w0[NP], w1[NP];
-                load_weights<PATH>(T.weight, p, at, w0, w1);
-                for (; h < T.heads; h += stride) {
-                    const Raw<PATH, SRC_F32> raw_x = load_row<PATH, SRC_F32>(x + (int64_t)h * T.x.head, at, on);
-                    const Raw<PATH, DST_F32> raw_g = load_row<PATH, DST_F32>(dy + (int64_t)h * T.dy.head, at, on);
-                    float x0[NP], x1[NP], g0[NP], g1[NP];
-                    unpack<PATH, SRC_F32>(raw_x, x0, x1);
-                    unpack<PATH, DST_F32>(raw_g, g0, g1);
-                    rotate<PATH>(g0, g1, cs, sn, at, -1.f);
-                    float sum = 0.f;
-#pragma unroll
-                    for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
-                    const float r = rsqrtf(fmaf(row_sum<L>(sum), p.inv_D, p.eps));
-                    float dot = 0.f;
-#pragma unroll
-                    for (int j = 0; j < NP; ++j) {
-                        x0[j] *= r;
-                        x1[j] *= r;
-                        sum0[j] = fmaf(g0[j], x0[j], sum0[j]);
-                        sum1[j] = fmaf(g1[j], x1[j], sum1[j]);
-                        g0[j] *= w0[j];
-                        g1[j] *= w1[j];
-                        dot = fmaf(g0[j], x0[j], fmaf(g1[j], x1[j], dot));
-                    }
-                    dot = row_sum<L>(dot) * p.inv_D;
-#pragma unroll
-                    for (int j = 0; j < NP; ++j) {
-                        x0[j] = r * fmaf(-dot, x0[j], g0[j]);
-                        x1[j] = r * fmaf(-dot, x1[j], g1[j]);
-                    }
-                    store_row<PATH, SRC_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
-                }
-            }
-            h -= T.heads;
-        };
-        tensor(p.t[0], dw0[0], dw1[0]);
-        tensor(p.t[1], dw0[1], dw1[1]);
-        if (p.n_tensors > 2 && h < p.t[2].heads) {              // values: moved back
-            const Tensor &T = p.t[2];
+    const uint32_t tensor = blockIdx.x < p.share[1].first ? 0 : blockIdx.x < p.share[2].first ? 1 : 2;
+    const Tensor &T = p.t[tensor];
+    const Share &share = p.share[tensor];
+    const uint32_t stride = share.splits.d * kWaves;
+    if (!T.norm) {                                          // values: moved back
+#pragma unroll 1
+        for (uint32_t unit = blockIdx.x - share.first; unit < share.units; unit += share.blocks) {
+            const uint32_t group = fast_div(unit, share.splits), id = group * (64 / L) + lane / L;
+            const bool on = id < p.tokens;
+            const Token t = token_of(on ? id : 0, p);
             const char *dy = row_at(T.dy, t.b, t.place);
             char *out = const_cast<char *>(row_at(T.out, t.b, t.n));
-            for (; h < T.heads; h += stride) {
+#pragma unroll 2
+            for (uint32_t h = (unit - group * share.splits.d) * kWaves + wave; h < T.heads; h += stride) {
                 float x0[NP], x1[NP];
                 unpack<PATH, DST_F32>(load_row<PATH, DST_F32>(dy + (int64_t)h * T.dy.head, at, on), x0, x1);
                 store_row<PATH, SRC_F32>(out + (int64_t)h * T.out.head, at, on, x0, x1);
             }
         }
+        return;
+    }
+    float w0[NP], w1[NP], dw0[NP], dw1[NP];
+    load_weights<PATH>(T.weight, p, at, w0, w1);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) dw0[j] = dw1[j] = 0.f;
+#pragma unroll 1
+    for (uint32_t unit = blockIdx.x - share.first; unit < share.units; unit += share.blocks) {
+        const uint32_t group = fast_div(unit, share.splits), id = group * (64 / L) + lane / L;
+        const bool in = id < p.tokens;
+        Token t = token_of(in ? id : 0, p);
+        const char *x = row_at(T.x, t.b, t.n), *dy = row_at(T.dy, t.b, t.place);
+        char *out = const_cast<char *>(row_at(T.out, t.b, t.n));
+        // all waves go around as often; one without a head left works on the last one and drops it
+        const uint32_t first_head = (unit - group * share.splits.d) * kWaves;
+        uint32_t h = first_head + wave;
+        auto address = [&](uint32_t head) { return (int64_t)(head < T.heads ? head : T.heads - 1); };
+        Raw<PATH, SRC_F32> next_x = load_row<PATH, SRC_F32>(x + address(h) * T.x.head, at, in);
+        Raw<PATH, DST_F32> next_g = load_row<PATH, DST_F32>(dy + address(h) * T.dy.head, at, in);
+        float cs[NP] = {}, sn[NP] = {};
+        if (p.turns) {
+            int64_t step[NP];
+            bool first[NP], second[NP];
+            load_steps<PATH>(c, at, p, step, first, second);
+            load_positions(t, p);
+            turns_of<PATH, true>(t, step, first, second, p, cs, sn);
+        }
+        uint32_t left = (T.heads - first_head + stride - 1) / stride;
+#pragma unroll 1
+        do {
+            const bool on = in && h < T.heads;
+            float x0[NP], x1[NP], g0[NP], g1[NP];
+            unpack<PATH, SRC_F32>(next_x, x0, x1);
+            unpack<PATH, DST_F32>(next_g, g0, g1);
+            if (left > 1) {
+                next_x = load_row<PATH, SRC_F32>(x + address(h + stride) * T.x.head, at, in);
+                next_g = load_row<PATH, DST_F32>(dy + address(h + stride) * T.dy.head, at, in);
+            }
+            rotate<PATH>(g0, g1, cs, sn, at, -1.f);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) sum = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], sum));
+            // 0 where there is no row: it is then no term of the weights' gradient either
+            const float r = on ? rsqrtf(fmaf(row_sum<L>(at.in ? sum : 0.f), p.inv_D, p.eps)) : 0.f;
+            float dot = 0.f;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                x0[j] *= r;
+                x1[j] *= r;
+                dw0[j] = fmaf(g0[j], x0[j], dw0[j]);
+                dw1[j] = fmaf(g1[j], x1[j], dw1[j]);
+                g0[j] *= w0[j];
+                g1[j] *= w1[j];
+                dot = fmaf(g0[j], x0[j], fmaf(g1[j], x1[j], dot));
+            }
+            dot = row_sum<L>(at.in ? dot : 0.f) * p.inv_D;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                x0[j] = r * fmaf(-dot, x0[j], g0[j]);
+                x1[j] = r * fmaf(-dot, x1[j], g1[j]);
+            }
+            store_row<PATH, SRC_F32>(out + address(h) * T.out.head, at, on, x0, x1);
+            h += stride;
+        } while (--left > 0);
     }
     if (!p.partial) return;
     // over the tokens of a wave, then over the waves; channels in their places
-    __shared__ float sums[kWaves][2][256];
+    __shared__ float sums[kWaves][256];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < NP; ++j) {
+        float a = dw0[j], b = dw1[j];
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            float a = dw0[i][j], b = dw1[i][j];
-#pragma unroll
-            for (int m = L; m < 64; m *= 2) {
-                a += __shfl_xor(a, m, 64);
-                b += __shfl_xor(b, m, 64);
-            }
-            if (lane < L && (PATH == kGeneral && j ? at.in2 : at.in)) {
-                uint32_t ea, eb;
-                if constexpr (PATH == kGeneral) { ea = at.e[2 * j]; eb = at.e[2 * j + 1]; }
-                else if constexpr (PATH == kHalf) { ea = at.a + j; eb = at.b + j; }
-                else { ea = j < 4 ? at.a + 2 * j : at.b + 2 * (j - 4); eb = ea + 1; }
-                sums[wave][i][ea] = a;
-                sums[wave][i][eb] = b;
-            }
+        for (int m = L; m < 64; m *= 2) {
+            a += __shfl_xor(a, m, 64);
+            b += __shfl_xor(b, m, 64);
         }
-    __syncthreads();
-    float *to = p.partial + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.D;
-    for (uint32_t e = threadIdx.x; e < 2 * p.D; e += kThreads) {
-        const uint32_t i = e >= p.D, ch = e - i * p.D;
-        to[e] = (sums[0][i][ch] + sums[1][i][ch]) + (sums[2][i][ch] + sums[3][i][ch]);
+        if (lane < L && (PATH == kGeneral && j ? at.in2 : at.in)) {
+            uint32_t ea, eb;
+            if constexpr (PATH == kGeneral) { ea = at.e[2 * j]; eb = at.e[2 * j + 1]; }
+            else if constexpr (PATH == kHalf) { ea = at.a + j; eb = at.b + j; }
+            else { ea = j < 4 ? at.a + 2 * j : at.b + 2 * (j - 4); eb = ea + 1; }
+            sums[wave][ea] = a;
+            sums[wave][eb] = b;
+        }
     }
+    __syncthreads();
+    float *to = p.partial + (size_t)blockIdx.x * p.D;
+    for (uint32_t e = threadIdx.x; e < p.D; e += kThreads) to[e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
 }
 
-// d_weight = sum of the workgroups' sums: 16 columns a workgroup, 16 slices of the rows, then the slices in order.
-__global__ __launch_bounds__(256) void sta_rows_weights_kernel(const float *partial, uint32_t rows, uint32_t D, float *d_q, float *d_k)
+// d_weight = sum of the workgroups' sums: 16 columns a workgroup, 64 slices of the rows of which a lane has eight on their way, then the slices in
+// order.
+constexpr int kSlices = 64;
+__global__ __launch_bounds__(16 * kSlices) void sta_rows_weights_kernel(const float *partial, uint32_t q_rows, uint32_t k_rows, uint32_t D, float *d_q, float *d_k)
 {
-    __shared__ float sums[16][17];
-    const uint32_t col = threadIdx.x & 15, slice = threadIdx.x >> 4, e = blockIdx.x * 16 + col;
+    __shared__ float sums[kSlices][17];
+    const uint32_t col = threadIdx.x & 15, slice = threadIdx.x >> 4, e = blockIdx.x * 16 + col, rows = blockIdx.y ? k_rows : q_rows;
+    if (blockIdx.y) partial += (size_t)q_rows * D;
+    const bool in = e < D;
     float sum = 0.f;
-    if (e < 2 * D)
-        for (uint32_t r = slice; r < rows; r += 16) sum += partial[(size_t)r * 2 * D + e];
+    for (uint32_t r = slice; r < rows; r += 8 * kSlices) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = in && r + i * kSlices < rows ? partial[(size_t)(r + i * kSlices) * D + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i];
+    }
     sums[slice][col] = sum;
     __syncthreads();
-    if (slice == 0 && e < 2 * D) {
+    float *to = blockIdx.y ? d_k : d_q;
+    if (slice == 0 && in && to) {
         sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += sums[i][col];
-        float *to = e < D ? d_q : d_k;
-        if (to) to[e < D ? e : e - D] = sum;
+        for (int i = 0; i < kSlices; ++i) sum += sums[i][col];
+        to[e] = sum;
     }
 }
 
@@ -601,7 +675,7 @@ int path_of(const Params &p)
 }
 
 constexpr uint32_t kWantBlocks = 1024;          // four workgroups a CU
-constexpr uint32_t kMostPartials = 1024;
+constexpr uint32_t kMostPartials = 1024;        // workgroups of the gradients, four a CU
 
 // Heads are dealt to gridDim.y workgroups where the tokens alone do not make enough of them.
 uint32_t split_of(uint32_t groups, uint32_t heads)
@@ -611,39 +685,50 @@ uint32_t split_of(uint32_t groups, uint32_t heads)
 }
 
 template <int PATH, int L, bool SRC_F32, bool DST_F32>
-hipError_t launch(const Params &p, bool backward, uint32_t *rows, hipStream_t stream)
+hipError_t launch(Params &p, bool backward, hipStream_t stream)
 {
     const uint32_t per = 64 / L, groups = (p.tokens + per - 1) / per;
     uint32_t heads = 0;
     for (uint32_t i = 0; i < p.n_tensors; ++i) heads += p.t[i].heads;
-    const uint32_t y = split_of(groups, heads);
-    if (!backward) return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, y), dim3(kThreads), stream, p);
-    const uint32_t x = groups * (uint64_t)y > kMostPartials ? kMostPartials / y : groups;
-    *rows = x * y;
-    return sta::launch_kernel(sta_rows_backward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(x, y), dim3(kThreads), stream, p);
+    if (!backward)
+        return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, split_of(groups, heads)), dim3(kThreads), stream, p);
+    // workgroups by heads, units of as few heads a wave as it takes to have that many
+    uint32_t first = 0;
+    for (uint32_t i = 0; i < 3; ++i) {
+        Share &s = p.share[i];
+        const uint32_t h = i < p.n_tensors ? p.t[i].heads : 0;
+        uint32_t blocks = (uint32_t)((uint64_t)(kMostPartials - 3) * h / heads) + (h > 0);
+        const uint32_t most = (h + kWaves - 1) / kWaves, want = (blocks + groups - 1) / groups, splits = want < 1 ? 1 : want < most ? want : most;
+        s.units = h > 0 ? groups * (splits > 0 ? splits : 1) : 0;
+        s.splits = fast_div_of(splits > 0 ? splits : 1);
+        s.blocks = blocks < s.units ? blocks : s.units;
+        s.first = first;
+        first += s.blocks;
+    }
+    return sta::launch_kernel(sta_rows_backward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(first), dim3(kThreads), stream, p);
 }
 
 template <int PATH, int L>
-hipError_t launch_types(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+hipError_t launch_types(Params &p, bool src_f32, bool dst_f32, bool backward, hipStream_t stream)
 {
-    if (src_f32) return dst_f32 ? launch<PATH, L, true, true>(p, backward, rows, stream) : launch<PATH, L, true, false>(p, backward, rows, stream);
-    return dst_f32 ? launch<PATH, L, false, true>(p, backward, rows, stream) : launch<PATH, L, false, false>(p, backward, rows, stream);
+    if (src_f32) return dst_f32 ? launch<PATH, L, true, true>(p, backward, stream) : launch<PATH, L, true, false>(p, backward, stream);
+    return dst_f32 ? launch<PATH, L, false, true>(p, backward, stream) : launch<PATH, L, false, false>(p, backward, stream);
 }
 
 template <int PATH>
-hipError_t launch_lanes(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+hipError_t launch_lanes(Params &p, bool src_f32, bool dst_f32, bool backward, hipStream_t stream)
 {
-    if (p.D <= 64) return launch_types<PATH, 4>(p, src_f32, dst_f32, backward, rows, stream);
-    if (p.D <= 128) return launch_types<PATH, 8>(p, src_f32, dst_f32, backward, rows, stream);
-    return launch_types<PATH, 16>(p, src_f32, dst_f32, backward, rows, stream);
+    if (p.D <= 64) return launch_types<PATH, 4>(p, src_f32, dst_f32, backward, stream);
+    if (p.D <= 128) return launch_types<PATH, 8>(p, src_f32, dst_f32, backward, stream);
+    return launch_types<PATH, 16>(p, src_f32, dst_f32, backward, stream);
 }
 
-hipError_t launch_rows(const Params &p, bool src_f32, bool dst_f32, bool backward, uint32_t *rows, hipStream_t stream)
+hipError_t launch_rows(Params &p, bool src_f32, bool dst_f32, bool backward, hipStream_t stream)
 {
     switch (path_of(p)) {
-    case kHalf: return launch_lanes<kHalf>(p, src_f32, dst_f32, backward, rows, stream);
-    case kInterleaved: return launch_lanes<kInterleaved>(p, src_f32, dst_f32, backward, rows, stream);
-    default: return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, rows, stream);
+    case kHalf: return launch_lanes<kHalf>(p, src_f32, dst_f32, backward, stream);
+    case kInterleaved: return launch_lanes<kInterleaved>(p, src_f32, dst_f32, backward, stream);
+    default: return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, stream);
     }
 }
 
@@ -703,7 +788,7 @@ int sta_rope(const sta_head_rows *in, const sta_head_rows *out, int n_tensors, i
         p.t[i].heads = in[i].heads;
         p.t[i].rotate = p.turns;
     }
-    const hipError_t e = launch_rows(p, in[0].dtype == STA_F32, out[0].dtype == STA_F32, false, nullptr, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_rows(p, in[0].dtype == STA_F32, out[0].dtype == STA_F32, false, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
 
@@ -737,13 +822,13 @@ int sta_qk_norm_rope(const sta_head_rows *q, const sta_head_rows *k, const sta_h
             if (!(i == j && !tile && same_rows(*in[i], *out[j])) && rows_overlap(*in[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
             if (i < j && rows_overlap(*out[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
         }
-    const hipError_t e = launch_rows(p, q->dtype == STA_F32, q_out->dtype == STA_F32, false, nullptr, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_rows(p, q->dtype == STA_F32, q_out->dtype == STA_F32, false, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
 
 size_t sta_qk_norm_rope_workspace_bytes(int D)
 {
-    return D < 2 || D > kMostD || D % 2 ? 0 : (size_t)kMostPartials * 2 * D * sizeof(float);
+    return D < 2 || D > kMostD || D % 2 ? 0 : (size_t)kMostPartials * D * sizeof(float);
 }
 
 int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *d_q_out, const sta_head_rows *d_k_out,
@@ -763,7 +848,6 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
     p.n_tensors = d_v ? 3 : 2;
     p.weight_f32 = weight_dt == STA_F32;
     p.partial = sums ? static_cast<float *>(workspace) : nullptr;
-    uint32_t rows = 0;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (p.tokens != 0) {
         for (uint32_t i = 0; i < p.n_tensors; ++i) {
@@ -790,9 +874,10 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
                 for (const sta_head_rows *r : {x[i], dy[i], dx[i]})
                     if (sums && r && w0 < (uintptr_t)r->data + extent_of(*r, B, N, D) && (uintptr_t)r->data < w1) return STA_ERR_ALIAS;
             }
-        if (launch_rows(p, q->dtype == STA_F32, d_q_out->dtype == STA_F32, true, &rows, stream) != hipSuccess) return STA_ERR_HIP;
+        if (launch_rows(p, q->dtype == STA_F32, d_q_out->dtype == STA_F32, true, stream) != hipSuccess) return STA_ERR_HIP;
     }
-    if (sums && sta::launch_kernel(sta_rows_weights_kernel, dim3((2 * D + 15) / 16), dim3(256), stream, p.partial, rows, p.D, d_q_weight, d_k_weight) != hipSuccess)
+    if (sums && sta::launch_kernel(sta_rows_weights_kernel, dim3((D + 15) / 16, 2), dim3(16 * kSlices), stream, p.partial, p.share[0].blocks,
+                                  p.share[1].blocks, p.D, d_q_weight, d_k_weight) != hipSuccess)
         return STA_ERR_HIP;
     return STA_OK;
 }
