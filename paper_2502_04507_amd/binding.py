@@ -3,8 +3,8 @@
 Tensors are torch tensors used purely as device-memory handles (data_ptr);
 the stream is torch's current HIP stream unless one is given.
 
-The permutations, sta_forward, sta_forward_lse and sta_backward go through the extension sta_fastcall where their arguments are
-ordinary ones, everything else (and every error message) through ctypes; without the extension, with a warning, everything.
+The permutations, sta_forward, sta_forward_lse and sta_backward (and the operators of layer_ops) go through the extension sta_fastcall where their
+arguments are ordinary ones, everything else (and every error message) through ctypes; without the extension, with a warning, everything.
 """
 import ctypes
 import importlib
@@ -104,11 +104,13 @@ def load_library():
 
 
 _FAST_ENTRIES = ("sta_tile_permute", "sta_untile", "sta_forward", "sta_forward_lse", "sta_backward")
+_FAST_LAYER_ENTRIES = ("sta_rope", "sta_qk_norm_rope", "sta_qk_norm_rope_backward", "sta_packed_forward", "sta_packed_backward")
 
 
 class _GeneralPath:
     """Stands for the extension where it cannot be loaded: leaves every call to the general path."""
     tile_permute = untile = forward = forward_lse = backward = staticmethod(lambda *args: None)
+    rope = norm_rope = norm_rope_backward = packed_forward = packed_backward = tile_permute
 
 
 def _load_fast():
@@ -121,6 +123,7 @@ def _load_fast():
         return _GeneralPath
     if _raw_stream is not None and _current_device is not None:     # unbound, it leaves every call to the general path
         fast.bind(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _FAST_ENTRIES], _current_device, _raw_stream)
+        fast.bind_layers(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _FAST_LAYER_ENTRIES])
     return fast
 
 

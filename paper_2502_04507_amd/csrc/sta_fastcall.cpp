@@ -15,6 +15,8 @@
 
 #include <cstdint>
 
+#include "../../include/sta.h"
+
 namespace {
 
 using PermuteFn = int (*)(const void *, void *, int, int, int, int, int, const int *, const int *, void *);
@@ -242,6 +244,276 @@ PyObject *py_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---- rows of heads and packed sequences: strided device tensors, one launch each; us per call, host alone, ctypes against this:
+// sta_qk_norm_rope of q, k and v 10.7, 4.7; sta_packed_forward 8.8, 3.9; sta_rope of two tensors 8.7, 3.8
+struct LayerEntries {
+    decltype(&sta_rope) rope;
+    decltype(&sta_qk_norm_rope) norm_rope;
+    decltype(&sta_qk_norm_rope_backward) norm_rope_backward;
+    decltype(&sta_packed_forward) packed_forward;
+    decltype(&sta_packed_backward) packed_backward;
+} layers = {};
+
+bool small(int64_t x) { return x <= INT32_MAX; }
+
+// A device tensor [B, N, H, D] whose channels are adjacent.
+bool head_rows(PyObject *o, int64_t B, int64_t N, int64_t D, sta_head_rows &r)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() != 4 || t.numel() == 0) return false;
+    const auto size = t.sizes(), stride = t.strides();
+    const auto type = t.scalar_type();
+    if (size[0] != B || size[1] != N || size[3] != D || stride[3] != 1 || !small(size[2]) || (type != at::kBFloat16 && type != at::kFloat)) return false;
+    r = {t.data_ptr(), stride[0], stride[1], stride[2], (int)size[2], type == at::kBFloat16 ? kBf16 : kF32};
+    return true;
+}
+// B, N and D of the first tensor.
+bool first_shape(PyObject *o, int64_t (&s)[3])
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.dim() != 4) return false;
+    s[0] = t.size(0); s[1] = t.size(1); s[2] = t.size(3);
+    return small(s[0]) && small(s[1]) && small(s[2]);
+}
+// None, or (address of a sta_rotary, tokens its positions are for or -1, batch entries or -1)
+bool rotary_of(PyObject *o, int64_t B, int64_t N, const sta_rotary *&out)
+{
+    out = nullptr;
+    if (o == Py_None) return true;
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 3) return false;
+    const long long n = PyLong_AsLongLong(PyTuple_GET_ITEM(o, 1)), b = PyLong_AsLongLong(PyTuple_GET_ITEM(o, 2));
+    out = static_cast<const sta_rotary *>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(o, 0)));
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return out != nullptr && (n < 0 || n == N) && (b < 0 || b == B);
+}
+// One dimension of n elements, dense; None: null.
+bool vector(PyObject *o, int64_t n, at::ScalarType type, const void *&out)
+{
+    out = nullptr;
+    if (o == Py_None) return true;
+    View v;
+    if (!dense(o, v) || v.t->dim() != 1 || v.t->size(0) != n || v.t->scalar_type() != type) return false;
+    out = v.ptr;
+    return out != nullptr || n == 0;
+}
+// The two weights, of one type.
+bool weights(PyObject *a, PyObject *b, int64_t D, const void *(&w)[2], int &type)
+{
+    if (vector(a, D, at::kFloat, w[0]) && vector(b, D, at::kFloat, w[1])) {
+        type = kF32;
+        return true;
+    }
+    type = kBf16;
+    return vector(a, D, at::kBFloat16, w[0]) && vector(b, D, at::kBFloat16, w[1]);
+}
+bool grid_tile(PyObject *g, PyObject *t, int (&grid)[3], int (&tile)[3])
+{
+    return (g == Py_None || ints(g, 3, grid)) && (t == Py_None || (g != Py_None && ints(t, 3, tile)));
+}
+bool scratch(PyObject *o, void *&ptr, size_t &bytes)
+{
+    ptr = nullptr;
+    bytes = 0;
+    if (o == Py_None) return true;
+    View v;
+    if (!dense(o, v)) return false;
+    ptr = v.ptr;
+    bytes = v.t->numel() * v.t->element_size();
+    return true;
+}
+bool integer(PyObject *o, int &out)
+{
+    int overflow;
+    if (!PyLong_CheckExact(o)) return false;
+    const long x = PyLong_AsLongAndOverflow(o, &overflow);
+    out = (int)x;
+    return overflow == 0 && x >= INT32_MIN && x <= INT32_MAX;
+}
+
+// (inputs, outputs, rotary, inverse)
+PyObject *py_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        sta_head_rows in[3], out[3];
+        PyObject **items[2];
+        Py_ssize_t count[2];
+        if (!layers.rope || n != 4 || !PyBool_Check(args[3])) Py_RETURN_NONE;
+        for (int i = 0; i < 2; ++i) {
+            if (PyTuple_CheckExact(args[i])) { items[i] = &PyTuple_GET_ITEM(args[i], 0); count[i] = PyTuple_GET_SIZE(args[i]); }
+            else if (PyList_CheckExact(args[i])) { items[i] = &PyList_GET_ITEM(args[i], 0); count[i] = PyList_GET_SIZE(args[i]); }
+            else Py_RETURN_NONE;
+        }
+        int64_t s[3];
+        const sta_rotary *rotary;
+        if (count[0] < 1 || count[0] > 3 || count[1] != count[0] || !first_shape(items[0][0], s) || !rotary_of(args[2], s[0], s[1], rotary) || !rotary)
+            Py_RETURN_NONE;
+        for (Py_ssize_t i = 0; i < count[0]; ++i)
+            if (!head_rows(items[0][i], s[0], s[1], s[2], in[i]) || !head_rows(items[1][i], s[0], s[1], s[2], out[i])) Py_RETURN_NONE;
+        const int inverse = args[3] == Py_True;
+        void *stream;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() { return layers.rope(in, out, (int)count[0], (int)s[0], (int)s[1], (int)s[2], rotary, inverse, stream); });
+    });
+}
+
+// (q, k, v, q_out, k_out, v_out, q_weight, k_weight, rotary, eps, grid, tile)
+PyObject *py_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        sta_head_rows r[6];
+        int64_t s[3];
+        const sta_rotary *rotary;
+        const void *w[2];
+        int type, grid[3], tile[3];
+        float eps;
+        if (!layers.norm_rope || n != 12 || !first_shape(args[0], s) || !rotary_of(args[8], s[0], s[1], rotary) || !weights(args[6], args[7], s[2], w, type) ||
+            !number(args[9], eps) || !grid_tile(args[10], args[11], grid, tile) || (args[2] == Py_None) != (args[5] == Py_None))
+            Py_RETURN_NONE;
+        for (int i = 0; i < 6; ++i)
+            if (args[i] == Py_None ? i % 3 != 2 : !head_rows(args[i], s[0], s[1], s[2], r[i])) Py_RETURN_NONE;
+        const bool values = args[2] != Py_None;
+        void *stream;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return layers.norm_rope(&r[0], &r[1], values ? &r[2] : nullptr, &r[3], &r[4], values ? &r[5] : nullptr, w[0], w[1], type, eps, rotary, (int)s[0],
+                                    (int)s[1], (int)s[2], args[10] == Py_None ? nullptr : grid, args[11] == Py_None ? nullptr : tile, stream);
+        });
+    });
+}
+
+// (q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_weight, k_weight, d_q_weight, d_k_weight, rotary, workspace, eps, grid, tile)
+PyObject *py_norm_rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        sta_head_rows r[8];
+        int64_t s[3];
+        const sta_rotary *rotary;
+        const void *w[2], *dw[2];
+        int type, grid[3], tile[3];
+        float eps;
+        void *ws, *stream;
+        size_t bytes;
+        if (!layers.norm_rope_backward || n != 17 || !first_shape(args[0], s) || !rotary_of(args[12], s[0], s[1], rotary) ||
+            !weights(args[8], args[9], s[2], w, type) || !vector(args[10], s[2], at::kFloat, dw[0]) || !vector(args[11], s[2], at::kFloat, dw[1]) ||
+            !scratch(args[13], ws, bytes) || !number(args[14], eps) || !grid_tile(args[15], args[16], grid, tile) ||
+            (args[4] == Py_None) != (args[7] == Py_None))
+            Py_RETURN_NONE;
+        for (int i = 0; i < 8; ++i)
+            if (args[i] == Py_None ? i != 4 && i != 7 : !head_rows(args[i], s[0], s[1], s[2], r[i])) Py_RETURN_NONE;
+        const bool values = args[4] != Py_None;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return layers.norm_rope_backward(&r[0], &r[1], &r[2], &r[3], values ? &r[4] : nullptr, &r[5], &r[6], values ? &r[7] : nullptr, w[0], w[1], type,
+                                             static_cast<float *>(const_cast<void *>(dw[0])), static_cast<float *>(const_cast<void *>(dw[1])), eps, rotary,
+                                             (int)s[0], (int)s[1], (int)s[2], args[15] == Py_None ? nullptr : grid, args[16] == Py_None ? nullptr : tile, ws,
+                                             bytes, stream);
+        });
+    });
+}
+
+// A device tensor [tokens, H, D] of bf16 whose channels are adjacent.
+bool packed_rows(PyObject *o, int64_t tokens, int64_t heads, int64_t D, sta_head_rows &r)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() != 3 || t.numel() == 0 || t.scalar_type() != at::kBFloat16) return false;
+    const auto size = t.sizes(), stride = t.strides();
+    if (size[0] != tokens || size[1] != heads || size[2] != D || stride[2] != 1) return false;
+    r = {t.data_ptr(), 0, stride[0], stride[1], (int)heads, kBf16};
+    return true;
+}
+struct PackedShape {
+    int64_t tq, Hq, tk, Hkv, D, S;
+};
+bool packed_shape(PyObject *q, PyObject *k, PyObject *cu_q, PackedShape &s)
+{
+    if (!THPVariable_CheckExact(q) || !THPVariable_CheckExact(k) || !THPVariable_CheckExact(cu_q)) return false;
+    const at::Tensor &a = THPVariable_Unpack(q), &b = THPVariable_Unpack(k);
+    if (a.dim() != 3 || b.dim() != 3) return false;
+    s = {a.size(0), a.size(1), b.size(0), b.size(1), a.size(2), THPVariable_Unpack(cu_q).numel() - 1};
+    return small(s.tq) && small(s.Hq) && small(s.tk) && small(s.Hkv) && small(s.D) && s.S >= 0 && small(s.S);
+}
+bool packed_lse(PyObject *o, const PackedShape &s, const void *&out)
+{
+    out = nullptr;
+    if (o == Py_None) return true;
+    View v;
+    if (!dense(o, v) || v.t->dim() != 2 || v.t->size(0) != s.Hq || v.t->size(1) != s.tq || v.t->scalar_type() != at::kFloat) return false;
+    out = v.ptr;
+    return out != nullptr;
+}
+
+// (q, k, v, o, cu_q, cu_k, max_q, max_k, causal, scale, lse, k_used, workspace)
+PyObject *py_packed_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        PackedShape s;
+        sta_head_rows r[4];
+        const void *cu_q, *cu_k, *used, *lse;
+        int max_q, max_k;
+        float scale;
+        void *ws, *stream;
+        size_t bytes;
+        if (!layers.packed_forward || n != 13 || !packed_shape(args[0], args[1], args[4], s) || !packed_rows(args[0], s.tq, s.Hq, s.D, r[0]) ||
+            !packed_rows(args[1], s.tk, s.Hkv, s.D, r[1]) || !packed_rows(args[2], s.tk, s.Hkv, s.D, r[2]) || !packed_rows(args[3], s.tq, s.Hq, s.D, r[3]) ||
+            args[4] == Py_None || args[5] == Py_None || !vector(args[4], s.S + 1, at::kInt, cu_q) || !vector(args[5], s.S + 1, at::kInt, cu_k) ||
+            !integer(args[6], max_q) || !integer(args[7], max_k) || !PyBool_Check(args[8]) || !number(args[9], scale) || !packed_lse(args[10], s, lse) ||
+            !vector(args[11], s.S, at::kInt, used) || !scratch(args[12], ws, bytes))
+            Py_RETURN_NONE;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return layers.packed_forward(&r[0], &r[1], &r[2], &r[3], static_cast<float *>(const_cast<void *>(lse)), s.tq, s.tk,
+                                         static_cast<const int32_t *>(cu_q), static_cast<const int32_t *>(cu_k), static_cast<const int32_t *>(used),
+                                         (int)s.S, max_q, max_k, (int)s.D, args[8] == Py_True, scale, ws, bytes, stream);
+        });
+    });
+}
+
+// (q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, max_k, workspace, causal, scale)
+PyObject *py_packed_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        PackedShape s;
+        sta_head_rows r[8];
+        const void *cu_q, *cu_k, *lse;
+        int max_q, max_k;
+        float scale;
+        void *ws, *stream;
+        size_t bytes;
+        if (!layers.packed_backward || n != 16 || !packed_shape(args[0], args[1], args[9], s) || args[5] == Py_None || !packed_lse(args[5], s, lse) ||
+            args[9] == Py_None || args[10] == Py_None || !vector(args[9], s.S + 1, at::kInt, cu_q) || !vector(args[10], s.S + 1, at::kInt, cu_k) ||
+            !integer(args[11], max_q) || !integer(args[12], max_k) || !scratch(args[13], ws, bytes) || !PyBool_Check(args[14]) || !number(args[15], scale))
+            Py_RETURN_NONE;
+        for (int i = 0; i < 8; ++i) {                       // q k v o d_o d_q d_k d_v
+            const bool keys = i == 1 || i == 2 || i >= 6;
+            if (!packed_rows(args[i < 5 ? i : i + 1], keys ? s.tk : s.tq, keys ? s.Hkv : s.Hq, s.D, r[i])) Py_RETURN_NONE;
+        }
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return layers.packed_backward(&r[0], &r[1], &r[2], &r[3], &r[4], static_cast<const float *>(lse), &r[5], &r[6], &r[7], s.tq, s.tk,
+                                          static_cast<const int32_t *>(cu_q), static_cast<const int32_t *>(cu_k), (int)s.S, max_q, max_k, (int)s.D,
+                                          args[14] == Py_True, scale, ws, bytes, stream);
+        });
+    });
+}
+
+// (addresses of the five entry points in the order of LayerEntries); the streams are bind's
+PyObject *py_bind_layers(PyObject *, PyObject *args)
+{
+    unsigned long long a[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &a[0], &a[1], &a[2], &a[3], &a[4])) return nullptr;
+    if (current_device && current_raw_stream)
+        layers = {reinterpret_cast<decltype(&sta_rope)>(a[0]), reinterpret_cast<decltype(&sta_qk_norm_rope)>(a[1]),
+                  reinterpret_cast<decltype(&sta_qk_norm_rope_backward)>(a[2]), reinterpret_cast<decltype(&sta_packed_forward)>(a[3]),
+                  reinterpret_cast<decltype(&sta_packed_backward)>(a[4])};
+    Py_RETURN_NONE;
+}
+
 // (addresses of the five entry points in the order of Entries, torch's current device and raw current stream)
 PyObject *py_bind(PyObject *, PyObject *args)
 {
@@ -263,7 +535,8 @@ PyObject *py_bind(PyObject *, PyObject *args)
 #define STA_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, nullptr}, STA_FAST(tile_permute), STA_FAST(untile), STA_FAST(forward), STA_FAST(forward_lse),
-    STA_FAST(backward), {nullptr, nullptr, 0, nullptr},
+    STA_FAST(backward), {"bind_layers", py_bind_layers, METH_VARARGS, nullptr}, STA_FAST(rope), STA_FAST(norm_rope), STA_FAST(norm_rope_backward),
+    STA_FAST(packed_forward), STA_FAST(packed_backward), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "sta_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -6,7 +6,7 @@ import ctypes
 
 import torch
 
-from .binding import STA_BF16, STA_F32, StaError, _check, _dev, _i3, _stream_ptr, load_library, sta_strerror  # noqa: F401
+from .binding import STA_BF16, STA_F32, StaError, _check, _dev, _fast, _i3, _stream_ptr, load_library, sta_strerror  # noqa: F401
 
 STA_ROPE_NONE, STA_ROPE_LINEAR, STA_ROPE_NTK, STA_ROPE_YARN = 0, 1, 2, 3
 _DTYPES = {torch.bfloat16: STA_BF16, torch.float32: STA_F32}
@@ -87,6 +87,8 @@ class StaRotary:
         self.channels = 2 * steps.numel()
         self._c = _Rotary(_dev(steps, "steps"), ptr, batch, token, self.channels, (ctypes.c_int * 3)(*pairs), int(self.interleaved),
                           self.magnitude)
+        # for the extension: where the struct is, and which tokens the positions are for
+        self._at = (ctypes.addressof(self._c), -1 if self._N is None else self._N, -1 if self._B is None else self._B)
 
     def _struct(self, B, N):
         if self._N is not None and (self._N != N or self._B not in (None, B)):
@@ -125,6 +127,11 @@ def _rows(t, name, B, N, D):
 def sta_rope(xs, outs, rotary, inverse=False, stream=None):
     """Rotation of one to three [B, N, H, D] tensors (or strided views with adjacent channels) into outs, which may be the tensors
     themselves; inverse: back, which is the gradient."""
+    if stream is None:
+        status = _fast().rope(xs, outs, rotary._at, inverse)
+        if status is not None:
+            _check(status)
+            return outs
     xs, outs = ([xs], [outs]) if isinstance(xs, torch.Tensor) else (list(xs), list(outs))
     n = len(xs)
     if not 1 <= n <= 3 or len(outs) != n:
@@ -163,6 +170,11 @@ def sta_qk_norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight, rotary, e
     """RMS norm with weight [D] (None: ones) and rotation (rotary None: none) of query and key rows; v (may be None) is moved along.  All
     tensors [B, N, H, D], strided views with adjacent channels.  With grid and tile the tokens go from raster to tiled order; a [B, H, N, D]
     tensor for sta_forward is given as out.transpose(1, 2)."""
+    if stream is None:
+        status = _fast().norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight, None if rotary is None else rotary._at, eps, grid, tile)
+        if status is not None:
+            _check(status)
+            return q_out, k_out, v_out
     if q.dim() != 4:
         raise ValueError("expect [B, N, H, D] tensors")
     if (v is None) != (v_out is None):
@@ -184,6 +196,12 @@ def sta_qk_norm_rope_backward(q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_
                               eps=1e-6, grid=None, tile=None, stream=None):
     """Gradients of sta_qk_norm_rope: d_*_out laid out like its outputs, d_q, d_k, d_v like its inputs; d_q_weight, d_k_weight float32 [D] or None;
     workspace: device bytes, at least sta_qk_norm_rope_workspace_bytes(D)."""
+    if stream is None:
+        status = _fast().norm_rope_backward(q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_weight, k_weight, d_q_weight, d_k_weight,
+                                            None if rotary is None else rotary._at, workspace, eps, grid, tile)
+        if status is not None:
+            _check(status)
+            return d_q, d_k, d_v
     if q.dim() != 4:
         raise ValueError("expect [B, N, H, D] tensors")
     if (d_v is None) != (d_v_out is None):
@@ -247,6 +265,11 @@ def sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k) -> int:
 def sta_packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal=True, scale=0.0, lse=None, k_used=None, workspace=None, stream=None):
     """Attention over packed sequences: q, o bf16 [tokens, Hq, D], k, v bf16 [key tokens, Hkv, D] (strided views with adjacent channels); cu_q, cu_k
     int32 [S + 1] where the sequences begin, k_used int32 [S] or None; lse float32 [Hq, tokens] or None; max_q, max_k upper bounds of the lengths."""
+    if stream is None:
+        status = _fast().packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal, scale, lse, k_used, workspace)
+        if status is not None:
+            _check(status)
+            return o
     tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
     S = cu_q.numel() - 1
     if S < 0:
@@ -265,6 +288,11 @@ def sta_packed_backward_workspace_bytes(Hq, tokens_q) -> int:
 
 def sta_packed_backward(q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, max_k, workspace, causal=True, scale=0.0, stream=None):
     """Gradients of sta_packed_forward; tensors as there, workspace: device bytes, at least sta_packed_backward_workspace_bytes(Hq, tokens)."""
+    if stream is None:
+        status = _fast().packed_backward(q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, max_k, workspace, causal, scale)
+        if status is not None:
+            _check(status)
+            return d_q, d_k, d_v
     tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
     S = cu_q.numel() - 1
     if S < 0:
