@@ -158,12 +158,12 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
     return true;
 }
 
-// The lane, found again: what is worked out from it behind a loop is not kept in registers through it.
+// The lane, counted again: neither it nor what is worked out from it behind a loop is kept in registers through it.
 __device__ __forceinline__ int fresh_lane()
 {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    return lane;
+    uint32_t none = 0;
+    asm volatile("" : "+s"(none));
+    return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
 }
 
 // DMA of rows into LDS: where a lane's 16 bytes of a group of rows come from, and the rows beyond the last one read as the last one.

@@ -5,7 +5,8 @@
 // column (a row of queries) and its softmax needs exchanges only among four lanes; P, rounded to bf16, goes from the accumulators
 // straight into O^T += V^T P^T.
 //
-// sta_packed_tile_kernel   four waves of 32 rows share the staged keys and values: prompts.  Bound by the matrix pipe.
+// sta_packed_tile_kernel   four waves (small launches: two waves by two groups, one by four) of 32 rows share the staged keys and values: prompts.
+//                          Bound by the matrix pipe.
 // sta_packed_few_kernel    at most 16 or 32 rows per sequence and key head (single tokens and a few more): four waves take sub-blocks of
 //                          32 keys in turn, each with LDS of its own and no barrier, and merge at the end.  Bound by reading the keys and values.
 // sta_packed_merge_kernel  joins the parts of tiles that were cut along the keys to fill the chip.
@@ -20,7 +21,6 @@
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kTile = 128;                                  // rows of a workgroup of the tile kernel
 
 // Running softmax of a wave's columns: offsets in the units of the scores, sums, accumulators [channel block][column block] of O^T.
 template <int D, int NC, bool LSE>
@@ -133,12 +133,17 @@ __device__ __forceinline__ void add_no_numbers(const uint32_t (&v_addr)[4], floa
 }
 
 // U sub-blocks of 32 keys, SUB bytes apart in LDS: K at OFF of k_addr in the layout StagedRows, V at OFF of v_addr in the layout Staged.  lim: how
-// many keys a column sees; first: the first sub-block's first key.  MASKED: some column may not see all of them.
-template <int D, int NC, bool LSE, bool MASKED, int U, int SUB, int OFF>
+// many keys a column sees; first: the first sub-block's first key.
+// kFollow: every column sees all keys, and the offsets follow the largest scores.  kFixed: the same with the offsets as they are: probabilities, sums
+// and accumulators have eight exponent bits, so an offset that is too low costs nothing until the sums near the end of that range, which is
+// looked at behind the walk.  kMasked: some column may not see all keys; the offsets follow.  kCareful: so, and V may hold more than numbers.
+constexpr int kFollow = 0, kFixed = 1, kMasked = 2, kCareful = 3;
+template <int D, int NC, bool LSE, int MODE, int U, int SUB, int OFF>
 __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint32_t k_addr, const uint32_t (&v_addr)[4],
                                                    const bf16x8 (&Q)[NC][D / 32], float c, float grow_above, int first,
                                                    const int (&lim)[NC], int g4)
 {
+    constexpr bool MASKED = MODE >= kMasked;
     floatx4 S[U][2][NC];
     static_for<0, U>([&](auto uc) {
         constexpr int u = decltype(uc)::value;
@@ -158,55 +163,57 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
             }
         }
     });
-    // The offset only moves when a score exceeds it by more than 2^8 in the exponent.
-    float mx[NC];
-    bool grown = false;
-#pragma unroll
-    for (int col = 0; col < NC; ++col) {
-        float m = S[0][0][col][0];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            m = max3(m, S[u][0][col][0], S[u][0][col][1]);
-            m = max3(m, S[u][0][col][2], S[u][0][col][3]);
-            m = max3(m, S[u][1][col][0], S[u][1][col][1]);
-            m = max3(m, S[u][1][col][2], S[u][1][col][3]);
-        }
-        mx[col] = quad_lane_max(m);
-        grown = grown || mx[col] > st.m[col] + grow_above;
-    }
-    if (__builtin_amdgcn_ballot_w64(grown) != 0) {
-        bool far = false;
+    if constexpr (MODE != kFixed) {
+        // The offset only moves when a score exceeds it by more than 2^8 in the exponent.
+        float mx[NC];
+        bool grown = false;
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
-            const bool up = mx[col] > st.m[col] + grow_above;
-            const float alpha = up ? __builtin_amdgcn_exp2f((st.m[col] - mx[col]) * c) : 1.f;
-            st.m[col] = up ? mx[col] : st.m[col];
-            st.l[col] *= alpha;
+            float m = S[0][0][col][0];
 #pragma unroll
-            for (int cb = 0; cb < D / 16; ++cb) st.acc[cb][col] *= alpha;
-            far = far || (fabsf(st.m[col] * c) > 1024.f && st.m[col] != -INFINITY);
+            for (int u = 0; u < U; ++u) {
+                m = max3(m, S[u][0][col][0], S[u][0][col][1]);
+                m = max3(m, S[u][0][col][2], S[u][0][col][3]);
+                m = max3(m, S[u][1][col][0], S[u][1][col][1]);
+                m = max3(m, S[u][1][col][2], S[u][1][col][3]);
+            }
+            mx[col] = quad_lane_max(m);
+            grown = grown || mx[col] > st.m[col] + grow_above;
         }
-        st.far = __builtin_amdgcn_ballot_w64(far) != 0;
-    }
-    if (__builtin_expect(st.far, 0)) {                      // the difference first, which is exact
+        if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+            bool far = false;
 #pragma unroll
-        for (int col = 0; col < NC; ++col)
+            for (int col = 0; col < NC; ++col) {
+                const bool up = mx[col] > st.m[col] + grow_above;
+                const float alpha = up ? __builtin_amdgcn_exp2f((st.m[col] - mx[col]) * c) : 1.f;
+                st.m[col] = up ? mx[col] : st.m[col];
+                st.l[col] *= alpha;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+                for (int cb = 0; cb < D / 16; ++cb) st.acc[cb][col] *= alpha;
+                far = far || (fabsf(st.m[col] * c) > 1024.f && st.m[col] != -INFINITY);
+            }
+            st.far = __builtin_amdgcn_ballot_w64(far) != 0;
+        }
+        if (__builtin_expect(st.far, 0)) {                      // the difference first, which is exact
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+            for (int col = 0; col < NC; ++col)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[u][kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) S[u][kb][col][r] -= st.m[col] == -INFINITY ? 0.f : st.m[col];
+        }
     }
     StagedTransposedProduct<D, OFF> pv;
-    if constexpr (!MASKED) {
+    if constexpr (MODE != kCareful) {
         pv.prefetch(v_addr);
         __builtin_amdgcn_sched_barrier(0);
     }
     bf16x8 P[U][NC];
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
-        const float mc = st.far || st.m[col] == -INFINITY ? 0.f : st.m[col] * c;
+        const float mc = MODE == kFixed ? st.m[col] * c : st.far || st.m[col] == -INFINITY ? 0.f : st.m[col] * c;
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -220,6 +227,9 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
                 }
         if constexpr (LSE) {
             st.l[col] += sum;
+            // Here, and not in the next stage: the compiler would keep the probabilities until then, and its registers run out in the loop, where
+            // a reload waits for the stage that has just been asked for.
+            asm volatile("" : "+v"(st.l[col]));
             __builtin_amdgcn_sched_barrier(0);              // one column's scores at a time: fewer registers
         }
     }
@@ -232,7 +242,7 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
 #pragma unroll
             for (int col = 0; col < NC; ++col) st.l[col] = mfma_16x16x32(ones, P[u][col], st.l[col]);
     }
-    if constexpr (MASKED) {
+    if constexpr (MODE == kCareful) {
         static_for<0, U>([&](auto uc) { product_of_numbers<D, NC, OFF + decltype(uc)::value * SUB>(v_addr, st.acc, P[decltype(uc)::value], st.odd); });
     } else {
         pv.template run<NC>(v_addr, P[0], st.acc);
@@ -298,23 +308,33 @@ __device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, ui
     return p.ws + ((slot * p.Hkv + kv) * p.parts + part) * floats;
 }
 
-template <int D, bool LSE, int U>
-__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(PackedParams p)
+// RW waves of 32 rows; KG groups of them take the stages of U sub-blocks in turn, each with LDS of its own, and are joined at the end: small launches
+// are cut that way inside the workgroups.
+// The walk.  Of the stages that every row sees all of, the first sets the offsets and the others run without following the scores (20 of 83
+// vector instructions a sub-block at head dimension 128 go with that, and the matrix pipe bounds it instead of them: prompts of 8192 and 4097 tokens, 32 heads over 8,
+// us at best 706, 623); the stages that some row does not see all of follow and mask.  At the end the results are looked at: sums beyond 2^96 or below
+// 2^-64, offsets too large to be multiplied by the scale, or accumulators that are no numbers (a value that is none, seen or not), and the workgroup
+// walks again with care.
+template <int D, bool LSE, int U, int RW, int KG>
+__global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 1 ? 2 : 3) void sta_packed_tile_kernel(PackedParams p)
 {
-    constexpr int NC = 2, CB = D / 16;
+    constexpr int NC = 2, CB = D / 16, TILE = 32 * RW;
     using LK = StagedRows<D>;
     using LV = Staged<D>;
-    constexpr int SUB = LK::Tile + LV::Tile, STAGE = U * SUB, V_AT = LK::Tile, PER_WAVE = LV::Groups / 4;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    constexpr int SUB = LK::Tile + LV::Tile, STAGE = U * SUB, V_AT = LK::Tile, PER_WAVE = LV::Groups / RW;
+    constexpr int WAVE_ACC = CB * NC * 1024, MERGE = KG > 1 ? RW * KG * WAVE_ACC : 0;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * KG * STAGE > MERGE ? 2 * KG * STAGE : MERGE];
+    __shared__ float2 stats[KG > 1 ? KG : 1][TILE];         // offset (base-2 units) and sum of a group's rows
+    const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const int kg = all_waves / RW, wave = all_waves % RW;
     // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
     const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
     const uint32_t rank = sta::fast_div(item, p.by_parts), part = item - rank * p.parts;
     PackedTile tile;
-    if (!find_tile<kTile, false>(rank, p, lane, &tile)) return;
+    if (!find_tile<TILE, false>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
-    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * kTile;
-    const uint32_t last_row = row0 + kTile < rows ? row0 + kTile - 1 : rows - 1;
+    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * TILE;
+    const uint32_t last_row = row0 + TILE < rows ? row0 + TILE - 1 : rows - 1;
     const int n_keys = uniform(seq.keys_of((int)sta::fast_div(last_row, p.by_g), p));
     const int n_all = (n_keys + kSub - 1) / kSub;
     const int sub0 = (int)(part * p.part_subs);
@@ -333,6 +353,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
     PackedDma<D, false> v_dma;
     k_dma.start(lane, p.k.token);
     v_dma.start(lane, p.v.token);
+    char *own = smem + 2 * kg * STAGE;
     auto issue_v = [&](char *to, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER_WAVE; ++i) {
@@ -345,7 +366,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
         if (sub >= sub1) return;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            char *to = smem + stage * STAGE + u * SUB;
+            char *to = own + stage * STAGE + u * SUB;
 #pragma unroll
             for (int i = 0; i < PER_WAVE; ++i) {
                 const int group = PER_WAVE * wave + i;
@@ -354,88 +375,167 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void sta_packed_tile_kernel(
             issue_v(to, sub + u);
         }
     };
-    issue(0, sub0);
+    // the group's stage number i begins with sub-block sub_of(i); all groups go around n_steps times
+    auto sub_of = [&](int i) { return sub0 + U * (kg + KG * i); };
+    const int n_steps = (sub1 - sub0 + U * KG - 1) / (U * KG);
+    issue(0, sub_of(0));
 
     bf16x8 Q[NC][D / 32];
     load_queries<D, NC>(p, seq, kv, wave_row, rows, lane, Q);
-    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    const uint32_t base = (uint32_t)(uintptr_t)own;
     const uint32_t k_addr = LK::address(base, lane);
     uint32_t v_addr[4];
     LV::transposed_addresses(base + V_AT, lane, v_addr);
     Softmax<D, NC, LSE> st;
-    st.start();
     const float c = p.scale_log2e, grow_above = 8.0f / c;
     int lim[NC] = {};                                       // found where the tail begins
-    auto step = [&](auto stage_c, auto masked_c, int sub) __attribute__((always_inline)) {
-        constexpr int ST = decltype(stage_c)::value;
-        constexpr bool MASKED = decltype(masked_c)::value;
+    auto step = [&](auto stage_c, auto mode_c, int i) __attribute__((always_inline)) {
+        constexpr int ST = decltype(stage_c)::value, MODE = decltype(mode_c)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's part of the stage has landed
         __syncthreads();                                    // ... and everyone's, and nobody reads the other stage any more
-        issue(ST ^ 1, sub + U);
-        const int first = sub * kSub;
-        if (!MASKED || first < lim_hi)
-            softmax_sub_blocks<D, NC, LSE, MASKED, U, SUB, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
+        issue(ST ^ 1, sub_of(i + 1));
+        const int sub = sub_of(i), first = sub * kSub;
+        if (MODE < kMasked || (sub < sub1 && first < lim_hi))
+            softmax_sub_blocks<D, NC, LSE, MODE, U, SUB, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
-    // pairs of stages that every row of the tile sees all of, then the others
-    int sub = sub0;
+    using Follow = std::integral_constant<int, kFollow>;
+    using Fixed = std::integral_constant<int, kFixed>;
+    using Masked = std::integral_constant<int, kMasked>;
+    using Careful = std::integral_constant<int, kCareful>;
+    // stages of all groups that every row of the tile sees all of
+    const int seen_by_all = (n_whole / kSub < sub1 ? n_whole / kSub : sub1) - sub0, n_fixed = seen_by_all > 0 ? seen_by_all / (U * KG) : 0;
+    int i = 0;
+    st.start();
+    if (n_fixed >= 2) {
+        step(Stage0{}, Follow{}, 0);
+        step(Stage1{}, Fixed{}, 1);
 #pragma unroll 1
-    for (; sub + 2 * U <= sub1 && (sub + 2 * U) * kSub <= n_whole; sub += 2 * U) {
-        step(Stage0{}, std::false_type{}, sub);
-        step(Stage1{}, std::false_type{}, sub + U);
+        for (i = 2; i + 2 <= n_fixed; i += 2) {
+            step(Stage0{}, Fixed{}, i);
+            step(Stage1{}, Fixed{}, i + 1);
+        }
     }
-    const int tail = sub;
+    const bool fixed = i > 0;
     limits_of<NC>(p, seq, wave_row, rows, fresh_lane(), lim);
 #pragma unroll 1
-    for (; sub < sub1; sub += 2 * U) {
-        step(Stage0{}, std::true_type{}, sub);
-        if (sub + U < sub1) step(Stage1{}, std::true_type{}, sub + U);
+    for (; i < n_steps; i += 2) {                           // i is even
+        step(Stage0{}, Masked{}, i);
+        if (i + 1 < n_steps) step(Stage1{}, Masked{}, i + 1);
     }
-    if (__builtin_expect(__syncthreads_or(st.odd != 0), 0)) {
+    constexpr float kRedoAbove = 79228162514264337593543950336.f, kRedoBelow = 5.42101086242752217e-20f;     // 2^96, 2^-64
+    bool bad = false;
+    uint32_t most = 0;
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        const float l = st.sum(col);
+        bad = bad || (fixed && (st.far || !(l < kRedoAbove) || l < kRedoBelow));
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) most = max(most, __float_as_uint(st.acc[cb][col][r]) & 0x7fffffffu);
+    }
+    if (__builtin_expect(__syncthreads_or(bad || most >= 0x7f800000u), 0)) {
+        st.start();
+        issue(0, sub_of(0));
 #pragma unroll 1
-        for (sub = tail; sub < sub1; ++sub) {
-            issue_v(smem, sub);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (sub * kSub < lim_hi) add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
-            __syncthreads();
+        for (i = 0; i < n_steps; i += 2) {
+            step(Stage0{}, Careful{}, i);
+            if (i + 1 < n_steps) step(Stage1{}, Careful{}, i + 1);
+        }
+        if (__syncthreads_or(st.odd != 0)) {
+#pragma unroll 1
+            for (i = 0; i < n_steps; ++i) {
+#pragma unroll 1
+                for (int sub = sub_of(i); sub < sub_of(i) + U; ++sub) {
+                    issue_v(own, sub);
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    __syncthreads();
+                    if (sub < sub1 && sub * kSub < lim_hi) add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
+                    __syncthreads();
+                }
+            }
         }
     }
 
-    const bool whole = parts_of(n_all, p) <= 1;
-    if (!whole) {
-        float *ws = part_at(p, tile.slot, kv, part, part_floats<D, kTile>());
+    // ---- the groups' sums are joined: a wave takes its rows' channel blocks of its group's share, the groups' parts in ascending order
+    float m[NC], l[NC];                                     // base-2 units
+#pragma unroll
+    for (int col = 0; col < NC; ++col) {
+        m[col] = st.m[col] * c;
+        l[col] = st.sum(col);
+    }
+    constexpr int OWN = CB / KG;                            // channel blocks that a wave writes
+    const int cb0 = KG > 1 ? OWN * kg : 0;
+    if constexpr (KG > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int col = 0; col < NC; ++col)
+                *reinterpret_cast<floatx4 *>(smem + (kg * RW + wave) * WAVE_ACC + (cb * NC + col) * 1024 + lane * 16) = st.acc[cb][col];
+        if (g4 == 0)
+#pragma unroll
+            for (int col = 0; col < NC; ++col) stats[kg][32 * wave + 16 * col + c16] = make_float2(m[col], l[col]);
+        __syncthreads();
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
-            const int r = 32 * wave + 16 * col + c16;
-            const float l = st.sum(col);
-            if (idle) continue;
+            float weight[KG];
+            m[col] = -INFINITY;
+            l[col] = 0.f;
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<floatx4 *>(ws + (size_t)r * D + 16 * cb + 4 * g4) = st.acc[cb][col];
-            if (g4 == 0) {
-                ws[(size_t)kTile * D + r] = st.m[col] * c;
-                ws[(size_t)kTile * D + kTile + r] = l;
+            for (int g = 0; g < KG; ++g) m[col] = fmaxf(m[col], stats[g][32 * wave + 16 * col + c16].x);
+#pragma unroll
+            for (int g = 0; g < KG; ++g) {
+                const float2 x = stats[g][32 * wave + 16 * col + c16];
+                weight[g] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m[col]);
+                l[col] += x.y * weight[g];
+            }
+#pragma unroll
+            for (int j = 0; j < OWN; ++j) {
+                floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int g = 0; g < KG; ++g) {
+                    const floatx4 x = *reinterpret_cast<const floatx4 *>(smem + (g * RW + wave) * WAVE_ACC + ((cb0 + j) * NC + col) * 1024 + lane * 16);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[r] = fmaf(x[r], weight[g], sum[r]);
+                }
+                st.acc[j][col] = sum;
+            }
+        }
+    }
+    if (idle) return;
+    const int last_lane = fresh_lane(), last_g4 = last_lane >> 4;
+    if (parts_of(n_all, p) > 1) {
+        float *ws = part_at(p, tile.slot, kv, part, part_floats<D, TILE>());
+#pragma unroll
+        for (int col = 0; col < NC; ++col) {
+            const int r = 32 * wave + 16 * col + (last_lane & 15);
+#pragma unroll
+            for (int j = 0; j < OWN; ++j) *reinterpret_cast<floatx4 *>(ws + (size_t)r * D + 16 * (cb0 + j) + 4 * last_g4) = st.acc[j][col];
+            if (last_g4 == 0 && kg == 0) {
+                ws[(size_t)TILE * D + r] = m[col];
+                ws[(size_t)TILE * D + TILE + r] = l[col];
             }
         }
         return;
     }
-    const int last_lane = fresh_lane();
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
-        const float l = st.sum(col), inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l[col] > 0.f ? 1.f / l[col] : 0.f;
         const RowAt at = row_at(wave_row + 16 * col + (last_lane & 15), rows, p);
         if (!at.on) continue;
         const int64_t token = seq.q0 + at.token, head = kv * p.g + at.head;
         char *row = p.o.data + token * p.o.token + head * p.o.head;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
+        for (int j = 0; j < OWN; ++j) {
             bf16x4 v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(st.acc[cb][col][r] * inv);
-            *reinterpret_cast<bf16x4 *>(row + 32 * cb + 8 * g4) = v;
+            for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(st.acc[j][col][r] * inv);
+            *reinterpret_cast<bf16x4 *>(row + 32 * (cb0 + j) + 8 * last_g4) = v;
         }
-        if (LSE && p.lse && g4 == 0) p.lse[head * p.tokens_q + token] = l > 0.f ? st.m[col] * c * kLn2 + __logf(l) : -INFINITY;
+        if (LSE && p.lse && last_g4 == 0 && kg == 0) p.lse[head * p.tokens_q + token] = l[col] > 0.f ? m[col] * kLn2 + __logf(l[col]) : -INFINITY;
     }
 }
 
@@ -502,7 +602,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
             wait_dma<0>();
         }
         const int first = sub * kSub;
-        softmax_sub_blocks<D, NC, LSE, decltype(masked_c)::value, 1, STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
+        softmax_sub_blocks<D, NC, LSE, decltype(masked_c)::value ? kCareful : kFollow, 1, STAGE, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
@@ -640,10 +740,11 @@ PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(
 
 // How a launch is cut.  Rows of one sequence and key head that fit 16 or 32 columns take the kernel for few rows.
 struct PackedPlan {
-    int few;                        // 0: tiles of 128 rows; 1, 2: blocks of 16 columns
+    int few;                        // 0: tiles; 1, 2: blocks of 16 columns
+    int waves;                      // tiles of 32 * waves rows by 4 / waves groups
     uint32_t slots;                 // tiles (few: sequences), an upper bound
     uint32_t parts, part_subs;
-    size_t floats;                  // of one part
+    size_t floats;                  // of the parts
     size_t workspace() const { return parts > 1 ? floats : 0; }
 };
 
@@ -651,23 +752,29 @@ constexpr uint32_t kNoParts = 1u << 30;
 
 bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
 {
-    const int64_t g = Hq / Hkv, rows = g * max_q;
+    const int64_t g = Hq / Hkv, rows = g * max_q, cus = sta::compute_units(), subs = ((int64_t)max_k + kSub - 1) / kSub;
+    auto tiles = [&](int64_t tile) {
+        const int64_t by_tokens = tokens_q * g / tile + S, by_longest = (rows + tile - 1) / tile * S;
+        return by_tokens < by_longest ? by_tokens : by_longest;
+    };
     plan->few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
-    const int R = plan->few ? 16 * plan->few : kTile;
-    int64_t slots = S;
+    plan->waves = 4;
     if (!plan->few) {
-        const int64_t by_tokens = tokens_q * g / kTile + S, by_longest = (rows + kTile - 1) / kTile * S;
-        slots = by_tokens < by_longest ? by_tokens : by_longest;
+        // groups where tiles of 128 rows, or the parts that they can be cut into, are fewer than two rounds, and of 64 than one
+        const int64_t resident = 3 * cus, parts = cut && subs >= 32 ? subs / 16 : 1;
+        if (tiles(128) * parts * Hkv < 2 * resident) plan->waves = tiles(64) * parts * Hkv < resident ? 1 : 2;
     }
+    const int R = plan->few ? 16 * plan->few : 32 * plan->waves;
+    const int64_t slots = plan->few ? S : tiles(R);
     plan->parts = 1;
     plan->part_subs = kNoParts;
-    const int64_t items = slots * Hkv, subs = ((int64_t)max_k + kSub - 1) / kSub;
+    const int64_t items = slots * Hkv;
     if (items > 0x7fffffff) return false;
     plan->slots = (uint32_t)slots;
-    const int64_t cus = sta::compute_units(), want = cut ? (plan->few ? 4 : 6) * cus : 0;
+    const int64_t want = cut ? (plan->few ? 4 : 6) * cus : 0;
     if (items > 0 && items < want / 2) {
         int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
-        each = each < 16 ? 16 : (each + 1) & ~(int64_t)1;          // stages of two sub-blocks end with a part
+        each = each < 16 ? 16 : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
         parts = (subs + each - 1) / each;
         if (parts > 1 && items * parts <= 0x7fffffff) {
             plan->parts = (uint32_t)parts;
@@ -678,20 +785,31 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     return true;
 }
 
+template <int D, bool LSE, int RW>
+hipError_t launch_tiles(const PackedParams &p, const PackedPlan &plan, hipStream_t stream)
+{
+    constexpr int KG = 4 / RW, U = D == 64 && KG < 4 ? 2 : 1, ROWS = 1024 / D;
+    const uint32_t items = plan.slots * p.Hkv;
+    const hipError_t e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE, U, RW, KG>, dim3(items * plan.parts), dim3(256), stream, p);
+    if (e != hipSuccess || plan.parts == 1) return e;
+    return sta::launch_kernel(sta_packed_merge_kernel<D, 32 * RW, true>, dim3(items, 32 * RW / ROWS), dim3(256), stream, p);
+}
+
+template <int D, bool LSE, int NC>
+hipError_t launch_few(const PackedParams &p, const PackedPlan &plan, hipStream_t stream)
+{
+    constexpr int ROWS = 1024 / D;
+    const uint32_t items = plan.slots * p.Hkv;
+    const hipError_t e = sta::launch_kernel(sta_packed_few_kernel<D, NC, LSE>, dim3(items * plan.parts), dim3(256), stream, p);
+    if (e != hipSuccess || plan.parts == 1) return e;
+    return sta::launch_kernel(sta_packed_merge_kernel<D, 16 * NC, false>, dim3(items, 16 * NC / ROWS), dim3(256), stream, p);
+}
+
 template <int D, bool LSE>
 hipError_t launch_packed(const PackedParams &p, const PackedPlan &plan, hipStream_t stream)
 {
-    const dim3 grid(plan.slots * p.Hkv * plan.parts), block(256);
-    hipError_t e;
-    if (plan.few == 1) e = sta::launch_kernel(sta_packed_few_kernel<D, 1, LSE>, grid, block, stream, p);
-    else if (plan.few == 2) e = sta::launch_kernel(sta_packed_few_kernel<D, 2, LSE>, grid, block, stream, p);
-    else e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE, D == 64 ? 2 : 1>, grid, block, stream, p);
-    if (e != hipSuccess || plan.parts == 1) return e;
-    constexpr int ROWS = 1024 / D;
-    const uint32_t items = plan.slots * p.Hkv;
-    if (plan.few == 1) return sta::launch_kernel(sta_packed_merge_kernel<D, 16, false>, dim3(items, 16 / ROWS), block, stream, p);
-    if (plan.few == 2) return sta::launch_kernel(sta_packed_merge_kernel<D, 32, false>, dim3(items, 32 / ROWS), block, stream, p);
-    return sta::launch_kernel(sta_packed_merge_kernel<D, kTile, true>, dim3(items, kTile / ROWS), block, stream, p);
+    if (plan.few) return plan.few == 1 ? launch_few<D, LSE, 1>(p, plan, stream) : launch_few<D, LSE, 2>(p, plan, stream);
+    return plan.waves == 4 ? launch_tiles<D, LSE, 4>(p, plan, stream) : plan.waves == 2 ? launch_tiles<D, LSE, 2>(p, plan, stream) : launch_tiles<D, LSE, 1>(p, plan, stream);
 }
 
 }  // namespace
