@@ -83,6 +83,16 @@ __device__ __forceinline__ uint32_t scan64(uint32_t x)
     x += from_lane<0x143, 0xc>(x);          // the last lane of row 1: rows 2 and 3
     return x;
 }
+__device__ __forceinline__ uint32_t or64(uint32_t x)
+{
+    x |= from_lane<0x111, 0xf>(x);
+    x |= from_lane<0x112, 0xf>(x);
+    x |= from_lane<0x114, 0xf>(x);
+    x |= from_lane<0x118, 0xf>(x);
+    x |= from_lane<0x142, 0xa>(x);
+    x |= from_lane<0x143, 0xc>(x);
+    return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ uint32_t sum64(uint32_t x) { return __builtin_amdgcn_readlane(scan64(x), 63); }
 
 // A tile of a sequence: TILE rows, or keys (KEYS).  Launches have an upper bound of the tiles, which only the device can count.
@@ -121,11 +131,8 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
             return own > below ? own - below : 0;
         };
         uint32_t lo = 0;
-        for (uint32_t step = 1u << 25; step > 0; step >>= 1) {
-            // levels that no tile reaches are left out without a sum
-            if (__builtin_amdgcn_ballot_w64(reach(lo + step) != 0) == 0) continue;
+        for (uint32_t step = 0x80000000u >> __builtin_clz(or64(longer + own)); step > 0; step >>= 1)         // (own is not 0 everywhere)
             if (sum64(reach(lo + step)) > rank) lo += step;
-        }
         uint32_t left = rank - sum64(reach(lo + 1));
         uint64_t here = __builtin_amdgcn_ballot_w64(own != 0 && longer <= lo && lo < longer + own);
         while (left-- > 0) here &= here - 1;
@@ -179,20 +186,53 @@ struct PackedDma {
         else return (uint32_t)(D == 128 ? (pos ^ (r << 2)) << 4 : (pos ^ (((r >> 1) & 3) << 1)) << 4);
     }
     __device__ __forceinline__ void start(int lane, int64_t token) { off = (uint32_t)((lane / LPR) * (int)token) + chunk_of(lane); }
-    // Rows `first` .. of base (already at the sequence's first row), of which `rows` exist, to LDS address dst.
-    __device__ __forceinline__ void bring(const char *base, int64_t token, int first, int rows, char *dst) const
+    // A group of rows that are there, from a scalar address, to LDS address dst: no vector arithmetic.
+    __device__ __forceinline__ void bring_whole(const char *group, char *dst) const
     {
-        const char *src;
-        if (first + GroupRows <= rows) {
-            uint32_t o = off;
-            asm volatile("" : "+v"(o));                             // a 32-bit lane offset next to a scalar base
-            src = base + (int64_t)first * token + o;
-        } else {
-            const int lane = fresh_lane(), row = first + lane / LPR;
-            src = base + (int64_t)(row < rows ? row : rows - 1) * token + chunk_of(lane);
-        }
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, STA_LDS_PTR(dst), 16, 0, 0);
+        uint32_t o = off;
+        asm volatile("" : "+v"(o));                                 // a 32-bit lane offset next to a scalar base
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(group + o), STA_LDS_PTR(dst), 16, 0, 0);
+    }
+    // Rows `first` .. of base (already at the sequence's first row), of which only `rows` exist.
+    static __device__ __forceinline__ void bring_part(const char *base, int64_t token, int first, int rows, char *dst)
+    {
+        const int lane = fresh_lane(), row = first + lane / LPR;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + (int64_t)(row < rows ? row : rows - 1) * token + chunk_of(lane)),
+                                         STA_LDS_PTR(dst), 16, 0, 0);
     }
 };
+
+// Rows of K and V of `subs` sub-blocks from sub-block `sub` on to LDS: K at `to` in groups K::Group apart, V v_at behind it, sub-blocks `apart` bytes apart;
+// the wave's share is COUNT groups of each from its group `from` on.  Two paths that the compiler is kept from joining: joined, the common one
+// works addresses out in vector registers as the other has to, 336 cycles of a sub-block's 770 at head dimension 128.
+template <int SUBS, int COUNT, int K_GROUP, int V_GROUP, int D, bool K_ROWS, bool V_ROWS>
+__device__ __forceinline__ void bring_stage(const PackedDma<D, K_ROWS> &k_dma, const PackedDma<D, V_ROWS> &v_dma, const char *kh, const char *vh, int64_t k_token,
+                                            int64_t v_token, int sub, int rows, int from, char *to, int v_at, int apart)
+{
+    constexpr int GR = Staged<D>::GroupRows;
+    const int first = sub * kSub + from * GR;
+    if (__builtin_expect((sub + SUBS) * kSub <= rows, 1)) {
+        const char *k = kh + (int64_t)first * k_token, *v = vh + (int64_t)first * v_token;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int64_t row = u * kSub + i * GR;
+                k_dma.bring_whole(k + row * k_token, to + u * apart + (from + i) * K_GROUP);
+                v_dma.bring_whole(v + row * v_token, to + u * apart + v_at + (from + i) * V_GROUP);
+            }
+        asm volatile("; whole" ::: "memory");
+    } else {
+#pragma unroll 1
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll 1
+            for (int i = 0; i < COUNT; ++i) {
+                const int row = first + u * kSub + i * GR;
+                k_dma.bring_part(kh, k_token, row, rows, to + u * apart + (from + i) * K_GROUP);
+                v_dma.bring_part(vh, v_token, row, rows, to + u * apart + v_at + (from + i) * V_GROUP);
+            }
+        asm volatile("; part" ::: "memory");
+    }
+}
 
 }  // namespace

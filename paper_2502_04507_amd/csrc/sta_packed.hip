@@ -316,7 +316,7 @@ __device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, ui
 // 2^-64, offsets too large to be multiplied by the scale, or accumulators that are no numbers (a value that is none, seen or not), and the workgroup
 // walks again with care.
 template <int D, bool LSE, int U, int RW, int KG>
-__global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 1 ? 2 : 3) void sta_packed_tile_kernel(PackedParams p)
+__global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 : KG > 1 ? (D == 64 ? 4 : 2) : 3) void sta_packed_tile_kernel(PackedParams p)
 {
     constexpr int NC = 2, CB = D / 16, TILE = 32 * RW;
     using LK = StagedRows<D>;
@@ -354,26 +354,10 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 1 ? 2 :
     k_dma.start(lane, p.k.token);
     v_dma.start(lane, p.v.token);
     char *own = smem + 2 * kg * STAGE;
-    auto issue_v = [&](char *to, int sub) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i;
-            v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, to + V_AT + group * LV::Group);
-        }
-    };
     // sub .. sub + U - 1; those of the last stage that nobody sees are brought as well, from the last key's row
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        if (sub >= sub1) return;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            char *to = own + stage * STAGE + u * SUB;
-#pragma unroll
-            for (int i = 0; i < PER_WAVE; ++i) {
-                const int group = PER_WAVE * wave + i;
-                k_dma.bring(kh, p.k.token, (sub + u) * kSub + group * LV::GroupRows, seq.lk, to + group * LK::Group);
-            }
-            issue_v(to, sub + u);
-        }
+        if (sub < sub1)
+            bring_stage<U, PER_WAVE, LK::Group, LV::Group>(k_dma, v_dma, kh, vh, p.k.token, p.v.token, sub, seq.lk, PER_WAVE * wave, own + stage * STAGE, V_AT, SUB);
     };
     // the group's stage number i begins with sub-block sub_of(i); all groups go around n_steps times
     auto sub_of = [&](int i) { return sub0 + U * (kg + KG * i); };
@@ -449,7 +433,9 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 1 ? 2 :
             for (i = 0; i < n_steps; ++i) {
 #pragma unroll 1
                 for (int sub = sub_of(i); sub < sub_of(i) + U; ++sub) {
-                    issue_v(own, sub);
+#pragma unroll 1
+                    for (int j = 0; j < PER_WAVE; ++j)
+                        v_dma.bring_part(vh, p.v.token, sub * kSub + (PER_WAVE * wave + j) * LV::GroupRows, seq.lk, own + V_AT + (PER_WAVE * wave + j) * LV::Group);
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     __syncthreads();
                     if (sub < sub1 && sub * kSub < lim_hi) add_no_numbers<D, NC>(v_addr, st.acc, lim, sub * kSub, g4);
@@ -575,11 +561,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
     v_dma.start(lane, p.v.token);
     char *own = smem + wave * WAVE;
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        char *to = own + stage * STAGE;
-#pragma unroll
-        for (int group = 0; group < LK::Groups; ++group) k_dma.bring(kh, p.k.token, sub * kSub + group * LV::GroupRows, seq.lk, to + group * LK::Group);
-#pragma unroll
-        for (int group = 0; group < LV::Groups; ++group) v_dma.bring(vh, p.v.token, sub * kSub + group * LV::GroupRows, seq.lk, to + V_AT + group * LV::Group);
+        bring_stage<1, LK::Groups, LK::Group, LV::Group>(k_dma, v_dma, kh, vh, p.k.token, p.v.token, sub, seq.lk, 0, own + stage * STAGE, V_AT, 0);
     };
     int sub = sub0 + wave;
     bf16x8 Q[NC][D / 32];
@@ -788,7 +770,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
 template <int D, bool LSE, int RW>
 hipError_t launch_tiles(const PackedParams &p, const PackedPlan &plan, hipStream_t stream)
 {
-    constexpr int KG = 4 / RW, U = D == 64 && KG < 4 ? 2 : 1, ROWS = 1024 / D;
+    constexpr int KG = 4 / RW, U = D == 64 && KG < 2 ? 2 : 1, ROWS = 1024 / D;
     const uint32_t items = plan.slots * p.Hkv;
     const hipError_t e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE, U, RW, KG>, dim3(items * plan.parts), dim3(256), stream, p);
     if (e != hipSuccess || plan.parts == 1) return e;

@@ -132,14 +132,8 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
     k_dma.start(lane, p.k.token);
     v_dma.start(lane, p.v.token);
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        if (sub >= n_sub) return;
-        char *to = smem + stage * STAGE;
-#pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i, first = sub * kSub + group * LK::GroupRows;
-            k_dma.bring(kh, p.k.token, first, seq.lk, to + group * LK::Group);
-            v_dma.bring(vh, p.v.token, first, seq.lk, to + V_AT + group * LV::Group);
-        }
+        if (sub < n_sub)
+            bring_stage<1, PER_WAVE, LK::Group, LV::Group>(k_dma, v_dma, kh, vh, p.k.token, p.v.token, sub, seq.lk, PER_WAVE * wave, smem + stage * STAGE, V_AT, 0);
     };
     issue(0, 0);
     const uint32_t base = (uint32_t)(uintptr_t)smem;
@@ -258,20 +252,43 @@ void sta_packed_dkv_kernel(BackwardParams b)
     // then are not in the loop.
     const char *qh = p.q.data + (int64_t)seq.q0 * p.q.token + (int64_t)kv * p.g * p.q.head;
     const char *gh = b.d_o.data + (int64_t)seq.q0 * b.d_o.token + (int64_t)kv * p.g * b.d_o.head;
+    // what 24-bit products and 32-bit offsets hold: of 32 + g rows
+    const int64_t most = (int64_t)1 << 24;
+    const bool small = p.g <= 64 && p.q.token < most && p.q.head < most && b.d_o.token < most && b.d_o.head < most;
+    const uint32_t magic = (65535u + p.g) / p.g;            // n / g = n * magic >> 16 for n < 32 + g <= 96
     const size_t stat0 = ((size_t)kv * p.tokens_q + seq.q0) * p.g;
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
         if (sub >= n_sub) return;
         char *to = smem + (2 * walk + stage) * STAGE;
-        const int at = fresh_lane(), r_in = at / LPR;
+        const int at = fresh_lane(), r_in = at / LPR, first = sub * kSub;
         const uint32_t chunk = PackedDma<D, false>::chunk_of(at);
+        if (__builtin_expect(small && first + kSub <= rows, 1)) {
+            // rows relative to the stage's first token, in 24-bit products: 8 instructions for a row of Q and dO where whole addresses take 24,
+            // 10 of them at a quarter of the rate
+            const uint32_t t0 = sta::fast_div((uint32_t)first, p.by_g), h0 = (uint32_t)first - t0 * p.g;
+            const char *q0 = qh + (int64_t)t0 * p.q.token, *g0 = gh + (int64_t)t0 * b.d_o.token;
 #pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i, row = sub * kSub + group * L::GroupRows + r_in;
-            const uint32_t r = (uint32_t)(row < rows ? row : rows - 1), t = sta::fast_div(r, p.by_g), h = r - t * p.g;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(qh + ((int64_t)t * p.q.token + (int64_t)h * p.q.head + chunk)),
-                                             STA_LDS_PTR(to + group * L::Group), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + ((int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head + chunk)),
-                                             STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int group = PER_WAVE * wave + i;
+                const uint32_t n = h0 + (uint32_t)(group * L::GroupRows + r_in), t = __umul24(n, magic) >> 16, h = n - __umul24(t, p.g);
+                uint32_t oq = __umul24(t, (uint32_t)p.q.token) + __umul24(h, (uint32_t)p.q.head) + chunk;
+                uint32_t og = __umul24(t, (uint32_t)b.d_o.token) + __umul24(h, (uint32_t)b.d_o.head) + chunk;
+                asm volatile("" : "+v"(oq), "+v"(og));
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(q0 + oq), STA_LDS_PTR(to + group * L::Group), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(g0 + og), STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
+            }
+            asm volatile("; whole" ::: "memory");
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int group = PER_WAVE * wave + i, row = first + group * L::GroupRows + r_in;
+                const uint32_t r = (uint32_t)(row < rows ? row : rows - 1), t = sta::fast_div(r, p.by_g), h = r - t * p.g;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(qh + ((int64_t)t * p.q.token + (int64_t)h * p.q.head + chunk)),
+                                                 STA_LDS_PTR(to + group * L::Group), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gh + ((int64_t)t * b.d_o.token + (int64_t)h * b.d_o.head + chunk)),
+                                                 STA_LDS_PTR(to + G_AT + group * L::Group), 16, 0, 0);
+            }
+            asm volatile("; part" ::: "memory");
         }
         if (wave == KW - 1) {
             const int row = sub * kSub + (at & (kSub - 1));
