@@ -20,8 +20,6 @@
 
 namespace {
 
-constexpr int kTile = 128;          // rows or keys of a workgroup
-
 struct BackwardParams {
     PackedParams p;                 // q, k, v, o and the bounds
     PackedRows d_o, d_q, d_k, d_v;
@@ -67,22 +65,26 @@ __device__ __forceinline__ void join_groups(char *smem, int walk, int wave, int 
                     acc[cb][col] += *reinterpret_cast<const floatx4 *>(smem + (other * KW + wave) * WAVE + (cb * NC + col) * 1024 + lane * 16);
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
+// RW waves of 32 rows; KG groups of them take the sub-blocks of keys in turn, each with stages of its own, and the groups' sums are joined at the end.
+template <int D, int RW, int KG>
+__global__ __launch_bounds__(RW * KG * 64, D == 64 ? 3 : 2) void sta_packed_dq_kernel(BackwardParams b)
 {
     const PackedParams &p = b.p;
-    constexpr int NC = 2, KS = D / 32, CB = D / 16;
+    constexpr int NC = 2, KS = D / 32, CB = D / 16, TILE = 32 * RW;
     using LK = Staged<D>;
     using LV = StagedRows<D>;
-    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, PER_WAVE = LK::Groups / 4;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    constexpr int STAGE = LK::Tile + LV::Tile, V_AT = LK::Tile, PER_WAVE = LK::Groups / RW;
+    constexpr int MERGE = (KG - 1) * RW * CB * NC * 1024;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * KG * STAGE > MERGE ? 2 * KG * STAGE : MERGE];
+    const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
+    const int walk = all_waves / RW, wave = all_waves % RW;
+    char *own = smem + 2 * walk * STAGE;
     const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
     PackedTile tile;
-    if (!find_tile<kTile, false>(rank, p, lane, &tile)) return;
+    if (!find_tile<TILE, false>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
-    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * kTile;
-    const uint32_t last_row = row0 + kTile < rows ? row0 + kTile - 1 : rows - 1;
+    const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * TILE;
+    const uint32_t last_row = row0 + TILE < rows ? row0 + TILE - 1 : rows - 1;
     const int n_keys = uniform(seq.keys_of((int)sta::fast_div(last_row, p.by_g), p));
     const int n_sub = (n_keys + kSub - 1) / kSub;
 
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
         }
         neg_delta[col] = -quad_lane_sum(delta);
         neg_lse[col] = -b.lse[head[col] * p.tokens_q + seq.q0 + token[col]] * b.inv_scale;
-        if (on[col] && g4 == 0) {
+        if (on[col] && g4 == 0 && walk == 0) {
             const size_t stat = ((size_t)kv * p.tokens_q + seq.q0) * p.g + r;
             b.neg_lse[stat] = neg_lse[col];
             b.neg_delta[stat] = neg_delta[col];
@@ -133,10 +135,10 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
     v_dma.start(lane, p.v.token);
     auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
         if (sub < n_sub)
-            bring_stage<1, PER_WAVE, LK::Group, LV::Group>(k_dma, v_dma, kh, vh, p.k.token, p.v.token, sub, seq.lk, PER_WAVE * wave, smem + stage * STAGE, V_AT, 0);
+            bring_stage<1, PER_WAVE, LK::Group, LV::Group>(k_dma, v_dma, kh, vh, p.k.token, p.v.token, sub, seq.lk, PER_WAVE * wave, own + stage * STAGE, V_AT, 0);
     };
-    issue(0, 0);
-    const uint32_t base = (uint32_t)(uintptr_t)smem;
+    issue(0, walk);
+    const uint32_t base = (uint32_t)(uintptr_t)own;
     uint32_t k_addr[KS], k_tr[4];
     LK::addresses(base, lane, k_addr, k_tr);
     const uint32_t v_addr = LV::address(base + V_AT, lane);
@@ -150,9 +152,9 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
         constexpr int ST = decltype(stage_c)::value * STAGE;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        issue(decltype(stage_c)::value ^ 1, sub + 1);
+        issue(decltype(stage_c)::value ^ 1, sub + KG);
         const int first = sub * kSub;
-        if (first >= lim_hi) return;
+        if (first >= lim_hi) return;                        // (and sub-blocks that the other groups alone still have)
         floatx4 S[2][NC], dP[2][NC];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -201,9 +203,13 @@ __global__ __launch_bounds__(256, 2) void sta_packed_dq_kernel(BackwardParams b)
         product.template run<NC>(k_tr, dS, acc);                                    // dQ^T += K^T dS^T
     };
 #pragma unroll 1
-    for (int sub = 0; sub < n_sub; sub += 2) {
-        step(std::integral_constant<int, 0>{}, sub);
-        if (sub + 1 < n_sub) step(std::integral_constant<int, 1>{}, sub + 1);
+    for (int sub = 0; sub < n_sub; sub += 2 * KG) {         // the same number of barriers for every group
+        step(std::integral_constant<int, 0>{}, sub + walk);
+        if (sub + KG < n_sub) step(std::integral_constant<int, 1>{}, sub + KG + walk);
+    }
+    if constexpr (KG > 1) {
+        join_groups<D, RW, KG>(smem, walk, wave, lane, acc);
+        if (walk != 0) return;
     }
 #pragma unroll
     for (int col = 0; col < NC; ++col)
@@ -418,18 +424,24 @@ hipError_t launch_dkv(const BackwardParams &b, int64_t tiles, hipStream_t stream
     return sta::launch_kernel(sta_packed_dkv_kernel<D, KW, G>, dim3((uint32_t)tiles * b.p.Hkv), dim3(KW * G * 64), stream, b);
 }
 
+template <int D, int RW, int KG>
+hipError_t launch_dq(const BackwardParams &b, int64_t tiles, hipStream_t stream)
+{
+    return sta::launch_kernel(sta_packed_dq_kernel<D, RW, KG>, dim3((uint32_t)tiles * b.p.Hkv), dim3(RW * KG * 64), stream, b);
+}
+
 template <int D>
 hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipStream_t stream)
 {
     const PackedParams &p = b.p;
-    const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, kTile), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
+    const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, 128), half_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 64), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
                   half_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 64);
-    if (row_tiles * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
+    if (half_rows * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
     hipError_t e = hipSuccess;
-    if (p.tokens_q > 0 && row_tiles > 0)
-        e = sta::launch_kernel(sta_packed_dq_kernel<D>, dim3((uint32_t)row_tiles * p.Hkv), dim3(256), stream, b);
-    if (e != hipSuccess || key_tiles == 0) return e;
     const int64_t resident = (D == 64 ? 3 : 2) * (int64_t)sta::compute_units();
+    if (p.tokens_q > 0 && row_tiles > 0)
+        e = row_tiles * p.Hkv >= 2 * resident ? launch_dq<D, 4, 1>(b, row_tiles, stream) : launch_dq<D, 2, 2>(b, half_rows, stream);
+    if (e != hipSuccess || key_tiles == 0) return e;
     if (key_tiles * p.Hkv >= 3 * resident) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
     return launch_dkv<D, 2, 2>(b, half_tiles, stream);
 }
