@@ -13,7 +13,7 @@
 // tokens side by side and walks over heads; the four waves of a workgroup take its tokens' heads in turn.  Tokens go in the order of
 // the outputs' places, so that a wave writes whole runs of a head (2 KB at D = 128), and the workgroup reads its tokens' heads from
 // end to end.
-// General path: a wave per row, two pairs a lane, single elements from any address.
+// General path: two pairs a lane, single elements from any address; 16, 32 or 64 lanes a row.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -120,14 +120,14 @@ __device__ __forceinline__ Place place_of(uint32_t c, const Params &p)
         const uint32_t pairs = p.rot / 2;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t i = c + 64 * j;
+            const uint32_t i = c + L * j;
             const bool turned = i < pairs;
             at.e[2 * j] = turned && !p.interleaved ? i : 2 * i;           // unrotated pairs are neighbours behind the rotated ones
             at.e[2 * j + 1] = turned && !p.interleaved ? i + pairs : 2 * i + 1;
             (j ? at.turn_b : at.turn_a) = turned;
         }
         at.in = 2 * c < p.D;
-        at.in2 = 2 * (c + 64) < p.D;
+        at.in2 = 2 * (c + L) < p.D;
 #pragma unroll
         for (int j = 0; j < 4; ++j) at.e[j] = (j < 2 ? at.in : at.in2) ? at.e[j] : 0;
     }
@@ -293,14 +293,14 @@ __device__ __forceinline__ void load_positions(Token &t, const Params &p)
 }
 
 // The steps of a lane's pairs; 0 for those that are not rotated.
-template <int PATH>
+template <int PATH, int L>
 __device__ __forceinline__ void load_steps(uint32_t lane_in_row, const Place &at, const Params &p, int64_t (&step)[pairs_of(PATH)], bool (&first)[pairs_of(PATH)],
                                            bool (&second)[pairs_of(PATH)])
 {
 #pragma unroll
     for (int i = 0; i < pairs_of(PATH); ++i) {
         const bool b = PATH == kGeneral ? i == 1 : PATH == kInterleaved && i >= 4;
-        const uint32_t pair = PATH == kHalf ? at.a + i : PATH == kGeneral ? lane_in_row + 64 * i : b ? at.b / 2 + i - 4 : at.a / 2 + i;
+        const uint32_t pair = PATH == kHalf ? at.a + i : PATH == kGeneral ? lane_in_row + L * i : b ? at.b / 2 + i - 4 : at.a / 2 + i;
         step[i] = p.steps[(b ? at.turn_b : at.turn_a) ? pair : 0];
         first[i] = pair < p.axis1;
         second[i] = pair < p.axis2;
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void sta_rows_forward_kernel(Params p)
     if (p.turns) {
         int64_t step[NP];
         bool first[NP], second[NP];
-        load_steps<PATH>(c, at, p, step, first, second);
+        load_steps<PATH, L>(c, at, p, step, first, second);
         load_positions(t, p);
         turns_of<PATH, false>(t, step, first, second, p, cs, sn);
     }
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kThreads, 3) void sta_rows_backward_kernel(Params p
         if (p.turns) {
             int64_t step[NP];
             bool first[NP], second[NP];
-            load_steps<PATH>(c, at, p, step, first, second);
+            load_steps<PATH, L>(c, at, p, step, first, second);
             load_positions(t, p);
             turns_of<PATH, true>(t, step, first, second, p, cs, sn);
         }
@@ -728,7 +728,10 @@ hipError_t launch_rows(Params &p, bool src_f32, bool dst_f32, bool backward, hip
     switch (path_of(p)) {
     case kHalf: return launch_lanes<kHalf>(p, src_f32, dst_f32, backward, stream);
     case kInterleaved: return launch_lanes<kInterleaved>(p, src_f32, dst_f32, backward, stream);
-    default: return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, stream);
+    default:
+        if (p.D <= 64) return launch_types<kGeneral, 16>(p, src_f32, dst_f32, backward, stream);
+        if (p.D <= 128) return launch_types<kGeneral, 32>(p, src_f32, dst_f32, backward, stream);
+        return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, stream);
     }
 }
 

@@ -48,6 +48,9 @@ ROPE = [
     (1, 5, (2,), 80, 20, True), (1, 9, (2, 2), 96, 48, False), (1, 6, (3,), 96, 24, False), (1, 13, (2, 1), 256, 256, True),
     (1, 3, (1, 1), 256, 128, False), (1, 3, (2,), 2, 2, True), (1, 4, (3,), 6, 4, False), (2, 300, (1,), 16, 16, True),
     (1, 5, (33, 9), 48, 32, False), (1, 5, (3,), 130, 66, False),
+    # aligned rows whose pairs or chunks are split by lanes
+    (2, 19, (3, 2), 64, 8, False), (1, 21, (2,), 256, 40, False), (1, 7, (5,), 128, 2, True), (1, 9, (4, 1), 96, 94, False), (3, 4, (2, 2), 128, 100, True),
+    (1, 40, (1,), 16, 6, False),
 ]
 
 
@@ -125,6 +128,7 @@ NORM = [
     (1, 5, None, 2, 1, 10, 6, False, True), (1, (4, 8, 8), (2, 4, 8), 3, 3, 64, 64, True, True),
     (2, (3, 10, 14), (3, 5, 7), 2, 2, 128, 128, True, True), (1, (1, 16, 24), (1, 8, 8), 5, 5, 64, 64, False, True),
     (1, (6, 8, 8), None, 2, 2, 128, 96, True, True), (1, (12, 24, 24), (6, 8, 8), 1, 1, 128, 128, True, True), (3, 700, None, 1, 1, 64, 0, False, True),
+    (2, 45, None, 3, 2, 96, 24, False, True), (1, 77, None, 2, 1, 256, 200, False, True), (1, (4, 8, 8), (2, 4, 8), 2, 2, 80, 20, True, True),
 ]
 
 

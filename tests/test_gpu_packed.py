@@ -184,6 +184,16 @@ def test_tiles_cut_along_the_keys(case):
     check(Hq, Hkv, D, lq, lk, False, cache=cache)
 
 
+# Launches that fill the chip: workgroups of four waves of rows, or of keys, in one walk; more sequences than a wave has lanes.
+@pytest.mark.parametrize("case", [
+    (12, 12, 64, [260] * 30 + [1, 0, 129] + [256] * 37, None, True), (16, 8, 128, [258] * 64, None, True), (8, 8, 128, [300, 290] * 32, [270, 310] * 32, False),
+])
+def test_large_launches(case):
+    Hq, Hkv, D, lq, lk, causal = case
+    check(Hq, Hkv, D, lq, lk or lq, causal, train=True)
+    check(Hq, Hkv, D, lq, lk or lq, causal)
+
+
 @pytest.mark.parametrize("layout", ["heads", "wide"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_layouts(layout, D):
