@@ -245,3 +245,28 @@ def test_another_stream_and_a_graph():
         sta.sta_qk_norm_rope(x, x, None, a, b, None, w, w, rotary)
         torch.cuda.synchronize()
         assert torch.equal(a, y) and torch.equal(b, q)
+
+
+def test_rows_beyond_4_gb():
+    """The last tokens of a tensor whose offsets pass 32 bits, forward and backward, against the same rows alone."""
+    N, D, n = 9_000_000, 256, 40
+    x = torch.zeros((1, N, 1, D), dtype=torch.bfloat16, device=DEV)
+    assert x.numel() * 2 > 2 ** 32
+    tail = make((1, n, 1, D), 3, torch.bfloat16).to(DEV)
+    x[:, -n:] = tail
+    steps = sta.sta_rope_steps(D)[0].to(DEV)
+    w = torch.ones(D, device=DEV)
+    positions = torch.arange(N, dtype=torch.int32, device=DEV)
+    big, small = sta.StaRotary(steps), sta.StaRotary(steps, positions=positions[-n:].clone())
+    y, z = torch.empty_like(x), torch.empty_like(tail)
+    sta.sta_rope(x, y, big)
+    sta.sta_rope(tail, z, small)
+    assert torch.equal(y[:, -n:], z)
+    k, k_out = x[:, :, :, :].narrow(1, 0, N), torch.empty_like(x)
+    sta.sta_qk_norm_rope(x, k, None, y, k_out, None, w, None, big)
+    sta.sta_qk_norm_rope(tail, tail, None, z, torch.empty_like(tail), None, w, None, small)
+    assert torch.equal(y[:, -n:], z) and torch.equal(k_out[:, -n:], z)
+    d, dz = [k_out, torch.empty_like(x)], [torch.empty_like(tail) for _ in range(2)]
+    sta.sta_qk_norm_rope_backward(x, x, y, y, None, *d, None, w, None, None, None, big, None)
+    sta.sta_qk_norm_rope_backward(tail, tail, z, z, None, *dz, None, w, None, None, None, small, None)
+    assert torch.equal(d[0][:, -n:], dz[0]) and torch.equal(d[1][:, -n:], dz[1])

@@ -360,3 +360,21 @@ def test_another_stream_and_a_graph():
         sta.sta_packed_forward(q1, kc, vc, z, cu1, cuk, 1, 2000, k_used=used, workspace=torch.empty_like(ws))
         torch.cuda.synchronize()
         assert torch.equal(y, z), lengths
+
+
+def test_a_cache_beyond_4_gb():
+    """Slots whose offsets pass 32 bits give what the same keys give in a small tensor; prompts as well as single tokens."""
+    D, Hq, slot, S = 128, 4, 5_400_000, 4
+    big = [torch.zeros((S * slot, 1, D), dtype=BF, device=DEV) for _ in range(2)]
+    assert big[0].numel() * 2 > 5 * 2 ** 30
+    for lq, lk in (([1] * S, [700, 33, 1, 512]), ([70, 1, 33, 140], [700, 33, 65, 512])):
+        k, v, q = randn((sum(lk), 1, D), 2).to(DEV), randn((sum(lk), 1, D), 3).to(DEV), randn((sum(lq), Hq, D), 4).to(DEV)
+        at = starts(lk)
+        for s in range(S):
+            for x, y in zip(big, (k, v)):
+                x[s * slot:s * slot + lk[s]] = y[at[s]:at[s + 1]]
+        want, got = torch.empty_like(q), torch.empty_like(q)
+        cu_q, n = ints(starts(lq)), max(lq)
+        sta.sta_packed_forward(q, k, v, want, cu_q, ints(at), n, 700)
+        sta.sta_packed_forward(q, *big, got, cu_q, ints([s * slot for s in range(S + 1)]), n, 700, k_used=ints(lk))
+        assert torch.equal(got, want)
