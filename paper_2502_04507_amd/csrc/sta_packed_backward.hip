@@ -437,12 +437,15 @@ hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipSt
     const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, 128), half_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 64), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
                   half_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 64);
     if (half_rows * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
+    // Four waves of 32 rows (keys) share a stage; where that makes fewer workgroups than the chip holds at once, two waves by two groups that
+    // take the stages in turn.  32 heads over 8 of 128 channels, us of both kernels, four waves against groups: [512] * 8 137, 127;
+    // [2048, 1999, 77, 1023, 949] 411, 382; [1024] * 16 561, 627; 16 heads of 64 channels, [2048] * 4: 138, 147.
     hipError_t e = hipSuccess;
     const int64_t resident = (D == 64 ? 3 : 2) * (int64_t)sta::compute_units();
     if (p.tokens_q > 0 && row_tiles > 0)
-        e = row_tiles * p.Hkv >= 2 * resident ? launch_dq<D, 4, 1>(b, row_tiles, stream) : launch_dq<D, 2, 2>(b, half_rows, stream);
+        e = row_tiles * p.Hkv >= resident ? launch_dq<D, 4, 1>(b, row_tiles, stream) : launch_dq<D, 2, 2>(b, half_rows, stream);
     if (e != hipSuccess || key_tiles == 0) return e;
-    if (key_tiles * p.Hkv >= 3 * resident) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
+    if (key_tiles * p.Hkv >= resident) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
     return launch_dkv<D, 2, 2>(b, half_tiles, stream);
 }
 

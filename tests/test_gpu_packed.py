@@ -175,7 +175,7 @@ def test_few_rows_with_lse_and_parts(D):
 
 
 @pytest.mark.parametrize("case", [
-    (4, 1, 128, [100, 260], [3000, 2049], 3072 - 64), (3, 3, 64, [200], [1800], 1800), (8, 2, 128, [40], [5000], 5000), (2, 1, 64, [129, 17, 300], [4097, 17, 301], 4100),
+    (4, 1, 128, [100, 260], [3000, 2049], 3008), (3, 3, 64, [200], [1800], 1800), (8, 2, 128, [40], [5000], 5000), (2, 1, 64, [129, 17, 300], [4097, 17, 301], 4100),
 ])
 def test_tiles_cut_along_the_keys(case):
     Hq, Hkv, D, lq, lk, cache = case
