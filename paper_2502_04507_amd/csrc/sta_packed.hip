@@ -720,7 +720,16 @@ namespace {
 
 PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(r.data), r.token * 2, r.head * 2}; }
 
-// How a launch is cut.  Rows of one sequence and key head that fit 16 or 32 columns take the kernel for few rows.
+// How a launch is cut.  Rows of one sequence and key head that fit 16 or 32 columns take the kernel for few rows.  Others: tiles of 128 rows that
+// share every stage where they are two and a quarter a CU (head dimension 64: three) or more, else tiles of 64 rows by two groups that take the stages
+// in turn, or of 32 by four.  Tiles are cut along the keys where that puts more of the chip to work than the sums in memory and their merge, 5 to
+// 9 us, take.  us of a call, causal unless said, heads / key heads x channels (tiles of 128 rows | two groups | four groups):
+//   32/8 x 128, [400] * 6              22 | 30 | -       24/24 x 128, [1000] * 4   40 | 50 | -       40/8 x 128, [774]         22 | 18.5 | 36
+//   16/16 x 64, [2048] * 4             51 | 60 | -       333 .. 2048 (1088 tiles of 64, 576 of 128)  31 | 25 | -
+//   2/2 x 64, [2100, 300]              28 | 19 | 14.6    8/8 x 128, five of 8 .. 819 (256 of 64)     22 | 16 | 18
+// and cut: 32/8 x 128, 512 rows on 16384 keys: 280 | 188 | 272 whole, 148 in parts of 64 sub-blocks of tiles of 128; 24/24 x 64, 333 on 20000: 217 | 151 | 119
+// whole, 67; 16/2 x 128, 200 on 4000: 74 | 47 | 34, 30 in parts of two groups; not worth it: 40/8 x 128, 300 on 1500 (24 whole, 32 cut), [774] (18.5, 27).
+// Few rows, 48 single tokens on caches of 1 to 16384 keys, parts of a chip's 2, 4, 8, 16, 32 workgroups a CU, with the merge: 356, 323, 324, 316, 330.
 struct PackedPlan {
     int few;                        // 0: tiles; 1, 2: blocks of 16 columns
     int waves;                      // tiles of 32 * waves rows by 4 / waves groups
@@ -741,10 +750,19 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     };
     plan->few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     plan->waves = 4;
-    if (!plan->few) {
-        // groups where tiles of 128 rows, or the parts that they can be cut into, are fewer than two rounds, and of 64 than one
-        const int64_t resident = 3 * cus, parts = cut && subs >= 32 ? subs / 16 : 1;
-        if (tiles(128) * parts * Hkv < 2 * resident) plan->waves = tiles(64) * parts * Hkv < resident ? 1 : 2;
+    int64_t want = cut && plan->few ? 4 * cus : 0, least = 16;
+    if (!plan->few && tiles(128) * Hkv < (D == 64 ? 12 : 9) * cus / 4) {
+        const int64_t halves = tiles(64) * Hkv;
+        plan->waves = 2;
+        if (halves < 2 * cus && cut && subs >= 256) {
+            plan->waves = 4;
+            want = 6 * cus;
+            least = 64;
+        } else if (halves < cus / 4 && cut && subs >= 48) {
+            want = 2 * cus;
+        } else if (halves < 3 * cus / 4) {
+            plan->waves = 1;
+        }
     }
     const int R = plan->few ? 16 * plan->few : 32 * plan->waves;
     const int64_t slots = plan->few ? S : tiles(R);
@@ -753,10 +771,9 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     const int64_t items = slots * Hkv;
     if (items > 0x7fffffff) return false;
     plan->slots = (uint32_t)slots;
-    const int64_t want = cut ? (plan->few ? 4 : 6) * cus : 0;
     if (items > 0 && items < want / 2) {
         int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
-        each = each < 16 ? 16 : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
+        each = each < least ? least : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
         parts = (subs + each - 1) / each;
         if (parts > 1 && items * parts <= 0x7fffffff) {
             plan->parts = (uint32_t)parts;
@@ -773,8 +790,9 @@ hipError_t launch_tiles(const PackedParams &p, const PackedPlan &plan, hipStream
     constexpr int KG = 4 / RW, U = D == 64 && KG < 2 ? 2 : 1, ROWS = 1024 / D;
     const uint32_t items = plan.slots * p.Hkv;
     const hipError_t e = sta::launch_kernel(sta_packed_tile_kernel<D, LSE, U, RW, KG>, dim3(items * plan.parts), dim3(256), stream, p);
-    if (e != hipSuccess || plan.parts == 1) return e;
-    return sta::launch_kernel(sta_packed_merge_kernel<D, 32 * RW, true>, dim3(items, 32 * RW / ROWS), dim3(256), stream, p);
+    if constexpr (RW == 1) return e;                       // (never cut)
+    else if (e != hipSuccess || plan.parts == 1) return e;
+    else return sta::launch_kernel(sta_packed_merge_kernel<D, 32 * RW, true>, dim3(items, 32 * RW / ROWS), dim3(256), stream, p);
 }
 
 template <int D, bool LSE, int NC>

@@ -67,7 +67,7 @@ __device__ __forceinline__ void join_groups(char *smem, int walk, int wave, int 
 
 // RW waves of 32 rows; KG groups of them take the sub-blocks of keys in turn, each with stages of its own, and the groups' sums are joined at the end.
 template <int D, int RW, int KG>
-__global__ __launch_bounds__(RW * KG * 64, D == 64 ? 3 : 2) void sta_packed_dq_kernel(BackwardParams b)
+__global__ __launch_bounds__(RW * KG * 64, KG > 2 ? D == 64 ? 2 : 1 : D == 64 ? 3 : 2) void sta_packed_dq_kernel(BackwardParams b)
 {
     const PackedParams &p = b.p;
     constexpr int NC = 2, KS = D / 32, CB = D / 16, TILE = 32 * RW;
@@ -436,16 +436,22 @@ hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipSt
     const PackedParams &p = b.p;
     const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, 128), half_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 64), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
                   half_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 64);
+    const int64_t quarter_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 32), quarter_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 32);
     if (half_rows * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
-    // Four waves of 32 rows (keys) share a stage; where that makes fewer workgroups than the chip holds at once, two waves by two groups that
-    // take the stages in turn.  32 heads over 8 of 128 channels, us of both kernels, four waves against groups: [512] * 8 137, 127;
-    // [2048, 1999, 77, 1023, 949] 411, 382; [1024] * 16 561, 627; 16 heads of 64 channels, [2048] * 4: 138, 147.
+    // Four waves of 32 rows (keys) share a stage where that makes workgroups for the chip (head dimension 128: two and a quarter a CU, 64: three); else
+    // two waves by two groups that take the stages in turn, or, where these are fewer than a workgroup a CU (rows: half one, and walks worth it), one by
+    // four.  Causal, heads / key heads x channels, us of dQ, dK/dV in that order:
+    //   32/8 x 128, [1024] * 16         561 in all | 627 | -           4/4 x 128, 33 of 1 .. 2642   73, 104 | 52, 69 | -
+    //   40/8 x 128, [774]               -, - | 24, 80 | 42, 53         16/2 x 128, [1500]           -, - | 33, 224 | 43, 139
+    //   2/2 x 64, [2100, 300]           -, - | 23, 32 | 16, 21         5/5 x 64, [128] * 16         -, - | 6.9, 7.6 | 8.0, 8.1
     hipError_t e = hipSuccess;
-    const int64_t resident = (D == 64 ? 3 : 2) * (int64_t)sta::compute_units();
+    const int64_t cus = sta::compute_units(), full = (D == 64 ? 12 : 9) * cus / 4;
     if (p.tokens_q > 0 && row_tiles > 0)
-        e = row_tiles * p.Hkv >= resident ? launch_dq<D, 4, 1>(b, row_tiles, stream) : launch_dq<D, 2, 2>(b, half_rows, stream);
+        e = row_tiles * p.Hkv >= full ? launch_dq<D, 4, 1>(b, row_tiles, stream) :
+            half_rows * p.Hkv >= cus / 2 || max_k < 256 ? launch_dq<D, 2, 2>(b, half_rows, stream) : launch_dq<D, 1, 4>(b, quarter_rows, stream);
     if (e != hipSuccess || key_tiles == 0) return e;
-    if (key_tiles * p.Hkv >= resident) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
+    if (key_tiles * p.Hkv >= full) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
+    if (half_tiles * p.Hkv < cus) return launch_dkv<D, 1, 4>(b, quarter_tiles, stream);
     return launch_dkv<D, 2, 2>(b, half_tiles, stream);
 }
 

@@ -176,6 +176,7 @@ def test_few_rows_with_lse_and_parts(D):
 
 @pytest.mark.parametrize("case", [
     (4, 1, 128, [100, 260], [3000, 2049], 3008), (3, 3, 64, [200], [1800], 1800), (8, 2, 128, [40], [5000], 5000), (2, 1, 64, [129, 17, 300], [4097, 17, 301], 4100),
+    (8, 2, 128, [70, 150], [9000, 100], 9000), (2, 2, 64, [300], [8200], 8200), (2, 2, 64, [1, 70, 0], [8300, 8191, 300], 8300),
 ])
 def test_tiles_cut_along_the_keys(case):
     Hq, Hkv, D, lq, lk, cache = case
@@ -192,6 +193,15 @@ def test_large_launches(case):
     Hq, Hkv, D, lq, lk, causal = case
     check(Hq, Hkv, D, lq, lk or lq, causal, train=True)
     check(Hq, Hkv, D, lq, lk or lq, causal)
+
+
+# Between a few tiles and a full chip: one wave, or two, of rows (keys) by four, or two, groups.
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("case", [(4, 2, [300], [300], True), (6, 2, [290, 1, 40], [257, 300, 0], False), (16, 16, [300] * 4, [300] * 4, True), (20, 10, [513, 33, 700], [500, 270, 733], True)])
+def test_walk_groups(case, D):
+    Hq, Hkv, lq, lk, causal = case
+    check(Hq, Hkv, D, lq, lk, causal, train=True)
+    check(Hq, Hkv, D, lq, lk, causal)
 
 
 @pytest.mark.parametrize("layout", ["heads", "wide"])
