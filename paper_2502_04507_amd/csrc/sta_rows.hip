@@ -665,22 +665,31 @@ int fill_params(Params *p, const sta_rotary *rotary, int B, int N, int D, const 
     return STA_OK;
 }
 
-// Which kernel: the general one where a chunk of 8 channels is not 16 aligned bytes or would be split by the rotation.
+// Which kernel: the general one where a chunk of 8 channels is not 16 aligned bytes or would be split by the rotation (4000 tokens of 24 heads of 128
+// channels, queries, keys and values: 32 us, gradients 47; fast 29, 37; the clip of 115,200: 897, 1795; 775, 1162), and for few rows, where its
+// lanes, with 2 pairs each and not 8, are done sooner: up to 2^21 channels (12 heads of 128 in bf16, forward and backward alone: one token 3.8, 6.7 us
+// against 5.2, 9.0; 200 tokens of 24 heads, at that bound, 5.3, 10.3 against 7.2, 10.9; 1000 tokens 12.8, 20.3 against 12.8, 16.5).
+constexpr uint64_t kFewChannels = 1u << 21;
 int path_of(const Params &p)
 {
-    if (p.D % 16 || p.rot % (p.interleaved ? 8 : 16)) return kGeneral;
+    uint64_t heads = 0;
+    for (uint32_t i = 0; i < p.n_tensors; ++i) heads += p.t[i].heads;
+    if (p.D % 16 || p.rot % (p.interleaved ? 8 : 16) || p.tokens * heads * p.D <= kFewChannels) return kGeneral;
     for (uint32_t i = 0; i < p.n_tensors; ++i)
         if (!chunked(p.t[i].x) || !chunked(p.t[i].out) || !chunked(p.t[i].dy)) return kGeneral;
     return p.interleaved ? kInterleaved : kHalf;
 }
 
-constexpr uint32_t kWantBlocks = 1024;          // four workgroups a CU
-constexpr uint32_t kMostPartials = 1024;        // workgroups of the gradients, four a CU
+// Workgroups: forward, fast path: two a CU (2 x 2180 tokens of 16 heads of 128 11.6 us; four 13.6; 4000 tokens of 72 heads 28.0; four 28.8, eight 33.4,
+// sixteen 39.6); general path, forward and backward: four (256 tokens of 36 heads 5.1 us; two 5.9, one 7.0); gradients: four (18,432 tokens of 24 heads,
+// with the forward, 96 us; two 105, one 131).
+constexpr uint32_t kWantBlocks = 512, kWantGeneral = 1024;
+constexpr uint32_t kMostPartials = 1024;        // workgroups of the gradients
 
 // Heads are dealt to gridDim.y workgroups where the tokens alone do not make enough of them.
-uint32_t split_of(uint32_t groups, uint32_t heads)
+uint32_t split_of(uint32_t groups, uint32_t heads, uint32_t blocks)
 {
-    const uint32_t most = (heads + kWaves - 1) / kWaves, want = (kWantBlocks + groups - 1) / groups;
+    const uint32_t most = (heads + kWaves - 1) / kWaves, want = (blocks + groups - 1) / groups;
     return want < 1 ? 1 : want < most ? want : most;
 }
 
@@ -691,7 +700,7 @@ hipError_t launch(Params &p, bool backward, hipStream_t stream)
     uint32_t heads = 0;
     for (uint32_t i = 0; i < p.n_tensors; ++i) heads += p.t[i].heads;
     if (!backward)
-        return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, split_of(groups, heads)), dim3(kThreads), stream, p);
+        return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, split_of(groups, heads, PATH == kGeneral ? kWantGeneral : kWantBlocks)), dim3(kThreads), stream, p);
     // workgroups by heads, units of as few heads a wave as it takes to have that many
     uint32_t first = 0;
     for (uint32_t i = 0; i < 3; ++i) {
@@ -728,7 +737,7 @@ hipError_t launch_rows(Params &p, bool src_f32, bool dst_f32, bool backward, hip
     switch (path_of(p)) {
     case kHalf: return launch_lanes<kHalf>(p, src_f32, dst_f32, backward, stream);
     case kInterleaved: return launch_lanes<kInterleaved>(p, src_f32, dst_f32, backward, stream);
-    default:
+    default:                    // two pairs a lane; 32 and 64 lanes where 16 do: 4000 tokens of 72 heads of 48 19 us, 29, 53
         if (p.D <= 64) return launch_types<kGeneral, 16>(p, src_f32, dst_f32, backward, stream);
         if (p.D <= 128) return launch_types<kGeneral, 32>(p, src_f32, dst_f32, backward, stream);
         return launch_types<kGeneral, 64>(p, src_f32, dst_f32, backward, stream);

@@ -54,9 +54,24 @@ ROPE = [
 ]
 
 
+def many(B, N, heads, D):
+    """Batch entries that make more than 2^21 channels: launches of fewer may go to another kernel."""
+    return max(B, 2 ** 21 // (N * heads * D) + 1)
+
+
 @pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("B,N,heads,D,rot,interleaved", ROPE)
 def test_rope(B, N, heads, D, rot, interleaved, src, dst):
+    check_rope(B, N, heads, D, rot, interleaved, src, dst)
+
+
+@pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("B,N,heads,D,rot,interleaved", [c for c in ROPE if c[3] % 16 == 0 and c[4] % 8 == 0])
+def test_rope_of_many_rows(B, N, heads, D, rot, interleaved, src, dst):
+    check_rope(many(B, N, sum(heads), D), N, heads, D, rot, interleaved, src, dst)
+
+
+def check_rope(B, N, heads, D, rot, interleaved, src, dst):
     types = {"bf16": torch.bfloat16, "f32": torch.float32}
     xs = [make((B, N, h, D), 5 + i, types[src]) for i, h in enumerate(heads)]
     rotary, angle = rotary_of(rot, (rot // 2,), interleaved, N, start=1000003, magnitude=1.25)
@@ -69,18 +84,20 @@ def test_rope(B, N, heads, D, rot, interleaved, src, dst):
             assert torch.equal(y[..., rot:].cpu().double(), x[..., rot:].to(types[dst]).double())      # the rest is copied
 
 
+@pytest.mark.parametrize("batches", [1, 1040])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("start", [0, 2 ** 20 + 1, 2 ** 31 - 8, -(2 ** 31), -3])
-def test_rope_far_positions(start, interleaved):
-    x = make((1, 8, 2, 128), 3, torch.float32)
+def test_rope_far_positions(start, interleaved, batches):
+    x = make((batches, 8, 2, 128), 3, torch.float32)
     rotary, angle = rotary_of(128, (64,), interleaved, 8, start=start)
     y = torch.empty(x.shape, device=DEV)
     sta.sta_rope(x.to(DEV), y, rotary)
     lu.assert_rounded(y, lu.rotate(x.double(), angle, interleaved), slack(x.double(), 32), "rope at %d" % start)
 
 
-def test_rope_in_place_inside_a_fused_tensor_and_per_batch_positions():
-    B, N, D = 2, 19, 128
+@pytest.mark.parametrize("N", [19, 1500])
+def test_rope_in_place_inside_a_fused_tensor_and_per_batch_positions(N):
+    B, D = 2, 128
     qkv = make((B, N, 8, D), 7, torch.bfloat16)
     steps = sta.sta_rope_steps(D)[0]
     positions = torch.randint(0, 50000, (B, N), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
@@ -96,9 +113,10 @@ def test_rope_in_place_inside_a_fused_tensor_and_per_batch_positions():
 
 @pytest.mark.parametrize("D,offset,pad", [(128, 1, 0), (64, 0, 3), (128, 8, 8), (64, 4, 4)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_rows_at_any_address_and_stride(D, offset, pad, dtype):
+@pytest.mark.parametrize("N", [21, 5600])
+def test_rows_at_any_address_and_stride(N, D, offset, pad, dtype):
     """Rows that start at single elements, wider apart than they are long."""
-    B, N, H = 2, 21, 3
+    B, H = 2, 3
     flat = make((offset + B * N * H * (D + pad) + 64,), 11, dtype)
     view = (B, N, H, D), (N * H * (D + pad), D + pad, N * (D + pad), 1)       # head-major inside a batch
     x = flat.as_strided(*view, offset)
@@ -135,6 +153,18 @@ NORM = [
 @pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32"), ("bf16", "f32")])
 @pytest.mark.parametrize("case", NORM, ids=[str(i) for i in range(len(NORM))])
 def test_norm_rope_and_gradients(case, src, dst):
+    check_norm_rope(case, src, dst)
+
+
+@pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("case", [c for c in NORM if c[5] % 16 == 0 and c[6] % 8 == 0], ids=lambda c: "-".join(str(x) for x in c).replace(" ", ""))
+def test_norm_rope_and_gradients_of_many_rows(case, src, dst):
+    B, where, tile, Hq, Hkv, D = case[:6]
+    N = where[0] * where[1] * where[2] if isinstance(where, tuple) else where
+    check_norm_rope((many(B, N, Hq + Hkv, D),) + case[1:], src, dst)
+
+
+def check_norm_rope(case, src, dst):
     B, where, tile, Hq, Hkv, D, rot, interleaved, values = case
     types = {"bf16": torch.bfloat16, "f32": torch.float32}
     grid = where if isinstance(where, tuple) else None
@@ -222,9 +252,10 @@ def test_weight_gradients_of_no_tokens_are_zero():
     assert all(bool((x == 0).all()) for x in dw)
 
 
-def test_another_stream_and_a_graph():
-    x = make((1, 300, 4, 128), 81, torch.bfloat16).to(DEV)
-    rotary, angle = rotary_of(128, (64,), False, 300)
+@pytest.mark.parametrize("N", [300, 5000])
+def test_another_stream_and_a_graph(N):
+    x = make((1, N, 4, 128), 81, torch.bfloat16).to(DEV)
+    rotary, angle = rotary_of(128, (64,), False, N)
     want = torch.empty_like(x)
     sta.sta_rope(x, want, rotary)
     y = torch.empty_like(x)
@@ -249,7 +280,7 @@ def test_another_stream_and_a_graph():
 
 def test_rows_beyond_4_gb():
     """The last tokens of a tensor whose offsets pass 32 bits, forward and backward, against the same rows alone."""
-    N, D, n = 9_000_000, 256, 40
+    N, D, n = 9_000_000, 256, 9000
     x = torch.zeros((1, N, 1, D), dtype=torch.bfloat16, device=DEV)
     assert x.numel() * 2 > 2 ** 32
     tail = make((1, n, 1, D), 3, torch.bfloat16).to(DEV)
