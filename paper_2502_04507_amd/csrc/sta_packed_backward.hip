@@ -218,7 +218,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 ? D == 64 ? 2 : 1 : D == 64 ? 
 
 // KW waves of 32 keys; G groups of them take the sub-blocks of rows in turn, each with stages of its own, and the groups' sums are joined at the end.
 template <int D, int KW, int G>
-__global__ __attribute__((amdgpu_flat_work_group_size(KW * G * 64, KW * G * 64), amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
+__global__ __attribute__((amdgpu_flat_work_group_size(KW * G * 64, KW * G * 64), amdgpu_waves_per_eu((D == 64 ? 3 : 2) - (G > 2))))
 void sta_packed_dkv_kernel(BackwardParams b)
 {
     const PackedParams &p = b.p;
@@ -263,8 +263,12 @@ void sta_packed_dkv_kernel(BackwardParams b)
     const bool small = p.g <= 64 && p.q.token < most && p.q.head < most && b.d_o.token < most && b.d_o.head < most;
     const uint32_t magic = (65535u + p.g) / p.g;            // n / g = n * magic >> 16 for n < 32 + g <= 96
     const size_t stat0 = ((size_t)kv * p.tokens_q + seq.q0) * p.g;
-    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        if (sub >= n_sub) return;
+    // The walk goes from the last rows, which all keys' walks begin with, towards the first that see the tile: workgroups of a sequence read the
+    // same rows at about the same time.
+    const int ends = sub0 + n_sub - 1;
+    auto issue = [&](int stage, int at_walk) __attribute__((always_inline)) {
+        if (at_walk >= n_sub) return;
+        const int sub = ends - at_walk;
         char *to = smem + (2 * walk + stage) * STAGE;
         const int at = fresh_lane(), r_in = at / LPR, first = sub * kSub;
         const uint32_t chunk = PackedDma<D, false>::chunk_of(at);
@@ -314,13 +318,13 @@ void sta_packed_dkv_kernel(BackwardParams b)
 #pragma unroll
         for (int col = 0; col < NC; ++col) dK[cb][col] = dV[cb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
     const float c = p.scale_log2e;
-    auto step = [&](auto stage_c, int sub) __attribute__((always_inline)) {
+    auto step = [&](auto stage_c, int at_walk) __attribute__((always_inline)) {
         constexpr int ST = decltype(stage_c)::value * STAGE;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        issue(decltype(stage_c)::value ^ 1, sub + G);
-        const int first = sub * kSub;
-        if (sub >= n_sub || first + kSub <= see_lo || wave_key >= seq.lk) return;
+        issue(decltype(stage_c)::value ^ 1, at_walk + G);
+        const int first = (ends - at_walk) * kSub;
+        if (at_walk >= n_sub || first + kSub <= see_lo || wave_key >= seq.lk) return;
         auto start = [&](auto off_c) {                      // four rows' statistics for every register of a row block
             floatx4 x[2];
             typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
