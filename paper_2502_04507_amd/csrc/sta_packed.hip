@@ -376,7 +376,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     auto step = [&](auto stage_c, auto mode_c, int i) __attribute__((always_inline)) {
         constexpr int ST = decltype(stage_c)::value, MODE = decltype(mode_c)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's part of the stage has landed
-        __syncthreads();                                    // ... and everyone's, and nobody reads the other stage any more
+        if constexpr (RW > 1) __syncthreads();              // ... and everyone's, and nobody reads the other stage any more (one wave: its own alone)
         issue(ST ^ 1, sub_of(i + 1));
         const int sub = sub_of(i), first = sub * kSub;
         if (MODE < kMasked || (sub < sub1 && first < lim_hi))
