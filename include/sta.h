@@ -10,7 +10,7 @@
  *     the caller; `grid`, `tile`, `window_tiles` and friends are HOST pointers
  *     that are read during the call and may be freed on return.
  *   - Tensors are contiguous [B, H, N, D] (batch, head, token, channel) with
- *     N = grid[0]*grid[1]*grid[2].  "raster" order puts token (t,h,w) at
+ *     N = grid[0]*grid[1]*grid[2], except where sta_head_rows describes them.  "raster" order puts token (t,h,w) at
  *     n = (t*grid[1] + h)*grid[2] + w.  "tiled" order puts it at
  *     n = tile_id*P + intra_id with tile_id row-major over the tile grid
  *     (grid[a]/tile[a] per axis), intra_id row-major inside the tile and
@@ -329,7 +329,8 @@ int sta_rope_steps(int channels, double theta, int scaling, double factor, doubl
  * (times the same magnitude), which is the gradient.  Channels beyond rotary->channels are copied.  out[i] may be in[i] itself;
  * other overlaps of outputs with inputs or each other are STA_ERR_ALIAS.  Arithmetic in fp32, rounded once.
  * D: even, 2 .. 256.  Rows that start at multiples of 16 bytes, D a multiple of 16 and rotary->channels a multiple of 16 (of 8
- * where interleaved) take the fast kernel; others one that reads single elements.  B or N of 0: nothing to do.
+ * where interleaved) take the fast kernel where there are many; few, and others, take one that reads single elements (sums of a row in another order, so
+ * a norm's last bit may differ).  B or N of 0: nothing to do.
  */
 int sta_rope(const sta_head_rows *in, const sta_head_rows *out, int n_tensors, int B, int N, int D, const sta_rotary *rotary,
              int inverse, void *hip_stream);
@@ -391,6 +392,8 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
  * d_q: like q; d_k, d_v: like k and v, summed over the query heads of a group.  Written for every token of a sequence (0 where no
  * row saw it).  P is recomputed from the scores and lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are
  * rounded once.  No atomics: repeated calls give identical bits.
+ * Infinities and NaN in q, k, v or d_o make NaN of gradients in their own sequence and key head, also of pairs that are not seen (0 times them is
+ * a term of the sums), and of no others.
  * workspace: device, 16-byte aligned, at least sta_packed_backward_workspace_bytes(Hq, tokens_q) bytes, else STA_ERR_WORKSPACE.
  */
 size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q);

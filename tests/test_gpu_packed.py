@@ -288,6 +288,32 @@ def test_no_number_of_an_unseen_key_reaches_a_row(D, few):
             lu.assert_rounded(x, torch.where(number, want[0], 0.0)[None], b_o + 1e-30, "row %d of %d" % (i, s))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("which", [0, 1, 2, 3])
+def test_no_number_leaves_its_sequence_and_head_in_the_gradients(which, D):
+    """One value of q, k, v or d_o of the middle sequence is no number: the gradients of other sequences and key heads keep their bits."""
+    Hq, Hkv, lens = 6, 3, [70, 45, 300]
+    T, cu, kv = sum(lens), ints(starts(lens)), 1
+    clean = [randn((T, h, D), i + 1).to(DEV) for i, h in enumerate((Hq, Hkv, Hkv, Hq))]
+    o, lse = torch.empty_like(clean[0]), torch.empty((Hq, T), device=DEV)
+    sta.sta_packed_forward(*clean[:3], o, cu, cu, max(lens), max(lens), lse=lse)
+    ws = torch.empty(sta.sta_packed_backward_workspace_bytes(Hq, T), dtype=torch.uint8, device=DEV)
+    results = []
+    for value in (None, float("nan"), float("inf")):
+        x = [t.clone() for t in clean]
+        if value is not None:
+            x[which][70 + 44, kv * (1 if which in (1, 2) else 2), 5] = value
+        d = [torch.empty_like(t) for t in x[:3]]
+        sta.sta_packed_backward(*x[:3], o, x[3], lse, *d, cu, cu, max(lens), max(lens), ws)
+        results.append(d)
+    for d in results[1:]:
+        for a, b in zip(d, results[0]):
+            g = a.shape[1] // Hkv
+            a, b = (t.cpu().view(torch.int16).view(T, Hkv, g, D) for t in (a, b))
+            assert torch.equal(a[:70], b[:70]) and torch.equal(a[115:], b[115:])
+            assert torch.equal(a[:, [0, 2]], b[:, [0, 2]])
+
+
 def test_rows_outside_every_sequence_are_left_alone():
     q, k, v = randn((50, 2, 64), 1).to(DEV), randn((60, 2, 64), 2).to(DEV), randn((60, 2, 64), 3).to(DEV)
     o = torch.full_like(q, 3.0)
