@@ -312,6 +312,17 @@ __device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, ui
     return p.ws + ((slot * p.Hkv + kv) * p.parts + part) * floats;
 }
 
+// The place of a workgroup in the order of the walks: every other round of workgroups over an XCD's CUs is turned around, so that the CU that has the
+// longest walk of one round has the shortest of the next.  XCDs, and so the key heads on them, stay as they are.  Not where tiles are cut: parts of a
+// tile are equal.  16 heads of 64 channels, [2048] * 4: 46.7 us, 50.0 without; 24 heads of 128, [1000] * 4: 38.8, 39.7; the chunk of 512 tokens, cut,
+// 224 with, 210 without; and the gradients' kernels, 5 % faster to 8 % slower, are left as they are.
+__device__ __forceinline__ uint32_t place_of_block(const PackedParams &p)
+{
+    constexpr uint32_t XCDS = 8, CUS = 32;
+    const uint32_t b = blockIdx.x, round = b / (XCDS * CUS);
+    return p.parts == 1 && (round & 1) && (round + 1) * XCDS * CUS <= gridDim.x ? (2 * round + 1) * XCDS * CUS - XCDS - b + 2 * (b % XCDS) : b;
+}
+
 // RW waves of 32 rows; KG groups of them take the stages of U sub-blocks in turn, each with LDS of its own, and are joined at the end: small launches
 // are cut that way inside the workgroups.
 // The walk.  Of the stages that every row sees all of, the first sets the offsets and the others run without following the scores (20 of 83
@@ -332,7 +343,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int kg = all_waves / RW, wave = all_waves % RW;
     // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
-    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    const uint32_t place = place_of_block(p), item = sta::fast_div(place, p.by_Hkv), kv = place - item * p.Hkv;
     const uint32_t rank = sta::fast_div(item, p.by_parts), part = item - rank * p.parts;
     PackedTile tile;
     if (!find_tile<TILE, false>(rank, p, lane, &tile)) return;
