@@ -833,10 +833,13 @@ namespace sta {
 
 int packed_check(const sta_head_rows *r, int64_t tokens, int heads_of, int D, bool written)
 {
-    if (int rc = check_rows(r, written, 1, tokens > 0 ? tokens : 1, D)) return rc;
+    if (!r) return STA_ERR_NULL;
+    sta_head_rows some = *r;
+    if (tokens == 0) some.data = reinterpret_cast<void *>(16);              // nothing is there to be read
+    if (int rc = check_rows(&some, written, 1, tokens > 0 ? tokens : 1, D)) return rc;
     if (r->dtype != STA_BF16) return STA_ERR_UNSUPPORTED;
     if (heads_of && r->heads != heads_of) return STA_ERR_SHAPE;
-    if (((uintptr_t)r->data & 15) || r->token % 8 || r->head % 8 || r->token >= (int64_t)1 << 26) return STA_ERR_SHAPE;
+    if (((uintptr_t)some.data & 15) || r->token % 8 || r->head % 8 || r->token >= (int64_t)1 << 26) return STA_ERR_SHAPE;
     return STA_OK;
 }
 
@@ -866,24 +869,20 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
     if (S == 0 || tokens_q == 0 || max_q == 0) return STA_OK;
     if (!cu_q || !cu_k) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)k_used | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
-    const int64_t nk = tokens_k > 0 ? tokens_k : 1;
-    if (rows_overlap(*o, tokens_q, *q, tokens_q, 1, D) || rows_overlap(*o, tokens_q, *k, nk, 1, D) || rows_overlap(*o, tokens_q, *v, nk, 1, D))
+    if (rows_overlap(*o, tokens_q, *q, tokens_q, 1, D) || rows_overlap(*o, tokens_q, *k, tokens_k, 1, D) || rows_overlap(*o, tokens_q, *v, tokens_k, 1, D))
         return STA_ERR_ALIAS;
     PackedPlan plan;
     if (!plan_of(q->heads, k->heads, D, S, tokens_q, max_q, max_k, workspace != nullptr, &plan)) return STA_ERR_SHAPE;
-    const struct { const sta_head_rows *r; int64_t n; } tensors[4] = {{q, tokens_q}, {k, nk}, {v, nk}, {o, tokens_q}};
+    const struct { const sta_head_rows *r; int64_t n; } tensors[4] = {{q, tokens_q}, {k, tokens_k}, {v, tokens_k}, {o, tokens_q}};
     if (workspace) {
         if (((uintptr_t)workspace & 15) || workspace_bytes < plan.workspace() * sizeof(float)) return STA_ERR_WORKSPACE;
         for (const auto &t : tensors)
-            if ((uintptr_t)workspace < (uintptr_t)t.r->data + extent_of(*t.r, 1, t.n, D) && (uintptr_t)t.r->data < (uintptr_t)workspace + workspace_bytes)
-                return STA_ERR_ALIAS;
+            if (rows_meet(*t.r, 1, t.n, D, workspace, workspace_bytes)) return STA_ERR_ALIAS;
     }
-    if (lse) {
-        const uintptr_t l0 = (uintptr_t)lse, l1 = l0 + (size_t)tokens_q * q->heads * sizeof(float);
-        for (const auto &t : tensors)
-            if (l0 < (uintptr_t)t.r->data + extent_of(*t.r, 1, t.n, D) && (uintptr_t)t.r->data < l1) return STA_ERR_ALIAS;
-        if (workspace && l0 < (uintptr_t)workspace + workspace_bytes && (uintptr_t)workspace < l1) return STA_ERR_ALIAS;
-    }
+    const size_t lse_bytes = (size_t)tokens_q * q->heads * sizeof(float);
+    for (const auto &t : tensors)
+        if (rows_meet(*t.r, 1, t.n, D, lse, lse_bytes)) return STA_ERR_ALIAS;
+    if (ranges_meet(lse, lse_bytes, workspace, workspace_bytes)) return STA_ERR_ALIAS;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     PackedParams p = {};
     p.q = packed_rows_of(*q);

@@ -486,12 +486,11 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
                         int64_t tokens_k, const int32_t *cu_q, const int32_t *cu_k, int S, int max_q, int max_k, int D, int causal, float scale,
                         void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    if (!q || !k || !v || !o || !d_o || !lse || !d_q || !d_k || !d_v) return STA_ERR_NULL;
+    if (!q || !k || !v || !o || !d_o || (!lse && tokens_q > 0) || !d_q || !d_k || !d_v) return STA_ERR_NULL;
     if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > 0x7fffffff || tokens_k > 0x7fffffff) return STA_ERR_SHAPE;
     if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
     const sta_head_rows *in[5] = {q, k, v, o, d_o}, *out[3] = {d_q, d_k, d_v};
-    const int64_t nq = tokens_q > 0 ? tokens_q : 1, nk = tokens_k > 0 ? tokens_k : 1;
-    const int64_t n_in[5] = {nq, nk, nk, nq, nq}, n_out[3] = {nq, nk, nk};
+    const int64_t nq = tokens_q, nk = tokens_k, n_in[5] = {nq, nk, nk, nq, nq}, n_out[3] = {nq, nk, nk};
     for (int i = 0; i < 5; ++i)
         if (int rc = sta::packed_check(in[i], n_in[i], i == 0 || i == 1 ? 0 : i == 2 ? k->heads : q->heads, D, false)) return rc;
     for (int i = 0; i < 3; ++i)
@@ -501,21 +500,17 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     if (!cu_q || !cu_k) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
     if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sta_packed_backward_workspace_bytes(q->heads, tokens_q)) return STA_ERR_WORKSPACE;
-    const uintptr_t w0 = (uintptr_t)workspace, w1 = w0 + sta_packed_backward_workspace_bytes(q->heads, tokens_q);
-    const uintptr_t l0 = (uintptr_t)lse, l1 = l0 + (size_t)tokens_q * q->heads * sizeof(float);
-    auto meets = [&](const sta_head_rows &r, int64_t n, uintptr_t a0, uintptr_t a1) {
-        return a0 < (uintptr_t)r.data + extent_of(r, 1, n, D) && (uintptr_t)r.data < a1;
-    };
-    if (w0 < l1 && l0 < w1) return STA_ERR_ALIAS;
+    const size_t used = sta_packed_backward_workspace_bytes(q->heads, tokens_q), lse_bytes = (size_t)tokens_q * q->heads * sizeof(float);
+    if (ranges_meet(workspace, used, lse, lse_bytes)) return STA_ERR_ALIAS;
     for (int j = 0; j < 3; ++j) {
         for (int i = 0; i < 5; ++i)
             if (rows_overlap(*in[i], n_in[i], *out[j], n_out[j], 1, D)) return STA_ERR_ALIAS;
         for (int i = 0; i < j; ++i)
             if (rows_overlap(*out[i], n_out[i], *out[j], n_out[j], 1, D)) return STA_ERR_ALIAS;
-        if (meets(*out[j], n_out[j], w0, w1) || meets(*out[j], n_out[j], l0, l1)) return STA_ERR_ALIAS;
+        if (rows_meet(*out[j], 1, n_out[j], D, workspace, used) || rows_meet(*out[j], 1, n_out[j], D, lse, lse_bytes)) return STA_ERR_ALIAS;
     }
     for (int i = 0; i < 5; ++i)
-        if (meets(*in[i], n_in[i], w0, w1)) return STA_ERR_ALIAS;
+        if (rows_meet(*in[i], 1, n_in[i], D, workspace, used)) return STA_ERR_ALIAS;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     BackwardParams b = {};
     PackedParams &p = b.p;

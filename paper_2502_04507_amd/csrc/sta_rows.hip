@@ -837,6 +837,7 @@ int sta_qk_norm_rope(const sta_head_rows *q, const sta_head_rows *k, const sta_h
         for (uint32_t j = 0; j < p.n_tensors; ++j) {
             if (!(i == j && !tile && same_rows(*in[i], *out[j])) && rows_overlap(*in[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
             if (i < j && rows_overlap(*out[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
+            if (rows_meet(*out[i], B, N, D, p.t[j].weight, (uint64_t)D * size_of(weight_dt))) return STA_ERR_ALIAS;
         }
     const hipError_t e = launch_rows(p, q->dtype == STA_F32, q_out->dtype == STA_F32, false, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
@@ -860,6 +861,14 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
     const bool sums = d_q_weight || d_k_weight;
     if (sums && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sta_qk_norm_rope_workspace_bytes(D))) return STA_ERR_WORKSPACE;
     if (((uintptr_t)d_q_weight | (uintptr_t)d_k_weight) & 3) return STA_ERR_SHAPE;
+    const size_t sum_bytes = D * sizeof(float);
+    const float *sum_of[2] = {d_q_weight, d_k_weight};
+    if (ranges_meet(d_q_weight, sum_bytes, d_k_weight, sum_bytes)) return STA_ERR_ALIAS;
+    for (const float *s : sum_of) {
+        if (sums && ranges_meet(s, sum_bytes, workspace, sta_qk_norm_rope_workspace_bytes(D))) return STA_ERR_ALIAS;
+        for (const void *w : {q_weight, k_weight})
+            if (ranges_meet(s, sum_bytes, w, (uint64_t)D * size_of(weight_dt))) return STA_ERR_ALIAS;
+    }
     const sta_head_rows *x[3] = {q, k, nullptr}, *dy[3] = {d_q_out, d_k_out, d_v_out}, *dx[3] = {d_q, d_k, d_v};
     p.n_tensors = d_v ? 3 : 2;
     p.weight_f32 = weight_dt == STA_F32;
@@ -882,13 +891,18 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
             p.t[i].weight = i == 0 ? q_weight : i == 1 ? k_weight : nullptr;
             if ((uintptr_t)p.t[i].weight % size_of(weight_dt)) return STA_ERR_SHAPE;
         }
-        const uintptr_t w0 = (uintptr_t)workspace, w1 = w0 + (sums ? sta_qk_norm_rope_workspace_bytes(D) : 0);
         for (uint32_t i = 0; i < p.n_tensors; ++i)
             for (uint32_t j = 0; j < p.n_tensors; ++j) {
                 if ((x[i] && rows_overlap(*x[i], *dx[j], B, N, D)) || rows_overlap(*dy[i], *dx[j], B, N, D)) return STA_ERR_ALIAS;
                 if (i < j && rows_overlap(*dx[i], *dx[j], B, N, D)) return STA_ERR_ALIAS;
-                for (const sta_head_rows *r : {x[i], dy[i], dx[i]})
-                    if (sums && r && w0 < (uintptr_t)r->data + extent_of(*r, B, N, D) && (uintptr_t)r->data < w1) return STA_ERR_ALIAS;
+                if (rows_meet(*dx[i], B, N, D, p.t[j].weight, (uint64_t)D * size_of(weight_dt))) return STA_ERR_ALIAS;
+            }
+        for (uint32_t i = 0; i < p.n_tensors; ++i)
+            for (const sta_head_rows *r : {x[i], dy[i], dx[i]}) {
+                if (!r) continue;
+                if (sums && rows_meet(*r, B, N, D, workspace, sta_qk_norm_rope_workspace_bytes(D))) return STA_ERR_ALIAS;
+                for (const float *s : sum_of)
+                    if (rows_meet(*r, B, N, D, s, sum_bytes)) return STA_ERR_ALIAS;
             }
         if (launch_rows(p, q->dtype == STA_F32, d_q_out->dtype == STA_F32, true, stream) != hipSuccess) return STA_ERR_HIP;
     }

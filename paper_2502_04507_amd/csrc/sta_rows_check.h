@@ -47,9 +47,10 @@ inline uint64_t extent_of(const sta_head_rows &r, int64_t B, int64_t N, int D)
     return (uint64_t)((B - 1) * r.batch + (N - 1) * r.token + (r.heads - 1) * r.head + D) * size_of(r.dtype);
 }
 
-// Whether an element of a may lie in b.  Heads of one fused tensor interleave: same strides, other heads.
+// Whether an element of a may lie in b (not without tokens).  Heads of one fused tensor interleave: same strides, other heads.
 inline bool rows_overlap(const sta_head_rows &a, int64_t Na, const sta_head_rows &b, int64_t Nb, int64_t B, int D)
 {
+    if (Na <= 0 || Nb <= 0 || B <= 0) return false;
     const uintptr_t a0 = (uintptr_t)a.data, b0 = (uintptr_t)b.data;
     if (a0 + extent_of(a, B, Na, D) <= b0 || b0 + extent_of(b, B, Nb, D) <= a0) return false;
     if (a.dtype != b.dtype || a.token != b.token || a.token <= 0) return true;
@@ -61,6 +62,17 @@ inline bool rows_overlap(const sta_head_rows &a, int64_t Na, const sta_head_rows
     return off < wide_a || off + wide_b > period;
 }
 inline bool rows_overlap(const sta_head_rows &a, const sta_head_rows &b, int B, int N, int D) { return rows_overlap(a, N, b, N, B, D); }
+
+// Whether `bytes` from `at` on (null: none) touch what the rows span.
+inline bool rows_meet(const sta_head_rows &r, int64_t B, int64_t N, int D, const void *at, uint64_t bytes)
+{
+    const uintptr_t a = (uintptr_t)at, b = (uintptr_t)r.data;
+    return at && B > 0 && N > 0 && a < b + extent_of(r, B, N, D) && b < a + bytes;
+}
+inline bool ranges_meet(const void *a, uint64_t a_bytes, const void *b, uint64_t b_bytes)
+{
+    return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
 
 inline bool same_rows(const sta_head_rows &a, const sta_head_rows &b)
 {

@@ -321,6 +321,24 @@ def test_rows_outside_every_sequence_are_left_alone():
     assert bool((o[:5] == 3).all()) and bool((o[40:] == 3).all()) and not bool((o[5:40] == 3).all(-1).any())
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [3, 200])
+def test_no_keys_and_no_queries_at_all(n, D):
+    """Tensors without a token: rows that see nothing are 0 with lse -infinity, gradients of keys that nothing saw are 0."""
+    x, none, two = randn((n, 4, D), 1).to(DEV), torch.empty((0, 2, D), dtype=BF, device=DEV), ints([0, n, n])
+    o, lse, dq = torch.full_like(x, 3.0), torch.zeros((4, n), device=DEV), torch.full_like(x, 3.0)
+    sta.sta_packed_forward(x, none, none, o, two, ints([0, 0, 0]), n, 0, lse=lse)
+    assert bool((o == 0).all()) and bool((lse == -float("inf")).all())
+    ws = torch.empty(sta.sta_packed_backward_workspace_bytes(4, n), dtype=torch.uint8, device=DEV)
+    sta.sta_packed_backward(x, none, none, o, x, lse, dq, none.clone(), none.clone(), two, ints([0, 0, 0]), n, 0, ws)
+    assert bool((dq == 0).all())
+    q0, k = torch.empty((0, 4, D), dtype=BF, device=DEV), randn((n, 2, D), 2).to(DEV)
+    dk, dv = torch.full_like(k, 3.0), torch.full_like(k, 3.0)
+    sta.sta_packed_forward(q0, k, k, q0.clone(), ints([0, 0, 0]), two, 0, n)
+    sta.sta_packed_backward(q0, k, k, q0, q0, torch.empty((4, 0), device=DEV), q0.clone(), dk, dv, ints([0, 0, 0]), two, 0, n, ws)
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
+
+
 def test_bounds_that_leave_the_tensors_are_cut():
     """Wrong bounds: no access leaves the tensors, and sequences that are right keep their results."""
     q, k, v = randn((40, 2, 64), 1).to(DEV), randn((40, 2, 64), 2).to(DEV), randn((40, 2, 64), 3).to(DEV)

@@ -75,6 +75,23 @@ def test_norm_rope_backward_refuses(want, kw):
     assert got == want
 
 
+def test_norm_rope_refuses_weights_inside_an_output():
+    assert norm(wq=(1 << 30) + 512) == ALIAS
+    assert norm(wq=(1 << 31) + 1024) == ALIAS
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dw=(1 << 42) + 64), dict(dw=1 << 20), dict(dw=1 << 27), dict(dw=(1 << 30) + 256), dict(dw=1 << 44, dw2=(1 << 44) + 256), dict(dw=(1 << 45) + 256),
+    dict(wq=(1 << 30) + 256), dict(dw2=1 << 31),
+])
+def test_norm_rope_backward_refuses_weight_gradients_inside_what_it_uses(kw):
+    a = dict(ws=1 << 42, dw=1 << 43, dw2=None, wq=1 << 45)
+    a.update(kw)
+    assert lo._lib().sta_qk_norm_rope_backward(rows(), rows(1 << 25), rows(1 << 27), rows(1 << 28), None, rows(1 << 30), rows(1 << 31), None, a["wq"],
+                                               None, 1, a["dw"], a["dw2"], 1e-6, None, 2, 8, 128, None, None, a["ws"],
+                                               sta.sta_qk_norm_rope_workspace_bytes(128), None) == ALIAS
+
+
 def test_workspace_bytes():
     assert sta.sta_qk_norm_rope_workspace_bytes(128) > 0
     assert sta.sta_qk_norm_rope_workspace_bytes(0) == sta.sta_qk_norm_rope_workspace_bytes(129) == sta.sta_qk_norm_rope_workspace_bytes(258) == 0

@@ -58,6 +58,17 @@ def test_backward_refuses(want, kw):
     assert backward(**kw) == want
 
 
+def test_tensors_without_tokens_need_no_memory_and_meet_nothing():
+    none, keys = rows(None), rows(None, 2, 256)
+    assert forward(q=none, o=none, tq=0) == OK
+    assert backward(q=none, k=keys, v=keys, o=none, d_o=none, lse=None, dq=none, dk=keys, dv=keys, tq=0, tk=0) == OK
+    same = rows(100 * M, 2, 256)                # where nothing is, nothing overlaps; what is there still does
+    assert forward(k=same, v=same, tk=0, o=rows(100 * M)) == ALIAS
+    assert backward(k=same, v=same, dk=same, dv=same, tk=0, dq=rows(100 * M)) == ALIAS
+    assert forward(k=rows(None, 2, 256), tk=0, tq=1 << 31) == SHAPE
+    assert forward(k=keys, v=keys, tk=1) == NULL
+
+
 def test_workspace_bytes():
     f, b = sta.sta_packed_workspace_bytes, sta.sta_packed_backward_workspace_bytes
     assert f(8, 3, 128, 1, 1, 1, 100) == f(8, 2, 96, 1, 1, 1, 100) == f(8, 2, 128, -1, 1, 1, 100) == f(0, 1, 64, 1, 1, 1, 100) == 0
