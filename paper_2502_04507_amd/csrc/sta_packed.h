@@ -99,7 +99,6 @@ __device__ __forceinline__ uint32_t sum64(uint32_t x) { return __builtin_amdgcn_
 struct PackedTile {
     PackedSeq seq;
     uint32_t index;                 // of the tile in its sequence
-    uint32_t slot;                  // of the tile among all sequences' tiles
 };
 
 // The tile of a workgroup, the longest walks first: with up to 64 sequences, a lane each, in the order of how many tiles' walks a tile's is
@@ -139,7 +138,6 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
         at = __builtin_ctzll(here);
         const uint32_t level = lo - __builtin_amdgcn_readlane(longer, at), n = __builtin_amdgcn_readlane(own, at);
         out->index = KEYS ? n - 1 - level : level;
-        out->slot = __builtin_amdgcn_readlane(upto, at) - n + out->index;
     } else {
         uint32_t total = 0;
         for (uint32_t s = 0; s < p.S; s += 64) total += sum64(tiles_of(s + lane, &longer));
@@ -154,7 +152,6 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
             before += all;
         }
         at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > idx));
-        out->slot = idx;
         out->index = idx - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(own, at));
     }
     out->seq = seq_of(s0 + at, p);

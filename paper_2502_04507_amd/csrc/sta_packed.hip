@@ -307,6 +307,7 @@ __device__ __forceinline__ int part_end(uint32_t part, int n, const PackedParams
     return part + 1 == p.parts || end > n ? n : end;
 }
 
+// slot: the tile's rank (few rows: the sequence), below what the launch and the workspace have, whatever the bounds on the device say.
 __device__ __forceinline__ float *part_at(const PackedParams &p, size_t slot, uint32_t kv, uint32_t part, size_t floats)
 {
     return p.ws + ((slot * p.Hkv + kv) * p.parts + part) * floats;
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     if (idle) return;
     const int last_lane = fresh_lane(), last_g4 = last_lane >> 4;
     if (parts_of(n_all, p) > 1) {
-        float *ws = part_at(p, tile.slot, kv, part, part_floats<D, TILE>());
+        float *ws = part_at(p, rank, kv, part, part_floats<D, TILE>());
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
             const int r = 32 * wave + 16 * col + (last_lane & 15);
@@ -696,7 +697,6 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
     } else {
         tile.seq = seq_of(item, p);
         tile.index = 0;
-        tile.slot = item;
     }
     const PackedSeq seq = tile.seq;
     const uint32_t rows = (uint32_t)seq.lq * p.g, row0 = tile.index * R;
@@ -707,7 +707,7 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
     const int n = parts_of(n_all, p), ch = 4 * (threadIdx.x % LPR);
     if (r >= in_tile || n <= 1) return;
     const size_t floats = part_floats<D, R>();
-    const float *ws = part_at(p, tile.slot, kv, 0, floats);
+    const float *ws = part_at(p, item, kv, 0, floats);
     float m = -INFINITY, l = 0.f;
     for (int j = 0; j < n; ++j) m = fmaxf(m, ws[j * floats + (size_t)R * D + r]);
     floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};

@@ -350,6 +350,23 @@ def test_bounds_that_leave_the_tensors_are_cut():
     assert torch.equal(o[:20], good[:20])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_lengths_beyond_max_q_leave_the_workspace(D):
+    """Bounds that are too low: rows may stay unwritten, nothing outside the workspace is written, and what is written is right."""
+    Hq, Hkv, lq, lk, most = 8, 2, [300, 290, 310], [9000, 8000, 8500], 60
+    q, k, v = randn((sum(lq), Hq, D), 1).to(DEV), randn((sum(lk), Hkv, D), 2).to(DEV), randn((sum(lk), Hkv, D), 3).to(DEV)
+    n = sta.sta_packed_workspace_bytes(Hq, Hkv, D, 3, sum(lq), most, max(lk))
+    assert n > 0
+    room = torch.full((n + (256 << 20),), 77, dtype=torch.uint8, device=DEV)
+    args = (q, k, v), (ints(starts(lq)), ints(starts(lk)))
+    o, right = (torch.full_like(q, float("nan")) for _ in range(2))
+    sta.sta_packed_forward(*args[0], o, *args[1], most, max(lk), workspace=room[:n])
+    sta.sta_packed_forward(*args[0], right, *args[1], max(lq), max(lk))
+    assert bool((room[n:] == 77).all())
+    written = ~torch.isnan(o).any(-1)
+    assert bool(written.any()) and float((o.float() - right.float())[written].abs().max()) < 2e-2
+
+
 def test_keys_beyond_max_k_still_count():
     """max_k only chooses how a launch is cut."""
     q, k, v = randn((2, 4, 64), 1).to(DEV), randn((3000, 1, 64), 2).to(DEV), randn((3000, 1, 64), 3).to(DEV)
