@@ -395,7 +395,8 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
  * rounded once.  No atomics: repeated calls give identical bits.
  * Infinities and NaN in q, k, v or d_o make NaN of gradients in their own sequence and key head, also of pairs that are not seen (0 times them is
  * a term of the sums), and of no others.
- * workspace: device, 16-byte aligned, at least sta_packed_backward_workspace_bytes(Hq, tokens_q) bytes, else STA_ERR_WORKSPACE.
+ * workspace: device, 16-byte aligned, at least sta_packed_backward_workspace_bytes(Hq, tokens_q) bytes (the rows' statistics, and from 8192 rows on room for
+ * parts of the sums of dK and dV, at most 67 MB), else STA_ERR_WORKSPACE.
  */
 size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q);
 int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o,

@@ -3,10 +3,11 @@
 //   P_ij = exp(S_ij - lse_i),  dV_j = sum_i P_ij dO_i,  dP_ij = dO_i . V_j,  dS_ij = P_ij (dP_ij - delta_i),  delta_i = dO_i . O_i
 //   dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i       (i: the rows of all heads of a group)
 //
-// Two kernels, no atomics:
+// Two or three kernels, no atomics:
 //   sta_packed_dq_kernel      four waves of 32 rows walk the keys they see: three products per block.  It also forms -delta_i and -lse_i / scale of
 //                             its rows and leaves them, in the order of the rows, for the second kernel;
-//   sta_packed_dkv_kernel     waves of 32 keys walk the rows that see them: four products per block.
+//   sta_packed_dkv_kernel     waves of 32 keys walk the rows that see them: four products per block;
+//   sta_packed_join_kernel    where few keys are seen by many rows, workgroups walk parts of them, and this one adds the parts' sums.
 // The heads of a group are rows like any others, so their gradients of K and V are summed in the accumulators.
 //
 // Roundings.  P and dS go into the matrix instructions as bf16, the only type that those take next to bf16 operands, and delta is formed from O as
@@ -227,8 +228,25 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 ? D == 64 ? 2 : 1 : D == 64 ? 
         if (on[col]) store_column<D, NC>(acc, col, p.scale, b.d_q.data + (int64_t)(seq.q0 + token[col]) * b.d_q.token + head[col] * b.d_q.head, g4);
 }
 
+// Where a tile's walk of rows is cut into parts: n sub-blocks, `each` a part, the last one less.
+struct RowParts {
+    int parts, each;
+};
+__device__ __forceinline__ RowParts row_parts_of(int n, const PackedParams &p)
+{
+    const int each = max((n + (int)p.parts - 1) / (int)p.parts, 1);
+    return {max((n + each - 1) / each, 1), each};
+}
+// A part's sums of dV, then dK: [key of the tile][D].  Tiles are counted by rank, as the launch and the workspace are.
+template <int D, int TILE>
+__device__ __forceinline__ float *row_part_at(const PackedParams &p, uint32_t rank, uint32_t kv, int part)
+{
+    return p.ws + (((size_t)rank * p.Hkv + kv) * p.parts + part) * (2 * TILE * D);
+}
+
 // KW waves of 32 keys; G groups of them take the sub-blocks of rows in turn, each with stages of its own, and the groups' sums are joined at the end.
-template <int D, int KW, int G>
+// CUT: workgroups take parts of a tile's rows and leave their sums in memory, which sta_packed_join_kernel adds up.
+template <int D, int KW, int G, bool CUT>
 __global__ __attribute__((amdgpu_flat_work_group_size(KW * G * 64, KW * G * 64), amdgpu_waves_per_eu((D == 64 ? 3 : 2) - (G > 2))))
 void sta_packed_dkv_kernel(BackwardParams b)
 {
@@ -240,7 +258,9 @@ void sta_packed_dkv_kernel(BackwardParams b)
     __shared__ __attribute__((aligned(1024))) char smem[2 * G * STAGE > MERGE ? 2 * G * STAGE : MERGE];
     const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int walk = all_waves / KW, wave = all_waves % KW;
-    const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    const uint32_t rank = CUT ? sta::fast_div(item, p.by_parts) : item;
+    const int part = CUT ? (int)(item - rank * p.parts) : 0;
     PackedTile tile;
     if (!find_tile<TILE, true>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
@@ -250,7 +270,13 @@ void sta_packed_dkv_kernel(BackwardParams b)
         const int t = j - ahead;
         return !p.causal || t <= 0 ? 0 : t < seq.lq ? t * (int)p.g : rows;
     };
-    const int sub0 = uniform(first_row(key0) / kSub), n_sub = (rows + kSub - 1) / kSub;
+    int sub0 = uniform(first_row(key0) / kSub), n_sub = (rows + kSub - 1) / kSub;
+    if constexpr (CUT) {
+        const RowParts cut = row_parts_of(n_sub - sub0, p);
+        if (part >= cut.parts) return;
+        sub0 += part * cut.each;
+        n_sub = min(sub0 + cut.each, n_sub);
+    }
     const int wave_key = key0 + 32 * wave;
     const int see_lo = uniform(first_row(wave_key)), see_hi = uniform(first_row(wave_key + 31));        // of the wave's first and last key
     bf16x8 K[NC][KS], V[NC][KS];
@@ -421,9 +447,50 @@ void sta_packed_dkv_kernel(BackwardParams b)
     for (int col = 0; col < NC; ++col) {
         const int key = wave_key + 16 * col + c16;
         if (key >= seq.lk) continue;
+        if constexpr (CUT) {
+            float *to = row_part_at<D, TILE>(p, rank, kv, part) + (size_t)(key - key0) * D + 4 * g4;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                *reinterpret_cast<floatx4 *>(to + 16 * cb) = dV[cb][col];
+                *reinterpret_cast<floatx4 *>(to + TILE * D + 16 * cb) = dK[cb][col];
+            }
+            continue;
+        }
         store_column<D, NC>(dV, col, 1.0f, b.d_v.data + (int64_t)(seq.k0 + key) * b.d_v.token + (int64_t)kv * b.d_v.head, g4);
         store_column<D, NC>(dK, col, p.scale, b.d_k.data + (int64_t)(seq.k0 + key) * b.d_k.token + (int64_t)kv * b.d_k.head, g4);
     }
+}
+
+// Sums the parts of a tile's keys in ascending order: workgroup (tile and key head, keys), D / 4 lanes a key.
+template <int D, int TILE>
+__global__ __launch_bounds__(256) void sta_packed_join_kernel(BackwardParams b)
+{
+    const PackedParams &p = b.p;
+    constexpr int LPR = D / 4, KEYS = 256 / LPR;
+    const uint32_t rank = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - rank * p.Hkv;
+    PackedTile tile;
+    if (!find_tile<TILE, true>(rank, p, threadIdx.x & 63, &tile)) return;
+    const PackedSeq seq = tile.seq;
+    const int key0 = (int)tile.index * TILE, in = (int)(blockIdx.y * KEYS + threadIdx.x / LPR), ch = 4 * (threadIdx.x % LPR);
+    if (key0 + in >= seq.lk) return;
+    // as in sta_packed_dkv_kernel
+    const int rows = seq.lq * (int)p.g, t = key0 - (seq.lk - seq.lq), first = !p.causal || t <= 0 ? 0 : t < seq.lq ? t * (int)p.g : rows;
+    const int parts = row_parts_of((rows + kSub - 1) / kSub - first / kSub, p).parts;
+    const float *from = row_part_at<D, TILE>(p, rank, kv, 0) + (size_t)in * D + ch;
+    floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f}, k = v;
+    for (int j = 0; j < parts; ++j, from += 2 * TILE * D) {
+        v += *reinterpret_cast<const floatx4 *>(from);
+        k += *reinterpret_cast<const floatx4 *>(from + TILE * D);
+    }
+    const int64_t key = seq.k0 + key0 + in;
+    bf16x4 dv, dk;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        dv[r] = static_cast<__bf16>(v[r]);
+        dk[r] = static_cast<__bf16>(k[r] * p.scale);
+    }
+    *reinterpret_cast<bf16x4 *>(b.d_v.data + key * b.d_v.token + (int64_t)kv * b.d_v.head + 2 * ch) = dv;
+    *reinterpret_cast<bf16x4 *>(b.d_k.data + key * b.d_k.token + (int64_t)kv * b.d_k.head + 2 * ch) = dk;
 }
 
 // Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than max_length x g.
@@ -436,7 +503,7 @@ int64_t tiles_of(int64_t tokens, int64_t g, int S, int64_t max_length, int tile)
 template <int D, int KW, int G>
 hipError_t launch_dkv(const BackwardParams &b, int64_t tiles, hipStream_t stream)
 {
-    return sta::launch_kernel(sta_packed_dkv_kernel<D, KW, G>, dim3((uint32_t)tiles * b.p.Hkv), dim3(KW * G * 64), stream, b);
+    return sta::launch_kernel(sta_packed_dkv_kernel<D, KW, G, false>, dim3((uint32_t)tiles * b.p.Hkv), dim3(KW * G * 64), stream, b);
 }
 
 template <int D, int RW, int KG>
@@ -446,7 +513,7 @@ hipError_t launch_dq(const BackwardParams &b, int64_t tiles, hipStream_t stream)
 }
 
 template <int D>
-hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipStream_t stream)
+hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, int64_t slots, hipStream_t stream)
 {
     const PackedParams &p = b.p;
     const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, 128), half_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 64), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
@@ -465,12 +532,36 @@ hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, hipSt
         e = row_tiles * p.Hkv >= full ? launch_dq<D, 4, 1>(b, row_tiles, stream) :
             half_rows * p.Hkv >= cus / 2 || max_k < 256 ? launch_dq<D, 2, 2>(b, half_rows, stream) : launch_dq<D, 1, 4>(b, quarter_rows, stream);
     if (e != hipSuccess || key_tiles == 0) return e;
+    // Few keys that many rows see (a video's queries against a prompt): parts of the rows, whose sums go through memory, 5 to 14 us.  Not causal, 24 heads
+    // of 128 channels, 115,200 tokens on 512, 256 and 77 keys, us of dK/dV: 1318, 645, 300 with, 2345, 1090, 1087 by one wave by four groups; 12 heads of
+    // 64, 27,648 tokens on 512 keys 106 + 7, 191; causal, 16/2 x 128, [1500] 74 + 6, 119; [774] of 40/8, shorter than that, 47 by groups.
+    const int64_t items = key_tiles * p.Hkv, subs = ((int64_t)max_q * p.g + kSub - 1) / kSub;
+    if (items < cus && subs >= 256) {
+        const int64_t room = slots / items, long_enough = subs / 32, parts = room < long_enough ? room : long_enough;
+        if (parts > 1) {
+            BackwardParams cut = b;
+            cut.p.parts = (uint32_t)parts;
+            cut.p.by_parts = sta::fast_div_of((uint32_t)parts);
+            if ((e = sta::launch_kernel(sta_packed_dkv_kernel<D, 4, 1, true>, dim3((uint32_t)(items * parts)), dim3(256), stream, cut)) != hipSuccess) return e;
+            return sta::launch_kernel(sta_packed_join_kernel<D, 128>, dim3((uint32_t)items, D / 8), dim3(256), stream, cut);
+        }
+    }
     if (key_tiles * p.Hkv >= full) return launch_dkv<D, 4, 1>(b, key_tiles, stream);
     if (half_tiles * p.Hkv < cus) return launch_dkv<D, 1, 4>(b, quarter_tiles, stream);
     return launch_dkv<D, 2, 2>(b, half_tiles, stream);
 }
 
 constexpr size_t kStatPad = 64;     // floats behind either array
+
+size_t stat_bytes(int Hq, int64_t tokens_q) { return (2 * ((size_t)Hq * tokens_q + kStatPad) * sizeof(float) + 15) & ~(size_t)15; }
+
+// Parts of tiles of 128 keys that there is room for: two workgroups a CU, and a part for every 128 rows of all heads, so that small calls need little.
+int64_t part_slots(int Hq, int64_t tokens_q)
+{
+    const int64_t most = 2 * sta::compute_units(), by_rows = (int64_t)Hq * tokens_q / 128;
+    return by_rows < 64 ? 0 : by_rows < most ? by_rows : most;
+}
+constexpr size_t kPartBytes = 2 * 128 * 128 * sizeof(float);
 
 }  // namespace
 
@@ -479,7 +570,7 @@ extern "C" {
 size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q)
 {
     if (Hq < 1 || tokens_q < 0 || tokens_q > 0x7fffffff) return 0;
-    return 2 * ((size_t)Hq * tokens_q + kStatPad) * sizeof(float);
+    return stat_bytes(Hq, tokens_q) + (size_t)part_slots(Hq, tokens_q) * kPartBytes;
 }
 
 int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o, const sta_head_rows *d_o,
@@ -538,12 +629,14 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     p.scale = scale;
     p.scale_log2e = scale * 1.4426950408889634f;
     p.parts = 1;
+    p.ws = reinterpret_cast<float *>(static_cast<char *>(workspace) + stat_bytes(q->heads, tokens_q));
     b.lse = lse;
     b.neg_lse = static_cast<float *>(workspace);
     b.neg_delta = b.neg_lse + (size_t)q->heads * tokens_q + kStatPad;
     b.inv_scale = 1.0f / scale;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = D == 64 ? launch_gradients<64>(b, max_q, max_k, stream) : launch_gradients<128>(b, max_q, max_k, stream);
+    const int64_t slots = part_slots(q->heads, tokens_q);
+    const hipError_t e = D == 64 ? launch_gradients<64>(b, max_q, max_k, slots, stream) : launch_gradients<128>(b, max_q, max_k, slots, stream);
     if (e == hipErrorInvalidValue) return STA_ERR_SHAPE;
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }

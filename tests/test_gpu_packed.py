@@ -204,6 +204,16 @@ def test_walk_groups(case, D):
     check(Hq, Hkv, D, lq, lk, causal)
 
 
+# Few keys that many rows see: their gradients in parts of the rows.
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("case", [(16, 1, [600, 3, 0], [300, 5, 9]), (24, 2, [700], [129]), (16, 1, [0, 530, 515], [70, 77, 400]), (8, 1, [1300], [1300]), (1, 1, [9000], [40])])
+def test_gradients_of_keys_cut_along_the_rows(case, causal, D):
+    Hq, Hkv, lq, lk = case
+    assert sta.sta_packed_backward_workspace_bytes(Hq, sum(lq)) > 2 * 4 * (Hq * sum(lq) + 64) + 16
+    check(Hq, Hkv, D, lq, lk, causal, train=True)
+
+
 @pytest.mark.parametrize("layout", ["heads", "wide"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_layouts(layout, D):
