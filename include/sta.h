@@ -375,7 +375,8 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
  * With the sequence's lq query and lk key tokens, query token i sees, if causal is not 0, the keys j <= i + lk - lq (the last token sees
  * all), else all.  A row that sees no key: o = 0, lse = -infinity.  A length may be 0.  Query tokens that no sequence has keep what o
  * and lse hold.  Keys that a row does not see take no part in it, whatever they hold, infinities and NaN in V included.
- * lse: NULL, or device float32 [Hq, tokens_q], ln of each row's softmax denominator.  scale <= 0 selects 1 / sqrt(D).
+ * lse: NULL, or device float32 [Hq, tokens_q], ln of each row's softmax denominator; NaN, as o, where the row meets NaN in q or in keys that it sees.
+ * scale <= 0 selects 1 / sqrt(D).
  * Arithmetic as sta_forward (with lse, the sum is taken before the probabilities are rounded).
  * workspace: as sta_forward, of at least sta_packed_workspace_bytes(...) bytes: launches that would not fill the chip are cut along the keys.
  * NULL: no parts.  Results are repeatable bit for bit.

@@ -24,8 +24,9 @@ FLAGS = [
     # packed fp32 instructions are kept out of every kernel
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
-    # no NaN is ever produced inside the kernels (the only infinities are the initial running maxima, which meet
-    # finite values only); saying so lets max chains compile to v_max3_f32 without per-operand canonicalisation
+    # numbers make no NaN inside the kernels (the only infinities are the initial running maxima, which meet finite values only);
+    # saying so lets max chains compile to v_max3_f32 without per-operand canonicalisation.  NaN that inputs bring go through sums and
+    # products as ever, but a comparison with one may go either way: code that has to tell them looks at the bits
     "-fno-honor-nans",
     # matrix instructions accumulate in vector registers everywhere.  Left to itself the compiler moves the accumulators of
     # kernels whose LDS allows one wave per SIMD into accumulation registers and copies them to scale or test them (40 heads of

@@ -258,6 +258,15 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
     }
 }
 
+// ln of the denominator of a row whose offset is m (base-2 units) and whose sum is l: -infinity where no key was seen, which leaves the sum at 0.  NaN
+// stays NaN; the bits are looked at, because the kernels are compiled as if comparisons met none.
+__device__ __forceinline__ float lse_of(float m, float l)
+{
+    uint32_t bits = __float_as_uint(l);
+    asm volatile("" : "+v"(bits));
+    return bits == 0 ? -INFINITY : m * kLn2 + __logf(l);
+}
+
 // Where a column's row lies.
 struct RowAt {
     int token, head;                // inside the sequence and the group
@@ -537,7 +546,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
             for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(st.acc[j][col][r] * inv);
             *reinterpret_cast<bf16x4 *>(row + 32 * (cb0 + j) + 8 * last_g4) = v;
         }
-        if (LSE && p.lse && last_g4 == 0 && kg == 0) p.lse[head * p.tokens_q + token] = l[col] > 0.f ? m[col] * kLn2 + __logf(l[col]) : -INFINITY;
+        if (LSE && p.lse && last_g4 == 0 && kg == 0) p.lse[head * p.tokens_q + token] = lse_of(m[col], l[col]);
     }
 }
 
@@ -677,7 +686,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
                 ws[(size_t)R * D + 16 * col + c16] = m;
                 ws[(size_t)R * D + R + 16 * col + c16] = l;
             } else if (LSE && p.lse) {
-                p.lse[head * p.tokens_q + token] = l > 0.f ? m * kLn2 + __logf(l) : -INFINITY;
+                p.lse[head * p.tokens_q + token] = lse_of(m, l);
             }
         }
     }
@@ -726,7 +735,7 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>(sum[i] * inv);
     *reinterpret_cast<bf16x4 *>(p.o.data + token * p.o.token + head * p.o.head + 2 * ch) = v;
-    if (p.lse && ch == 0) p.lse[head * p.tokens_q + token] = l > 0.f ? m * kLn2 + __logf(l) : -INFINITY;
+    if (p.lse && ch == 0) p.lse[head * p.tokens_q + token] = lse_of(m, l);
 }
 
 }  // namespace

@@ -1,0 +1,87 @@
+"""Attention over packed sequences at the edges of its arguments, against the definition in 64 bits; errors allowed as in test_gpu_packed."""
+import math
+
+import pytest
+import torch
+
+import paper_2502_04507_amd as sta
+from tests import layer_util as lu
+from tests.test_gpu_packed import BF, DEV, bounds, close, ints, randn, starts
+
+pytestmark = pytest.mark.gpu
+
+# Hq, Hkv, queries, keys, whether the launch is cut into parts: single tokens whole and in parts, two groups and four in a workgroup,
+# tiles in parts, workgroups of four waves that share their stages
+LSE = [(4, 2, [1, 3], [40, 70], False), (4, 2, [1, 2], [3000, 77], True), (16, 8, [300] * 4, [300] * 4, False), (6, 3, [70, 45, 300], [70, 45, 300], False),
+       (8, 2, [100, 40], [4000, 300], True), (32, 16, [520] * 9, [520] * 9, False)]
+
+
+def forward(q, k, v, lq, lk, parts=False, **kw):
+    Hq, Hkv, D = q.shape[1], k.shape[1], q.shape[2]
+    o, lse = torch.full_like(q, 7.0, device=DEV), torch.full((Hq, sum(lq)), 7.0, device=DEV)
+    n = sta.sta_packed_workspace_bytes(Hq, Hkv, D, len(lq), sum(lq), max(lq), max(lk))
+    assert (n > 0) or not parts
+    sta.sta_packed_forward(q.to(DEV), k.to(DEV), v.to(DEV), o, ints(starts(lq)), ints(starts(lk)), max(lq), max(lk), lse=lse,
+                           workspace=torch.empty(n, dtype=torch.uint8, device=DEV) if parts else None, **kw)
+    return o, lse
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("which", ["q", "k"])
+@pytest.mark.parametrize("case", LSE, ids=[str(i) for i in range(len(LSE))])
+def test_lse_of_rows_that_meet_nan_is_nan(case, which, D):
+    """-infinity is the mark of rows that see no key, and of no others; rows that meet no NaN keep their lse."""
+    Hq, Hkv, lq, lk, parts = case
+    g = Hq // Hkv
+    q, k, v = randn((sum(lq), Hq, D), 1), randn((sum(lk), Hkv, D), 2), randn((sum(lk), Hkv, D), 3)
+    for s in range(len(lq)):
+        if which == "q":
+            q[starts(lq)[s] + lq[s] - 1, g, 3] = float("nan")
+        else:
+            k[starts(lk)[s] + lk[s] - lq[s], 1, D - 1] = float("nan")            # the first row sees it
+    o, lse = forward(q, k, v, lq, lk, parts)
+    o, lse = o.cpu(), lse.cpu().double()
+    for s in range(len(lq)):
+        a, b = slice(starts(lq)[s], starts(lq)[s] + lq[s]), slice(starts(lk)[s], starts(lk)[s] + lk[s])
+        Q, K, V = q[a].double(), k[b].double(), v[b].double()
+        meets = torch.zeros((Hq, lq[s]), dtype=torch.bool)
+        if which == "q":
+            meets[g, -1] = True
+        else:
+            meets[g:2 * g] = True
+        assert torch.equal(torch.isnan(lse[:, a]), meets), s
+        assert torch.equal(torch.isnan(o[a]).all(-1).T, meets) and torch.equal(torch.isnan(o[a]).any(-1).T, meets), s
+        _, want = lu.attention(Q.nan_to_num(0.0), K.nan_to_num(0.0), V, True, D ** -0.5)
+        _, b_lse, _ = bounds(Q.nan_to_num(0.0), K.nan_to_num(0.0), V, True, D ** -0.5, want)
+        assert bool(((lse[:, a] - want).abs() <= b_lse)[~meets].all()), s
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("which", ["q", "k"])
+def test_gradients_of_rows_that_met_nan_in_the_forward(which, D):
+    """NaN in q or k when o and lse are formed as well: the gradients of such rows and of all that they see are NaN, none is an infinity, other sequences
+    and key heads keep their bits."""
+    Hq, Hkv, lens = 6, 3, [70, 45, 300]
+    T, cu = sum(lens), ints(starts(lens))
+    at, head, kv = 70 + 20, 3, 1                            # token 20 of the second sequence
+    x = [randn((T, h, D), i + 1) for i, h in enumerate((Hq, Hkv, Hkv))]
+    d_o = randn((T, Hq, D), 4).to(DEV)
+    results = []
+    for bad in (False, True):
+        if bad:
+            x[which == "k"][at, kv if which == "k" else head, 5] = float("nan")
+        o, lse = forward(*x, lens, lens)
+        dev = [t.to(DEV) for t in x]
+        d = [torch.empty_like(t) for t in dev]
+        ws = torch.empty(sta.sta_packed_backward_workspace_bytes(Hq, T), dtype=torch.uint8, device=DEV)
+        sta.sta_packed_backward(*dev, o, d_o, lse, *d, cu, cu, max(lens), max(lens), ws)
+        results.append([t.cpu() for t in d])
+    before, (dq, dk, dv) = results
+    rows, keys = (slice(at, 115), slice(70, 115)) if which == "k" else (slice(at, at + 1), slice(70, at + 1))
+    assert bool(torch.isnan(dq[rows, head]).all())
+    assert bool(torch.isnan(dk[keys, kv]).all()) and bool(torch.isnan(dv[keys, kv]).all())
+    assert not any(bool(torch.isinf(t).any()) for t in (dq, dk, dv))
+    for a, b in zip((dq, dk, dv), before):
+        a, b = (t.view(torch.int16).view(T, Hkv, -1, D) for t in (a, b))
+        assert torch.equal(a[:70], b[:70]) and torch.equal(a[115:], b[115:])
+        assert torch.equal(a[:, [0, 2]], b[:, [0, 2]])
