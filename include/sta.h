@@ -371,7 +371,8 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
  * n.  Strides as sta_head_rows says (batch is not looked at); all bf16.  Sequence s has the query tokens cu_q[s] .. cu_q[s + 1] - 1 and the
  * key tokens cu_k[s] .. cu_k[s + 1] - 1, of which, with k_used (NULL: all), the first k_used[s]: a cache with room to grow is cu_k at its
  * slots' bounds and k_used the lengths.  cu_q, cu_k, k_used: device int32 of S + 1, S + 1 and S entries; entries that leave the tensors or do
- * not ascend are cut to what is there.  max_q, max_k: host, upper bounds of the sequences' lengths (rows beyond may stay unwritten).
+ * not ascend are cut to what is there.  max_q, max_k: host, upper bounds of the sequences' lengths; of a longer sequence the query tokens beyond max_q
+ * may stay unwritten, and the others are not touched by it.
  * With the sequence's lq query and lk key tokens, query token i sees, if causal is not 0, the keys j <= i + lk - lq (the last token sees
  * all), else all.  A row that sees no key: o = 0, lse = -infinity.  A length may be 0.  Query tokens that no sequence has keep what o
  * and lse hold.  Keys that a row does not see take no part in it, whatever they hold, infinities and NaN in V included.
@@ -392,7 +393,7 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
 /*
  * Gradients of sta_packed_forward (of all keys: no k_used), o and lse as it returned them for the same q, k, v, bounds, causal and scale.
  * d_q: like q; d_k, d_v: like k and v, summed over the query heads of a group.  Written for every token of a sequence (0 where no
- * row saw it).  P is recomputed from the scores and lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are
+ * row saw it; of a sequence longer than max_q the query tokens beyond it are no rows here, and keys beyond max_k may stay unwritten).  P is recomputed from the scores and lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are
  * rounded once.  No atomics: repeated calls give identical bits.
  * Infinities and NaN in q, k, v or d_o make NaN of gradients in their own sequence and key head, also of pairs that are not seen (0 times them is
  * a term of the sums), and of no others.

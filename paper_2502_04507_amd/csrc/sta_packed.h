@@ -33,6 +33,7 @@ struct PackedParams {
     float *lse;                     // [Hq, tokens_q] or null
     const int32_t *cu_q, *cu_k, *k_used;
     uint32_t S, tokens_q, tokens_k;
+    int32_t max_q, max_k;           // what the caller says no sequence is longer than, and what launches are counted by
     uint32_t Hkv, g;                // key heads, query heads of each
     sta::FastDiv by_g, by_Hkv, by_parts;
     uint32_t causal;
@@ -46,6 +47,9 @@ struct PackedParams {
 // One sequence; every wave finds it for itself, so all members are the same in all lanes.
 struct PackedSeq {
     int32_t q0, lq, k0, lk;         // first query and key token, and how many
+    // query tokens that are worked on: those beyond max_q have no tile.  Also what the gradients of the keys sum over, so that they use no row
+    // whose statistics this call has not formed
+    __device__ __forceinline__ int worked(const PackedParams &p) const { return lq < p.max_q ? lq : p.max_q; }
     // keys that a row of query token t sees: the first keys_of(t)
     __device__ __forceinline__ int keys_of(int t, const PackedParams &p) const
     {
@@ -116,7 +120,7 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
             const uint64_t more = (uint64_t)(q.lk - q.lq) * p.g / TILE;
             *longer = more < (1u << 24) ? (uint32_t)more : 1u << 24;
         }
-        return ((KEYS ? (uint32_t)q.lk : (uint32_t)q.lq * p.g) + TILE - 1) / TILE;
+        return ((KEYS ? (uint32_t)(q.lk < p.max_k ? q.lk : p.max_k) : (uint32_t)q.worked(p) * p.g) + TILE - 1) / TILE;
     };
     uint32_t longer;
     int at;                         // lane of the sequence

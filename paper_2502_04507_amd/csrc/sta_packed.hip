@@ -905,6 +905,8 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
     p.S = S;
     p.tokens_q = (uint32_t)tokens_q;
     p.tokens_k = (uint32_t)tokens_k;
+    p.max_q = max_q;
+    p.max_k = max_k;
     p.Hkv = k->heads;
     p.g = q->heads / k->heads;
     p.by_g = sta::fast_div_of(p.g);

@@ -264,11 +264,11 @@ void sta_packed_dkv_kernel(BackwardParams b)
     PackedTile tile;
     if (!find_tile<TILE, true>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
-    const int rows = seq.lq * (int)p.g, key0 = (int)tile.index * TILE, ahead = seq.lk - seq.lq;
+    const int worked = seq.worked(p), rows = worked * (int)p.g, key0 = (int)tile.index * TILE, ahead = seq.lk - seq.lq;
     // key j is seen by the rows from first_row(j) on
     auto first_row = [&](int j) {
         const int t = j - ahead;
-        return !p.causal || t <= 0 ? 0 : t < seq.lq ? t * (int)p.g : rows;
+        return !p.causal || t <= 0 ? 0 : t < worked ? t * (int)p.g : rows;
     };
     int sub0 = uniform(first_row(key0) / kSub), n_sub = (rows + kSub - 1) / kSub;
     if constexpr (CUT) {
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256) void sta_packed_join_kernel(BackwardParams b)
     const int key0 = (int)tile.index * TILE, in = (int)(blockIdx.y * KEYS + threadIdx.x / LPR), ch = 4 * (threadIdx.x % LPR);
     if (key0 + in >= seq.lk) return;
     // as in sta_packed_dkv_kernel
-    const int rows = seq.lq * (int)p.g, t = key0 - (seq.lk - seq.lq), first = !p.causal || t <= 0 ? 0 : t < seq.lq ? t * (int)p.g : rows;
+    const int worked = seq.worked(p), rows = worked * (int)p.g, t = key0 - (seq.lk - seq.lq), first = !p.causal || t <= 0 ? 0 : t < worked ? t * (int)p.g : rows;
     const int parts = row_parts_of((rows + kSub - 1) / kSub - first / kSub, p).parts;
     const float *from = row_part_at<D, TILE>(p, rank, kv, 0) + (size_t)in * D + ch;
     floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f}, k = v;
@@ -620,6 +620,8 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     p.S = S;
     p.tokens_q = (uint32_t)tokens_q;
     p.tokens_k = (uint32_t)tokens_k;
+    p.max_q = max_q;
+    p.max_k = max_k;
     p.Hkv = k->heads;
     p.g = q->heads / k->heads;
     p.by_g = sta::fast_div_of(p.g);

@@ -85,3 +85,53 @@ def test_gradients_of_rows_that_met_nan_in_the_forward(which, D):
         a, b = (t.view(torch.int16).view(T, Hkv, -1, D) for t in (a, b))
         assert torch.equal(a[:70], b[:70]) and torch.equal(a[115:], b[115:])
         assert torch.equal(a[:, [0, 2]], b[:, [0, 2]])
+
+
+# Hq, Hkv, queries, keys, max_q, max_k: few tiles and many, more sequences than a wave has lanes, keys' gradients cut along the rows, nothing at all
+TOO_LOW = [(4, 2, [300, 20, 70], [300, 25, 70], 60, 300), (4, 2, [300, 20, 70], [200, 25, 90], 60, 50), (32, 16, [520] * 9 + [40], [520] * 9 + [40], 200, 520),
+           (2, 2, [130, 1, 7] * 30, [130, 3, 5] * 30, 40, 130), (16, 1, [900, 600], [300, 5], 700, 300), (4, 2, [50, 3], [50, 9], 0, 50), (4, 2, [50, 3], [50, 9], 50, 0)]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("case", TOO_LOW, ids=[str(i) for i in range(len(TOO_LOW))])
+def test_gradients_where_bounds_of_lengths_are_too_low(case, D, causal):
+    """Query tokens beyond max_q, and keys beyond max_k, may stay unwritten; what is written sums over the rows up to max_q, whatever the workspace held."""
+    Hq, Hkv, lq, lk, max_q, max_k = case
+    q, k, v, g = (randn((sum(n), h, D), i + 1) for i, (h, n) in enumerate(((Hq, lq), (Hkv, lk), (Hkv, lk), (Hq, lq))))
+    x = [t.to(DEV) for t in (q, k, v)]
+    o, lse = torch.empty_like(x[0]), torch.empty((Hq, sum(lq)), device=DEV)
+    cu = ints(starts(lq)), ints(starts(lk))
+    sta.sta_packed_forward(*x, o, *cu, max(lq), max(lk), causal=causal, lse=lse)
+    results = []
+    for held in (0, 255, 63):
+        ws = torch.full((sta.sta_packed_backward_workspace_bytes(Hq, sum(lq)),), held, dtype=torch.uint8, device=DEV)
+        d = [torch.full_like(t, 7.0) for t in x]
+        sta.sta_packed_backward(*x, o, g.to(DEV), lse, *d, *cu, max_q, max_k, ws, causal=causal)
+        results.append(d)
+    for d in results[1:]:
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(d, results[0]))
+    dq, dk, dv = (t.cpu() for t in results[0])
+    c = D ** -0.5
+    for s in range(len(lq)):
+        a, b = slice(starts(lq)[s], starts(lq)[s] + lq[s]), slice(starts(lk)[s], starts(lk)[s] + lk[s])
+        nq, nk = min(lq[s], max_q), min(lk[s], max_k)
+        Q, K, V, G = q[a].double(), k[b].double(), v[b].double(), g[a].double()
+        G[nq:] = 0.0                                        # rows that are left out add nothing
+        _, want_lse, *want = lu.attention(Q, K, V, causal, c, G)
+        _, _, off = bounds(Q, K, V, causal, c, want_lse, G)
+        for name, got, w, e, n in (("dq", dq[a], want[0], off[0], nq), ("dk", dk[b], want[1], off[1], nk), ("dv", dv[b], want[2], off[2], nk)):
+            close(got[:n], w[:n], e[:n], "sequence %d %s" % (s, name), norm=False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_within_bounds_that_are_too_low_are_written(D):
+    """A sequence longer than max_q takes nothing from the others."""
+    Hq, Hkv, lq, lk = 4, 2, [700, 60, 33, 60], [700, 60, 90, 61]
+    q, k, v = randn((sum(lq), Hq, D), 1).to(DEV), randn((sum(lk), Hkv, D), 2).to(DEV), randn((sum(lk), Hkv, D), 3).to(DEV)
+    o, right = torch.full_like(q, 7.0), torch.empty_like(q)
+    sta.sta_packed_forward(q, k, v, o, ints(starts(lq)), ints(starts(lk)), 60, 90)
+    sta.sta_packed_forward(q, k, v, right, ints(starts(lq)), ints(starts(lk)), 700, 700)
+    for a, n in zip(starts(lq), lq):
+        n = min(n, 60)
+        assert float((o[a:a + n].float() - right[a:a + n].float()).abs().max()) < 2e-2
