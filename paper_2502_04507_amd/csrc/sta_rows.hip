@@ -375,14 +375,18 @@ __device__ __forceinline__ HeadAt head_at(uint32_t u, const Params &p)
     return u < h1 ? HeadAt{0, u} : u < h2 ? HeadAt{1, u - h1} : HeadAt{2, u - h2};
 }
 
-// Workgroup (x, y): tokens 64 / L * x .., heads y * kWaves + wave and every gridDim.y * kWaves after that, of all tensors one after the other.
+constexpr int kGridShift = 23;                              // a grid holds fewer than 2^32 lanes along x
+
+// Workgroup (x, y, z): tokens 64 / L * (z * 2^23 + x) .., heads y * kWaves + wave and every gridDim.y * kWaves after that, of all tensors one after the other.
 // AHEAD rows are on their way while one is worked on; the first are asked for before the positions and steps.
 template <int PATH, int L, bool SRC_F32, bool DST_F32>
 __global__ __launch_bounds__(kThreads) void sta_rows_forward_kernel(Params p)
 {
     constexpr int NP = pairs_of(PATH), AHEAD = SRC_F32 ? 1 : 2;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t c = lane % L, id = blockIdx.x * (64 / L) + lane / L;
+    const uint32_t first_id = ((blockIdx.z << kGridShift) + blockIdx.x) * (64 / L);        // at most 2^31 + 2^27
+    if (first_id >= p.tokens) return;
+    const uint32_t c = lane % L, id = first_id + lane / L;
     const bool on = id < p.tokens;
     Token t = token_of(on ? id : 0, p);
     const Place at = place_of<PATH, L>(c, p);
@@ -697,6 +701,13 @@ uint32_t split_of(uint32_t groups, uint32_t heads, uint32_t blocks)
     return want < 1 ? 1 : want < most ? want : most;
 }
 
+// The forward's grid: `per` tokens a workgroup.
+dim3 forward_grid(uint32_t tokens, uint32_t per, uint32_t heads, uint32_t blocks)
+{
+    const uint32_t groups = (tokens + per - 1) / per;
+    return dim3(groups >> kGridShift ? 1u << kGridShift : groups, split_of(groups, heads, blocks), ((groups - 1) >> kGridShift) + 1);
+}
+
 template <int PATH, int L, bool SRC_F32, bool DST_F32>
 hipError_t launch(Params &p, bool backward, hipStream_t stream)
 {
@@ -704,7 +715,7 @@ hipError_t launch(Params &p, bool backward, hipStream_t stream)
     uint32_t heads = 0;
     for (uint32_t i = 0; i < p.n_tensors; ++i) heads += p.t[i].heads;
     if (!backward)
-        return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, dim3(groups, split_of(groups, heads, PATH == kGeneral ? kWantGeneral : kWantBlocks)), dim3(kThreads), stream, p);
+        return sta::launch_kernel(sta_rows_forward_kernel<PATH, L, SRC_F32, DST_F32>, forward_grid(p.tokens, per, heads, PATH == kGeneral ? kWantGeneral : kWantBlocks), dim3(kThreads), stream, p);
     // workgroups by heads, units of as few heads a wave as it takes to have that many
     uint32_t first = 0;
     for (uint32_t i = 0; i < 3; ++i) {
@@ -751,6 +762,13 @@ hipError_t launch_rows(Params &p, bool src_f32, bool dst_f32, bool backward, hip
 }  // namespace
 
 extern "C" {
+
+// Not part of the ABI (include/sta.h), for the tests: the grid of a forward launch of `per` tokens a workgroup.
+void sta_rows_grid(uint32_t tokens, uint32_t per, uint32_t heads, uint32_t grid[3])
+{
+    const dim3 g = forward_grid(tokens, per, heads, kWantGeneral);
+    grid[0] = g.x; grid[1] = g.y; grid[2] = g.z;
+}
 
 int sta_rope_steps(int channels, double theta, int scaling, double factor, double original_positions, int64_t *steps, float *magnitude)
 {

@@ -301,3 +301,24 @@ def test_rows_beyond_4_gb():
     sta.sta_qk_norm_rope_backward(x, x, y, y, None, *d, None, w, None, None, None, big, None)
     sta.sta_qk_norm_rope_backward(tail, tail, z, z, None, *dz, None, w, None, None, None, small, None)
     assert torch.equal(d[0][:, -n:], dz[0]) and torch.equal(d[1][:, -n:], dz[1])
+
+
+def test_rows_of_more_than_2_to_the_24_workgroups():
+    """Tokens beyond 2^24 of rows that take a wave each: those around the places where the grid is folded, and the last, against the same rows alone."""
+    N, D, n = 2 ** 24 + 777, 130, 300
+    x = torch.zeros((1, N, 1, D), dtype=torch.bfloat16, device=DEV)
+    steps = sta.sta_rope_steps(D)[0].to(DEV)
+    w = torch.ones(D, device=DEV)
+    places = [slice(a, a + n) for a in (0, 2 ** 23 - 150, 2 ** 24 - 150, N - n)]
+    for i, at in enumerate(places):
+        x[:, at] = make((1, n, 1, D), 3 + i, torch.bfloat16).to(DEV)
+    turned, normed, other = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    sta.sta_rope(x, turned, sta.StaRotary(steps))
+    sta.sta_qk_norm_rope(x, x, None, normed, other, None, w, None, sta.StaRotary(steps))
+    for at in places:
+        positions = torch.arange(at.start, at.stop, dtype=torch.int32, device=DEV)
+        rotary, rows = sta.StaRotary(steps, positions=positions), x[:, at].contiguous()
+        a, b, c = (torch.empty_like(rows) for _ in range(3))
+        sta.sta_rope(rows, a, rotary)
+        sta.sta_qk_norm_rope(rows, rows, None, b, c, None, w, None, rotary)
+        assert torch.equal(turned[:, at], a) and torch.equal(normed[:, at], b) and torch.equal(other[:, at], c), at
