@@ -27,6 +27,20 @@ struct PackedRows {
     char *data;
     int64_t token, head;
 };
+inline PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(r.data), r.token * 2, r.head * 2}; }
+
+// Tokens of a tensor, and rows of all query heads: the kernels count keys and rows in int, up to a few hundred beyond the last one.
+constexpr int64_t kMostTokens = 0x7ffff000;
+// Workgroups of 256 lanes of a launch: a grid holds fewer than 2^32 lanes along x.
+constexpr int64_t kMostWorkgroups = (1 << 24) - 1;
+
+// Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than `longest` x g.
+inline int64_t tiles_of(int64_t tokens, int64_t g, int64_t S, int64_t longest, int64_t tile)
+{
+    if (longest > tokens) longest = tokens;                 // no sequence is; and so all products stay below 2^58
+    const int64_t by_tokens = tokens * g / tile + S, by_longest = (longest * g + tile - 1) / tile * S;
+    return by_tokens < by_longest ? by_tokens : by_longest;
+}
 
 struct PackedParams {
     PackedRows q, k, v, o;

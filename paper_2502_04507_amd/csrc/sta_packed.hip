@@ -742,8 +742,6 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
 
 namespace {
 
-PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(r.data), r.token * 2, r.head * 2}; }
-
 // How a launch is cut.  Rows of one sequence and key head that fit 16 or 32 columns take the kernel for few rows.  Others: tiles of 128 rows that
 // share every stage where they are two and a quarter a CU (head dimension 64: three) or more, else tiles of 64 rows by two groups that take the stages
 // in turn, or of 32 by four.  Tiles are cut along the keys where that puts more of the chip to work than the sums in memory and their merge, 5 to
@@ -768,10 +766,7 @@ constexpr uint32_t kNoParts = 1u << 30;
 bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
 {
     const int64_t g = Hq / Hkv, rows = g * max_q, cus = sta::compute_units(), subs = ((int64_t)max_k + kSub - 1) / kSub;
-    auto tiles = [&](int64_t tile) {
-        const int64_t by_tokens = tokens_q * g / tile + S, by_longest = (rows + tile - 1) / tile * S;
-        return by_tokens < by_longest ? by_tokens : by_longest;
-    };
+    auto tiles = [&](int64_t tile) { return tiles_of(tokens_q, g, S, max_q, tile); };
     plan->few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     plan->waves = 4;
     int64_t want = cut && plan->few ? 4 * cus : 0, least = 16;
@@ -793,13 +788,13 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     plan->parts = 1;
     plan->part_subs = kNoParts;
     const int64_t items = slots * Hkv;
-    if (items > 0x7fffffff) return false;
+    if (items > kMostWorkgroups) return false;
     plan->slots = (uint32_t)slots;
     if (items > 0 && items < want / 2) {
         int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
         each = each < least ? least : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
         parts = (subs + each - 1) / each;
-        if (parts > 1 && items * parts <= 0x7fffffff) {
+        if (parts > 1 && items * parts <= kMostWorkgroups) {
             plan->parts = (uint32_t)parts;
             plan->part_subs = (uint32_t)each;
         }
@@ -858,7 +853,7 @@ extern "C" {
 
 size_t sta_packed_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
 {
-    if (Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128) || S < 0 || tokens_q < 0 || max_q < 0 || max_k < 0) return 0;
+    if (Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128) || S < 0 || tokens_q < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens / Hq) return 0;
     PackedPlan plan;
     return plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, true, &plan) ? plan.workspace() * sizeof(float) : 0;
 }
@@ -868,13 +863,13 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
                        int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!q || !k || !v || !o) return STA_ERR_NULL;
-    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > 0x7fffffff || tokens_k > 0x7fffffff) return STA_ERR_SHAPE;
+    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens || tokens_k > kMostTokens) return STA_ERR_SHAPE;
     if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
     if (int rc = sta::packed_check(q, tokens_q, 0, D, false)) return rc;
     if (int rc = sta::packed_check(k, tokens_k, 0, D, false)) return rc;
     if (int rc = sta::packed_check(v, tokens_k, k->heads, D, false)) return rc;
     if (int rc = sta::packed_check(o, tokens_q, q->heads, D, true)) return rc;
-    if (q->heads % k->heads || tokens_q * q->heads > 0x7fffffff) return STA_ERR_SHAPE;
+    if (q->heads % k->heads || tokens_q * q->heads > kMostTokens) return STA_ERR_SHAPE;
     if (S == 0 || tokens_q == 0 || max_q == 0) return STA_OK;
     if (!cu_q || !cu_k) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)k_used | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;

@@ -493,13 +493,6 @@ __global__ __launch_bounds__(256) void sta_packed_join_kernel(BackwardParams b)
     *reinterpret_cast<bf16x4 *>(b.d_k.data + key * b.d_k.token + (int64_t)kv * b.d_k.head + 2 * ch) = dk;
 }
 
-// Upper bound of the tiles of S sequences that hold `tokens` x g rows, none of more than max_length x g.
-int64_t tiles_of(int64_t tokens, int64_t g, int S, int64_t max_length, int tile)
-{
-    const int64_t by_tokens = tokens * g / tile + S, by_longest = (max_length * g + tile - 1) / tile * S;
-    return by_tokens < by_longest ? by_tokens : by_longest;
-}
-
 template <int D, int KW, int G>
 hipError_t launch_dkv(const BackwardParams &b, int64_t tiles, hipStream_t stream)
 {
@@ -519,7 +512,6 @@ hipError_t launch_gradients(const BackwardParams &b, int max_q, int max_k, int64
     const int64_t row_tiles = tiles_of(p.tokens_q, p.g, p.S, max_q, 128), half_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 64), key_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 128),
                   half_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 64);
     const int64_t quarter_rows = tiles_of(p.tokens_q, p.g, p.S, max_q, 32), quarter_tiles = tiles_of(p.tokens_k, 1, p.S, max_k, 32);
-    if (half_rows * p.Hkv > 0x7fffffff || half_tiles * p.Hkv > 0x7fffffff) return hipErrorInvalidValue;
     // Four waves of 32 rows (keys) share a stage where that makes workgroups for the chip (head dimension 128: two and a quarter a CU, 64: three); else
     // two waves by two groups that take the stages in turn, or, where these are fewer than a workgroup a CU (rows: half one, and walks worth it), one by
     // four.  Causal, heads / key heads x channels, us of dQ, dK/dV in that order:
@@ -569,7 +561,7 @@ extern "C" {
 
 size_t sta_packed_backward_workspace_bytes(int Hq, int64_t tokens_q)
 {
-    if (Hq < 1 || tokens_q < 0 || tokens_q > 0x7fffffff) return 0;
+    if (Hq < 1 || tokens_q < 0 || tokens_q > kMostTokens / Hq) return 0;
     return stat_bytes(Hq, tokens_q) + (size_t)part_slots(Hq, tokens_q) * kPartBytes;
 }
 
@@ -579,7 +571,7 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
                         void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!q || !k || !v || !o || !d_o || (!lse && tokens_q > 0) || !d_q || !d_k || !d_v) return STA_ERR_NULL;
-    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > 0x7fffffff || tokens_k > 0x7fffffff) return STA_ERR_SHAPE;
+    if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens || tokens_k > kMostTokens) return STA_ERR_SHAPE;
     if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
     const sta_head_rows *in[5] = {q, k, v, o, d_o}, *out[3] = {d_q, d_k, d_v};
     const int64_t nq = tokens_q, nk = tokens_k, n_in[5] = {nq, nk, nk, nq, nq}, n_out[3] = {nq, nk, nk};
@@ -587,7 +579,7 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
         if (int rc = sta::packed_check(in[i], n_in[i], i == 0 || i == 1 ? 0 : i == 2 ? k->heads : q->heads, D, false)) return rc;
     for (int i = 0; i < 3; ++i)
         if (int rc = sta::packed_check(out[i], n_out[i], i == 0 ? q->heads : k->heads, D, true)) return rc;
-    if (q->heads % k->heads || tokens_q * q->heads > 0x7fffffff) return STA_ERR_SHAPE;
+    if (q->heads % k->heads || tokens_q * q->heads > kMostTokens) return STA_ERR_SHAPE;
     if (S == 0 || (tokens_q == 0 && tokens_k == 0)) return STA_OK;
     if (!cu_q || !cu_k) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
@@ -603,18 +595,20 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     }
     for (int i = 0; i < 5; ++i)
         if (rows_meet(*in[i], 1, n_in[i], D, workspace, used)) return STA_ERR_ALIAS;
+    // (smaller tiles are for launches that tiles of 128 do not fill the chip with)
+    const int64_t g = q->heads / k->heads;
+    if (tiles_of(tokens_q, g, S, max_q, 128) * k->heads > kMostWorkgroups || tiles_of(tokens_k, 1, S, max_k, 128) * k->heads > kMostWorkgroups) return STA_ERR_SHAPE;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     BackwardParams b = {};
     PackedParams &p = b.p;
-    auto rows = [](const sta_head_rows &r) { return PackedRows{static_cast<char *>(r.data), r.token * 2, r.head * 2}; };
-    p.q = rows(*q);
-    p.k = rows(*k);
-    p.v = rows(*v);
-    p.o = rows(*o);
-    b.d_o = rows(*d_o);
-    b.d_q = rows(*d_q);
-    b.d_k = rows(*d_k);
-    b.d_v = rows(*d_v);
+    p.q = packed_rows_of(*q);
+    p.k = packed_rows_of(*k);
+    p.v = packed_rows_of(*v);
+    p.o = packed_rows_of(*o);
+    b.d_o = packed_rows_of(*d_o);
+    b.d_q = packed_rows_of(*d_q);
+    b.d_k = packed_rows_of(*d_k);
+    b.d_v = packed_rows_of(*d_v);
     p.cu_q = cu_q;
     p.cu_k = cu_k;
     p.S = S;
@@ -623,7 +617,7 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     p.max_q = max_q;
     p.max_k = max_k;
     p.Hkv = k->heads;
-    p.g = q->heads / k->heads;
+    p.g = (uint32_t)g;
     p.by_g = sta::fast_div_of(p.g);
     p.by_Hkv = sta::fast_div_of(p.Hkv);
     p.by_parts = sta::fast_div_of(1);
@@ -639,7 +633,6 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const int64_t slots = part_slots(q->heads, tokens_q);
     const hipError_t e = D == 64 ? launch_gradients<64>(b, max_q, max_k, slots, stream) : launch_gradients<128>(b, max_q, max_k, slots, stream);
-    if (e == hipErrorInvalidValue) return STA_ERR_SHAPE;
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
 

@@ -1,0 +1,34 @@
+"""Sizes at which launches of packed sequences end: host side, nothing is launched."""
+import pytest
+
+import paper_2502_04507_amd as sta
+from tests.test_packed_refusals import M, SHAPE, WORKSPACE, backward, forward, rows
+
+S24 = 1 << 24
+
+
+@pytest.mark.parametrize("kw", [
+    dict(S=S24 // 2, max_q=4), dict(S=S24 // 2, max_q=8),                                   # few rows of 2 key heads: a workgroup each
+    dict(S=S24 // 2, max_q=50), dict(S=1 << 30, max_q=1 << 30, max_k=1 << 30),              # tiles
+    dict(S=S24, k=rows(200 * M, 1, 128), v=rows(300 * M, 1, 128), max_q=2),
+    dict(tq=0x7ffff000 // 8 + 1), dict(tk=0x7ffff001, max_k=200),                           # rows of all heads, and keys, that are counted in 32 bits
+])
+def test_forward_refuses_launches_of_2_to_the_24_workgroups(kw):
+    assert forward(**kw) == SHAPE
+
+
+@pytest.mark.parametrize("kw", [dict(S=S24 // 2), dict(S=1 << 30), dict(tq=0x7ffff000 // 8 + 1), dict(tk=0x7ffff001)])
+def test_gradients_refuse_launches_of_2_to_the_24_workgroups(kw):
+    assert backward(nbytes=1 << 40, **kw) == SHAPE
+
+
+def test_bounds_of_tiles_do_not_overflow():
+    # 65,536 heads of one group, as many sequences and as long as 32 bits hold, of one token in all: the products of these pass 64 bits
+    f, most = sta.sta_packed_workspace_bytes, 2 ** 31 - 1
+    assert f(65536, 1, 64, most, 1, most, most) == 0                                        # more workgroups than a launch has
+    assert f(16, 1, 64, 10, 1000, most, 100000) == f(16, 1, 64, 10, 1000, 1000, 100000) > 0  # no sequence is longer than all are together
+    # tokens times heads past 64 bits, and past what a call accepts
+    assert f(most, 1, 64, 1, 2 ** 62, 1, 100) == f(8, 2, 64, 1, 0x7ffff000 // 8 + 1, 100, 100) == 0
+    b = sta.sta_packed_backward_workspace_bytes
+    assert b(most, most - 4096) == b(8, 0x7ffff000 // 8 + 1) == 0 and b(8, 0x7ffff000 // 8) > 0
+    assert forward(tq=1, tk=100000, S=1, max_q=most, max_k=100000, ws=700 * M, nbytes=f(8, 2, 128, 1, 1, most, 100000) - 1) == WORKSPACE
