@@ -840,6 +840,7 @@ int packed_check(const sta_head_rows *r, int64_t tokens, int heads_of, int D, bo
     if (!r) return STA_ERR_NULL;
     sta_head_rows some = *r;
     if (tokens == 0) some.data = reinterpret_cast<void *>(16);              // nothing is there to be read
+    some.batch = 0;                                         // whatever the caller left there
     if (int rc = check_rows(&some, written, 1, tokens > 0 ? tokens : 1, D)) return rc;
     if (r->dtype != STA_BF16) return STA_ERR_UNSUPPORTED;
     if (heads_of && r->heads != heads_of) return STA_ERR_SHAPE;

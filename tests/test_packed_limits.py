@@ -2,7 +2,7 @@
 import pytest
 
 import paper_2502_04507_amd as sta
-from tests.test_packed_refusals import M, SHAPE, WORKSPACE, backward, forward, rows
+from tests.test_packed_refusals import ALIAS, M, SHAPE, WORKSPACE, backward, forward, rows
 
 S24 = 1 << 24
 
@@ -32,3 +32,15 @@ def test_bounds_of_tiles_do_not_overflow():
     b = sta.sta_packed_backward_workspace_bytes
     assert b(most, most - 4096) == b(8, 0x7ffff000 // 8 + 1) == 0 and b(8, 0x7ffff000 // 8) > 0
     assert forward(tq=1, tk=100000, S=1, max_q=most, max_k=100000, ws=700 * M, nbytes=f(8, 2, 128, 1, 1, most, 100000) - 1) == WORKSPACE
+
+
+@pytest.mark.parametrize("batch", [-1, 1 << 41, -(1 << 63)])
+def test_the_batch_stride_is_not_looked_at(batch):
+    q, k, v, o, g = (rows(*a) for a in ((100 * M,), (200 * M, 2, 256), (300 * M, 2, 256), (400 * M,), (450 * M,)))
+    dq, dk, dv = rows(700 * M), rows(800 * M, 2, 256), rows(900 * M, 2, 256)
+    for r in (q, k, v, o, g, dq, dk, dv):
+        r.batch = batch
+    assert forward(q=q, k=k, v=v, o=o, max_q=0) == 0
+    assert backward(q=q, k=k, v=v, o=o, d_o=g, dq=dq, dk=dk, dv=dv, S=0) == 0
+    assert forward(q=q, k=k, v=v, o=q) == ALIAS             # and does not hide what overlaps
+    assert backward(q=q, k=k, v=v, o=o, d_o=g, dq=dq, dk=dk, dv=v) == ALIAS
