@@ -770,6 +770,9 @@ void sta_rows_grid(uint32_t tokens, uint32_t per, uint32_t heads, uint32_t grid[
     grid[0] = g.x; grid[1] = g.y; grid[2] = g.z;
 }
 
+// Nor this: whether the checks of arguments take a and b to overlap.
+int sta_rows_overlap(const sta_head_rows *a, int64_t Na, const sta_head_rows *b, int64_t Nb, int64_t B, int D) { return rows_overlap(*a, Na, *b, Nb, B, D); }
+
 int sta_rope_steps(int channels, double theta, int scaling, double factor, double original_positions, int64_t *steps, float *magnitude)
 {
     if (!steps) return STA_ERR_NULL;

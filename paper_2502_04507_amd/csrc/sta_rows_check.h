@@ -47,19 +47,59 @@ inline uint64_t extent_of(const sta_head_rows &r, int64_t B, int64_t N, int D)
     return (uint64_t)((B - 1) * r.batch + (N - 1) * r.token + (r.heads - 1) * r.head + D) * size_of(r.dtype);
 }
 
-// Whether an element of a may lie in b (not without tokens).  Heads of one fused tensor interleave: same strides, other heads.
+// The rows of a tensor as nested progressions, in bytes: the widest stride first, without those that do not move.
+struct RowSet {
+    int64_t stride[3], count[3], extent[4];         // extent[i]: from the first to behind the last byte of what dimensions i .. span
+    int dims;
+};
+inline RowSet row_set_of(const sta_head_rows &r, int64_t B, int64_t N, int D)
+{
+    const int64_t size = size_of(r.dtype), stride[3] = {r.batch * size, r.token * size, r.head * size}, count[3] = {B, N, r.heads};
+    RowSet s = {};
+    for (int i = 0; i < 3; ++i) {
+        if (count[i] <= 1 || stride[i] == 0) continue;
+        int at = s.dims++;
+        for (; at > 0 && s.stride[at - 1] < stride[i]; --at) {
+            s.stride[at] = s.stride[at - 1];
+            s.count[at] = s.count[at - 1];
+        }
+        s.stride[at] = stride[i];
+        s.count[at] = count[i];
+    }
+    s.extent[s.dims] = D * size;
+    for (int i = s.dims - 1; i >= 0; --i) s.extent[i] = s.extent[i + 1] + (s.count[i] - 1) * s.stride[i];
+    return s;
+}
+inline int64_t floor_div(int64_t x, int64_t d) { return x / d - (x % d < 0); }
+
+// Whether dimensions i .. of a and j .. of b, which begins `off` bytes behind a, share a byte.  The wider stride is taken apart (where both have it, only
+// the difference of the two indices counts), and of its indices those alone are followed whose spans meet: one or two for tensors side by side in one
+// allocation.  The answer is exact unless `visits` run out, and then it is yes.
+inline bool sets_overlap(const RowSet &a, int i, const RowSet &b, int j, int64_t off, int *visits)
+{
+    if (off >= a.extent[i] || off + b.extent[j] <= 0) return false;
+    if (i == a.dims && j == b.dims) return true;
+    if (--*visits < 0) return true;
+    const int64_t sa = i < a.dims ? a.stride[i] : 0, sb = j < b.dims ? b.stride[j] : 0, s = sa > sb ? sa : sb;
+    const int ni = i + (sa == s), nj = j + (sb == s);
+    // what is left of b begins at off + m s, and has to begin above -extent[nj] and below extent[ni]
+    int64_t lo = floor_div(-b.extent[nj] - off, s) + 1, hi = -floor_div(off - a.extent[ni], s) - 1;
+    const int64_t least = sa == s ? -(a.count[i] - 1) : 0, most = sb == s ? b.count[j] - 1 : 0;
+    lo = lo > least ? lo : least;
+    hi = hi < most ? hi : most;
+    for (int64_t m = lo; m <= hi; ++m)
+        if (sets_overlap(a, ni, b, nj, off + m * s, visits)) return true;
+    return false;
+}
+
+// Whether a byte of a lies in b (not without tokens).
 inline bool rows_overlap(const sta_head_rows &a, int64_t Na, const sta_head_rows &b, int64_t Nb, int64_t B, int D)
 {
     if (Na <= 0 || Nb <= 0 || B <= 0) return false;
     const uintptr_t a0 = (uintptr_t)a.data, b0 = (uintptr_t)b.data;
     if (a0 + extent_of(a, B, Na, D) <= b0 || b0 + extent_of(b, B, Nb, D) <= a0) return false;
-    if (a.dtype != b.dtype || a.token != b.token || a.token <= 0) return true;
-    if (B > 1 && (a.batch != b.batch || a.batch % a.token)) return true;
-    const int64_t size = size_of(a.dtype), period = a.token * size;
-    const int64_t wide_a = ((a.heads - 1) * a.head + D) * size, wide_b = ((b.heads - 1) * b.head + D) * size;
-    if (wide_a > period || wide_b > period) return true;
-    const int64_t off = (int64_t)(((int64_t)(b0 - a0) % period + period) % period);        // where b's rows of a token begin
-    return off < wide_a || off + wide_b > period;
+    int visits = 512;
+    return sets_overlap(row_set_of(a, B, Na, D), 0, row_set_of(b, B, Nb, D), 0, (int64_t)(b0 - a0), &visits);
 }
 inline bool rows_overlap(const sta_head_rows &a, const sta_head_rows &b, int B, int N, int D) { return rows_overlap(a, N, b, N, B, D); }
 

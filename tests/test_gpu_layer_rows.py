@@ -322,3 +322,41 @@ def test_rows_of_more_than_2_to_the_24_workgroups():
         sta.sta_rope(rows, a, rotary)
         sta.sta_qk_norm_rope(rows, rows, None, b, c, None, w, None, rotary)
         assert torch.equal(turned[:, at], a) and torch.equal(normed[:, at], b) and torch.equal(other[:, at], c), at
+
+
+@pytest.mark.parametrize("N", [33, 900])
+@pytest.mark.parametrize("layout", ["head-major", "cache", "token-major"])
+def test_outputs_side_by_side_in_one_tensor(layout, N):
+    """Queries, keys and values of two batch entries as views of one allocation, whose spans meet though no element does."""
+    B, Hq, Hkv, D = 2, 4, 2, 64
+    heads, slots = [Hq, Hkv, Hkv], N + 7
+    qkv, w = make((B, N, sum(heads), D), 3, torch.bfloat16).to(DEV), [make((D,), 4 + i, torch.float32).to(DEV) for i in range(2)]
+    ins = qkv.split(heads, 2)
+    rotary, _ = rotary_of(D, (D // 2,), False, N)
+    want = [torch.empty((B, N, h, D), dtype=torch.bfloat16, device=DEV) for h in heads]
+    sta.sta_qk_norm_rope(*ins, *want, *w, rotary)
+    if layout == "head-major":
+        room = torch.full((B, sum(heads), N, D), 7.0, dtype=torch.bfloat16, device=DEV)
+        outs = room.transpose(1, 2).split(heads, 2)
+    elif layout == "cache":
+        room = torch.full((B, 2, Hkv, slots, D), 7.0, dtype=torch.bfloat16, device=DEV)
+        outs = [torch.empty_like(want[0])] + [room[:, i, :, :N].transpose(1, 2) for i in range(2)]
+    else:
+        room = torch.full((B, N * sum(heads) * D + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+        outs = room[:, :-8].unflatten(1, (N, sum(heads), D)).split(heads, 2)
+    sta.sta_qk_norm_rope(*ins, *outs, *w, rotary)
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    if layout == "cache":
+        assert bool((room[:, :, :, N:] == 7.0).all())
+    if layout == "token-major":
+        assert bool((room[:, -8:] == 7.0).all())
+    turned = [torch.empty_like(x) for x in want[:2]]
+    sta.sta_rope(want[:2], turned, rotary)
+    sta.sta_rope(outs[:2], outs[:2], rotary)                # in place, next to each other
+    assert all(torch.equal(a, b) for a, b in zip(outs[:2], turned)) and torch.equal(outs[2], want[2])
+    grads = [make((B, N, h, D), 9 + i, torch.bfloat16).to(DEV) for i, h in enumerate(heads)]
+    d_want = [torch.empty_like(x) for x in want]
+    d_outs = torch.empty((B, sum(heads), N, D), dtype=torch.bfloat16, device=DEV).transpose(1, 2).split(heads, 2)
+    for d in (d_want, d_outs):
+        sta.sta_qk_norm_rope_backward(ins[0], ins[1], *grads, *d, *w, None, None, rotary, None)
+    assert all(torch.equal(a, b) for a, b in zip(d_outs, d_want))
