@@ -24,8 +24,6 @@
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
-
 // Running softmax of a wave's columns: offsets in the units of the scores, sums, accumulators [channel block][column block] of O^T.
 template <int D, int NC, bool LSE>
 struct Softmax {
@@ -258,14 +256,18 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
     }
 }
 
-// ln of the denominator of a row whose offset is m (base-2 units) and whose sum is l: -infinity where no key was seen, which leaves the sum at 0.  NaN
+// ln of the denominator of a row whose offset is m (in scores) and whose sum is l: -infinity where no key was seen, which leaves the sum at 0.  NaN
 // stays NaN; the bits are looked at, because the kernels are compiled as if comparisons met none.
-__device__ __forceinline__ float lse_of(float m, float l)
+__device__ __forceinline__ float lse_of(float m, float l, const PackedParams &p)
 {
     uint32_t bits = __float_as_uint(l);
     asm volatile("" : "+v"(bits));
-    return bits == 0 ? -INFINITY : m * kLn2 + __logf(l);
+    return bits == 0 ? -INFINITY : fmaf(m, p.scale, __logf(l));
 }
+
+// What a part of a row whose offset is `own` counts where the row's is m.  Offsets are compared as scores: their products with the scale, in units of
+// two to the one, may pass the largest number where they do not, and the smallest of those would be a part that has seen no key.
+__device__ __forceinline__ float weight_of(float own, float m, float c) { return own == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((own - m) * c); }
 
 // Where a column's row lies.
 struct RowAt {
@@ -300,7 +302,7 @@ __device__ __forceinline__ void limits_of(const PackedParams &p, const PackedSeq
     for (int col = 0; col < NC; ++col) lim[col] = seq.keys_of(row_at(row0 + 16 * col + (lane & 15), rows, p).token, p);
 }
 
-// Partial sums of a tile's part: accumulators [R][D], then offsets (base-2 units) and sums of the rows.
+// Partial sums of a tile's part: accumulators [R][D], then offsets (in scores) and sums of the rows.
 template <int D, int R>
 constexpr size_t part_floats() { return (size_t)R * D + 2 * R; }
 
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     constexpr int SUB = LK::Tile + LV::Tile, STAGE = U * SUB, V_AT = LK::Tile, PER_WAVE = LV::Groups / RW;
     constexpr int WAVE_ACC = CB * NC * 1024, MERGE = KG > 1 ? RW * KG * WAVE_ACC : 0;
     __shared__ __attribute__((aligned(1024))) char smem[2 * KG * STAGE > MERGE ? 2 * KG * STAGE : MERGE];
-    __shared__ float2 stats[KG > 1 ? KG : 1][TILE];         // offset (base-2 units) and sum of a group's rows
+    __shared__ float2 stats[KG > 1 ? KG : 1][TILE];         // offset (in scores) and sum of a group's rows
     const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int kg = all_waves / RW, wave = all_waves % RW;
     // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
@@ -471,10 +473,10 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     }
 
     // ---- the groups' sums are joined: a wave takes its rows' channel blocks of its group's share, the groups' parts in ascending order
-    float m[NC], l[NC];                                     // base-2 units
+    float m[NC], l[NC];
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
-        m[col] = st.m[col] * c;
+        m[col] = st.m[col];
         l[col] = st.sum(col);
     }
     constexpr int OWN = CB / KG;                            // channel blocks that a wave writes
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
 #pragma unroll
             for (int g = 0; g < KG; ++g) {
                 const float2 x = stats[g][32 * wave + 16 * col + c16];
-                weight[g] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m[col]);
+                weight[g] = weight_of(x.x, m[col], c);
                 l[col] += x.y * weight[g];
             }
 #pragma unroll
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
             for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(st.acc[j][col][r] * inv);
             *reinterpret_cast<bf16x4 *>(row + 32 * (cb0 + j) + 8 * last_g4) = v;
         }
-        if (LSE && p.lse && last_g4 == 0 && kg == 0) p.lse[head * p.tokens_q + token] = lse_of(m[col], l[col]);
+        if (LSE && p.lse && last_g4 == 0 && kg == 0) p.lse[head * p.tokens_q + token] = lse_of(m[col], l[col], p);
     }
 }
 
@@ -642,7 +644,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
         const float l = st.sum(col);
-        if (g4 == 0) stats[wave][16 * col + c16] = make_float2(st.m[col] * c, l);
+        if (g4 == 0) stats[wave][16 * col + c16] = make_float2(st.m[col], l);
     }
     __syncthreads();
     const bool whole = parts_of(n_all, p) <= 1;
@@ -655,7 +657,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float2 x = stats[w][16 * col + c16];
-            weight[w] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+            weight[w] = weight_of(x.x, m, c);
             l += x.y * weight[w];
         }
         const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
@@ -686,7 +688,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
                 ws[(size_t)R * D + 16 * col + c16] = m;
                 ws[(size_t)R * D + R + 16 * col + c16] = l;
             } else if (LSE && p.lse) {
-                p.lse[head * p.tokens_q + token] = lse_of(m, l);
+                p.lse[head * p.tokens_q + token] = lse_of(m, l, p);
             }
         }
     }
@@ -722,7 +724,7 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
     floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < n; ++j) {
         const float *part = ws + j * floats;
-        const float mj = part[(size_t)R * D + r], w = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - m);
+        const float w = weight_of(part[(size_t)R * D + r], m, p.scale_log2e);
         l = fmaf(part[(size_t)R * D + R + r], w, l);
         const floatx4 x = *reinterpret_cast<const floatx4 *>(part + (size_t)r * D + ch);
 #pragma unroll
@@ -735,7 +737,7 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(PackedParams p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>(sum[i] * inv);
     *reinterpret_cast<bf16x4 *>(p.o.data + token * p.o.token + head * p.o.head + 2 * ch) = v;
-    if (p.lse && ch == 0) p.lse[head * p.tokens_q + token] = lse_of(m, l);
+    if (p.lse && ch == 0) p.lse[head * p.tokens_q + token] = lse_of(m, l, p);
 }
 
 }  // namespace

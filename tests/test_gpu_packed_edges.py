@@ -135,3 +135,28 @@ def test_rows_within_bounds_that_are_too_low_are_written(D):
     for a, n in zip(starts(lq), lq):
         n = min(n, 60)
         assert float((o[a:a + n].float() - right[a:a + n].float()).abs().max()) < 2e-2
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("with_lse", [False, True])
+@pytest.mark.parametrize("case", LSE, ids=[str(i) for i in range(len(LSE))])
+def test_rows_whose_keys_all_have_the_lowest_or_largest_score(case, with_lse, sign, D):
+    """Scores that a scale of 1 leaves finite, and whose products with log2(e) are not: all keys that a row sees count alike."""
+    Hq, Hkv, lq, lk, parts = case
+    g, most = Hq // Hkv, sign * torch.finfo(BF).max
+    q, k, v = torch.zeros((sum(lq), Hq, D), dtype=BF), randn((sum(lk), Hkv, D), 2), randn((sum(lk), Hkv, D), 3)
+    q[..., 0], k[..., 0] = 1.0, most
+    o, lse = torch.full_like(q, 7.0, device=DEV), torch.full((Hq, sum(lq)), 7.0, device=DEV) if with_lse else None
+    n = sta.sta_packed_workspace_bytes(Hq, Hkv, D, len(lq), sum(lq), max(lq), max(lk))
+    sta.sta_packed_forward(q.to(DEV), k.to(DEV), v.to(DEV), o, ints(starts(lq)), ints(starts(lk)), max(lq), max(lk), scale=1.0, lse=lse,
+                           workspace=torch.empty(n, dtype=torch.uint8, device=DEV) if parts else None)
+    for s in range(len(lq)):
+        a, b = starts(lq)[s], starts(lk)[s]
+        seen = lk[s] - lq[s] + 1 + torch.arange(lq[s])
+        V = v[b:b + lk[s]].double()
+        want = (V.cumsum(0)[seen - 1] / seen[:, None, None]).repeat_interleave(g, 1)
+        size = (V.abs().cumsum(0)[seen - 1] / seen[:, None, None]).repeat_interleave(g, 1)
+        close(o[a:a + lq[s]], want, (2.0 ** -7 + 2.0 ** -11) * size, "sequence %d" % s, norm=False)
+    if with_lse:
+        assert bool((lse == most).all())                    # ln of how many is far below the spacing there
