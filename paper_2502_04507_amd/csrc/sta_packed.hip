@@ -24,6 +24,10 @@
 
 namespace {
 
+// By how much a score has to exceed a row's offset for the offset to move: 2^8 in the exponent.  Finite where the scale is next to nothing: an offset
+// that no score was compared with is -infinity, and stays so only where no key is seen.
+__device__ __forceinline__ float grow_above_of(float c) { return fminf(8.0f / c, 3.4028234663852886e38f); }
+
 // Running softmax of a wave's columns: offsets in the units of the scores, sums, accumulators [channel block][column block] of O^T.
 template <int D, int NC, bool LSE>
 struct Softmax {
@@ -166,7 +170,7 @@ __device__ __forceinline__ void softmax_sub_blocks(Softmax<D, NC, LSE> &st, uint
         }
     });
     if constexpr (MODE != kFixed) {
-        // The offset only moves when a score exceeds it by more than 2^8 in the exponent.
+        // The offset only moves when a score exceeds it by more than grow_above.
         float mx[NC];
         bool grown = false;
 #pragma unroll
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     uint32_t v_addr[4];
     LV::transposed_addresses(base + V_AT, lane, v_addr);
     Softmax<D, NC, LSE> st;
-    const float c = p.scale_log2e, grow_above = 8.0f / c;
+    const float c = p.scale_log2e, grow_above = grow_above_of(c);
     int lim[NC] = {};                                       // found where the tail begins
     auto step = [&](auto stage_c, auto mode_c, int i) __attribute__((always_inline)) {
         constexpr int ST = decltype(stage_c)::value, MODE = decltype(mode_c)::value;
@@ -600,7 +604,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(PackedParams p)
     LV::transposed_addresses(base + V_AT, lane, v_addr);
     Softmax<D, NC, LSE> st;
     st.start();
-    const float c = p.scale_log2e, grow_above = 8.0f / c;
+    const float c = p.scale_log2e, grow_above = grow_above_of(c);
     auto step = [&](auto stage_c, auto masked_c, int sub) __attribute__((always_inline)) {
         constexpr int ST = decltype(stage_c)::value;
         __builtin_amdgcn_sched_barrier(0);                  // reads of the other stage are done: their values have been used

@@ -160,3 +160,26 @@ def test_rows_whose_keys_all_have_the_lowest_or_largest_score(case, with_lse, si
         close(o[a:a + lq[s]], want, (2.0 ** -7 + 2.0 ** -11) * size, "sequence %d" % s, norm=False)
     if with_lse:
         assert bool((lse == most).all())                    # ln of how many is far below the spacing there
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("with_lse", [False, True])
+@pytest.mark.parametrize("case", LSE, ids=[str(i) for i in range(len(LSE))])
+def test_a_scale_next_to_nothing(case, with_lse, D):
+    """Every key that a row sees counts alike."""
+    Hq, Hkv, lq, lk, parts = case
+    q, k, v = randn((sum(lq), Hq, D), 1), randn((sum(lk), Hkv, D), 2), randn((sum(lk), Hkv, D), 3)
+    o, lse = torch.full_like(q, 7.0, device=DEV), torch.full((Hq, sum(lq)), 7.0, device=DEV) if with_lse else None
+    n = sta.sta_packed_workspace_bytes(Hq, Hkv, D, len(lq), sum(lq), max(lq), max(lk))
+    sta.sta_packed_forward(q.to(DEV), k.to(DEV), v.to(DEV), o, ints(starts(lq)), ints(starts(lk)), max(lq), max(lk), scale=1e-38, lse=lse,
+                           workspace=torch.empty(n, dtype=torch.uint8, device=DEV) if parts else None)
+    for s in range(len(lq)):
+        a, b = starts(lq)[s], starts(lk)[s]
+        seen = lk[s] - lq[s] + 1 + torch.arange(lq[s])
+        V = v[b:b + lk[s]].double()
+        want = (V.cumsum(0)[seen - 1] / seen[:, None, None]).repeat_interleave(Hq // Hkv, 1)
+        size = (V.abs().cumsum(0)[seen - 1] / seen[:, None, None]).repeat_interleave(Hq // Hkv, 1)
+        close(o[a:a + lq[s]], want, (2.0 ** -7 + 2.0 ** -11) * size, "sequence %d" % s, norm=False)
+        if with_lse:
+            off = (lse[:, a:a + lq[s]].cpu().double() - torch.log(seen.double())).abs()
+            assert bool((off <= 2.0 ** -20 * (1 + torch.log(seen.double())) + lk[s] * 2.0 ** -24).all())
