@@ -378,7 +378,7 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
  * all), else all.  A row that sees no key: o = 0, lse = -infinity.  A length may be 0.  Query tokens that no sequence has keep what o
  * and lse hold.  Keys that a row does not see take no part in it, whatever they hold, infinities and NaN in V included.
  * lse: NULL, or device float32 [Hq, tokens_q], ln of each row's softmax denominator; NaN, as o, where the row meets NaN in q or in keys that it sees.
- * scale <= 0 selects 1 / sqrt(D).
+ * scale <= 0 selects 1 / sqrt(D); NaN and more than 2^100 are STA_ERR_UNSUPPORTED.
  * Arithmetic as sta_forward (with lse, the sum is taken before the probabilities are rounded).
  * workspace: as sta_forward, of at least sta_packed_workspace_bytes(...) bytes: launches that would not fill the chip are cut along the keys.
  * NULL: no parts.  Results are repeatable bit for bit.
@@ -394,9 +394,10 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
 
 /*
  * Gradients of sta_packed_forward (of all keys: no k_used), o and lse as it returned them for the same q, k, v, bounds, causal and scale.
- * d_q: like q; d_k, d_v: like k and v, summed over the query heads of a group.  Written for every token of a sequence (0 where no
- * row saw it; of a sequence longer than max_q the query tokens beyond it are no rows here, and keys beyond max_k may stay unwritten).  P is recomputed from the scores and lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are
- * rounded once.  No atomics: repeated calls give identical bits.
+ * d_q: like q; d_k, d_v: like k and v, summed over the query heads of a group.  Written for every token of a sequence (0 where no row saw it); of a
+ * sequence longer than max_q the query tokens beyond it are no rows here, and keys beyond max_k may stay unwritten.  P is recomputed from the scores and
+ * lse in fp32, P and dS are rounded to bf16 for the matrix products, sums are fp32, results are rounded once.  No atomics: repeated calls give identical
+ * bits.  A scale between 0 and 2^-100, by which lse could not be divided, is STA_ERR_UNSUPPORTED.
  * Infinities and NaN in q, k, v or d_o make NaN of gradients in their own sequence and key head, also of pairs that are not seen (0 times them is
  * a term of the sums), and of no others.
  * workspace: device, 16-byte aligned, at least sta_packed_backward_workspace_bytes(Hq, tokens_q) bytes (the rows' statistics, and from 8192 rows on room for

@@ -6,6 +6,7 @@
 // never shrink.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "../../include/sta.h"
@@ -28,6 +29,16 @@ struct PackedRows {
     int64_t token, head;
 };
 inline PackedRows packed_rows_of(const sta_head_rows &r) { return {static_cast<char *>(r.data), r.token * 2, r.head * 2}; }
+
+// The scale that is meant by the caller's: 1 / sqrt(D) where that is 0 or negative.  False: NaN, or more than 2^100, or (gradients, which divide by it)
+// less than 2^-100.  By the bits: comparisons are compiled as if there were no NaN.
+inline bool scale_of(float given, int D, bool gradients, float *scale)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, given), size = bits & 0x7fffffffu;
+    if (size > 0x7f800000u) return false;
+    *scale = size == 0 || bits != size ? 1.0f / sqrtf((float)D) : given;
+    return *scale <= 0x1p100f && !(gradients && *scale < 0x1p-100f);
+}
 
 // Tokens of a tensor, and rows of all query heads: the kernels count keys and rows in int, up to a few hundred beyond the last one.
 constexpr int64_t kMostTokens = 0x7ffff000;

@@ -871,7 +871,7 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
 {
     if (!q || !k || !v || !o) return STA_ERR_NULL;
     if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens || tokens_k > kMostTokens) return STA_ERR_SHAPE;
-    if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
+    if ((D != 64 && D != 128) || !scale_of(scale, D, false, &scale)) return STA_ERR_UNSUPPORTED;
     if (int rc = sta::packed_check(q, tokens_q, 0, D, false)) return rc;
     if (int rc = sta::packed_check(k, tokens_k, 0, D, false)) return rc;
     if (int rc = sta::packed_check(v, tokens_k, k->heads, D, false)) return rc;
@@ -894,7 +894,6 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
     for (const auto &t : tensors)
         if (rows_meet(*t.r, 1, t.n, D, lse, lse_bytes)) return STA_ERR_ALIAS;
     if (ranges_meet(lse, lse_bytes, workspace, workspace_bytes)) return STA_ERR_ALIAS;
-    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     PackedParams p = {};
     p.q = packed_rows_of(*q);
     p.k = packed_rows_of(*k);

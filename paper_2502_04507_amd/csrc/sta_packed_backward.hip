@@ -572,7 +572,7 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
 {
     if (!q || !k || !v || !o || !d_o || (!lse && tokens_q > 0) || !d_q || !d_k || !d_v) return STA_ERR_NULL;
     if (S < 0 || tokens_q < 0 || tokens_k < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens || tokens_k > kMostTokens) return STA_ERR_SHAPE;
-    if (D != 64 && D != 128) return STA_ERR_UNSUPPORTED;
+    if ((D != 64 && D != 128) || !scale_of(scale, D, true, &scale)) return STA_ERR_UNSUPPORTED;
     const sta_head_rows *in[5] = {q, k, v, o, d_o}, *out[3] = {d_q, d_k, d_v};
     const int64_t nq = tokens_q, nk = tokens_k, n_in[5] = {nq, nk, nk, nq, nq}, n_out[3] = {nq, nk, nk};
     for (int i = 0; i < 5; ++i)
@@ -598,7 +598,6 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     // (smaller tiles are for launches that tiles of 128 do not fill the chip with)
     const int64_t g = q->heads / k->heads;
     if (tiles_of(tokens_q, g, S, max_q, 128) * k->heads > kMostWorkgroups || tiles_of(tokens_k, 1, S, max_k, 128) * k->heads > kMostWorkgroups) return STA_ERR_SHAPE;
-    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     BackwardParams b = {};
     PackedParams &p = b.p;
     p.q = packed_rows_of(*q);

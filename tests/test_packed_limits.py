@@ -2,9 +2,21 @@
 import pytest
 
 import paper_2502_04507_amd as sta
-from tests.test_packed_refusals import ALIAS, M, SHAPE, WORKSPACE, backward, forward, rows
+from paper_2502_04507_amd import layer_ops as lo
+from tests import test_packed_refusals as refusals
+from tests.test_packed_refusals import ALIAS, M, OK, SHAPE, UNSUPPORTED, WORKSPACE, forward, rows
 
 S24 = 1 << 24
+
+
+def backward(scale=0.0, **kw):
+    if scale == 0.0:
+        return refusals.backward(**kw)
+    a = dict(S=3, tq=100, tk=300)
+    a.update(kw)
+    keys = [rows(x * M, 2, 256) for x in (200, 300, 800, 900)]
+    return lo._lib().sta_packed_backward(rows(100 * M), keys[0], keys[1], rows(400 * M), rows(450 * M), 600 * M, rows(700 * M), keys[2], keys[3], a["tq"], a["tk"],
+                                         500 * M, 501 * M, a["S"], 50, 200, 128, 1, scale, 1000 * M, 1 << 40, None)
 
 
 @pytest.mark.parametrize("kw", [
@@ -44,3 +56,15 @@ def test_the_batch_stride_is_not_looked_at(batch):
     assert backward(q=q, k=k, v=v, o=o, d_o=g, dq=dq, dk=dk, dv=dv, S=0) == 0
     assert forward(q=q, k=k, v=v, o=q) == ALIAS             # and does not hide what overlaps
     assert backward(q=q, k=k, v=v, o=o, d_o=g, dq=dq, dk=dk, dv=v) == ALIAS
+
+
+@pytest.mark.parametrize("scale", [float("nan"), -float("nan"), float("inf"), 2.0 ** 101, 3.0e38])
+def test_scales_that_are_no_numbers_or_too_large_are_refused(scale):
+    assert forward(scale=scale, max_q=0) == UNSUPPORTED and backward(scale=scale, S=0) == UNSUPPORTED
+
+
+def test_scales_at_the_ends():
+    for scale in (0.0, -0.0, -1.0, -float("inf"), 2.0 ** 100, 2.0 ** -100, 1.0):
+        assert forward(scale=scale, max_q=0) == OK and backward(scale=scale, S=0) == OK
+    for scale in (2.0 ** -101, 1e-38, 1e-44):                # gradients divide by it
+        assert forward(scale=scale, max_q=0) == OK and backward(scale=scale, S=0) == UNSUPPORTED
