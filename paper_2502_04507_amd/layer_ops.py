@@ -3,6 +3,7 @@ sequences.  Same names as the C entry points of libsta.so; tensors are torch ten
 given by the caller, the stream is torch's current HIP stream unless one is given.
 """
 import ctypes
+import operator
 
 import torch
 
@@ -10,6 +11,14 @@ from .binding import STA_BF16, STA_F32, StaError, _check, _dev, _fast, _i3, _str
 
 STA_ROPE_NONE, STA_ROPE_LINEAR, STA_ROPE_NTK, STA_ROPE_YARN = 0, 1, 2, 3
 _DTYPES = {torch.bfloat16: STA_BF16, torch.float32: STA_F32}
+
+
+def _int32(x, name):
+    """x as the library's int: ctypes would drop the upper bits."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError("%s does not fit 32 bits" % name)
+    return x
 
 
 class _HeadRows(ctypes.Structure):
@@ -59,7 +68,7 @@ class StaRotary:
     def __init__(self, steps, positions=None, pairs=None, interleaved=False, magnitude=1.0):
         if steps.dtype != torch.int64 or steps.dim() != 1:
             raise ValueError("steps must be int64 [channels / 2]")
-        pairs = [int(n) for n in ((steps.numel(),) if pairs is None else pairs)]
+        pairs = [_int32(n, "pairs") for n in ((steps.numel(),) if pairs is None else pairs)]
         if not 1 <= len(pairs) <= 3 or min(pairs) < 0 or sum(pairs) != steps.numel():
             raise ValueError("pairs must have one to three entries that sum to the number of steps")
         axes = 3 if any(pairs[1:]) else 1
@@ -98,18 +107,25 @@ class StaRotary:
 
 def sta_rope_steps(channels, theta=10000.0, scaling=STA_ROPE_NONE, factor=1.0, original_positions=4096):
     """Turns per position of every pair in units of 2^-64 (host int64 tensor [channels / 2]) and the magnitude."""
-    channels = int(channels)
+    channels = _int32(channels, "channels")
     if channels < 2:
         _check(2)
     steps, magnitude = torch.empty(channels // 2, dtype=torch.int64), ctypes.c_float(1.0)
-    _check(_lib().sta_rope_steps(channels, float(theta), int(scaling), float(factor), float(original_positions), steps.data_ptr(),
+    _check(_lib().sta_rope_steps(channels, float(theta), _int32(scaling, "scaling"), float(factor), float(original_positions), steps.data_ptr(),
                                  ctypes.byref(magnitude)))
     return steps, float(magnitude.value)
+
+
+def _sizes(t):
+    """B, N and D of the first [B, N, H, D] tensor."""
+    B, N, _, D = t.shape
+    return _int32(B, "the batch"), _int32(N, "the number of tokens"), _int32(D, "the number of channels")
 
 
 def _rows(t, name, B, N, D):
     """One [B, N, H, D] tensor, its channels adjacent."""
     shape = t.shape
+    _int32(shape[2] if len(shape) == 4 else 0, "the number of heads")
     if len(shape) != 4 or shape[0] != B or shape[1] != N or shape[3] != D:
         raise ValueError("%s must be [B, N, H, D] like the others" % name)
     dtype = _DTYPES.get(t.dtype)
@@ -138,7 +154,7 @@ def sta_rope(xs, outs, rotary, inverse=False, stream=None):
         raise ValueError("expect one to three tensors and as many outputs")
     if xs[0].dim() != 4:
         raise ValueError("expect [B, N, H, D] tensors")
-    B, N, _, D = xs[0].shape
+    B, N, D = _sizes(xs[0])
     a = (_HeadRows * n)(*[_rows(t, "input", B, N, D) for t in xs])
     b = (_HeadRows * n)(*[_rows(t, "output", B, N, D) for t in outs])
     _check(_lib().sta_rope(a, b, n, B, N, D, rotary._struct(B, N), int(bool(inverse)), _stream_ptr(stream)))
@@ -179,7 +195,7 @@ def sta_qk_norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight, rotary, e
         raise ValueError("expect [B, N, H, D] tensors")
     if (v is None) != (v_out is None):
         raise ValueError("v and v_out go together")
-    B, N, _, D = q.shape
+    B, N, D = _sizes(q)
     rows = [None if t is None else _rows(t, name, B, N, D) for t, name in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out"), (k_out, "k_out"), (v_out, "v_out"))]
     (wq, wk), dtype = _weights((q_weight, k_weight), D)
     g, t = _grid_tile(grid, tile)
@@ -189,7 +205,7 @@ def sta_qk_norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight, rotary, e
 
 
 def sta_qk_norm_rope_workspace_bytes(D) -> int:
-    return int(_lib().sta_qk_norm_rope_workspace_bytes(int(D)))
+    return int(_lib().sta_qk_norm_rope_workspace_bytes(_int32(D, "D")))
 
 
 def sta_qk_norm_rope_backward(q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_weight, k_weight, d_q_weight, d_k_weight, rotary, workspace,
@@ -206,7 +222,7 @@ def sta_qk_norm_rope_backward(q, k, d_q_out, d_k_out, d_v_out, d_q, d_k, d_v, q_
         raise ValueError("expect [B, N, H, D] tensors")
     if (d_v is None) != (d_v_out is None):
         raise ValueError("d_v and d_v_out go together")
-    B, N, _, D = q.shape
+    B, N, D = _sizes(q)
     rows = [None if t is None else _rows(t, name, B, N, D) for t, name in
             ((q, "q"), (k, "k"), (d_q_out, "d_q_out"), (d_k_out, "d_k_out"), (d_v_out, "d_v_out"), (d_q, "d_q"), (d_k, "d_k"), (d_v, "d_v"))]
     (wq, wk), dtype = _weights((q_weight, k_weight), D)
@@ -247,7 +263,14 @@ def _packed_shapes(q, k):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("expect [tokens, heads, D] tensors")
     (tq, Hq, D), (tk, Hkv, _) = q.shape, k.shape
-    return tq, Hq, D, tk, Hkv
+    return tq, _int32(Hq, "the number of heads"), _int32(D, "the number of channels"), tk, _int32(Hkv, "the number of heads")
+
+
+def _packed_counts(cu_q, max_q, max_k):
+    S = _int32(cu_q.numel() - 1, "the number of sequences")
+    if S < 0:
+        raise ValueError("cu_q needs an entry more than there are sequences")
+    return S, _int32(operator.index(max_q), "max_q"), _int32(operator.index(max_k), "max_k")
 
 
 def _lse_ptr(lse, Hq, tq):
@@ -259,7 +282,8 @@ def _lse_ptr(lse, Hq, tq):
 
 
 def sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k) -> int:
-    return int(_lib().sta_packed_workspace_bytes(int(Hq), int(Hkv), int(D), int(S), int(tokens_q), int(max_q), int(max_k)))
+    sizes = [_int32(x, name) for x, name in ((Hq, "Hq"), (Hkv, "Hkv"), (D, "D"), (S, "S"))]
+    return int(_lib().sta_packed_workspace_bytes(*sizes, int(tokens_q), _int32(max_q, "max_q"), _int32(max_k, "max_k")))
 
 
 def sta_packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal=True, scale=0.0, lse=None, k_used=None, workspace=None, stream=None):
@@ -271,9 +295,7 @@ def sta_packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal=True, scale=
             _check(status)
             return o
     tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
-    S = cu_q.numel() - 1
-    if S < 0:
-        raise ValueError("cu_q needs an entry more than there are sequences")
+    S, max_q, max_k = _packed_counts(cu_q, max_q, max_k)
     ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
     _check(_lib().sta_packed_forward(_packed_rows(q, "q", tq, Hq, D), _packed_rows(k, "k", tk, Hkv, D), _packed_rows(v, "v", tk, Hkv, D),
                                      _packed_rows(o, "o", tq, Hq, D), _lse_ptr(lse, Hq, tq), tq, tk, _bounds(cu_q, "cu_q", S + 1),
@@ -283,7 +305,7 @@ def sta_packed_forward(q, k, v, o, cu_q, cu_k, max_q, max_k, causal=True, scale=
 
 
 def sta_packed_backward_workspace_bytes(Hq, tokens_q) -> int:
-    return int(_lib().sta_packed_backward_workspace_bytes(int(Hq), int(tokens_q)))
+    return int(_lib().sta_packed_backward_workspace_bytes(_int32(Hq, "Hq"), int(tokens_q)))
 
 
 def sta_packed_backward(q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, max_k, workspace, causal=True, scale=0.0, stream=None):
@@ -294,9 +316,7 @@ def sta_packed_backward(q, k, v, o, d_o, lse, d_q, d_k, d_v, cu_q, cu_k, max_q, 
             _check(status)
             return d_q, d_k, d_v
     tq, Hq, D, tk, Hkv = _packed_shapes(q, k)
-    S = cu_q.numel() - 1
-    if S < 0:
-        raise ValueError("cu_q needs an entry more than there are sequences")
+    S, max_q, max_k = _packed_counts(cu_q, max_q, max_k)
     if lse is None:
         raise ValueError("lse is needed")
     _check(_lib().sta_packed_backward(_packed_rows(q, "q", tq, Hq, D), _packed_rows(k, "k", tk, Hkv, D), _packed_rows(v, "v", tk, Hkv, D),
