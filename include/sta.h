@@ -383,8 +383,8 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
  * workspace: as sta_forward, of at least sta_packed_workspace_bytes(...) bytes: launches that would not fill the chip are cut along the keys.
  * NULL: no parts.  Results are repeatable bit for bit.
  * Supported: D in {64, 128}; rows at multiples of 16 bytes; tokens_k and tokens_q * Hq up to 2^31 - 4096; fewer than 2^24 workgroups, of which every key
- * head has one a sequence where max_q * g <= 32, else one for up to 128 rows (token and head of the group) of a sequence (else STA_ERR_SHAPE).  o must not
- * overlap what is read.  Tensors without tokens may have no data.
+ * head has one a sequence where max_q * g <= 32, else one for up to 128 rows (token and head of the group) of a sequence (else STA_ERR_SHAPE).  o, lse
+ * and the workspace must not overlap what is read, cu_q, cu_k and k_used included.  Tensors without tokens may have no data.
  */
 size_t sta_packed_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k);
 int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta_head_rows *v, const sta_head_rows *o, float *lse,

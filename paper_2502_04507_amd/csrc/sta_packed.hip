@@ -894,6 +894,8 @@ int sta_packed_forward(const sta_head_rows *q, const sta_head_rows *k, const sta
     for (const auto &t : tensors)
         if (rows_meet(*t.r, 1, t.n, D, lse, lse_bytes)) return STA_ERR_ALIAS;
     if (ranges_meet(lse, lse_bytes, workspace, workspace_bytes)) return STA_ERR_ALIAS;
+    const PackedBounds bounds = {cu_q, cu_k, k_used, S};
+    if (bounds.meet(o, tokens_q, D, lse, lse_bytes) || bounds.meet(nullptr, 0, D, workspace, workspace_bytes)) return STA_ERR_ALIAS;
     PackedParams p = {};
     p.q = packed_rows_of(*q);
     p.k = packed_rows_of(*k);

@@ -581,6 +581,9 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
         if (int rc = sta::packed_check(out[i], n_out[i], i == 0 ? q->heads : k->heads, D, true)) return rc;
     if (q->heads % k->heads || tokens_q * q->heads > kMostTokens) return STA_ERR_SHAPE;
     if (S == 0 || (tokens_q == 0 && tokens_k == 0)) return STA_OK;
+    // (smaller tiles are for launches that tiles of 128 do not fill the chip with)
+    const int64_t g = q->heads / k->heads;
+    if (tiles_of(tokens_q, g, S, max_q, 128) * k->heads > kMostWorkgroups || tiles_of(tokens_k, 1, S, max_k, 128) * k->heads > kMostWorkgroups) return STA_ERR_SHAPE;
     if (!cu_q || !cu_k) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
     if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < sta_packed_backward_workspace_bytes(q->heads, tokens_q)) return STA_ERR_WORKSPACE;
@@ -595,9 +598,9 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
     }
     for (int i = 0; i < 5; ++i)
         if (rows_meet(*in[i], 1, n_in[i], D, workspace, used)) return STA_ERR_ALIAS;
-    // (smaller tiles are for launches that tiles of 128 do not fill the chip with)
-    const int64_t g = q->heads / k->heads;
-    if (tiles_of(tokens_q, g, S, max_q, 128) * k->heads > kMostWorkgroups || tiles_of(tokens_k, 1, S, max_k, 128) * k->heads > kMostWorkgroups) return STA_ERR_SHAPE;
+    const PackedBounds bounds = {cu_q, cu_k, nullptr, S};
+    for (int j = 0; j < 3; ++j)
+        if (bounds.meet(out[j], n_out[j], D, workspace, used)) return STA_ERR_ALIAS;
     BackwardParams b = {};
     PackedParams &p = b.p;
     p.q = packed_rows_of(*q);

@@ -114,6 +114,21 @@ inline bool ranges_meet(const void *a, uint64_t a_bytes, const void *b, uint64_t
     return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
 
+// Whether what is written meets the bounds of S packed sequences: rows (null: none) or a range.
+struct PackedBounds {
+    const int32_t *cu_q, *cu_k, *k_used;
+    int S;
+    bool meet(const sta_head_rows *r, int64_t tokens, int D, const void *at, uint64_t bytes) const
+    {
+        const void *from[3] = {cu_q, cu_k, k_used};
+        for (int i = 0; i < 3; ++i) {
+            const uint64_t size = ((uint64_t)S + (i < 2)) * sizeof(int32_t);
+            if ((r && rows_meet(*r, 1, tokens, D, from[i], size)) || ranges_meet(at, bytes, from[i], size)) return true;
+        }
+        return false;
+    }
+};
+
 inline bool same_rows(const sta_head_rows &a, const sta_head_rows &b)
 {
     return a.data == b.data && a.batch == b.batch && a.token == b.token && a.head == b.head && a.heads == b.heads && a.dtype == b.dtype;

@@ -68,3 +68,16 @@ def test_scales_at_the_ends():
         assert forward(scale=scale, max_q=0) == OK and backward(scale=scale, S=0) == OK
     for scale in (2.0 ** -101, 1e-38, 1e-44):                # gradients divide by it
         assert forward(scale=scale, max_q=0) == OK and backward(scale=scale, S=0) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [
+    dict(cu_q=400 * M + 1024), dict(cu_k=400 * M), dict(used=400 * M + 100 * 2048 - 4), dict(cu_q=600 * M + 64, lse=600 * M), dict(used=600 * M + 3196, lse=600 * M),
+    dict(cu_k=600 * M - 12, lse=600 * M), dict(cu_k=700 * M + 4, ws=700 * M, nbytes=1 << 20), dict(used=700 * M - 8, ws=700 * M, nbytes=1 << 20),
+])
+def test_forward_refuses_to_write_its_bounds(kw):
+    assert forward(**kw) == ALIAS
+
+
+@pytest.mark.parametrize("kw", [dict(cu_q=700 * M), dict(cu_k=700 * M + 2048), dict(cu_q=800 * M - 12), dict(cu_k=900 * M + 4), dict(cu_q=1000 * M + 8), dict(cu_k=1000 * M - 4)])
+def test_gradients_refuse_to_write_their_bounds(kw):
+    assert refusals.backward(**kw) == ALIAS
