@@ -132,7 +132,7 @@ struct PackedTile {
 
 // The tile of a workgroup, the longest walks first: with up to 64 sequences, a lane each, in the order of how many tiles' walks a tile's is
 // long (rows that see more keys stand later in a causal sequence, keys that more rows see stand earlier), which a search over that number finds;
-// with more, sequence after sequence from the last.  False: there are not so many tiles.
+// with more, sequence after sequence from the last.  False: there are not so many tiles.  Every loop ends whatever the bounds are.
 template <int TILE, bool KEYS>
 __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, int lane, PackedTile *out)
 {
@@ -174,10 +174,11 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
         const uint32_t idx = KEYS ? rank : total - 1 - rank;
         uint32_t before = 0, own, upto;
         for (;; s0 += 64) {
+            if (s0 >= p.S) return false;                        // (idx < total, unless the bounds have changed since)
             own = tiles_of(s0 + lane, &longer);
             upto = scan64(own);
             const uint32_t all = __builtin_amdgcn_readlane(upto, 63);
-            if (idx < before + all) break;                      // there is one: idx < total
+            if (idx < before + all) break;
             before += all;
         }
         at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > idx));
@@ -188,7 +189,9 @@ __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, 
     out->seq.lq = uniform(out->seq.lq);
     out->seq.k0 = uniform(out->seq.k0);
     out->seq.lk = uniform(out->seq.lk);
-    return true;
+    // The bounds have been read twice.  A caller that writes them from another stream meanwhile gets results that mean nothing, but no walk without an end and
+    // no access outside the tensors.
+    return out->index * TILE < (KEYS ? (uint32_t)out->seq.lk : (uint32_t)out->seq.lq * p.g);
 }
 
 // The lane, counted again: neither it nor what is worked out from it behind a loop is kept in registers through it.
