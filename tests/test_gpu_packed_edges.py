@@ -6,7 +6,7 @@ import torch
 
 import paper_2502_04507_amd as sta
 from tests import layer_util as lu
-from tests.test_gpu_packed import BF, DEV, bounds, close, ints, randn, starts
+from tests.test_gpu_packed import BF, DEV, bounds, check, close, ints, randn, starts
 
 pytestmark = pytest.mark.gpu
 
@@ -183,3 +183,14 @@ def test_a_scale_next_to_nothing(case, with_lse, D):
         if with_lse:
             off = (lse[:, a:a + lq[s]].cpu().double() - torch.log(seen.double())).abs()
             assert bool((off <= 2.0 ** -20 * (1 + torch.log(seen.double())) + lk[s] * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_hundreds_of_sequences_of_uneven_lengths(D, causal):
+    """More sequences than four waves have lanes, some without rows or keys, a few long: forward and gradients."""
+    lq = [(7 * i * i) % 41 if i % 97 else 300 for i in range(330)]
+    lk = [(5 * i * i + 3) % 47 if i % 61 else 257 for i in range(330)]
+    assert 0 in lq and 0 in lk and max(lq) == 300
+    check(2, 1, D, lq, lk, causal, train=True)
+    check(2, 1, D, lq, lk, causal)
