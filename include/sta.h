@@ -327,7 +327,7 @@ int sta_rope_steps(int channels, double theta, int scaling, double factor, doubl
 /*
  * Rotation of rows: n_tensors (1 to 3) tensors of B x N tokens, out[i] <- rotation of in[i], all in one launch.  inverse not 0 turns the other way
  * (times the same magnitude), which is the gradient.  Channels beyond rotary->channels are copied.  out[i] may be in[i] itself;
- * other overlaps of outputs with inputs or each other are STA_ERR_ALIAS (of rows: views side by side in one allocation, as head ranges of a fused
+ * other overlaps of outputs with inputs (steps and positions included) or each other are STA_ERR_ALIAS (of rows: views side by side in one allocation, as head ranges of a fused
  * tensor or keys and values in one cache, do not overlap, in whatever order of strides).  Arithmetic in fp32, rounded once.
  * D: even, 2 .. 256.  Rows that start at multiples of 16 bytes, D a multiple of 16 and rotary->channels a multiple of 16 (of 8
  * where interleaved) take the fast kernel where there are many; few, and others, take one that reads single elements (sums of a row in another order, so

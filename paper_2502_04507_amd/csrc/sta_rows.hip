@@ -814,6 +814,8 @@ int sta_rope(const sta_head_rows *in, const sta_head_rows *out, int n_tensors, i
         if (in[i].dtype != in[0].dtype || out[i].dtype != out[0].dtype) return STA_ERR_UNSUPPORTED;
     }
     for (int i = 0; i < n_tensors; ++i)
+        if (meets_rotary(rotary, B, N, out + i, D, nullptr, 0)) return STA_ERR_ALIAS;
+    for (int i = 0; i < n_tensors; ++i)
         for (int j = 0; j < n_tensors; ++j) {
             if (!(i == j && same_rows(in[i], out[j])) && rows_overlap(in[i], out[j], B, N, D)) return STA_ERR_ALIAS;
             if (i < j && rows_overlap(out[i], out[j], B, N, D)) return STA_ERR_ALIAS;
@@ -860,6 +862,8 @@ int sta_qk_norm_rope(const sta_head_rows *q, const sta_head_rows *k, const sta_h
             if (i < j && rows_overlap(*out[i], *out[j], B, N, D)) return STA_ERR_ALIAS;
             if (rows_meet(*out[i], B, N, D, p.t[j].weight, (uint64_t)D * size_of(weight_dt))) return STA_ERR_ALIAS;
         }
+    for (uint32_t i = 0; i < p.n_tensors; ++i)
+        if (meets_rotary(rotary, B, N, out[i], D, nullptr, 0)) return STA_ERR_ALIAS;
     const hipError_t e = launch_rows(p, q->dtype == STA_F32, q_out->dtype == STA_F32, false, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
@@ -925,6 +929,11 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
                 for (const float *s : sum_of)
                     if (rows_meet(*r, B, N, D, s, sum_bytes)) return STA_ERR_ALIAS;
             }
+        for (uint32_t i = 0; i < p.n_tensors; ++i)
+            if (meets_rotary(rotary, B, N, dx[i], D, nullptr, 0)) return STA_ERR_ALIAS;
+        for (const float *s : sum_of)
+            if (meets_rotary(rotary, B, N, nullptr, D, s, sum_bytes)) return STA_ERR_ALIAS;
+        if (sums && meets_rotary(rotary, B, N, nullptr, D, workspace, sta_qk_norm_rope_workspace_bytes(D))) return STA_ERR_ALIAS;
         if (launch_rows(p, q->dtype == STA_F32, d_q_out->dtype == STA_F32, true, stream) != hipSuccess) return STA_ERR_HIP;
     }
     if (sums && sta::launch_kernel(sta_rows_weights_kernel, dim3((D + 15) / 16, 2), dim3(16 * kSlices), stream, p.partial, p.share[0].blocks,

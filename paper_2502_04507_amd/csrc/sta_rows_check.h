@@ -114,6 +114,19 @@ inline bool ranges_meet(const void *a, uint64_t a_bytes, const void *b, uint64_t
     return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
 
+// Whether what is written, rows (null: none) or a range, meets the steps or positions of a rotation (null: none) of B x N tokens.
+inline bool meets_rotary(const sta_rotary *rotary, int64_t B, int64_t N, const sta_head_rows *r, int D, const void *at, uint64_t bytes)
+{
+    if (!rotary || rotary->channels < 2 || B < 1 || N < 1) return false;
+    const __int128 last = (__int128)(B - 1) * rotary->position_batch + (__int128)(N - 1) * rotary->position_token + (rotary->pairs[1] || rotary->pairs[2] ? 3 : 1);
+    const __int128 most = (__int128)1 << 60;
+    const void *from[2] = {rotary->steps, rotary->positions};
+    const uint64_t size[2] = {(uint64_t)rotary->channels / 2 * sizeof(int64_t), (uint64_t)(last < most ? last : most) * sizeof(int32_t)};
+    for (int i = 0; i < 2; ++i)
+        if ((r && rows_meet(*r, B, N, D, from[i], size[i])) || ranges_meet(at, bytes, from[i], size[i])) return true;
+    return false;
+}
+
 // Whether what is written meets the bounds of S packed sequences: rows (null: none) or a range.
 struct PackedBounds {
     const int32_t *cu_q, *cu_k, *k_used;
