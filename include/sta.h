@@ -380,6 +380,8 @@ int sta_qk_norm_rope_backward(const sta_head_rows *q, const sta_head_rows *k, co
  * lse: NULL, or device float32 [Hq, tokens_q], ln of each row's softmax denominator; NaN, as o, where the row meets NaN in q or in keys that it sees.
  * scale <= 0 selects 1 / sqrt(D); NaN and more than 2^100 are STA_ERR_UNSUPPORTED.
  * Arithmetic as sta_forward (with lse, the sum is taken before the probabilities are rounded).
+ * Beyond 64 sequences of more than 32 rows a key head every workgroup looks for its rows in all bounds in turn: S in the hundreds costs little, in the
+ * thousands more than the attention of short sequences.
  * workspace: as sta_forward, of at least sta_packed_workspace_bytes(...) bytes: launches that would not fill the chip are cut along the keys.
  * NULL: no parts.  Results are repeatable bit for bit.
  * Supported: D in {64, 128}; rows at multiples of 16 bytes; tokens_k and tokens_q * Hq up to 2^31 - 4096; fewer than 2^24 workgroups, of which every key

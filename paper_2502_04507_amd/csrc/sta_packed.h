@@ -132,7 +132,8 @@ struct PackedTile {
 
 // The tile of a workgroup, the longest walks first: with up to 64 sequences, a lane each, in the order of how many tiles' walks a tile's is
 // long (rows that see more keys stand later in a causal sequence, keys that more rows see stand earlier), which a search over that number finds;
-// with more, sequence after sequence from the last.  False: there are not so many tiles.  Every loop ends whatever the bounds are.
+// with more, sequence after sequence from the last, 64 bounds at a time (32 heads over 8 of 128 channels, 40 tokens each, forward and gradients: 64
+// sequences 19 and 41 us, 256 60 and 175, 1024 343 and 863, 4096 2694 and 6651: from some thousand on the search outweighs the walks).  False: there are not so many tiles.  Every loop ends whatever the bounds are.
 template <int TILE, bool KEYS>
 __device__ __forceinline__ bool find_tile(uint32_t rank, const PackedParams &p, int lane, PackedTile *out)
 {

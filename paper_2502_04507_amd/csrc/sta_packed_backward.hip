@@ -17,8 +17,8 @@
 // left (Q and K of 4 N(0,1): 1e-2).  Everything else, sums and statistics included, is fp32.
 //
 // What bounds them: the matrix pipe and, where workgroups are few, latencies.  32,768 tokens of 32 heads over 8 of 128 channels, causal: both kernels
-// 1330 TFLOP/s (seven products), the rate of a large library product on this chip; 4 * 4096 tokens 1200; [2048, 1999, 77, 1023, 949] dQ 130 us, dK/dV 197
-// (962 and 847 TFLOP/s; matrix pipe busy 41 and 36 %): a wave's 64 matrix instructions of a sub-block of dK/dV read 32 KB of LDS, what it can give in that
+// 1330 TFLOP/s of the seven products that they run (949 of the five that have to be), the rate of a large library product on this chip; 4 * 4096 tokens 1200; [2048, 1999, 77, 1023, 949] dQ 128 us, dK/dV 187
+// (977 and 892 TFLOP/s; matrix pipe busy 41 and 36 %): a wave's 64 matrix instructions of a sub-block of dK/dV read 32 KB of LDS, what it can give in that
 // time, with two waves a SIMD (accumulators 128 registers, K and V 128) that wait for one another's stages.
 #include <hip/hip_runtime.h>
 #include <math.h>
