@@ -517,6 +517,13 @@ __global__ __launch_bounds__(kThreads, 3) void sta_rows_backward_kernel(Params p
                 next_x = load_row<PATH, SRC_F32>(x + address(h + stride) * T.x.head, at, in);
                 next_g = load_row<PATH, DST_F32>(dy + address(h + stride) * T.dy.head, at, in);
             }
+            if (__builtin_amdgcn_ballot_w64(!on) != 0) {    // a row that is not there holds another's values, and 0 times an infinity would be no 0
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    g0[j] = on ? g0[j] : 0.f;
+                    g1[j] = on ? g1[j] : 0.f;
+                }
+            }
             rotate<PATH>(g0, g1, cs, sn, at, -1.f);
             float sum = 0.f;
 #pragma unroll

@@ -360,3 +360,26 @@ def test_outputs_side_by_side_in_one_tensor(layout, N):
     for d in (d_want, d_outs):
         sta.sta_qk_norm_rope_backward(ins[0], ins[1], *grads, *d, *w, None, None, rotary, None)
     assert all(torch.equal(a, b) for a, b in zip(d_outs, d_want))
+
+
+@pytest.mark.parametrize("N", [9, 6003])
+@pytest.mark.parametrize("heads", [3, 8])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weight_gradients_of_an_infinity(N, heads, dtype):
+    """An infinite gradient of the first token's, or the last head's, row makes an infinite weight gradient: rows that are not there add nothing."""
+    D, eps = 128, 1e-5
+    x, w = make((1, N, heads, D), 3, dtype), make((D,), 4, torch.float32) + 1.0
+    dy = [make((1, N, heads, D), 5 + i, dtype) for i in range(2)]
+    dy[0][0, 0, 0, 7], dy[1][0, N // 2, heads - 1, 30] = float("inf"), -float("inf")
+    dw = [torch.empty(D, device=DEV) for _ in range(2)]
+    dx = [torch.empty_like(x, device=DEV) for _ in range(2)]
+    ws = torch.empty(sta.sta_qk_norm_rope_workspace_bytes(D), dtype=torch.uint8, device=DEV)
+    xd, wd = x.to(DEV), w.to(DEV)
+    sta.sta_qk_norm_rope_backward(xd, xd, dy[0].to(DEV), dy[1].to(DEV), None, *dx, None, wd, wd, *dw, None, ws, eps=eps)
+    for got, g, at in ((dw[0], dy[0], (0, 0, 0, 7)), (dw[1], dy[1], (0, N // 2, heads - 1, 30))):
+        assert float(got[at[-1]]) == float(g[at]) * float(torch.sign(x[at]))
+        g = g.clone()
+        g[at] = 0.0
+        _, sums, absolute = lu.norm_rope_backward(x.double(), w.double(), eps, g.double(), lambda t: t)
+        others = torch.arange(D) != at[-1]
+        lu.assert_rounded(got.cpu()[others], sums[others], (512 * ULP * absolute + 1e-30)[others], "weight gradient")
