@@ -194,3 +194,37 @@ def test_hundreds_of_sequences_of_uneven_lengths(D, causal):
     assert 0 in lq and 0 in lk and max(lq) == 300
     check(2, 1, D, lq, lk, causal, train=True)
     check(2, 1, D, lq, lk, causal)
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,m,causal", [(4, 2, 200, 200, True), (16, 1, 900, 70, False)])
+def test_a_training_step_in_a_graph(Hq, Hkv, n, m, causal):
+    """Forward and gradients, the keys' cut along the rows in the second, with inputs and lengths that change between replays."""
+    D = 64
+    x = [torch.empty((t, h, D), dtype=BF, device=DEV) for t, h in ((n, Hq), (m, Hkv), (m, Hkv), (n, Hq))]
+    cu_q, cu_k = ints([0, n // 2, n]), ints([0, m // 2, m])
+    outs = [[torch.zeros_like(t) for t in (x[0], *x[:3])] + [torch.zeros((Hq, n), device=DEV)] for _ in range(2)]
+    ws = [torch.empty(sta.sta_packed_backward_workspace_bytes(Hq, n), dtype=torch.uint8, device=DEV) for _ in range(2)]
+
+    def step(i):
+        o, dq, dk, dv, lse = outs[i]
+        sta.sta_packed_forward(*x[:3], o, cu_q, cu_k, n, m, causal=causal, lse=lse)
+        sta.sta_packed_backward(*x[:3], o, x[3], lse, dq, dk, dv, cu_q, cu_k, n, m, ws[i], causal=causal)
+
+    for t in x:
+        t.zero_()
+    step(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    for seed, at in enumerate((n // 2, 3, n - 1)):
+        for i, t in enumerate(x):
+            t.copy_(randn(t.shape, 10 * seed + i))
+        cu_q.copy_(torch.tensor([0, at, n], dtype=torch.int32))
+        cu_k.copy_(torch.tensor([0, min(at, m - 1), m], dtype=torch.int32))
+        ws[0].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(1)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*outs)), at
