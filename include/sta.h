@@ -412,6 +412,44 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
                         int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes,
                         void *hip_stream);
 
+/*
+ * A cache of keys and values in pages.  k and v: bf16 [pages, page_size, Hkv, D], laid out alike; of sta_head_rows `batch` is from page to page and
+ * `token` from slot to slot.  Sequence s has used[s] keys; key j of it is slot j % page_size of page table[s * table_row + j / page_size].  Any page_size
+ * from 1 on; multiples of 8 (head dimension 128: of 4) are read fastest.  A page may stand in the rows of several sequences (a common beginning).
+ * table: device int32, S rows of table_pages entries; used: device int32 [S].  Lengths are cut to what a row of the table has places for.  Entries for keys that are
+ * not used are not looked at; entries of used keys that are no pages are read as some page (of what is written there nothing is written).
+ * Supported: D in {64, 128}; rows at multiples of 16 bytes; pages and the slots of one page less than 2^32 bytes apart; table_pages * page_size counts up to
+ * 2^31 - 4096.  Pages, tables and lengths must not overlap what a call writes, but for what it says.
+ */
+typedef struct {
+    sta_head_rows k, v;
+    int64_t pages;
+    int page_size;
+    const int32_t *table;
+    int64_t table_row;          /* entries from one sequence's row to the next */
+    int table_pages;
+    int32_t *used;
+} sta_paged_cache;
+
+/*
+ * Writes new rows into their pages: of the lq = cu[s + 1] - cu[s] new tokens of sequence s, token i becomes key used[s] - lq + i, so used are the lengths with
+ * the new ones, as the attention behind it takes them.  k, v: [tokens, Hkv, D], strides as sta_head_rows says (batch is not looked at), both bf16 or both
+ * float32 (rounded once).  cu: device int32 [S + 1].  max_new: host, an upper bound of the sequences' new tokens; tokens beyond it are not written, nor are those
+ * whose key would be below 0 or beyond the table.  A key that two calls' sequences write at once holds one row or the other.
+ * weights: NULL, or the keys' gathered attention weights, float32 [pages, Hkv, page_size]: 0 is written for every key that is.
+ */
+int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, int64_t tokens, const int32_t *cu, const sta_paged_cache *cache, int S, int max_new,
+                     int D, float *weights, void *hip_stream);
+
+/*
+ * sta_packed_forward with the keys in pages: chunks of new tokens (whose rows are in the cache by then) and single tokens against what is used.  With lq query
+ * tokens and used[s] keys, causal tokens see the keys j <= i + used[s] - lq.  Everything else, the order of the sums included, is as there: the same keys give the
+ * same bits wherever their pages lie.
+ */
+size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k);
+int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
+                      int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 const char *sta_strerror(int status);
 int sta_version(void);
 

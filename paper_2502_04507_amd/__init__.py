@@ -16,3 +16,6 @@ from .layer_ops import (  # noqa: F401
     sta_packed_backward_workspace_bytes, sta_packed_forward, sta_packed_workspace_bytes, sta_qk_norm_rope, sta_qk_norm_rope_backward,
     sta_qk_norm_rope_workspace_bytes, sta_rope, sta_rope_steps,
 )
+from .paged_ops import (  # noqa: F401
+    StaPagedCache, sta_paged_append, sta_paged_forward, sta_paged_workspace_bytes,
+)

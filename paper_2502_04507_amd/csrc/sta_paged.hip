@@ -1,0 +1,172 @@
+// Softmax attention over a cache in pages: the kernels of sta_packed_forward.h with keys that are looked up in a table.
+//
+// A lane looks up one row of the next stage while the present one is on its way: the entry of the table, as a load into a register, is older than the stage's
+// DMA, so the wait for a stage covers it.  Where every group of rows of a DMA instruction (4 rows of 128 channels, 8 of 64) lies in one page, its place goes from
+// the lane that has it into scalar registers, two v_readlane a group, and the DMA is as that of packed sequences; where a page ends inside a group, or the keys inside a
+// stage, every lane gets its row's place from the lane that has it.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/sta.h"
+#include "sta_paged.h"
+#include "sta_packed_forward.h"
+
+namespace {
+
+struct PagedParams : PackedParams {     // k and v: the pool; k.token and k.head as there
+    PagedCache c;
+    uint32_t whole_groups;              // no page ends inside a group of rows
+};
+
+// The keys of a sequence have no first row: its number stands in k0.
+__device__ __forceinline__ PackedSeq seq_of(uint32_t s, const PagedParams &p)
+{
+    PackedSeq q;
+    q.q0 = bound_of(p.cu_q[s], 0, (int)p.tokens_q);
+    q.lq = bound_of(p.cu_q[s + 1], q.q0, (int)p.tokens_q) - q.q0;
+    q.k0 = (int)s;
+    q.lk = used_of(s, p.c);
+    return q;
+}
+
+template <int D>
+struct KeysOf<PagedParams, D> {
+    static constexpr int LPR = D / 8, GR = Staged<D>::GroupRows;
+    const char *kh, *vh;
+    const int32_t *row;                 // of the table
+    PackedDma<D, true> k_dma;
+    PackedDma<D, false> v_dma;
+    int entry;                          // of the lane's row of the next stage, and its place in the page, in bytes
+    uint32_t slot;
+    __device__ __forceinline__ void start(const PagedParams &p, const PackedSeq &seq, uint32_t kv, int lane)
+    {
+        kh = p.c.k + (int64_t)kv * p.c.head;
+        vh = p.c.v + (int64_t)kv * p.c.head;
+        row = p.c.table + (int64_t)seq.k0 * p.c.table_row;
+        k_dma.start(lane, p.c.token);
+        v_dma.start(lane, p.c.token);
+        entry = 0;
+        slot = 0;
+    }
+    // The entries for the rows from sub-block `sub` on; rows beyond the last key have the last key's.  There are keys.
+    template <int SUBS>
+    __device__ __forceinline__ void look_up(const PagedParams &p, const PackedSeq &seq, int sub)
+    {
+        if (seq.lk <= 0) return;
+        const int key = sub * kSub + (SUBS == 1 ? fresh_lane() & 31 : fresh_lane()), last = seq.lk - 1;
+        uint32_t at;
+        const uint32_t n = entry_of((uint32_t)(key < last ? key : last), p.c, &at);
+        slot = at * p.c.token;
+        entry = row[n];
+    }
+    template <int SUBS, int COUNT, int K_GROUP, int V_GROUP>
+    __device__ __forceinline__ void bring(const PagedParams &p, const PackedSeq &seq, int sub, int next, int from, char *to, int v_at, int apart)
+    {
+        const uint64_t place = (uint64_t)page_inside(entry, p.c) * p.c.page + slot;
+        const uint32_t lo = (uint32_t)place, hi = (uint32_t)(place >> 32);
+        look_up<SUBS>(p, seq, next);
+        if (__builtin_expect((sub + SUBS) * kSub <= seq.lk && p.whole_groups, 1)) {
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int i = 0; i < COUNT; ++i) {
+                    const int r = u * kSub + (from + i) * GR;
+                    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, r) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, r);
+                    k_dma.bring_whole(kh + at, to + u * apart + (from + i) * K_GROUP);
+                    v_dma.bring_whole(vh + at, to + u * apart + v_at + (from + i) * V_GROUP);
+                }
+            asm volatile("; whole" ::: "memory");
+        } else {
+            const int lane = fresh_lane();
+#pragma unroll 1
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll 1
+                for (int i = 0; i < COUNT; ++i) {
+                    const int r = u * kSub + (from + i) * GR + lane / LPR;
+                    const uint64_t at = (uint64_t)(uint32_t)__shfl((int)hi, r) << 32 | (uint32_t)__shfl((int)lo, r);
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kh + at + k_dma.chunk_of(lane)),
+                                                     STA_LDS_PTR(to + u * apart + (from + i) * K_GROUP), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vh + at + v_dma.chunk_of(lane)),
+                                                     STA_LDS_PTR(to + u * apart + v_at + (from + i) * V_GROUP), 16, 0, 0);
+                }
+            asm volatile("; part" ::: "memory");
+        }
+    }
+    // Behind a wait that covers the entries: from here on the compiler has nothing to wait for at their use, where stages are on their way.
+    __device__ __forceinline__ void settle() { asm volatile("" : "+v"(entry)); }
+    __device__ __forceinline__ void bring_values(const PagedParams &p, const PackedSeq &seq, int first, char *dst) const
+    {
+        const int lane = fresh_lane(), key = first + lane / LPR, last = seq.lk - 1;
+        uint32_t at;
+        const uint32_t n = entry_of((uint32_t)(key < last ? key : last), p.c, &at);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vh + place_of(page_inside(row[n], p.c), at, p.c) + v_dma.chunk_of(lane)),
+                                         STA_LDS_PTR(dst), 16, 0, 0);
+    }
+};
+
+}  // namespace
+
+extern "C" {
+
+size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
+{
+    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);
+}
+
+int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
+                      int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!q || !o || !cache) return STA_ERR_NULL;
+    if (S < 0 || tokens_q < 0 || max_q < 0 || max_k < 0 || tokens_q > kMostTokens) return STA_ERR_SHAPE;
+    if ((D != 64 && D != 128) || !scale_of(scale, D, false, &scale)) return STA_ERR_UNSUPPORTED;
+    if (int rc = sta::packed_check(q, tokens_q, 0, D, false)) return rc;
+    if (int rc = sta::packed_check(o, tokens_q, q->heads, D, true)) return rc;
+    if (int rc = paged_check(cache, S, D, false)) return rc;
+    const int Hkv = cache->k.heads;
+    if (q->heads % Hkv || tokens_q * q->heads > kMostTokens) return STA_ERR_SHAPE;
+    if (S == 0 || tokens_q == 0 || max_q == 0) return STA_OK;
+    if (!cu_q) return STA_ERR_NULL;
+    if (((uintptr_t)cu_q | (uintptr_t)lse) & 3) return STA_ERR_SHAPE;
+    const size_t lse_bytes = (size_t)tokens_q * q->heads * sizeof(float);
+    if (rows_overlap(*o, tokens_q, *q, tokens_q, 1, D) || rows_in_pages(*cache, D, *o, tokens_q)) return STA_ERR_ALIAS;
+    PackedPlan plan;
+    if (!plan_of(q->heads, Hkv, D, S, tokens_q, max_q, max_k, workspace != nullptr, &plan)) return STA_ERR_SHAPE;
+    if (workspace && (((uintptr_t)workspace & 15) || workspace_bytes < plan.workspace() * sizeof(float))) return STA_ERR_WORKSPACE;
+    const struct { const void *at; uint64_t bytes; } ranges[2] = {{workspace, workspace_bytes}, {lse, lse_bytes}};
+    const PackedBounds bounds = {cu_q, nullptr, nullptr, S};
+    for (const auto &w : ranges)
+        if (rows_meet(*q, 1, tokens_q, D, w.at, w.bytes) || rows_meet(*o, 1, tokens_q, D, w.at, w.bytes) || meets_pages(*cache, D, w.at, w.bytes) ||
+            bounds.meet(o, tokens_q, D, w.at, w.bytes) || meets_table(*cache, S, o, 1, tokens_q, D, w.at, w.bytes))
+            return STA_ERR_ALIAS;
+    if (ranges_meet(lse, lse_bytes, workspace, workspace_bytes)) return STA_ERR_ALIAS;
+    PagedParams p = {};
+    p.q = packed_rows_of(*q);
+    p.o = packed_rows_of(*o);
+    p.lse = lse;
+    p.cu_q = cu_q;
+    p.S = S;
+    p.tokens_q = (uint32_t)tokens_q;
+    p.max_q = max_q;
+    p.max_k = max_k;
+    p.Hkv = Hkv;
+    p.g = q->heads / Hkv;
+    p.by_g = sta::fast_div_of(p.g);
+    p.by_Hkv = sta::fast_div_of(p.Hkv);
+    p.by_parts = sta::fast_div_of(plan.parts);
+    p.causal = causal != 0;
+    p.scale = scale;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.parts = plan.parts;
+    p.part_subs = plan.part_subs;
+    p.ws = static_cast<float *>(workspace);
+    p.c = paged_cache_of(*cache);
+    p.whole_groups = cache->page_size % (D == 128 ? Staged<128>::GroupRows : Staged<64>::GroupRows) == 0;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    hipError_t e;
+    if (D == 64) e = lse ? launch_packed<64, true>(p, plan, stream) : launch_packed<64, false>(p, plan, stream);
+    else e = lse ? launch_packed<128, true>(p, plan, stream) : launch_packed<128, false>(p, plan, stream);
+    return e == hipSuccess ? STA_OK : STA_ERR_HIP;
+}
+
+}  // extern "C"
