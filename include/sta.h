@@ -450,6 +450,33 @@ size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q
 int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
                       int max_q, int max_k, int D, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * The attention weight that the keys of a cache in pages gather from the rows of a call: for every key j of a sequence and key head n
+ *     weights_j = decay * before_j + sum over the query tokens i that see j, and the query heads of n, of exp(scale q_i . k_j - lse_i),
+ * the sums of the columns of the attention's probabilities.  q, cu_q, causal, scale: as sta_paged_forward; lse: float32 [Hq, tokens_q] as it wrote it (a call on the
+ * last rows of a prompt alone gives what those look at).  Rows without keys (lse -infinity) give nothing.  before, weights: float32 [pages, Hkv, page_size], key j's number where its
+ * row lies; before may be weights itself, or NULL (nothing); decay 0: it is not looked at; decay has to be finite.  Written for every key j < max_k of a sequence, with
+ * no query tokens too; the numbers of other slots are left as they are.  A page that several sequences share gets one sequence's numbers or the other's.
+ * max_q, max_k: host, upper bounds; query tokens beyond max_q give nothing.
+ * Scores, exponents and sums in fp32; no atomics: repeated calls give identical bits.  NaN in a row or key that meet makes NaN of that key's number.
+ * Supported: as sta_paged_forward; fewer than 2^24 workgroups, of which every sequence and key head has one for up to 256 keys of max_k (for 64 in small launches).
+ */
+int sta_paged_weights(const sta_head_rows *q, const float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S, int max_q, int max_k,
+                      int D, int causal, float scale, const float *before, float decay, float *weights, void *hip_stream);
+
+/*
+ * Takes what stays of the sequences of a cache to the pages of another table: of used[s] keys every key head keeps min(used[s], keep), the first `first`, the
+ * last `recent`, and of those between the ones of the greatest weights, of equal ones the earlier (NaN counts as the greatest, -0 as 0).  Their order stays; what was the
+ * row at index kept[s, n, j] is key j of head n in `into`, and so is its weight in into_weights (NULL: not taken).  Heads keep different keys, but equally many.
+ * weights: float32 [pages, Hkv, page_size] of cache, into_weights of into.  kept: device int32 [S, Hkv, keep], written; -1 from min(used[s], keep) on.  into->used: written,
+ * min(used[s], keep).  into's pool, page size and layout may be others, or the pool the same (then into_weights may be weights): the pages in into's table, which must be distinct, must then
+ * be none that cache's rows have among their used ones.  So pages that sequences share can be evicted from, and a call that is made again gives the same.
+ * first + recent may not exceed keep; into's rows of the table need places for keep keys (else STA_ERR_SHAPE).  Two launches; fewer than 2^22 heads of all sequences, fewer than 2^24
+ * blocks of 64 (head dimension 64: 128) kept rows of one head.
+ */
+int sta_paged_evict(const sta_paged_cache *cache, const float *weights, const sta_paged_cache *into, float *into_weights, int32_t *kept, int S, int keep,
+                    int first, int recent, int D, void *hip_stream);
+
 const char *sta_strerror(int status);
 int sta_version(void);
 

@@ -17,5 +17,5 @@ from .layer_ops import (  # noqa: F401
     sta_qk_norm_rope_workspace_bytes, sta_rope, sta_rope_steps,
 )
 from .paged_ops import (  # noqa: F401
-    StaPagedCache, sta_paged_append, sta_paged_forward, sta_paged_workspace_bytes,
+    StaPagedCache, sta_paged_append, sta_paged_evict, sta_paged_forward, sta_paged_weights, sta_paged_workspace_bytes,
 )

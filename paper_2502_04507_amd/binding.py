@@ -30,7 +30,7 @@ EXPORTED_SYMBOLS = (
     "sta_rope_steps", "sta_rope", "sta_qk_norm_rope", "sta_qk_norm_rope_workspace_bytes", "sta_qk_norm_rope_backward",
     "sta_packed_workspace_bytes", "sta_packed_forward", "sta_packed_backward_workspace_bytes", "sta_packed_backward",
     # bound in paged_ops
-    "sta_paged_append", "sta_paged_workspace_bytes", "sta_paged_forward",
+    "sta_paged_append", "sta_paged_workspace_bytes", "sta_paged_forward", "sta_paged_weights", "sta_paged_evict",
 )
 
 

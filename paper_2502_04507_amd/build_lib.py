@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsta.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["sta_api.hip", "sta_permute.hip", "sta_attention.hip", "sta_reduce.hip", "sta_backward.hip", "sta_rows.hip", "sta_packed.hip", "sta_packed_backward.hip",
-           "sta_paged.hip", "sta_paged_rows.hip"]
+           "sta_paged.hip", "sta_paged_rows.hip", "sta_paged_weights.hip"]
 PROBE_SOURCE = "bench_mfma_probe.hip"
 PROBE_OUT = os.path.join(HERE, "libsta_mfma_probe.so")
 

@@ -25,6 +25,8 @@ def _bind(lib):
     lib.sta_paged_workspace_bytes.argtypes = [ci, ci, ci, ci, i64, ci, ci]
     lib.sta_paged_workspace_bytes.restype = sz
     lib.sta_paged_forward.argtypes = [rows, rows, vp, i64, vp, cache, ci, ci, ci, ci, ci, cf, vp, sz, vp]
+    lib.sta_paged_weights.argtypes = [rows, vp, i64, vp, cache, ci, ci, ci, ci, ci, cf, vp, cf, vp, vp]
+    lib.sta_paged_evict.argtypes = [cache, vp, cache, vp, vp, ci, ci, ci, ci, ci, vp]
     lib._paged_ops_bound = True
     return lib
 
@@ -120,3 +122,30 @@ def sta_paged_forward(q, o, cu_q, cache, max_q, max_k, causal=True, scale=0.0, l
                                     _bounds(cu_q, "cu_q", cache.S + 1), cache._c, cache.S, max_q, max_k, cache.D, int(bool(causal)), scale, ws, nbytes,
                                     _stream_ptr(stream)))
     return o
+
+
+def sta_paged_weights(q, lse, weights, cu_q, cache, max_q, max_k, before=None, decay=1.0, causal=True, scale=0.0, stream=None):
+    """What every key of the cache gathers from these rows, added to decay times before (None: nothing; may be weights): weights float32 [pages, Hkv, page_size];
+    q bf16 [tokens, Hq, D] and lse float32 [Hq, tokens] as sta_paged_forward had and wrote them."""
+    tq, Hq, max_q, max_k = _paged_queries(q, cu_q, cache, max_q, max_k)
+    if lse is None or weights is None:
+        raise ValueError("lse and weights are needed")
+    _check(_lib().sta_paged_weights(_packed_rows(q, "q", tq, Hq, cache.D), _lse_ptr(lse, Hq, tq), tq, _bounds(cu_q, "cu_q", cache.S + 1), cache._c, cache.S, max_q,
+                                    max_k, cache.D, int(bool(causal)), scale, _weights_ptr(before, cache, "before"), decay,
+                                    _weights_ptr(weights, cache, "weights"), _stream_ptr(stream)))
+    return weights
+
+
+def sta_paged_evict(cache, weights, into, into_weights, kept, first=0, recent=0, stream=None):
+    """Keeps of every sequence and key head kept.shape[2] keys: the first and recent ones, and of the others those of the greatest weights.  Their rows go to the pages of
+    into, another StaPagedCache whose used is written; their weights to into_weights (or None); kept int32 [S, Hkv, keep]: which they were, -1 where there are fewer."""
+    if into.S != cache.S or into.Hkv != cache.Hkv or into.D != cache.D:
+        raise ValueError("both caches must have the same sequences, heads and channels")
+    if kept.dtype != torch.int32 or kept.dim() != 3 or kept.shape[:2] != (cache.S, cache.Hkv):
+        raise ValueError("kept must be int32 [S, Hkv, keep]")
+    if weights is None:
+        raise ValueError("weights are needed")
+    _check(_lib().sta_paged_evict(cache._c, _weights_ptr(weights, cache, "weights"), into._c, _weights_ptr(into_weights, into, "into_weights"),
+                                  _dev(kept, "kept") or 16, cache.S, _int32(kept.shape[2], "keep"), _int32(first, "first"), _int32(recent, "recent"), cache.D,
+                                  _stream_ptr(stream)))
+    return into

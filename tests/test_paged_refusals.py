@@ -91,6 +91,58 @@ def test_append_refuses(want, kw):
     assert append(**kw) == want
 
 
+def weights(**kw):
+    a = dict(q=rows(100 * M), lse=600 * M, tq=100, cu=502 * M, cache=cache(), S=3, max_q=50, max_k=200, D=128, scale=0.0, before=None, decay=1.0, weights=700 * M)
+    a.update(kw)
+    return po._lib().sta_paged_weights(a["q"], a["lse"], a["tq"], a["cu"], a["cache"], a["S"], a["max_q"], a["max_k"], a["D"], 1, a["scale"], a["before"], a["decay"],
+                                       a["weights"], None)
+
+
+@pytest.mark.parametrize("want,kw", CACHES + [
+    (NULL, dict(q=None)), (NULL, dict(lse=None)), (NULL, dict(weights=None)), (NULL, dict(cu=None)), (SHAPE, dict(tq=-1)), (SHAPE, dict(max_q=-1)), (SHAPE, dict(max_k=-1)),
+    (SHAPE, dict(tq=1 << 31)), (UNSUPPORTED, dict(q=rows(100 * M, dtype=1))), (UNSUPPORTED, dict(scale=float("nan"))), (UNSUPPORTED, dict(decay=float("nan"))),
+    (UNSUPPORTED, dict(decay=float("inf"))), (UNSUPPORTED, dict(decay=-float("inf"))), (SHAPE, dict(q=rows(100 * M, 7))), (SHAPE, dict(q=rows(100 * M + 4))),
+    (SHAPE, dict(cu=502 * M + 2)), (SHAPE, dict(lse=600 * M + 1)), (SHAPE, dict(weights=700 * M + 2)), (SHAPE, dict(before=800 * M + 2)),
+    (SHAPE, dict(S=1 << 24, max_k=64)), (SHAPE, dict(S=1 << 16, max_k=1 << 30, cache=cache(width=1 << 26, row=1 << 26))),
+    (ALIAS, dict(weights=100 * M)), (ALIAS, dict(weights=200 * M)), (ALIAS, dict(weights=300 * M + 4)), (ALIAS, dict(weights=500 * M)), (ALIAS, dict(weights=501 * M)),
+    (ALIAS, dict(weights=502 * M)), (ALIAS, dict(weights=600 * M)), (ALIAS, dict(before=700 * M + 4)), (ALIAS, dict(before=700 * M - 4)),
+    (OK, dict(S=0)), (OK, dict(max_k=0)), (OK, dict(cache=cache(width=0, table=None))), (OK, dict(cache=cache(pages=0, k=pool(None), v=pool(None)))),
+])
+def test_weights_refuses(want, kw):
+    assert weights(**kw) == want
+
+
+def into(**kw):
+    a = dict(k=pool(1200 * M), v=pool(1300 * M), pages=500, table=1500 * M, used=1501 * M)
+    a.update(kw)
+    return cache(**a)
+
+
+def evict(**kw):
+    a = dict(cache=cache(), weights=700 * M, into=into(), into_weights=1700 * M, kept=1800 * M, S=3, keep=128, first=4, recent=32, D=128)
+    a.update(kw)
+    return po._lib().sta_paged_evict(a["cache"], a["weights"], a["into"], a["into_weights"], a["kept"], a["S"], a["keep"], a["first"], a["recent"], a["D"], None)
+
+
+@pytest.mark.parametrize("want,kw", CACHES + [
+    (NULL, dict(into=None)), (NULL, dict(weights=None)), (NULL, dict(kept=None)), (NULL, dict(into=into(used=None))), (NULL, dict(into=into(table=None))),
+    (SHAPE, dict(keep=-1)), (SHAPE, dict(first=-1)), (SHAPE, dict(recent=-1)), (SHAPE, dict(first=100, recent=29)), (SHAPE, dict(first=2 ** 31 - 1, recent=2 ** 31 - 1)),
+    (SHAPE, dict(into=into(k=pool(1200 * M, 1), v=pool(1300 * M, 1)))), (SHAPE, dict(into=into(width=7))), (SHAPE, dict(keep=641)), (SHAPE, dict(S=1 << 21)),
+    (SHAPE, dict(S=1 << 20, keep=640)), (SHAPE, dict(into=into(k=pool(1200 * M, page=2048), v=pool(1300 * M, page=2048)))), (SHAPE, dict(weights=700 * M + 1)),
+    (SHAPE, dict(into_weights=1700 * M + 2)), (SHAPE, dict(kept=1800 * M + 2)),
+    # pools that share memory without being the same
+    (ALIAS, dict(into=into(k=pool(200 * M + 4096)))), (ALIAS, dict(into=into(v=pool(200 * M)))), (ALIAS, dict(into=into(k=pool(300 * M)))), (ALIAS, dict(into=into(k=pool(200 * M)))),
+    (ALIAS, dict(into=into(v=pool(1200 * M)))), (ALIAS, dict(into_weights=700 * M)), (ALIAS, dict(into_weights=700 * M + 4)), (ALIAS, dict(into_weights=200 * M)),
+    (ALIAS, dict(into_weights=1300 * M)), (ALIAS, dict(into_weights=500 * M)), (ALIAS, dict(into_weights=1500 * M)), (ALIAS, dict(into_weights=1501 * M)),
+    (ALIAS, dict(into_weights=1800 * M)), (ALIAS, dict(kept=700 * M)), (ALIAS, dict(kept=1700 * M)), (ALIAS, dict(kept=1200 * M)), (ALIAS, dict(kept=300 * M)),
+    (ALIAS, dict(kept=500 * M)), (ALIAS, dict(kept=501 * M)), (ALIAS, dict(kept=1500 * M)), (ALIAS, dict(kept=1501 * M)), (ALIAS, dict(into=into(used=501 * M))),
+    (ALIAS, dict(into=into(used=1500 * M))), (ALIAS, dict(into=into(used=700 * M))), (ALIAS, dict(into=into(used=200 * M))), (ALIAS, dict(into=into(used=1300 * M))),
+    (ALIAS, dict(into=into(k=pool(500 * M - 64)))), (ALIAS, dict(into=into(v=pool(700 * M)))), (ALIAS, dict(into=into(table=1200 * M))), (OK, dict(S=0)),
+])
+def test_evict_refuses(want, kw):
+    assert evict(**kw) == want
+
+
 def test_keys_and_values_of_a_page_side_by_side_do_not_overlap():
     # [pages, 2, slots, heads, D] and [pages, slots, 2, heads, D]; max_new 0, as anything else would be launched
     for apart, page, token in ((4096, 8192, 256), (256, 8192, 512)):
