@@ -2,8 +2,9 @@
 //
 // sta_paged_append_kernel  a row is D / 8 lanes of 16 bytes; a workgroup takes tokens of one sequence, which needs no search for it, and all their key and value heads.
 // sta_paged_select_kernel  a workgroup for each sequence and key head finds the smallest weight that stays, twelve, ten and ten bits of its place in the order of
-//                          numbers at a time, by counting how many have which; then writes down in order which keys stay.
-// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.
+//                          numbers at a time, by counting how many have which; then writes down in order which keys stay.  Bound by the instructions and LDS of the one CU that a head has:
+//                          8 heads of 32,768 keys 23 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 4 the others, 2.5 to count and 5 to write down).
+// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 82 us, 4.8 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -88,28 +89,118 @@ struct EvictParams {
     uint32_t Hkv;
     int32_t keep, first, recent;
     sta::FastDiv by_Hkv, by_blocks;
+    uint32_t page_weights;              // numbers of a page, of all key heads
+    uint32_t fours;                     // pages of a multiple of four slots, weights at a multiple of 16 bytes
 };
 
-// Numbers in an order of whole numbers: NaN above all others, 0 and -0 the same.
-__device__ __forceinline__ uint32_t order_of(float w)
+// The bits of a number as a whole number in their order: NaN above all others, 0 and -0 the same.  On the bits throughout: comparisons of numbers are compiled as if
+// there were no NaN.
+__device__ __forceinline__ uint32_t order_of(uint32_t bits)
 {
-    uint32_t bits = __float_as_uint(w);
-    asm volatile("" : "+v"(bits));                          // comparisons of numbers are compiled as if there were no NaN
     if ((bits & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
     if (bits == 0x80000000u) bits = 0;
-    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+    return bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u);
 }
 
 constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
 
+// What a wave looks at: a run of keys, four adjacent ones a lane and 256 at a time, as whole numbers in the order of their weights.  Keys that stay or go in any case (the first, the
+// recent ones, and places behind the last) count as 0, which no weight has, nor any up to 2^20.  A run of up to 256 * GROUPS keys stays in LDS from the first look on, of a longer one every
+// number is looked up every time.
+template <int GROUPS>
+struct Run {
+    u32x4 *own;                         // of the wave and lane, in LDS
+    int begin, end, length, lo, hi;     // length: of a run
+    bool kept;
+    const int32_t *row;
+    const uint32_t *weights;            // of the key head
+    __device__ __forceinline__ u32x4 look(const EvictParams &p, int j) const
+    {
+        u32x4 w = {0, 0, 0, 0};
+        if (p.fours) {
+            uint32_t slot;
+            if (j >= end) return w;
+            const int entry = row[entry_of((uint32_t)j, p.from, &slot)];
+            return *reinterpret_cast<const u32x4 *>(weights + ((uint64_t)page_inside(entry, p.from) * p.page_weights + slot));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (j + e >= end) return w;
+            uint32_t slot;
+            const uint32_t page = page_inside(row[entry_of((uint32_t)(j + e), p.from, &slot)], p.from);
+            w[e] = weights[(uint64_t)page * p.page_weights + slot];
+        }
+        return w;
+    }
+    // j0: the first lane's first key.  Numbers from 0 up to infinity, as weights are, have a short way.
+    __device__ __forceinline__ u32x4 order(int j0, int lane, u32x4 w) const
+    {
+        bool other = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) other = other || w[e] > 0x7f800000u;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(other) == 0, 1)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] |= 0x80000000u;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = order_of(w[e]);
+        }
+        if (!inside(j0)) {
+            const int j = j0 + 4 * lane;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = j + e >= lo && j + e < hi ? w[e] : 0;
+        }
+        return w;
+    }
+    // whether no key of 256 stays or goes in any case
+    __device__ __forceinline__ bool inside(int j0) const { return j0 >= lo && hi - j0 >= 256; }
+    __device__ __forceinline__ void start(const EvictParams &p, int n, int wave, int lane, const int32_t *table_row, uint32_t head, u32x4 *numbers)
+    {
+        length = ((n + kSelectWaves - 1) / kSelectWaves + 255) & ~255;
+        kept = length <= 256 * GROUPS;
+        begin = wave < (n + length - 1) / length ? wave * length : n;
+        end = n - begin < length ? n : begin + length;
+        const int all = n - p.recent;
+        lo = p.first > begin ? p.first : begin;
+        hi = all < end ? all : end;
+        row = table_row;
+        weights = reinterpret_cast<const uint32_t *>(p.weights) + (uint64_t)head * p.from.by_page.d;
+        own = numbers + wave * (64 * GROUPS) + lane;
+        if (!kept) return;
+        constexpr int AT_ONCE = 4;
+#pragma unroll 1
+        for (int j0 = begin; j0 < end; j0 += 256 * AT_ONCE) {
+            u32x4 w[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) w[i] = look(p, j0 + 256 * i + 4 * lane);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+                if (j0 + 256 * i < end) own[(j0 - begin) / 4 + 64 * i] = order(j0 + 256 * i, lane, w[i]);
+        }
+    }
+    // f(the first lane's first key, the numbers of four) of every lane, 256 keys at a time in ascending order.
+    template <typename F>
+    __device__ __forceinline__ void each(const EvictParams &p, int lane, F &&f) const
+    {
+        if (kept) {
+#pragma unroll 1
+            for (int j0 = begin; j0 < end; j0 += 256) f(j0, own[(j0 - begin) / 4]);
+        } else {
+#pragma unroll 1
+            for (int j0 = begin; j0 < end; j0 += 256) f(j0, order(j0, lane, look(p, j0 + 4 * lane)));
+        }
+    }
+};
+
+// Workgroup: a sequence and key head, runs of up to 256 * GROUPS keys in LDS.
+template <int GROUPS>
 __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p)
 {
-    __shared__ uint32_t counts[4096];
-    __shared__ uint32_t wave_sums[kSelectWaves], found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    __shared__ u32x4 numbers[kSelect * GROUPS];
+    __shared__ __attribute__((aligned(16))) uint32_t counts[4096];
+    __shared__ uint32_t wave_sums[kSelectWaves], found[2], totals[2][kSelectWaves];
     const uint32_t s = sta::fast_div(blockIdx.x, p.by_Hkv), h = blockIdx.x - s * p.Hkv;
-    const int n = used_of(s, p.from), stay = n < p.keep ? n : p.keep;
-    const int32_t *row = p.from.table + (int64_t)s * p.from.table_row;
+    const int n = uniform(used_of(s, p.from)), stay = n < p.keep ? n : p.keep, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     int32_t *kept = p.kept + (int64_t)blockIdx.x * p.keep;
     if (h == 0 && tid == 0) p.to_used[s] = stay;
     for (int j = stay + tid; j < p.keep; j += kSelect) kept[j] = -1;
@@ -117,118 +208,138 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
         for (int j = tid; j < n; j += kSelect) kept[j] = j;
         return;
     }
-    auto order_at = [&](int j) {
-        uint32_t slot;
-        const uint32_t page = page_inside(row[entry_of((uint32_t)j, p.from, &slot)], p.from);
-        return order_of(p.weights[((int64_t)page * p.Hkv + h) * p.from.by_page.d + slot]);
-    };
-    // what may go: keys lo .. hi - 1, of which `need` stay
-    const int lo = p.first, hi = n - p.recent;
-    uint32_t need = (uint32_t)(p.keep - p.first - p.recent), least = 0, known = 0;          // the bits of the least one that stays, those known so far
-    for (int digit = 0; digit < 3 && need > 0; ++digit) {
+    Run<GROUPS> run;
+    run.start(p, n, wave, lane, p.from.table + (int64_t)s * p.from.table_row, h, numbers);
+    uint32_t need = (uint32_t)(p.keep - p.first - p.recent);        // of those that may go so many stay
+    uint32_t least = need > 0 ? 0 : 0xffffffffu;                    // the bits that are known of the least one that does
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+        if (need == 0) break;
         const int shift = digit == 0 ? 20 : digit == 1 ? 10 : 0, bins = digit == 0 ? 4096 : 1024;
-        for (int b = tid; b < bins; b += kSelect) counts[b] = 0;
+        if (digit == 0) *reinterpret_cast<u32x4 *>(&counts[4 * tid]) = u32x4{0, 0, 0, 0};
+        else counts[tid] = 0;
         __syncthreads();
-#pragma unroll 4
-        for (int j = lo + tid; j < hi; j += kSelect) {
-            const uint32_t x = order_at(j);
-            if ((x & known) == least) atomicAdd(&counts[(x >> shift) & (bins - 1)], 1u);
+        run.each(p, lane, [&](int, u32x4 x) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (digit == 0) atomicAdd(&counts[x[e] >> 20], 1u);
+                else if ((x[e] ^ least) >> (shift + 10) == 0) atomicAdd(&counts[(x[e] >> shift) & (bins - 1)], 1u);
+            }
+        });
+        __syncthreads();
+        // a thread has four bins or one, the first thread the highest: how many stand in those above?
+        uint32_t own[4] = {0, 0, 0, 0};                             // the highest first
+        if (digit == 0) {
+            const u32x4 all = *reinterpret_cast<const u32x4 *>(&counts[4 * (kSelect - 1 - tid)]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own[e] = all[3 - e];
+        } else {
+            own[0] = counts[kSelect - 1 - tid];
         }
-        __syncthreads();
-        // every thread has `each` bins, the first one the highest: how many stand in bins above
-        const int each = bins / kSelect;
-        uint32_t own = 0;
-        for (int b = 0; b < each; ++b) own += counts[bins - 1 - (tid * each + b)];
-        const uint32_t upto = scan64(own);
+        const uint32_t sum = own[0] + own[1] + own[2] + own[3], upto = scan64(sum);
         if (lane == 63) wave_sums[wave] = upto;
         __syncthreads();
-        uint32_t above = upto - own;
-        for (int w = 0; w < wave; ++w) above += wave_sums[w];
-        if (above < need && above + own >= need) {          // one thread: in its bins the number that still has to stay is reached
-            int b = 0;
-            for (; above + counts[bins - 1 - (tid * each + b)] < need; ++b) above += counts[bins - 1 - (tid * each + b)];
-            found[0] = bins - 1 - (tid * each + b);
+        const uint32_t before = sum64(lane < wave ? wave_sums[lane] : 0);
+        uint32_t above = before + upto - sum;
+        if (above < need && above + sum >= need) {                  // one thread: in its bins the number that still has to stay is reached
+            int at = 0;
+            uint32_t there = own[0];
+#pragma unroll
+            for (int e = 1; e < 4; ++e)
+                if (at == e - 1 && above + there < need) {
+                    above += there;
+                    there = own[e];
+                    at = e;
+                }
+            found[0] = digit == 0 ? 4 * (kSelect - 1 - tid) + 3 - at : kSelect - 1 - tid;
             found[1] = above;
         }
         __syncthreads();
         least |= found[0] << shift;
-        known |= (uint32_t)(bins - 1) << shift;
         need -= found[1];
-        __syncthreads();
     }
-    // `need` of those equal to `least`, the first ones, stay, and all above it.  A wave has a run of keys: it counts them, and after those before it writes them down.
-    if (p.keep == p.first + p.recent) least = 0xffffffffu;
-    const int run = ((n + kSelectWaves - 1) / kSelectWaves + 63) & ~63, begin = wave * run, end = begin + run < n ? begin + run : n;
-    auto look = [&](int j, bool *sure, bool *equal) {
-        const bool inside = j >= lo && j < hi;
-        const uint32_t x = j < end ? order_at(j) : 0;
-        *sure = j < end && (!inside || x > least);
-        *equal = j < end && inside && x == least;
-    };
-    uint32_t sure_before = 0, equal_before = 0;
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        bool sure, equal;
-        look(j0 + lane, &sure, &equal);
-        sure_before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(sure));
-        equal_before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(equal));
-    }
+    // `need` of those equal to `least`, the first ones, stay, and all above it.  A wave counts its own, and after those before it writes them down.
+    auto always = [&](int j) { return j < run.end && (j < p.first || j >= n - p.recent); };
+    uint32_t sures = 0, equals = 0;
+    run.each(p, lane, [&](int j0, u32x4 x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sures += x[e] > least;
+            equals += x[e] == least;
+        }
+        if (!run.inside(j0)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sures += always(j0 + 4 * lane + e);
+        }
+    });
+    sures = sum64(sures);
+    equals = sum64(equals);
     if (lane == 0) {
-        counts[wave] = sure_before;
-        counts[kSelectWaves + wave] = equal_before;
+        totals[0][wave] = sures;
+        totals[1][wave] = equals;
     }
     __syncthreads();
-    sure_before = equal_before = 0;
-    for (int w = 0; w < wave; ++w) {
-        sure_before += counts[w];
-        equal_before += counts[kSelectWaves + w];
-    }
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        bool sure, equal;
-        look(j0 + lane, &sure, &equal);
-        const uint64_t sures = __builtin_amdgcn_ballot_w64(sure), equals = __builtin_amdgcn_ballot_w64(equal), below = ((uint64_t)1 << lane) - 1;
-        const uint32_t rank = equal_before + __builtin_popcountll(equals & below);
-        const uint32_t equal_taken = rank < need ? rank : need;
-        const uint32_t place = sure_before + __builtin_popcountll(sures & below) + equal_taken;
-        if ((sure || (equal && rank < need)) && place < (uint32_t)p.keep) kept[place] = j0 + lane;
-        sure_before += __builtin_popcountll(sures);
-        equal_before += __builtin_popcountll(equals);
-    }
+    uint32_t sures_before = sum64(lane < wave ? totals[0][lane] : 0), equals_before = sum64(lane < wave ? totals[1][lane] : 0);
+    run.each(p, lane, [&](int j0, u32x4 x) {
+        const int j = j0 + 4 * lane;
+        const bool even = __builtin_amdgcn_ballot_w64(x[0] == least || x[1] == least || x[2] == least || x[3] == least) != 0;
+        if (run.inside(j0) && !even) {
+            uint32_t mine = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine += x[e] > least;
+            const uint32_t upto = scan64(mine);
+            uint32_t place = sures_before + (equals_before < need ? equals_before : need) + upto - mine;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (x[e] > least) {
+                    if (place < (uint32_t)p.keep) kept[place] = j + e;
+                    ++place;
+                }
+            sures_before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+            return;
+        }
+        bool sure[4], equal[4];
+        uint32_t mine = 0;                                          // counts of both, at most 256 each
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sure[e] = x[e] > least || always(j + e);
+            equal[e] = x[e] == least;
+            mine += (sure[e] ? 1u : 0u) + (equal[e] ? 1u << 16 : 0u);
+        }
+        const uint32_t upto = scan64(mine), all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63), until = upto - mine;
+        uint32_t place = sures_before + (until & 0xffff), rank = equals_before + (until >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t at = place + (rank < need ? rank : need);
+            if ((sure[e] || (equal[e] && rank < need)) && at < (uint32_t)p.keep) kept[at] = j + e;
+            place += sure[e];
+            rank += equal[e];
+        }
+        sures_before += all & 0xffff;
+        equals_before += all >> 16;
+    });
 }
 
+// One row a lane: two and four at once, whose addresses and data leave room for fewer waves, took 86 and 96 us where one takes 81 (24 sequences, 8 heads, 2048 rows each).
 template <int D>
 __global__ __launch_bounds__(256) void sta_paged_move_kernel(EvictParams p)
 {
-    constexpr int LPR = D / 8, ROWS = 256 / LPR, AT_ONCE = 4;
+    constexpr int LPR = D / 8, ROWS = 256 / LPR;
     const uint32_t item = sta::fast_div(blockIdx.x, p.by_blocks), block = blockIdx.x - item * p.by_blocks.d;      // (sequence, key head), rows
     const uint32_t s = sta::fast_div(item, p.by_Hkv), h = item - s * p.Hkv;
-    const int n = used_of(s, p.from), stay = n < p.keep ? n : p.keep, c = threadIdx.x % LPR;
-    const int32_t *row = p.from.table + (int64_t)s * p.from.table_row, *to_row = p.to.table + (int64_t)s * p.to.table_row, *kept = p.kept + (int64_t)item * p.keep;
-    u32x4 k[AT_ONCE], v[AT_ONCE];
-    float w[AT_ONCE];
-    int64_t to[AT_ONCE], to_weight[AT_ONCE];
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-        const int j = (int)block * ROWS * AT_ONCE + i * ROWS + (int)(threadIdx.x / LPR);
-        to[i] = -1;
-        if (j >= stay) continue;
-        uint32_t slot, to_slot;
-        const int to_page = to_row[entry_of((uint32_t)j, p.to, &to_slot)];
-        if (to_page < 0 || to_page >= (int)p.to.pages) continue;
-        const uint32_t page = page_inside(row[entry_of((uint32_t)bound_of(kept[j], 0, n - 1), p.from, &slot)], p.from);
-        const uint64_t at = place_of(page, slot, p.from) + (int64_t)h * p.from.head + 16 * c;
-        k[i] = *reinterpret_cast<const u32x4 *>(p.from.k + at);
-        v[i] = *reinterpret_cast<const u32x4 *>(p.from.v + at);
-        if (c == 0 && p.to_weights) w[i] = p.weights[((int64_t)page * p.Hkv + h) * p.from.by_page.d + slot];
-        to[i] = (int64_t)(place_of((uint32_t)to_page, to_slot, p.to) + (int64_t)h * p.to.head + 16 * c);
-        to_weight[i] = ((int64_t)to_page * p.Hkv + h) * p.to.by_page.d + to_slot;
-    }
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-        if (to[i] < 0) continue;
-        *reinterpret_cast<u32x4 *>(p.to.k + to[i]) = k[i];
-        *reinterpret_cast<u32x4 *>(p.to.v + to[i]) = v[i];
-        if (c == 0 && p.to_weights) p.to_weights[to_weight[i]] = w[i];
-    }
+    const int n = used_of(s, p.from), stay = n < p.keep ? n : p.keep, c = threadIdx.x % LPR, j = (int)block * ROWS + (int)(threadIdx.x / LPR);
+    if (j >= stay) return;
+    uint32_t slot, to_slot;
+    const int to_page = p.to.table[(int64_t)s * p.to.table_row + entry_of((uint32_t)j, p.to, &to_slot)];
+    if (to_page < 0 || to_page >= (int)p.to.pages) return;
+    const uint32_t key = (uint32_t)bound_of(p.kept[(int64_t)item * p.keep + j], 0, n - 1);
+    const uint32_t page = page_inside(p.from.table[(int64_t)s * p.from.table_row + entry_of(key, p.from, &slot)], p.from);
+    const uint64_t at = place_of(page, slot, p.from) + (int64_t)h * p.from.head + 16 * c, to = place_of((uint32_t)to_page, to_slot, p.to) + (int64_t)h * p.to.head + 16 * c;
+    const u32x4 k = *reinterpret_cast<const u32x4 *>(p.from.k + at), v = *reinterpret_cast<const u32x4 *>(p.from.v + at);
+    *reinterpret_cast<u32x4 *>(p.to.k + to) = k;
+    *reinterpret_cast<u32x4 *>(p.to.v + to) = v;
+    if (c == 0 && p.to_weights)
+        p.to_weights[((uint64_t)to_page * p.Hkv + h) * p.to.by_page.d + to_slot] = p.weights[((uint64_t)page * p.Hkv + h) * p.from.by_page.d + slot];
 }
 
 // Whether two pools share memory without being one and the same.
@@ -327,12 +438,12 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     const int Hkv = cache->k.heads;
     if (into->k.heads != Hkv || (int64_t)into->table_pages * into->page_size < keep || keep > kMostTokens) return STA_ERR_SHAPE;
     for (const sta_paged_cache *c : {cache, into})
-        if ((__int128)c->pages * c->page_size * Hkv > (__int128)1 << 60) return STA_ERR_SHAPE;
+        if ((int64_t)c->page_size * Hkv > 0xffffffff || (__int128)c->pages * c->page_size * Hkv > (__int128)1 << 60) return STA_ERR_SHAPE;
     if (S == 0) return STA_OK;
     const uint64_t w_bytes = weight_bytes(*cache), to_bytes = into_weights ? weight_bytes(*into) : 0;
     if ((!weights && w_bytes > 0) || (!kept && keep > 0)) return STA_ERR_NULL;
     if (((uintptr_t)weights | (uintptr_t)into_weights | (uintptr_t)kept) & 3) return STA_ERR_SHAPE;
-    const int64_t blocks = ((int64_t)keep + 4096 / (D / 2) - 1) / (4096 / (D / 2)), items = (int64_t)S * Hkv;
+    const int64_t rows = 2048 / D, blocks = (keep + rows - 1) / rows, items = (int64_t)S * Hkv;
     constexpr int64_t most_selects = (1 << 22) - 1;         // of 1024 lanes
     if (items > most_selects || items * blocks > kMostWorkgroups) return STA_ERR_SHAPE;
     const uint64_t kept_bytes = (uint64_t)items * keep * sizeof(int32_t);
@@ -366,9 +477,13 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     p.first = first;
     p.recent = recent;
     p.by_Hkv = sta::fast_div_of(Hkv);
+    p.page_weights = (uint32_t)cache->page_size * Hkv;
+    p.fours = cache->page_size % 4 == 0 && ((uintptr_t)weights & 15) == 0;
     p.by_blocks = sta::fast_div_of(blocks > 0 ? (uint32_t)blocks : 1);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = sta::launch_kernel(sta_paged_select_kernel, dim3((uint32_t)items), dim3(kSelect), stream, p);
+    // up to 8192 keys two workgroups fit a CU, up to 32,768 one
+    hipError_t e = p.from.room <= 8 * kSelect ? sta::launch_kernel(sta_paged_select_kernel<2>, dim3((uint32_t)items), dim3(kSelect), stream, p)
+                                              : sta::launch_kernel(sta_paged_select_kernel<8>, dim3((uint32_t)items), dim3(kSelect), stream, p);
     if (e == hipSuccess && keep > 0 && into->pages > 0 && cache->pages > 0) {
         const dim3 grid((uint32_t)(items * blocks)), block(256);
         e = D == 64 ? sta::launch_kernel(sta_paged_move_kernel<64>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<128>, grid, block, stream, p);
