@@ -4,11 +4,14 @@
 // row block, and the four lanes of a key are joined once, at the end.  The log sums are given, so there is no running maximum, no order among workgroups and nothing to
 // join between them: a workgroup has all rows of its keys.  64 keys a wave stay in registers.
 //
-// Roundings.  Products of bf16 numbers are exact, scores, exponents and sums fp32: the sum of a stage's eight values is a tree, sixteen stages go into one sum, and
-// those into the key's.
+// Roundings.  Products of bf16 numbers are exact, scores, exponents and sums fp32: four values of a lane are a tree, those of 512 rows go into one sum, and those into the key's.
 //
-// sta_paged_few_weights_kernel   at most 16 or 32 rows per sequence and key head: rows and keys straight from memory to registers, no LDS.
-// sta_paged_weights_kernel       more: stages of 32 rows go through LDS, shared by the waves along the keys; small launches cut the rows among a workgroup's waves.
+// sta_paged_few_weights_kernel   at most 16 or 32 rows per sequence and key head: rows and keys straight from memory to registers, no LDS.  Bound by memory: 48 tokens of 32 heads over 8
+//                                on 1 to 16,384 keys 187 us, 4.7 TB/s (5.7 where nothing is written, though that is 12 of 870 MB).
+// sta_paged_weights_kernel       more: stages of 32 or 64 rows go through LDS, shared by the waves along the keys; small launches cut the rows among a workgroup's waves.  Bound by
+//                                vector and matrix instructions, which hardly overlap (per 64 rows and 64 keys of a wave 1024 cycles of the matrix pipe, 64 exponentials of 8 cycles, as
+//                                many multiply-adds and sums of 4): 2048 tokens of 32 heads over 8 of 128 channels on 16,384 keys 260 us, 990 TFLOP/s.  With stages of 32 rows 294 us, two stages
+//                                in place of three 265, 32 keys a wave 315, 128 keys a workgroup 274 to 296; the order of the instructions in a stage changes nothing.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -19,7 +22,8 @@
 
 namespace {
 
-constexpr int kKeys = 64;               // of a wave: four columns of 16
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
 
 struct WeightsParams {
     PackedRows q;
@@ -33,6 +37,7 @@ struct WeightsParams {
     int32_t max_q, max_k;
     sta::FastDiv by_g, by_Hkv, by_tiles;
     uint32_t causal;
+    uint32_t even, g_shift;             // whether g is a power of two up to 32, and which
 };
 
 struct WeightsSeq {
@@ -55,23 +60,33 @@ __device__ __forceinline__ WeightsSeq weights_seq(uint32_t s, const WeightsParam
     return q;
 }
 
-// The pages and slots of a lane's keys key0 + 16 col, and the fragments of their rows; keys that are not there are read as the last one.
-template <int D>
-__device__ __forceinline__ void load_keys(const WeightsParams &p, const int32_t *row, uint32_t kv, int key0, int lk, int lane, bf16x8 (&K)[4][D / 32])
+// A wave's 16 NC keys from key0 on.  A lane has one of them, key0 + lane, to look up and to write; its number before and the fragments of the rows, 16 keys a column block, are asked for at once.
+// Keys that are not there are read as the last one.
+struct OwnKey {
+    int64_t at;                         // of its number; below 0: none is written
+    float before;
+};
+template <int D, int NC>
+__device__ __forceinline__ OwnKey load_keys(const WeightsParams &p, uint32_t s, uint32_t kv, int key0, int lk, int lane, bf16x8 (&K)[NC][D / 32])
 {
-    uint64_t at[4];
-#pragma unroll
-    for (int col = 0; col < 4; ++col) {
-        const int key = key0 + 16 * col + (lane & 15);
-        uint32_t slot;
-        const uint32_t n = entry_of((uint32_t)(key < lk ? key : lk - 1), p.c, &slot);
-        at[col] = place_of(page_inside(row[n], p.c), slot, p.c);
-    }
+    const int mine = key0 + (NC < 4 ? lane % (16 * NC) : lane), key = mine < lk ? mine : lk - 1;
+    uint32_t slot;
+    const int page = p.c.table[(int64_t)s * p.c.table_row + entry_of((uint32_t)key, p.c, &slot)];
+    const uint64_t place = place_of(page_inside(page, p.c), slot, p.c);
     const char *head = p.c.k + (int64_t)kv * p.c.head + 16 * (lane >> 4);
 #pragma unroll
-    for (int col = 0; col < 4; ++col)
+    for (int col = 0; col < NC; ++col) {
+        const int from = 16 * col + (lane & 15);
+        const uint64_t at = (uint64_t)(uint32_t)__shfl((int)(place >> 32), from) << 32 | (uint32_t)__shfl((int)place, from);
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) K[col][ks] = *reinterpret_cast<const bf16x8 *>(head + at[col] + 64 * ks);
+        for (int ks = 0; ks < D / 32; ++ks) K[col][ks] = *reinterpret_cast<const bf16x8 *>(head + at + 64 * ks);
+    }
+    OwnKey own = {-1, 0.f};
+    if (lane < 16 * NC && mine < lk && mine < p.max_k && page >= 0 && page < (int)p.c.pages) {
+        own.at = ((int64_t)page * p.Hkv + kv) * p.c.by_page.d + slot;
+        if (p.before) own.before = p.before[own.at];
+    }
+    return own;
 }
 
 // Row R of a key head: its token inside the sequence, and where its query row and its log sum are.
@@ -95,39 +110,32 @@ __device__ __forceinline__ float offset_of(float lse)
     return bits == 0xff800000u ? INFINITY : lse * 1.4426950408889634f;
 }
 
-// A lane's key among the wave's 64 is 16 (lane / 16) + lane % 16: its sum goes to its place.
-__device__ __forceinline__ void store_weights(const WeightsParams &p, const int32_t *row, uint32_t kv, int key0, int lk, int lane, const float (&sum)[4])
+template <int NC>
+__device__ __forceinline__ void store_weights(const WeightsParams &p, const OwnKey &own, int lane, const float (&sum)[NC])
 {
     float mine = 0.f;
 #pragma unroll
-    for (int col = 0; col < 4; ++col) {
+    for (int col = 0; col < NC; ++col) {
         const float all = quad_lane_sum(sum[col]);
         mine = lane >> 4 == col ? all : mine;
     }
-    const int key = key0 + lane;
-    if (key >= lk || key >= p.max_k) return;
-    uint32_t slot;
-    const int page = row[entry_of((uint32_t)key, p.c, &slot)];
-    if (page < 0 || page >= (int)p.c.pages) return;
-    const int64_t at = ((int64_t)page * p.Hkv + kv) * p.c.by_page.d + slot;
-    p.weights[at] = p.before ? fmaf(p.before[at], p.decay, mine) : mine;
+    if (own.at >= 0) p.weights[own.at] = p.before ? fmaf(own.before, p.decay, mine) : mine;
 }
 
-// Workgroup (sequence, 256 keys, key head).
-template <int D, int RB>
+// Workgroup (sequence, 64 NC keys, key head).
+template <int D, int NC, int RB>
 __global__ __launch_bounds__(256) void sta_paged_few_weights_kernel(WeightsParams p)
 {
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g4 = lane >> 4;
     const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
     const uint32_t s = sta::fast_div(item, p.by_tiles), tile = item - s * p.by_tiles.d;
     const WeightsSeq seq = weights_seq(s, p);
-    const int key0 = ((int)tile * 4 + wave) * kKeys;
+    const int key0 = ((int)tile * 4 + wave) * (16 * NC);
     if (key0 >= seq.lk) return;
-    const int32_t *row = p.c.table + (int64_t)s * p.c.table_row;
-    bf16x8 K[4][D / 32], Q[RB][D / 32];
-    float offset[RB][4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+    bf16x8 K[NC][D / 32], Q[RB][D / 32];
+    float offset[RB][4], sum[NC] = {};
     int sees[RB][4];
-    load_keys<D>(p, row, kv, key0, seq.lk, lane, K);
+    const OwnKey own = load_keys<D, NC>(p, s, kv, key0, seq.lk, lane, K);
     const int rows = seq.rows < 16 * RB ? seq.rows : 16 * RB;
     if (rows > 0) {
 #pragma unroll
@@ -145,7 +153,7 @@ __global__ __launch_bounds__(256) void sta_paged_few_weights_kernel(WeightsParam
             }
         }
 #pragma unroll
-        for (int col = 0; col < 4; ++col)
+        for (int col = 0; col < NC; ++col)
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 floatx4 S = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -159,142 +167,250 @@ __global__ __launch_bounds__(256) void sta_paged_few_weights_kernel(WeightsParam
                 }
             }
     }
-    store_weights(p, row, kv, key0, seq.lk, lane, sum);
+    store_weights(p, own, lane, sum);
 }
 
-// Workgroup (sequence, KW * 64 keys, key head): KW waves next to each other along the keys, RG = 4 / KW groups of them that take the stages of 32 rows in turn.
-template <int D, int KW>
+// Up to 64 sequences, a lane each: those with at least half as many rows as there may be come first, so that no long walk begins among the last workgroups (32 new tokens on 32,768
+// keys and 512 on 20,001, 32 heads over 8: 106 us, 119 in the order of the sequences).
+__device__ __forceinline__ uint32_t sequence_of_turn(uint32_t turn, int lane, const WeightsParams &p)
+{
+    const bool there = lane < (int)p.S, many = there && 2 * (int64_t)weights_seq(there ? lane : 0, p).lq >= p.max_q;
+    const uint64_t first = __builtin_amdgcn_ballot_w64(many);
+    uint32_t left = turn;
+    uint64_t from = first;
+    if (turn >= (uint32_t)__builtin_popcountll(first)) {
+        left -= __builtin_popcountll(first);
+        from = ~first;                          // (turn is below S, so no lane without a sequence is reached)
+    }
+    while (left-- > 0) from &= from - 1;
+    return (uint32_t)__builtin_ctzll(from);
+}
+
+// Exponentials of a block of 16 rows, a column block of 16 keys: what the lane has of it is added up.
+template <bool MASKED>
+__device__ __forceinline__ float sum_of(const floatx4 &S, const floatx4 &offset, float c, int key, const intx4 &sees)
+{
+    float e[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        e[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c, -offset[r]));
+        if (MASKED) e[r] = key < sees[r] ? e[r] : 0.f;
+    }
+    return (e[0] + e[1]) + (e[2] + e[3]);
+}
+
+template <int PENDING>
+__device__ __forceinline__ void lds_wait1(bf16x8 &a)
+{
+    asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(PENDING));
+}
+
+// part[col] += the exponentials of BLOCKS blocks of 16 rows in the stage at AT of the addresses: their offsets stand at INFO of row_addr, how many keys they see SEES
+// behind.  The exponentials of one block stand between the matrix instructions of the next, which take about as long.
+template <int D, int NC, int BLOCKS, bool MASKED, int AT, int INFO, int SEES>
+__device__ __forceinline__ void add_rows(uint32_t q_addr, uint32_t row_addr, const bf16x8 (&K)[NC][D / 32], float c, int key0, float (&part)[NC])
+{
+    constexpr int KS = D / 32, EACH = NC / KS > 0 ? NC / KS : 1;     // column blocks whose exponentials go with a k-step
+    bf16x8 a[2][KS], o[2], l[2];
+    floatx4 S[2][NC];
+    auto read_info = [&](auto bc) {
+        constexpr int b = decltype(bc)::value;
+        o[b % 2] = ds_read_b128_at<INFO + 64 * b>(row_addr);
+        if constexpr (MASKED) l[b % 2] = ds_read_b128_at<INFO + SEES + 64 * b>(row_addr);
+    };
+    auto read = [&](auto bc, auto kc) {
+        constexpr int b = decltype(bc)::value, ks = decltype(kc)::value;
+        a[b % 2][ks] = ds_read_b128_at<AT + (b / 2) * StagedRows<D>::Tile + (b % 2) * StagedRows<D>::Rows16 + ks * 64>(q_addr);
+    };
+    auto exponentials = [&](int b, int col) __attribute__((always_inline)) {
+        part[col] += sum_of<MASKED>(S[b % 2][col], __builtin_bit_cast(floatx4, o[b % 2]), c, key0 + 16 * col, __builtin_bit_cast(intx4, l[b % 2]));
+    };
+    read_info(std::integral_constant<int, 0>{});
+    static_for<0, KS>([&](auto kc) { read(std::integral_constant<int, 0>{}, kc); });
+    static_for<0, BLOCKS>([&](auto bc) {
+        constexpr int b = decltype(bc)::value;
+        static_for<0, KS>([&](auto kc) {
+            constexpr int ks = decltype(kc)::value;
+            if constexpr (b + 1 < BLOCKS) {
+                read(std::integral_constant<int, b + 1>{}, kc);
+                lds_wait1<KS>(a[b % 2][ks]);                // (KS reads of the next block at most, so by the block's end its offsets are there as well)
+            } else {
+                lds_wait1<KS - 1 - ks>(a[b % 2][ks]);
+            }
+#pragma unroll
+            for (int col = 0; col < NC; ++col) S[b % 2][col] = mfma_16x16x32(a[b % 2][ks], K[col][ks], ks == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : S[b % 2][col]);
+            if constexpr (b > 0) {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (EACH * ks + i < NC) exponentials(b - 1, EACH * ks + i);
+#pragma unroll
+                for (int col = 0; col < NC; ++col) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, EACH * (MASKED ? 20 : 12) / NC, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (b + 1 < BLOCKS) read_info(std::integral_constant<int, b + 1>{});
+    });
+    if constexpr (MASKED) lds_wait2<0>(o[(BLOCKS - 1) % 2], l[(BLOCKS - 1) % 2]);
+    else lds_wait1<0>(o[(BLOCKS - 1) % 2]);
+#pragma unroll
+    for (int col = 0; col < NC; ++col) exponentials(BLOCKS - 1, col);
+}
+
+// Workgroup (sequence, KW * 64 keys, key head): KW waves next to each other along the keys, RG = 4 / KW groups of them that take the stages of 32 * U rows in turn.
+template <int D, int NC, int KW, int U>
 __global__ __launch_bounds__(256, 2) void sta_paged_weights_kernel(WeightsParams p)
 {
-    constexpr int RG = 4 / KW, KEYS = KW * kKeys, FOLD = 16;
+    constexpr int RG = 4 / KW, OWN = 16 * NC, KEYS = KW * OWN, ROWS = 32 * U, FOLD = 16 / U;
     using L = StagedRows<D>;
-    constexpr int PER_WAVE = L::Groups / KW > 0 ? L::Groups / KW : 1;       // DMA instructions of a wave for a stage
-    constexpr int ROWS_AT = L::Tile, STAGE = L::Tile + 2 * kSub * 4;        // rows, their offsets, how many keys they see
-    __shared__ __attribute__((aligned(1024))) char smem[RG * 2 * STAGE];
-    __shared__ float joined[RG > 1 ? RG : 1][KEYS][4];
+    constexpr int PER_WAVE = U * L::Groups / KW;                            // DMA instructions of a wave for a stage
+    constexpr int ROWS_AT = U * L::Tile, STAGE = ROWS_AT + 2 * ROWS * 4;    // rows, their offsets, how many keys they see
+    // stages: one that is read and two on their way, or one where the groups' stages would leave room for one workgroup a CU
+    constexpr int RING = RG == 1 ? 3 : 2;
+    __shared__ __attribute__((aligned(1024))) char smem[RG * RING * STAGE];
+    __shared__ float joined[RG > 1 ? RG : 1][RG > 1 ? KEYS : 1][4];
     const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), g4 = lane >> 4;
     const int rg = all_waves / KW, wave = all_waves % KW;
     const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
-    const uint32_t s = sta::fast_div(item, p.by_tiles), tile = item - s * p.by_tiles.d;
+    const uint32_t turn = sta::fast_div(item, p.by_tiles), tile = item - turn * p.by_tiles.d;
+    const uint32_t s = p.S <= 64 ? sequence_of_turn(turn, lane, p) : turn;
     WeightsSeq seq = weights_seq(s, p);
     seq.q0 = uniform(seq.q0);
     seq.lq = uniform(seq.lq);
     seq.lk = uniform(seq.lk);
     seq.rows = uniform(seq.rows);
-    const int tile0 = (int)tile * KEYS, key0 = tile0 + wave * kKeys;
+    const int tile0 = (int)tile * KEYS, key0 = tile0 + wave * OWN;
     if (tile0 >= seq.lk) return;
-    const int32_t *row = p.c.table + (int64_t)s * p.c.table_row;
     // the rows before token first_token see no key of the tile, those from whole_token on see all
     const int last = (tile0 + KEYS < seq.lk ? tile0 + KEYS : seq.lk) - 1, ahead = seq.lk - seq.lq;
     const int first_token = !p.causal || tile0 <= ahead ? 0 : tile0 - ahead, whole_token = !p.causal || last <= ahead ? 0 : last - ahead;
-    const int step0 = (int)((int64_t)first_token * p.g < seq.rows ? first_token * (int)p.g / kSub : (seq.rows + kSub - 1) / kSub);
-    const int steps_end = (seq.rows + kSub - 1) / kSub;
+    const int steps_end = (seq.rows + ROWS - 1) / ROWS;
+    const int step0 = (int64_t)first_token * p.g < seq.rows ? first_token * (int)p.g / ROWS : steps_end;
     const int64_t whole_row = (int64_t)whole_token * p.g;
-    const int masked_end = (int)(whole_row < seq.rows ? (whole_row + kSub - 1) / kSub : steps_end);
+    const int masked_end = (int)(whole_row < seq.rows ? (whole_row + ROWS - 1) / ROWS : steps_end);
 
-    char *own = smem + rg * 2 * STAGE;
+    char *own = smem + rg * RING * STAGE;
+    const bool describes = wave == 0 && lane < ROWS;                        // this lane brings what a row's offset is and how many keys it sees
     float lse_next = 0.f;
     int sees_next = 0;
+    const int r = lane / (D / 8), pos = lane % (D / 8);                     // of a DMA instruction: the lane's row and place
+    const uint32_t swizzled = (uint32_t)((pos ^ L::turn(r)) << 4);
+    // Where the group's size is a power of two that divides 32, the rows of a DMA instruction follow each other alike whichever it is: their first one's place is worked out in scalar
+    // registers.
+    const char *q_head = p.q.data + (int64_t)seq.q0 * p.q.token + (int64_t)(kv * p.g) * p.q.head;
+    const uint32_t even_off = p.even ? (uint32_t)((r >> p.g_shift) * (int)p.q.token + (r & (int)(p.g - 1)) * (int)p.q.head) + swizzled : 0;
+    const float *even_lse = p.lse + (int64_t)(kv * p.g + (p.even ? lane & (int)(p.g - 1) : 0)) * p.tokens + seq.q0 + (lane >> p.g_shift);
+    // What describes the rows comes into registers, older than the stage's DMA; a step later it is there and goes to LDS, where it is read a step after that.
     auto issue = [&](int stage, int step) __attribute__((always_inline)) {
         if (step >= steps_end) return;
-        const int first = step * kSub;
-#pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int group = PER_WAVE * wave + i;
-            if (L::Groups / KW == 0 && group >= L::Groups) break;
-            const int R = first + group * L::GroupRows + lane / (D / 8);
-            const char *from = weight_row((uint32_t)(R < seq.rows ? R : seq.rows - 1), seq, kv, p).q;
-            const int pos = lane % (D / 8), r = lane / (D / 8);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + ((pos ^ L::turn(r)) << 4)), STA_LDS_PTR(own + stage * STAGE + group * L::Group), 16,
-                                             0, 0);
+        const bool even = p.even && (step + 1) * ROWS <= seq.rows;
+        if (describes) {
+            if (even) {
+                lse_next = even_lse[(uint32_t)(step * ROWS) >> p.g_shift];
+                if (step < masked_end) sees_next = seq.keys_of((step * ROWS + lane) >> p.g_shift, p.causal);
+            } else {
+                const int R = step * ROWS + lane;
+                const WeightRow w = weight_row((uint32_t)(R < seq.rows ? R : seq.rows - 1), seq, kv, p);
+                lse_next = R < seq.rows ? *w.lse : -INFINITY;
+                sees_next = R < seq.rows ? seq.keys_of(w.token, p.causal) : 0;
+            }
         }
-        if (wave == 0 && lane < kSub) {
-            const int R = first + lane;
-            const WeightRow w = weight_row((uint32_t)(R < seq.rows ? R : seq.rows - 1), seq, kv, p);
-            lse_next = R < seq.rows ? *w.lse : -INFINITY;
-            sees_next = R < seq.rows ? seq.keys_of(w.token, p.causal) : 0;
+        if (even) {
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int group = PER_WAVE * wave + i, R = step * ROWS + group * L::GroupRows;
+                const char *from = q_head + (int64_t)(R >> p.g_shift) * p.q.token + (int64_t)(R & (int)(p.g - 1)) * p.q.head;
+                uint32_t o = even_off;
+                asm volatile("" : "+v"(o));                                 // a 32-bit lane offset next to a scalar base
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + o), STA_LDS_PTR(own + stage * STAGE + group * L::Group), 16, 0, 0);
+            }
+            asm volatile("; even" ::: "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int group = PER_WAVE * wave + i, R = step * ROWS + group * L::GroupRows + r;
+                const char *from = weight_row((uint32_t)(R < seq.rows ? R : seq.rows - 1), seq, kv, p).q + swizzled;       // rows beyond the last one are read as it
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, STA_LDS_PTR(own + stage * STAGE + group * L::Group), 16, 0, 0);
+            }
+            asm volatile("; any" ::: "memory");
         }
     };
+    auto describe = [&](int stage) __attribute__((always_inline)) {
+        if (!describes) return;
+        *reinterpret_cast<float *>(own + stage * STAGE + ROWS_AT + 4 * lane) = offset_of(lse_next);
+        *reinterpret_cast<int *>(own + stage * STAGE + ROWS_AT + 4 * ROWS + 4 * lane) = sees_next;
+    };
+    const int n_steps = (steps_end - step0 + RG - 1) / RG;                  // of every group
     issue(0, step0 + rg);
-    bf16x8 K[4][D / 32];
-    load_keys<D>(p, row, kv, key0, seq.lk, lane, K);
+    describe(0);
+    if (RING == 3) issue(1, step0 + rg + RG);
+    bf16x8 K[NC][D / 32];
+    const OwnKey own_key = load_keys<D, NC>(p, s, kv, key0, seq.lk, lane, K);
+    // Waited for here: at their first use in the loop the compiler would wait for all that is on its way, stages among it, every time.
+#pragma unroll
+    for (int col = 0; col < NC; ++col)
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) asm volatile("" : "+v"(K[col][ks]));
     const uint32_t base = (uint32_t)(uintptr_t)own, q_addr = L::address(base, lane), row_addr = base + ROWS_AT + 16 * g4;
     const float c = p.scale_log2e;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f}, part[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[NC] = {}, part[NC] = {};
     int folded = 0;
-    auto step = [&](auto stage_c, int at) __attribute__((always_inline)) {
-        constexpr int ST = decltype(stage_c)::value;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (wave == 0 && lane < kSub) {
-            *reinterpret_cast<float *>(own + ST * STAGE + ROWS_AT + 4 * lane) = offset_of(lse_next);
-            *reinterpret_cast<int *>(own + ST * STAGE + ROWS_AT + 4 * kSub + 4 * lane) = sees_next;
+    int stage = 0;
+#pragma unroll 1
+    for (int i = 0; i < n_steps; ++i) {
+        const int at = step0 + rg + RG * i, next = stage + 1 < RING ? stage + 1 : 0, after = next + 1 < RING ? next + 1 : 0;
+        // This wave's part of the stage has landed, the next one's may be on its way; what describes that is older than its DMA.
+        if (RING == 3 && at + RG < steps_end) {
+            wait_dma<PER_WAVE>();
+            asm volatile("" : "+v"(lse_next));
+        } else {
+            wait_dma<0>();
+            asm volatile("" : "+v"(lse_next));
         }
-        __syncthreads();
-        issue(ST ^ 1, at + RG);
+        if (RING == 3) describe(next);                      // (where there is no next stage nobody reads it)
+        else if (i > 0) describe(stage);
+        __syncthreads();                                    // ... and everyone's, and nobody reads the stage before any more
+        issue(RING == 3 ? after : next, at + (RING - 1) * RG);
         if (at < steps_end && key0 < seq.lk) {
-            floatx4 S[2][4];
-#pragma unroll
-            for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-                for (int col = 0; col < 4; ++col) S[rb][col] = floatx4{0.f, 0.f, 0.f, 0.f};
-            bf16x8 o0 = ds_read_b128_at<ST * STAGE>(row_addr), o1 = ds_read_b128_at<ST * STAGE + 64>(row_addr);
-            bf16x8 l0 = ds_read_b128_at<ST * STAGE + 4 * kSub>(row_addr), l1 = ds_read_b128_at<ST * STAGE + 4 * kSub + 64>(row_addr);
-            rows_times_resident<D, ST * STAGE, 4, 4>(q_addr, K, S);
-            lds_wait2<0>(o0, o1);
-            lds_wait2<0>(l0, l1);
-            typedef int intx4 __attribute__((ext_vector_type(4)));
-            const floatx4 offset[2] = {__builtin_bit_cast(floatx4, o0), __builtin_bit_cast(floatx4, o1)};
-            const intx4 sees[2] = {__builtin_bit_cast(intx4, l0), __builtin_bit_cast(intx4, l1)};
-            const bool masked = at < masked_end;
-#pragma unroll
-            for (int col = 0; col < 4; ++col) {
-                float e[2][4];
-#pragma unroll
-                for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) e[rb][r] = __builtin_amdgcn_exp2f(fmaf(S[rb][col][r], c, -offset[rb][r]));
-                if (masked) {
-                    const int key = key0 + 16 * col + (lane & 15);
-#pragma unroll
-                    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) e[rb][r] = key < sees[rb][r] ? e[rb][r] : 0.f;
-                }
-                part[col] += ((e[0][0] + e[0][1]) + (e[0][2] + e[0][3])) + ((e[1][0] + e[1][1]) + (e[1][2] + e[1][3]));
-            }
+            const uint32_t q_now = q_addr + (uint32_t)(stage * STAGE), row_now = row_addr + (uint32_t)(stage * STAGE);
+            if (at < masked_end) add_rows<D, NC, 2 * U, true, 0, 0, 4 * ROWS>(q_now, row_now, K, c, key0 + (lane & 15), part);
+            else add_rows<D, NC, 2 * U, false, 0, 0, 4 * ROWS>(q_now, row_now, K, c, key0 + (lane & 15), part);
             if (++folded == FOLD) {
                 folded = 0;
 #pragma unroll
-                for (int col = 0; col < 4; ++col) {
+                for (int col = 0; col < NC; ++col) {
                     sum[col] += part[col];
                     part[col] = 0.f;
                 }
             }
         }
-    };
-    const int n_steps = (steps_end - step0 + RG - 1) / RG;          // of every group
-#pragma unroll 1
-    for (int i = 0; i < n_steps; i += 2) {
-        step(std::integral_constant<int, 0>{}, step0 + rg + RG * i);
-        if (i + 1 < n_steps) step(std::integral_constant<int, 1>{}, step0 + rg + RG * (i + 1));
+        stage = next;
     }
 #pragma unroll
-    for (int col = 0; col < 4; ++col) sum[col] += part[col];
+    for (int col = 0; col < NC; ++col) sum[col] += part[col];
     if constexpr (RG > 1) {                                         // the groups' sums, in ascending order
 #pragma unroll
-        for (int col = 0; col < 4; ++col) joined[rg][wave * kKeys + 16 * col + (lane & 15)][g4] = sum[col];
+        for (int col = 0; col < NC; ++col) joined[rg][wave * OWN + 16 * col + (lane & 15)][g4] = sum[col];
         __syncthreads();
         if (rg > 0) return;
 #pragma unroll
-        for (int col = 0; col < 4; ++col) {
+        for (int col = 0; col < NC; ++col) {
             sum[col] = 0.f;
 #pragma unroll
-            for (int g = 0; g < RG; ++g) sum[col] += joined[g][wave * kKeys + 16 * col + (lane & 15)][g4];
+            for (int g = 0; g < RG; ++g) sum[col] += joined[g][wave * OWN + 16 * col + (lane & 15)][g4];
         }
     }
-    if (key0 < seq.lk) store_weights(p, row, kv, key0, seq.lk, lane, sum);
+    if (key0 < seq.lk) store_weights(p, own_key, lane, sum);
 }
 
+// Four waves along the keys where that makes two workgroups a CU, two waves by two groups where that does, or where walks are of 512 rows at most and three quarters of the CUs
+// have one, else one wave by four groups.  us, four | two | one along the keys, new tokens on keys of heads / key heads x channels:
+//   512 on 20,001, 32/8 x 128 (632 | 1256 | 2504 workgroups)  107 | 105 | 142       2048 on 16,384, 32/8 x 128 (512 | 1024 | 2048)  259 | 287 | 353
+//   300 on 1300 and 1000 on 5000, 8/8 x 128 (320 | 640 | 1264)  25.6 | 23.5 | 27.9  four of 200 on 3000, 40/8 x 64 (384 | 768 | 1504)  37 | 31 | 35
+//   512 on 4000, 32/8 x 128 (128 | 256 | 504)  49 | 35 | 31       300 on 9000, 16/2 x 128 (72 | 142 | 282)  65 | 40 | 34
+//   eight of 64 on 1300, 40/5 x 128 (240 | 440 | 840)  18.8 | 18.1 | 24.6       50 on 30,000, 8/1 x 128 (118 | 235 | 469)  15.2 | 11.3 | 13.0
 struct WeightsPlan {
     int few;                            // blocks of 16 rows, 0: stages
     int along;                          // waves of a workgroup along the keys
@@ -308,21 +424,25 @@ WeightsPlan weights_plan(int S, int Hkv, int64_t rows, int max_k)
     plan.workgroups = heads;
     if (heads > kMostWorkgroups) return plan;               // too many whatever the tiles are
     plan.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
-    plan.along = plan.few || tiles(256) * heads >= 2 * cus ? 4 : tiles(128) * heads >= 2 * cus ? 2 : 1;
+    plan.along = plan.few || tiles(256) * heads >= 2 * cus ? 4 : tiles(128) * heads >= (rows <= 512 ? 3 * cus / 4 : 2 * cus) ? 2 : 1;
     plan.tiles = tiles(64 * plan.along);
     plan.workgroups = plan.tiles * heads;
     return plan;
 }
 
+template <int D, int NC, int KW, int U>
+hipError_t launch_stages(const WeightsParams &p, uint32_t workgroups, hipStream_t stream)
+{
+    return sta::launch_kernel(sta_paged_weights_kernel<D, NC, KW, U>, dim3(workgroups), dim3(256), stream, p);
+}
+
 template <int D>
 hipError_t launch_weights(const WeightsParams &p, const WeightsPlan &plan, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)plan.workgroups), block(256);
-    if (plan.few == 1) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 1>, grid, block, stream, p);
-    if (plan.few == 2) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 2>, grid, block, stream, p);
-    if (plan.along == 4) return sta::launch_kernel(sta_paged_weights_kernel<D, 4>, grid, block, stream, p);
-    if (plan.along == 2) return sta::launch_kernel(sta_paged_weights_kernel<D, 2>, grid, block, stream, p);
-    return sta::launch_kernel(sta_paged_weights_kernel<D, 1>, grid, block, stream, p);
+    const uint32_t n = (uint32_t)plan.workgroups;
+    if (plan.few == 1) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 1>, dim3(n), dim3(256), stream, p);
+    if (plan.few == 2) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 2>, dim3(n), dim3(256), stream, p);
+    return plan.along == 4 ? launch_stages<D, 4, 4, 2>(p, n, stream) : plan.along == 2 ? launch_stages<D, 4, 2, 1>(p, n, stream) : launch_stages<D, 4, 1, 1>(p, n, stream);
 }
 
 }  // namespace
@@ -370,6 +490,8 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     p.by_g = sta::fast_div_of(p.g);
     p.by_Hkv = sta::fast_div_of(p.Hkv);
     p.causal = causal != 0;
+    p.even = (p.g & (p.g - 1)) == 0 && p.g <= 32 && q->head < (int64_t)1 << 25;
+    p.g_shift = p.even ? (uint32_t)__builtin_ctz(p.g) : 0;
     p.by_tiles = sta::fast_div_of((uint32_t)plan.tiles);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = D == 64 ? launch_weights<64>(p, plan, stream) : launch_weights<128>(p, plan, stream);
