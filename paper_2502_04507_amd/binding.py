@@ -3,7 +3,7 @@
 Tensors are torch tensors used purely as device-memory handles (data_ptr);
 the stream is torch's current HIP stream unless one is given.
 
-The permutations, sta_forward, sta_forward_lse and sta_backward (and the operators of layer_ops) go through the extension sta_fastcall where their
+The permutations, sta_forward, sta_forward_lse and sta_backward (and the operators of layer_ops and paged_ops) go through the extension sta_fastcall where their
 arguments are ordinary ones, everything else (and every error message) through ctypes; without the extension, with a warning, everything.
 """
 import ctypes
@@ -108,11 +108,14 @@ def load_library():
 _FAST_ENTRIES = ("sta_tile_permute", "sta_untile", "sta_forward", "sta_forward_lse", "sta_backward")
 _FAST_LAYER_ENTRIES = ("sta_rope", "sta_qk_norm_rope", "sta_qk_norm_rope_backward", "sta_packed_forward", "sta_packed_backward")
 
+_FAST_PAGED_ENTRIES = ("sta_paged_append", "sta_paged_forward", "sta_paged_weights", "sta_paged_evict")
+
 
 class _GeneralPath:
     """Stands for the extension where it cannot be loaded: leaves every call to the general path."""
     tile_permute = untile = forward = forward_lse = backward = staticmethod(lambda *args: None)
     rope = norm_rope = norm_rope_backward = packed_forward = packed_backward = tile_permute
+    paged_append = paged_forward = paged_weights = paged_evict = tile_permute
 
 
 def _load_fast():
@@ -126,6 +129,7 @@ def _load_fast():
     if _raw_stream is not None and _current_device is not None:     # unbound, it leaves every call to the general path
         fast.bind(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _FAST_ENTRIES], _current_device, _raw_stream)
         fast.bind_layers(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _FAST_LAYER_ENTRIES])
+        fast.bind_paged(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _FAST_PAGED_ENTRIES])
     return fast
 
 

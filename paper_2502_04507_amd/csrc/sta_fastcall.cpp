@@ -502,6 +502,169 @@ PyObject *py_packed_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---- a cache in pages; us per call of the smallest calls one after the other, ctypes against this: sta_paged_append 7.1, 4.0; sta_paged_forward 7.5, 4.5;
+// sta_paged_weights 7.4, 4.3
+struct PagedEntries {
+    decltype(&sta_paged_append) append;
+    decltype(&sta_paged_forward) forward;
+    decltype(&sta_paged_weights) weights;
+    decltype(&sta_paged_evict) evict;
+} paged = {};
+
+// (address of a sta_paged_cache, sequences, key heads, channels, pages, slots of a page), as the cache's object keeps them
+struct CacheArg {
+    const sta_paged_cache *c;
+    int64_t S, Hkv, D, pages, page_size;
+};
+bool cache_of(PyObject *o, CacheArg &a)
+{
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 6) return false;
+    long long x[5];
+    a.c = static_cast<const sta_paged_cache *>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(o, 0)));
+    for (int i = 0; i < 5; ++i) x[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, i + 1));
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    a = {a.c, x[0], x[1], x[2], x[3], x[4]};
+    return a.c != nullptr && small(a.S) && small(a.Hkv) && small(a.D);
+}
+// Numbers of all keys of the pool, dense float32 [pages, Hkv, page_size]; None: null.
+bool key_numbers(PyObject *o, const CacheArg &a, const void *&out)
+{
+    out = nullptr;
+    if (o == Py_None) return true;
+    View v;
+    if (!dense(o, v) || v.t->dim() != 3 || v.t->size(0) != a.pages || v.t->size(1) != a.Hkv || v.t->size(2) != a.page_size || v.t->scalar_type() != at::kFloat)
+        return false;
+    out = v.ptr;
+    return out != nullptr;
+}
+// A device tensor [tokens, heads, D] of bf16 or float32 whose channels are adjacent.
+bool new_rows(PyObject *o, int64_t tokens, const CacheArg &a, sta_head_rows &r)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() != 3 || t.numel() == 0) return false;
+    const auto size = t.sizes(), stride = t.strides();
+    const auto type = t.scalar_type();
+    if (size[0] != tokens || size[1] != a.Hkv || size[2] != a.D || stride[2] != 1 || (type != at::kBFloat16 && type != at::kFloat)) return false;
+    r = {t.data_ptr(), 0, stride[0], stride[1], (int)a.Hkv, type == at::kBFloat16 ? kBf16 : kF32};
+    return true;
+}
+bool tokens_and_heads(PyObject *o, int64_t &tokens, int64_t &heads)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.dim() != 3) return false;
+    tokens = t.size(0);
+    heads = t.size(1);
+    return small(tokens) && small(heads);
+}
+
+// (k, v, cu, cache, max_new, weights)
+PyObject *py_paged_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        CacheArg a;
+        sta_head_rows k, v;
+        int64_t tokens, heads;
+        const void *cu, *weights;
+        int max_new;
+        void *stream;
+        if (!paged.append || n != 6 || !cache_of(args[3], a) || !tokens_and_heads(args[0], tokens, heads) || !new_rows(args[0], tokens, a, k) ||
+            !new_rows(args[1], tokens, a, v) || args[2] == Py_None || !vector(args[2], a.S + 1, at::kInt, cu) || !integer(args[4], max_new) ||
+            !key_numbers(args[5], a, weights))
+            Py_RETURN_NONE;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return paged.append(&k, &v, tokens, static_cast<const int32_t *>(cu), a.c, (int)a.S, max_new, (int)a.D, static_cast<float *>(const_cast<void *>(weights)),
+                                stream);
+        });
+    });
+}
+
+// (q, o, cu_q, cache, max_q, max_k, causal, scale, lse, workspace)
+PyObject *py_paged_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        CacheArg a;
+        PackedShape s = {};
+        sta_head_rows q, o;
+        const void *cu, *lse;
+        int max_q, max_k;
+        float scale;
+        void *ws, *stream;
+        size_t bytes;
+        if (!paged.forward || n != 10 || !cache_of(args[3], a) || !tokens_and_heads(args[0], s.tq, s.Hq) || !packed_rows(args[0], s.tq, s.Hq, a.D, q) ||
+            !packed_rows(args[1], s.tq, s.Hq, a.D, o) || args[2] == Py_None || !vector(args[2], a.S + 1, at::kInt, cu) || !integer(args[4], max_q) ||
+            !integer(args[5], max_k) || !PyBool_Check(args[6]) || !number(args[7], scale) || !packed_lse(args[8], s, lse) || !scratch(args[9], ws, bytes))
+            Py_RETURN_NONE;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return paged.forward(&q, &o, static_cast<float *>(const_cast<void *>(lse)), s.tq, static_cast<const int32_t *>(cu), a.c, (int)a.S, max_q, max_k, (int)a.D,
+                                 args[6] == Py_True, scale, ws, bytes, stream);
+        });
+    });
+}
+
+// (q, lse, weights, cu_q, cache, max_q, max_k, before, decay, causal, scale)
+PyObject *py_paged_weights(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        CacheArg a;
+        PackedShape s = {};
+        sta_head_rows q;
+        const void *cu, *lse, *before, *weights;
+        int max_q, max_k;
+        float decay, scale;
+        void *stream;
+        if (!paged.weights || n != 11 || !cache_of(args[4], a) || !tokens_and_heads(args[0], s.tq, s.Hq) || !packed_rows(args[0], s.tq, s.Hq, a.D, q) ||
+            args[1] == Py_None || !packed_lse(args[1], s, lse) || args[2] == Py_None || !key_numbers(args[2], a, weights) || args[3] == Py_None ||
+            !vector(args[3], a.S + 1, at::kInt, cu) || !integer(args[5], max_q) || !integer(args[6], max_k) || !key_numbers(args[7], a, before) ||
+            !number(args[8], decay) || !PyBool_Check(args[9]) || !number(args[10], scale))
+            Py_RETURN_NONE;
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return paged.weights(&q, static_cast<const float *>(lse), s.tq, static_cast<const int32_t *>(cu), a.c, (int)a.S, max_q, max_k, (int)a.D,
+                                 args[9] == Py_True, scale, static_cast<const float *>(before), decay, static_cast<float *>(const_cast<void *>(weights)), stream);
+        });
+    });
+}
+
+// (cache, weights, into, into_weights, kept, first, recent)
+PyObject *py_paged_evict(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        CacheArg a, b;
+        const void *weights, *into_weights;
+        View kept;
+        int first, recent;
+        void *stream;
+        if (!paged.evict || n != 7 || !cache_of(args[0], a) || !cache_of(args[2], b) || a.S != b.S || a.Hkv != b.Hkv || a.D != b.D || args[1] == Py_None ||
+            !key_numbers(args[1], a, weights) || !key_numbers(args[3], b, into_weights) || !dense(args[4], kept) || kept.t->dim() != 3 || kept.t->size(0) != a.S ||
+            kept.t->size(1) != a.Hkv || !small(kept.t->size(2)) || kept.t->scalar_type() != at::kInt || !integer(args[5], first) || !integer(args[6], recent))
+            Py_RETURN_NONE;
+        const int keep = (int)kept.t->size(2);
+        if (!stream_of(stream)) return nullptr;
+        return status_of([&]() {
+            return paged.evict(a.c, static_cast<const float *>(weights), b.c, static_cast<float *>(const_cast<void *>(into_weights)), static_cast<int32_t *>(kept.ptr),
+                               (int)a.S, keep, first, recent, (int)a.D, stream);
+        });
+    });
+}
+
+// (addresses of the four entry points in the order of PagedEntries); the streams are bind's
+PyObject *py_bind_paged(PyObject *, PyObject *args)
+{
+    unsigned long long a[4];
+    if (!PyArg_ParseTuple(args, "KKKK", &a[0], &a[1], &a[2], &a[3])) return nullptr;
+    if (current_device && current_raw_stream)
+        paged = {reinterpret_cast<decltype(&sta_paged_append)>(a[0]), reinterpret_cast<decltype(&sta_paged_forward)>(a[1]),
+                 reinterpret_cast<decltype(&sta_paged_weights)>(a[2]), reinterpret_cast<decltype(&sta_paged_evict)>(a[3])};
+    Py_RETURN_NONE;
+}
+
 // (addresses of the five entry points in the order of LayerEntries); the streams are bind's
 PyObject *py_bind_layers(PyObject *, PyObject *args)
 {
@@ -536,7 +699,8 @@ PyObject *py_bind(PyObject *, PyObject *args)
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, nullptr}, STA_FAST(tile_permute), STA_FAST(untile), STA_FAST(forward), STA_FAST(forward_lse),
     STA_FAST(backward), {"bind_layers", py_bind_layers, METH_VARARGS, nullptr}, STA_FAST(rope), STA_FAST(norm_rope), STA_FAST(norm_rope_backward),
-    STA_FAST(packed_forward), STA_FAST(packed_backward), {nullptr, nullptr, 0, nullptr},
+    STA_FAST(packed_forward), STA_FAST(packed_backward), {"bind_paged", py_bind_paged, METH_VARARGS, nullptr}, STA_FAST(paged_append), STA_FAST(paged_forward),
+    STA_FAST(paged_weights), STA_FAST(paged_evict), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "sta_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

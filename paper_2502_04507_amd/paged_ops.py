@@ -5,8 +5,7 @@ import ctypes
 
 import torch
 
-from .binding import STA_BF16, STA_F32, _check, _dev, _stream_ptr
-from .binding import load_library
+from .binding import STA_BF16, STA_F32, _check, _dev, _fast, _stream_ptr, load_library
 from .layer_ops import _HeadRows, _bounds, _int32, _lse_ptr, _packed_counts, _packed_rows
 
 
@@ -62,6 +61,8 @@ class StaPagedCache:
         self._c = _PagedCache(_HeadRows(k.data_ptr() or 16, page, token, head, heads, STA_BF16), _HeadRows(v.data_ptr() or 16, page, token, head, heads, STA_BF16),
                               self.pages, _int32(self.page_size, "the page size"), table.data_ptr() or 16, table.stride(0), _int32(table.shape[1], "the pages of a row"),
                               _dev(used, "used") or 16)
+        # for the extension: where the struct is, and what goes with it
+        self._at = (ctypes.addressof(self._c), self.S, heads, self.D, self.pages, self.page_size)
 
     @property
     def room(self):
@@ -81,6 +82,11 @@ def _weights_ptr(w, cache, name):
 def sta_paged_append(k, v, cu, cache, max_new, weights=None, stream=None):
     """New rows k, v (bf16 or float32 [tokens, Hkv, D], strided views with adjacent channels) into their pages: cu int32 [S + 1] where the sequences' tokens
     begin; cache.used counts them already; weights float32 [pages, Hkv, page_size] or None, set to 0 for the new keys; max_new: upper bound of a sequence's tokens."""
+    if stream is None:
+        status = _fast().paged_append(k, v, cu, cache._at, max_new, weights)
+        if status is not None:
+            _check(status)
+            return cache
     rows = []
     for t, name in ((k, "k"), (v, "v")):
         if t.dim() != 3 or t.shape != (k.shape[0], cache.Hkv, cache.D):
@@ -116,6 +122,11 @@ def _paged_queries(q, cu_q, cache, max_q, max_k):
 def sta_paged_forward(q, o, cu_q, cache, max_q, max_k, causal=True, scale=0.0, lse=None, workspace=None, stream=None):
     """sta_packed_forward against a cache in pages: q, o bf16 [tokens, Hq, D], cu_q int32 [S + 1]; lse float32 [Hq, tokens] or None; max_q, max_k upper bounds of
     the sequences' tokens and keys; workspace: device bytes, at least sta_paged_workspace_bytes(...), or None."""
+    if stream is None:
+        status = _fast().paged_forward(q, o, cu_q, cache._at, max_q, max_k, causal, scale, lse, workspace)
+        if status is not None:
+            _check(status)
+            return o
     tq, Hq, max_q, max_k = _paged_queries(q, cu_q, cache, max_q, max_k)
     ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
     _check(_lib().sta_paged_forward(_packed_rows(q, "q", tq, Hq, cache.D), _packed_rows(o, "o", tq, Hq, cache.D), _lse_ptr(lse, Hq, tq), tq,
@@ -127,6 +138,11 @@ def sta_paged_forward(q, o, cu_q, cache, max_q, max_k, causal=True, scale=0.0, l
 def sta_paged_weights(q, lse, weights, cu_q, cache, max_q, max_k, before=None, decay=1.0, causal=True, scale=0.0, stream=None):
     """What every key of the cache gathers from these rows, added to decay times before (None: nothing; may be weights): weights float32 [pages, Hkv, page_size];
     q bf16 [tokens, Hq, D] and lse float32 [Hq, tokens] as sta_paged_forward had and wrote them."""
+    if stream is None:
+        status = _fast().paged_weights(q, lse, weights, cu_q, cache._at, max_q, max_k, before, decay, causal, scale)
+        if status is not None:
+            _check(status)
+            return weights
     tq, Hq, max_q, max_k = _paged_queries(q, cu_q, cache, max_q, max_k)
     if lse is None or weights is None:
         raise ValueError("lse and weights are needed")
@@ -139,6 +155,11 @@ def sta_paged_weights(q, lse, weights, cu_q, cache, max_q, max_k, before=None, d
 def sta_paged_evict(cache, weights, into, into_weights, kept, first=0, recent=0, stream=None):
     """Keeps of every sequence and key head kept.shape[2] keys: the first and recent ones, and of the others those of the greatest weights.  Their rows go to the pages of
     into, another StaPagedCache whose used is written; their weights to into_weights (or None); kept int32 [S, Hkv, keep]: which they were, -1 where there are fewer."""
+    if stream is None:
+        status = _fast().paged_evict(cache._at, weights, into._at, into_weights, kept, first, recent)
+        if status is not None:
+            _check(status)
+            return into
     if into.S != cache.S or into.Hkv != cache.Hkv or into.D != cache.D:
         raise ValueError("both caches must have the same sequences, heads and channels")
     if kept.dtype != torch.int32 or kept.dim() != 3 or kept.shape[:2] != (cache.S, cache.Hkv):
