@@ -105,13 +105,34 @@ struct KeysOf<PagedParams, D> {
     }
 };
 
+// As launches of packed sequences are cut, but where those are tiles of 64 rows by two groups that are not cut along the keys, and some walks are likely to be much longer than others (three quarters at
+// most of the tokens that S sequences of max_q would have, and 96 sub-blocks of keys or more), or a CU has less than one of them (and 64 sub-blocks): then tiles of 32 rows by four groups, which walk half
+// as long.  us, two groups | four | two, cut after 48 sub-blocks; heads / key heads x channels, new tokens on keys:
+//   15/5 x 64, 333, 1, 2048, 65, 1, 578 on 1333, 4097, 2048, 3001, 77, 578   45 | 38 | 43       32/8 x 128, 100, 1, 1, 1, 700 on 2000, 5000, 3000, 8000, 700   100 | 55 | 49
+//   16/16 x 64, 333, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578             67 | 49 | 55       12/4 x 128, 500, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578   87 | 68 | 74
+//   8/8 x 128, three of 512 on 512, 1000, 3000                               42 | 26 | 31
+// and where they stay: 40/8 x 128, 40 of 1 on 1000 and 300 on 1300  34 | 49 | 35; 32/8 x 128, four of 256 on 4096  80 | 124 | 117; 16 of 64 on 3000  64 | 128 | 97; 2048 on 4096  122 | 196 | 169.
+bool paged_plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
+{
+    if (!plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, cut, plan)) return false;
+    if (plan->few || plan->waves != 2 || plan->parts > 1) return true;
+    const int64_t subs = ((int64_t)max_k + kSub - 1) / kSub, items = (int64_t)plan->slots * Hkv;
+    const bool uneven = subs >= 96 && 4 * tokens_q <= 3 * (int64_t)S * max_q, sparse = subs >= 64 && items < sta::compute_units();
+    if (!uneven && !sparse) return true;
+    const int64_t slots = tiles_of(tokens_q, Hq / Hkv, S, max_q, 32);
+    if (slots * Hkv > kMostWorkgroups) return true;
+    plan->waves = 1;
+    plan->slots = (uint32_t)slots;
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
 {
-    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);
+    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);       // what is not cut there is not cut here
 }
 
 int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
@@ -131,7 +152,7 @@ int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse
     const size_t lse_bytes = (size_t)tokens_q * q->heads * sizeof(float);
     if (rows_overlap(*o, tokens_q, *q, tokens_q, 1, D) || rows_in_pages(*cache, D, *o, tokens_q)) return STA_ERR_ALIAS;
     PackedPlan plan;
-    if (!plan_of(q->heads, Hkv, D, S, tokens_q, max_q, max_k, workspace != nullptr, &plan)) return STA_ERR_SHAPE;
+    if (!paged_plan_of(q->heads, Hkv, D, S, tokens_q, max_q, max_k, workspace != nullptr, &plan)) return STA_ERR_SHAPE;
     if (workspace && (((uintptr_t)workspace & 15) || workspace_bytes < plan.workspace() * sizeof(float))) return STA_ERR_WORKSPACE;
     const struct { const void *at; uint64_t bytes; } ranges[2] = {{workspace, workspace_bytes}, {lse, lse_bytes}};
     const PackedBounds bounds = {cu_q, nullptr, nullptr, S};

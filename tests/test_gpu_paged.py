@@ -54,6 +54,25 @@ def test_the_same_as_keys_side_by_side_and_the_definition(case, lse):
             assert bool(((z[:, a].cpu().double() - want[1]).abs() <= b_lse).all()), s
 
 
+def test_walks_of_uneven_lengths():
+    """Tiles by four groups where those of packed sequences are by two: other orders of sums, so against the definition alone, and the same whatever the pages are."""
+    Hq, Hkv, D, new, used = 24, 24, 64, [300, 1, 1, 200], [3100, 3000, 50, 200]
+    cache = Cache(Hkv, D, 24, used, seed=5)
+    q = randn((sum(new), Hq, D), 3)
+    o, z = forward(q.to(DEV), cache, new, lse=True)
+    other = Cache(Hkv, D, 64, used, seed=6, layout="heads", keys=(cache.k, cache.v))
+    for a, b in zip((o, z), forward(q.to(DEV), other, new, lse=True)):
+        assert same(a, b)
+    cu = starts(new)
+    for s in range(len(new)):
+        a = slice(cu[s], cu[s] + new[s])
+        Q, K, V = q[a].double(), cache.k[s].double(), cache.v[s].double()
+        want = lu.attention(Q, K, V, True, D ** -0.5)
+        b_o, b_lse, _ = bounds(Q, K, V, True, D ** -0.5, want[1])
+        close(o[a], want[0], b_o, "sequence %d" % s)
+        assert bool(((z[:, a].cpu().double() - want[1]).abs() <= b_lse).all()), s
+
+
 @pytest.mark.parametrize("layout", ["tokens", "heads", "halves"])
 @pytest.mark.parametrize("page", [1, 4, 5, 8, 32, 33, 128])
 @pytest.mark.parametrize("D", [64, 128])
