@@ -5,7 +5,8 @@
 // sta_paged_select_kernel  a workgroup for each sequence and key head finds the smallest weight that stays, twelve, ten and ten bits of its place in the order of
 //                          numbers at a time, by counting how many have which; then writes down in order which keys stay.  Bound by the instructions and LDS of the one CU that a head has:
 //                          8 heads of 32,768 keys 23 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 4 the others, 2.5 to count and 5 to write down).
-// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 82 us, 4.8 TB/s.
+// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 78 us, 5.0 TB/s
+//                          (82 with stores through the caches).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -39,6 +40,15 @@ __device__ __forceinline__ u32x4 eight_of(const char *at)
         r[4 + i] = static_cast<__bf16>(b[i]);
     }
     return __builtin_bit_cast(u32x4, r);
+}
+
+// 16 bytes of a row; STREAM: past the caches, where more is written than they hold.
+constexpr int64_t kCaches = (int64_t)32 << 20;              // the L2 caches of the eight XCDs
+template <bool STREAM>
+__device__ __forceinline__ void store_row(char *to, u32x4 x)
+{
+    if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<u32x4 *>(to));
+    else *reinterpret_cast<u32x4 *>(to) = x;
 }
 
 template <int D, bool F32, bool STREAM>
@@ -76,10 +86,7 @@ __global__ __launch_bounds__(256) void sta_paged_append_kernel(AppendParams p)
             }
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
-                if (to[j]) {
-                    if (STREAM) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4 *>(to[j]));
-                    else *reinterpret_cast<u32x4 *>(to[j]) = x[j];
-                }
+                if (to[j]) store_row<STREAM>(to[j], x[j]);
         }
     }
 }
@@ -325,7 +332,7 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
 }
 
 // One row a lane: two and four at once, whose addresses and data leave room for fewer waves, took 86 and 96 us where one takes 81 (24 sequences, 8 heads, 2048 rows each).
-template <int D>
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void sta_paged_move_kernel(EvictParams p)
 {
     constexpr int LPR = D / 8, ROWS = 256 / LPR;
@@ -340,8 +347,8 @@ __global__ __launch_bounds__(256) void sta_paged_move_kernel(EvictParams p)
     const uint32_t page = page_inside(p.from.table[(int64_t)s * p.from.table_row + entry_of(key, p.from, &slot)], p.from);
     const uint64_t at = place_of(page, slot, p.from) + (int64_t)h * p.from.head + 16 * c, to = place_of((uint32_t)to_page, to_slot, p.to) + (int64_t)h * p.to.head + 16 * c;
     const u32x4 k = *reinterpret_cast<const u32x4 *>(p.from.k + at), v = *reinterpret_cast<const u32x4 *>(p.from.v + at);
-    *reinterpret_cast<u32x4 *>(p.to.k + to) = k;
-    *reinterpret_cast<u32x4 *>(p.to.v + to) = v;
+    store_row<STREAM>(p.to.k + to, k);
+    store_row<STREAM>(p.to.v + to, v);
     if (c == 0 && p.to_weights)
         p.to_weights[((uint64_t)to_page * p.Hkv + h) * p.to.by_page.d + to_slot] = p.weights[((uint64_t)page * p.Hkv + h) * p.from.by_page.d + slot];
 }
@@ -425,9 +432,9 @@ extern "C" int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, 
     const int64_t longest = max_new < tokens ? max_new : tokens, want = (longest + p.each - 1) / p.each, most = S < 16384 ? 16384 / S : 1;
     p.per_seq = (uint32_t)(want < most ? want : most);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    // What does not fit the L2 caches (32 MB) goes past them: 12,366 tokens of 8 heads from float32 29.8 -> 24.4 us.  What fits is read from there by the attention that follows: 2048 tokens and their
+    // What does not fit the caches goes past them: 12,366 tokens of 8 heads from float32 29.8 -> 24.4 us.  What fits is read from there by the attention that follows: 2048 tokens and their
     // attention, 32 heads over 8, 63.6 us, 67.1 with stores past the caches.
-    const bool past = 4 * tokens * Hkv * D > (int64_t)32 << 20;
+    const bool past = 4 * tokens * Hkv * D > kCaches;
     auto launch = [&](auto d, auto f32, auto streamed) {
         return sta::launch_kernel(sta_paged_append_kernel<decltype(d)::value, decltype(f32)::value, decltype(streamed)::value>, dim3(p.per_seq, S), dim3(256), stream, p);
     };
@@ -496,7 +503,10 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
                                               : sta::launch_kernel(sta_paged_select_kernel<8>, dim3((uint32_t)items), dim3(kSelect), stream, p);
     if (e == hipSuccess && keep > 0 && into->pages > 0 && cache->pages > 0) {
         const dim3 grid((uint32_t)(items * blocks)), block(256);
-        e = D == 64 ? sta::launch_kernel(sta_paged_move_kernel<64>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<128>, grid, block, stream, p);
+        const bool past = (__int128)4 * items * keep * D > kCaches;
+        e = D == 64 ? past ? sta::launch_kernel(sta_paged_move_kernel<64, true>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<64, false>, grid, block, stream, p)
+            : past  ? sta::launch_kernel(sta_paged_move_kernel<128, true>, grid, block, stream, p)
+                    : sta::launch_kernel(sta_paged_move_kernel<128, false>, grid, block, stream, p);
     }
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }
