@@ -6,7 +6,8 @@ attention, and the attention itself, forward, backward and token by token.
 video_layer    projection -> norms, rotation by (t, h, w) and tile order in one pass -> sliding tile attention -> raster order, and
                the gradients back to the projection's output and the norms' weights;
 prompt_layer   the same for packed prompts of different lengths with grouped heads -> causal attention, and its gradients;
-next_tokens    one further token of every prompt against a cache of keys and values.
+next_tokens    one further token of every prompt against a cache of keys and values;
+conversation   prompts, the part of them that is looked at, and next tokens with a cache in pages, which is cut to a budget of keys.
 """
 import os
 import sys
@@ -116,6 +117,66 @@ def next_tokens(qkv, weights, cache, Hq, Hkv, workspace=None):
     return o
 
 
+class PagedCache:
+    """Two pools of pages, one that is used and one that keys are taken over to when there are too many; every sequence has as many pages in either."""
+
+    def __init__(self, S, room, page, Hkv, D):
+        n = -(-room // page)
+        self.caches, self.weights, self.now = [], [], 0
+        for _ in range(2):
+            k, v = torch.zeros((2, S * n, page, Hkv, D), dtype=BF16, device=DEVICE)
+            table = torch.randperm(S * n, device=DEVICE).to(torch.int32).view(S, n)      # any pages that are free
+            self.caches.append(sta.StaPagedCache(k, v, table, torch.zeros(S, dtype=torch.int32, device=DEVICE)))
+            self.weights.append(torch.zeros((S * n, Hkv, page), device=DEVICE))
+
+    def step(self, q, k, v, lengths, longest, window):
+        """New rows into their pages, attention over them, and what the last `window` tokens of every sequence look at, added to what its keys have gathered.  longest: no sequence has
+        more keys.  Returns the attention's output."""
+        cache, weights, cu = self.caches[self.now], self.weights[self.now], starts(lengths)
+        Hq, most = q.shape[1], max(lengths)
+        cache.used.add_(torch.tensor(lengths, dtype=torch.int32, device=DEVICE))
+        sta.sta_paged_append(k, v, cu, cache, most, weights=weights)
+        o, lse = torch.empty_like(q), torch.empty((Hq, q.shape[0]), device=DEVICE)
+        workspace = scratch(sta.sta_paged_workspace_bytes(Hq, k.shape[1], q.shape[2], cache.S, q.shape[0], most, longest))
+        sta.sta_paged_forward(q, o, cu, cache, most, longest, lse=lse, workspace=workspace)
+        if most > window:
+            ends, last = [sum(lengths[:i + 1]) for i in range(len(lengths))], [min(n, window) for n in lengths]
+            rows = torch.cat([torch.arange(e - n, e, device=DEVICE) for e, n in zip(ends, last)])
+            q, lse, cu, most = q[rows], lse[:, rows].contiguous(), starts(last), max(last)
+        sta.sta_paged_weights(q, lse, weights, cu, cache, most, longest, before=weights)
+        return o
+
+    def cut(self, keep, first, recent):
+        """Leaves every sequence at most `keep` keys.  Returns which they were, [S, Hkv, keep]."""
+        old, new = self.caches[self.now], self.caches[1 - self.now]
+        kept = torch.empty((old.S, old.Hkv, keep), dtype=torch.int32, device=DEVICE)
+        sta.sta_paged_evict(old, self.weights[self.now], new, self.weights[1 - self.now], kept, first=first, recent=recent)
+        self.now = 1 - self.now
+        return kept
+
+
+def conversation(qkv, further, weights, lengths, Hq, Hkv, keep, page=16, window=32):
+    """qkv: [1, tokens, Hq + 2 Hkv, D], prompt after prompt; further: [steps, S, Hq + 2 Hkv, D], the next tokens of every prompt.  The prompts' keys are cut to `keep` by what the
+    prompts' last tokens look at, then the next tokens go on.  Returns the prompts' output, which keys stayed, and the next tokens' outputs."""
+    _, T, _, D = qkv.shape
+    S, steps, heads = len(lengths), further.shape[0], [Hq, Hkv, Hkv]
+    cache = PagedCache(S, max(lengths) + steps, page, Hkv, D)
+
+    def rows_of(x, positions):
+        out = [torch.empty((1, x.shape[1], h, D), dtype=BF16, device=DEVICE) for h in heads]
+        sta.sta_qk_norm_rope(*x.split(heads, 2), *out, *weights, prompt_rotary(D, positions))
+        return [r[0] for r in out]
+
+    q, k, v = rows_of(qkv, torch.cat([torch.arange(n, dtype=torch.int32) for n in lengths]).to(DEVICE))
+    o = cache.step(q, k, v, lengths, max(lengths), window)
+    kept = cache.cut(keep, 4, keep // 4)
+    outs = []
+    for i, x in enumerate(further):             # positions go on from the whole prompts: rotations tell the keys that stayed where they stood
+        q, k, v = rows_of(x[None], torch.tensor(lengths, dtype=torch.int32, device=DEVICE) + i)
+        outs.append(cache.step(q, k, v, [1] * S, max(lengths) + i + 1, 1))
+    return o, kept, outs
+
+
 def main(grid=(6, 16, 24), tile=(6, 8, 8), H=4, Hq=8, Hkv=2, D=128, lengths=(300, 41, 1)):
     g = torch.Generator(device=DEVICE).manual_seed(0)
 
@@ -142,6 +203,11 @@ def main(grid=(6, 16, 24), tile=(6, 8, 8), H=4, Hq=8, Hkv=2, D=128, lengths=(300
     again = next_tokens(qkv[0, last][:, None], weights, cache, Hq, Hkv)
     error = float((again.float() - o[last].float()).norm() / o[last].float().norm())
     print("next tokens against a cache of %d of %d slots: off the prompts' last rows by %.1e (2-norm)" % (int(cache.used.sum()), cache.k.shape[0], error))
+
+    steps, keep = 5, 64
+    o, kept, outs = conversation(qkv, randn(steps, len(lengths), Hq + 2 * Hkv, D), weights, lengths, Hq, Hkv, keep)
+    print("conversations of %s tokens cut to %s keys: output of the prompts %s, of %d tokens each %s" % (
+        lengths, [min(n, keep) for n in lengths], tuple(o.shape), steps, tuple(outs[-1].shape)))
     return error
 
 
