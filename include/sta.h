@@ -471,7 +471,7 @@ int sta_paged_weights(const sta_head_rows *q, const float *lse, int64_t tokens_q
  * weights: float32 [pages, Hkv, page_size] of cache, into_weights of into.  kept: device int32 [S, Hkv, keep], written; -1 from min(used[s], keep) on.  into->used: written,
  * min(used[s], keep).  into's pool, page size and layout may be others, or the pool the same (then into_weights may be weights): the pages in into's table, which must be distinct, must then
  * be none that cache's rows have among their used ones.  So pages that sequences share can be evicted from, and a call that is made again gives the same.
- * first + recent may not exceed keep; into's rows of the table need places for keep keys (else STA_ERR_SHAPE).  Two launches; fewer than 2^22 heads of all sequences, fewer than 2^24
+ * first + recent may not exceed keep; into's rows of the table need places for keep keys (else STA_ERR_SHAPE).  One or two launches; fewer than 2^22 heads of all sequences, fewer than 2^24
  * blocks of 16 (head dimension 64: 32) kept rows of one head.
  */
 int sta_paged_evict(const sta_paged_cache *cache, const float *weights, const sta_paged_cache *into, float *into_weights, int32_t *kept, int S, int keep,
