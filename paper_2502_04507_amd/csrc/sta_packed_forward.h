@@ -354,6 +354,17 @@ struct KeysOf<PackedParams, D> {
     __device__ __forceinline__ void bring_values(const PackedParams &p, const PackedSeq &seq, int first, char *dst) const { v_dma.bring_part(vh, p.v.token, first, seq.lk, dst); }
 };
 
+// The same for the kernel of tiles, whose KG groups take stages of U sub-blocks in turn: bring_turn() brings the group's stage number i, which begins with sub-block `sub`; all waves of a group
+// call it, behind a barrier that all who brought earlier stages have passed.
+template <class Params, int D, int KG>
+struct TileKeys : KeysOf<Params, D> {
+    template <int SUBS, int COUNT, int K_GROUP, int V_GROUP>
+    __device__ __forceinline__ void bring_turn(const Params &p, const PackedSeq &seq, int sub, int, int from, char *to, int v_at, int apart)
+    {
+        this->template bring<SUBS, COUNT, K_GROUP, V_GROUP>(p, seq, sub, sub + SUBS * KG, from, to, v_at, apart);
+    }
+};
+
 // RW waves of 32 rows; KG groups of them take the stages of U sub-blocks in turn, each with LDS of its own, and are joined at the end: small launches
 // are cut that way inside the workgroups.
 // The walk.  Of the stages that every row sees all of, the first sets the offsets and the others run without following the scores (20 of 83
@@ -393,19 +404,18 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     const int n_whole = uniform(seq.keys_of((int)sta::fast_div(row0, p.by_g), p));          // keys that all rows see
     const int lim_hi = idle ? 0 : uniform(seq.keys_of((int)sta::fast_div(wave_last, p.by_g), p));
 
-    KeysOf<Params, D> keys;
+    TileKeys<Params, D, KG> keys;
     keys.start(p, seq, kv, lane);
     char *own = smem + 2 * kg * STAGE;
     // sub .. sub + U - 1; those of the last stage that nobody sees are brought as well, from the last key's row
-    auto issue = [&](int stage, int sub) __attribute__((always_inline)) {
-        if (sub < sub1)
-            keys.template bring<U, PER_WAVE, LK::Group, LV::Group>(p, seq, sub, sub + U * KG, PER_WAVE * wave, own + stage * STAGE, V_AT, SUB);
+    auto issue = [&](int stage, int i, int sub) __attribute__((always_inline)) {
+        if (sub < sub1) keys.template bring_turn<U, PER_WAVE, LK::Group, LV::Group>(p, seq, sub, i, PER_WAVE * wave, own + stage * STAGE, V_AT, SUB);
     };
     // the group's stage number i begins with sub-block sub_of(i); all groups go around n_steps times
     auto sub_of = [&](int i) { return sub0 + U * (kg + KG * i); };
     const int n_steps = (sub1 - sub0 + U * KG - 1) / (U * KG);
     keys.template look_up<U>(p, seq, sub_of(0));
-    issue(0, sub_of(0));
+    issue(0, 0, sub_of(0));
 
     bf16x8 Q[NC][D / 32];
     load_queries<D, NC>(p, seq, kv, wave_row, rows, lane, Q);
@@ -420,7 +430,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
         constexpr int ST = decltype(stage_c)::value, MODE = decltype(mode_c)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's part of the stage has landed
         if constexpr (RW > 1) __syncthreads();              // ... and everyone's, and nobody reads the other stage any more (one wave: its own alone)
-        issue(ST ^ 1, sub_of(i + 1));
+        issue(ST ^ 1, i + 1, sub_of(i + 1));
         const int sub = sub_of(i), first = sub * kSub;
         if (MODE < kMasked || (sub < sub1 && first < lim_hi))
             softmax_sub_blocks<D, NC, LSE, MODE, U, SUB, ST * STAGE>(st, k_addr, v_addr, Q, c, grow_above, first, lim, g4);
@@ -466,7 +476,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     if (__builtin_expect(__syncthreads_or(bad || most >= 0x7f800000u), 0)) {
         st.start();
         keys.template look_up<U>(p, seq, sub_of(0));
-        issue(0, sub_of(0));
+        issue(0, 0, sub_of(0));
 #pragma unroll 1
         for (i = 0; i < n_steps; i += 2) {
             step(Stage0{}, Careful{}, i);
