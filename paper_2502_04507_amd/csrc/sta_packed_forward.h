@@ -354,8 +354,7 @@ struct KeysOf<PackedParams, D> {
     __device__ __forceinline__ void bring_values(const PackedParams &p, const PackedSeq &seq, int first, char *dst) const { v_dma.bring_part(vh, p.v.token, first, seq.lk, dst); }
 };
 
-// The same for the kernel of tiles, whose KG groups take stages of U sub-blocks in turn: bring_turn() brings the group's stage number i, which begins with sub-block `sub`; all waves of a group
-// call it, behind a barrier that all who brought earlier stages have passed.
+// The same for the kernel of tiles, whose KG groups take stages of U sub-blocks in turn: bring_turn() brings the group's stage number i, which begins with sub-block `sub`.
 template <class Params, int D, int KG>
 struct TileKeys : KeysOf<Params, D> {
     template <int SUBS, int COUNT, int K_GROUP, int V_GROUP>

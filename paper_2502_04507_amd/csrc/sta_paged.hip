@@ -105,45 +105,45 @@ struct KeysOf<PagedParams, D> {
     }
 };
 
-// Tiles of 128 rows of 128 channels: the places of the next stages are worked out together and kept in LDS, those of groups of rows where no page ends inside one, else of every row.  In registers, looked up
-// a stage ahead as above, they cost the walk its own, whose reloads wait for the stage that is on its way: prompts of 8192 and 4097 tokens, 32 heads over 8, 684 us, 581 this way, 554 on packed keys.
+// Tiles of 128 rows of 128 channels: a wave works out the places of what it brings in the next stages together and keeps them in LDS, those of groups of rows where no page ends inside one, else of every row.
+// In registers, looked up a stage ahead as above, they cost the walk its own, whose reloads wait for the stage that is on its way: prompts of 8192 and 4097 tokens, 32 heads over 8, 684 us where
+// packed keys take 554; this way 564 where those take 538.
 // Where groups of waves take stages in turn registers are left, and a look into LDS before each stage costs more than it saves (12 heads over 4, 500, 1, 65, 1 and 578 tokens on 77 to 7097: 69 us, 73 this
 // way; 8 heads of 128, four of 480 on 2200: 33.6 and 34.6), and with 64 channels there is nothing between them.
 template <>
 struct TileKeys<PagedParams, 128, 1> : KeysOf<PagedParams, 128> {
     using Base = KeysOf<PagedParams, 128>;
-    static constexpr int PLACES = 2048, WAVES = 4, LANES = 64 * WAVES, AT_ONCE = 4;
-    static_assert(PLACES % (LANES * AT_ONCE) == 0 && PLACES % kSub == 0, "");
-    uint64_t *places;
-    int shift;                                  // log2 of a stage's places
+    static constexpr int PLACES = 512, WAVES = 4, OF_STAGE = kSub / GR / WAVES, AT_ONCE = 4;        // of a wave, and its groups of a stage
+    static_assert(PLACES % (64 * AT_ONCE) == 0 && PLACES % (OF_STAGE * GR) == 0, "");
+    uint64_t *places;                           // a wave's own: no other looks at them
+    int shift;                                  // log2 of its places of a stage
     __device__ __forceinline__ void start(const PagedParams &p, const PackedSeq &seq, uint32_t kv, int lane)
     {
-        __shared__ uint64_t all[PLACES];
+        __shared__ uint64_t all[WAVES * PLACES];
         Base::start(p, seq, kv, lane);
-        places = all;
-        shift = p.whole_groups ? __builtin_ctz(kSub / GR) : __builtin_ctz(kSub);
+        places = all + uniform(threadIdx.x >> 6) * PLACES;
+        shift = __builtin_ctz(p.whole_groups ? OF_STAGE : OF_STAGE * GR);
     }
     template <int SUBS>
     __device__ __forceinline__ void look_up(const PagedParams &, const PackedSeq &, int) {}
-    // Those from sub-block `sub` on, as far as the keys go; rows beyond the last key have the last key's.  There are keys.
-    __device__ __forceinline__ void fill(const PagedParams &p, const PackedSeq &seq, int sub, int wave)
+    // Those of the wave's groups, the first of which is `from` in every stage, from sub-block `sub` on, as far as the keys go; behind the last key they are its own or its group's.  There are keys.
+    __device__ __forceinline__ void fill(const PagedParams &p, const PackedSeq &seq, int sub, int from)
     {
-        const int rows = p.whole_groups ? GR : 1, rows_shift = __builtin_ctz(rows), last = (seq.lk - 1) & -rows;        // of a place; the first of the last one's
-        const int at = LANES / WAVES * wave + fresh_lane();                                       // (not kept in a register through the walk)
+        const int rows = p.whole_groups ? GR : 1, last = (seq.lk - 1) & -rows, lane = fresh_lane();       // rows of a place; the first of the last one's
 #pragma unroll 1
-        for (int x0 = 0; x0 < PLACES && (int64_t)sub * kSub + ((int64_t)x0 << rows_shift) < seq.lk; x0 += LANES * AT_ONCE) {
+        for (int x0 = 0; x0 < PLACES && ((int64_t)sub + (x0 >> shift)) * kSub < seq.lk; x0 += 64 * AT_ONCE) {
             int entry[AT_ONCE];
             uint32_t slot[AT_ONCE];
 #pragma unroll
             for (int y = 0; y < AT_ONCE; ++y) {
-                const int64_t r = (int64_t)sub * kSub + ((int64_t)(x0 + LANES * y + at) << rows_shift);
+                const int x = x0 + 64 * y + lane, stage = x >> shift;
+                const int64_t r = ((int64_t)sub + stage) * kSub + from * GR + (x - (stage << shift)) * rows;
                 const uint32_t n = entry_of((uint32_t)(r < last ? r : last), p.c, &slot[y]);
                 entry[y] = row[n];
             }
 #pragma unroll
-            for (int y = 0; y < AT_ONCE; ++y) places[x0 + LANES * y + at] = place_of(page_inside(entry[y], p.c), slot[y], p.c);
+            for (int y = 0; y < AT_ONCE; ++y) places[x0 + 64 * y + lane] = place_of(page_inside(entry[y], p.c), slot[y], p.c);
         }
-        __syncthreads();
     }
     // A place, from LDS at byte address at.
     static __device__ __forceinline__ uint64_t read_place(uint32_t at)
@@ -155,14 +155,14 @@ struct TileKeys<PagedParams, 128, 1> : KeysOf<PagedParams, 128> {
     template <int SUBS, int COUNT, int K_GROUP, int V_GROUP>
     __device__ __forceinline__ void bring_turn(const PagedParams &p, const PackedSeq &seq, int sub, int i, int from, char *to, int v_at, int)
     {
-        static_assert(SUBS == 1 && COUNT * WAVES == kSub / GR, "");
+        static_assert(SUBS == 1 && COUNT == OF_STAGE, "");
         const int turn = i & ((PLACES >> shift) - 1);
-        if (turn == 0) fill(p, seq, sub, from / COUNT);
+        if (turn == 0) fill(p, seq, sub, from);
         const uint32_t first = (uint32_t)(uintptr_t)places + (uint32_t)(turn << shift) * 8;
         const int lane = fresh_lane();
         if (__builtin_expect((sub + 1) * kSub <= seq.lk && p.whole_groups, 1)) {
             // the wave's groups' places, one in each of the first lanes
-            const uint64_t mine = read_place(first + (uint32_t)(from + lane % COUNT) * 8);
+            const uint64_t mine = read_place(first + (uint32_t)(lane % COUNT) * 8);
             const int lo = (int)(uint32_t)mine, hi = (int)(mine >> 32);
             PackedDma<128, true> k_dma;         // worked out again, for registers
             PackedDma<128, false> v_dma;
@@ -178,8 +178,10 @@ struct TileKeys<PagedParams, 128, 1> : KeysOf<PagedParams, 128> {
         } else {
 #pragma unroll 1
             for (int n = 0; n < COUNT; ++n) {
-                const int inside = (from + n) * GR + lane / LPR, left = seq.lk - 1 - sub * kSub, r = inside < left ? inside : left;      // rows beyond the last key: its
-                const uint64_t at = read_place(first + (uint32_t)(p.whole_groups ? r / GR : r) * 8) + (p.whole_groups ? (uint32_t)(r % GR) * p.c.token : 0);
+                const int r = lane / LPR, inside = (from + n) * GR + r, left = seq.lk - 1 - sub * kSub;
+                // rows beyond the last key: its
+                const uint64_t at = p.whole_groups ? read_place(first + (uint32_t)n * 8) + (uint32_t)(inside < left ? r : left % GR) * p.c.token
+                                                   : read_place(first + (uint32_t)(n * GR + r) * 8);
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kh + at + k_dma.chunk_of(lane)), STA_LDS_PTR(to + (from + n) * K_GROUP), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vh + at + v_dma.chunk_of(lane)), STA_LDS_PTR(to + v_at + (from + n) * V_GROUP), 16, 0, 0);
             }

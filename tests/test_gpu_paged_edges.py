@@ -43,6 +43,24 @@ def test_what_is_no_number_or_the_lowest_one(shape, kind, page):
             assert torch.equal(nan, torch.isnan(b)) and same(torch.where(nan, 0.0, a).to(a.dtype), torch.where(nan, 0.0, b).to(b.dtype))
 
 
+@pytest.mark.parametrize("lse", [False, True])
+@pytest.mark.parametrize("page,used", [(16, [16500, 40]), (3, [4500, 40]), (4, [8193, 8192])])
+def test_walks_longer_than_the_places_that_are_kept(page, used, lse):
+    """Tiles of 128 rows of 128 channels keep the places of 2048 groups of 4 rows, or rows where a page ends inside a group: walks that take several fillings, also a second time where V holds an
+    infinity."""
+    cache = Cache(8, 128, page, used, seed=4)
+    new = [2400, 40]
+    q = randn((2440, 32, 128), 6).to(DEV)
+    for bad in (False, True):
+        if bad:
+            cache.v[0][used[0] - 100, 3, 7] = math.inf
+            j, slot = cache.place(0, used[0] - 100)
+            cache.pool[1][j, slot, 3, 7] = math.inf
+        for got, want in zip(forward(q, cache, new, lse=lse), packed(q, cache, new, lse=lse)):
+            assert got is None and want is None or same(got, want), bad
+        assert not bad or bool(forward(q, cache, new)[0][2390, 12, 7] == math.inf)
+
+
 def test_places_beyond_4_gb():
     """Pages 2.6 GB apart: the third lies beyond 32 bits of bytes, in either pool."""
     Hkv, Hq, D, page, stride = 2, 8, 128, 16, 1_300_000_000
