@@ -437,6 +437,7 @@ typedef struct {
  * float32 (rounded once).  cu: device int32 [S + 1].  max_new: host, an upper bound of the sequences' new tokens; tokens beyond it are not written, nor are those
  * whose key would be below 0 or beyond the table.  A key that two calls' sequences write at once holds one row or the other.
  * weights: NULL, or the keys' gathered attention weights, float32 [pages, Hkv, page_size]: 0 is written for every key that is.
+ * Supported: up to 65,535 sequences.
  */
 int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, int64_t tokens, const int32_t *cu, const sta_paged_cache *cache, int S, int max_new,
                      int D, float *weights, void *hip_stream);

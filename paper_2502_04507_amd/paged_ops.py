@@ -37,7 +37,7 @@ def _lib():
 class StaPagedCache:
     """A cache in pages: k, v (device bf16 [pages, page_size, Hkv, D], laid out alike, channels adjacent; strided views such as halves of one tensor or of
     [pages, Hkv, page_size, D] turned around), table (device int32 [S, n]: the pages of every sequence in the order of its keys), used (device int32 [S]: how many
-    keys it has).  The tensors are kept and used as they are: what they hold may change from call to call."""
+    keys it has).  The tensors are kept and used as they are: what they hold may change from call to call, other tensors need another cache."""
 
     def __init__(self, k, v, table, used):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
@@ -50,7 +50,7 @@ class StaPagedCache:
             raise ValueError("used must be int32 [S]")
         if not (k.is_cuda and v.is_cuda and table.is_cuda):
             raise ValueError("a cache must live in device memory")
-        self.k, self.v, self.table, self.used = k, v, table, used
+        self._tensors = k, v, table, used
         self.pages, self.page_size, self.Hkv, self.D = k.shape
         self.S = _int32(table.shape[0], "the number of sequences")
         page, token, head, channel = k.stride()
@@ -63,6 +63,12 @@ class StaPagedCache:
                               _dev(used, "used") or 16)
         # for the extension: where the struct is, and what goes with it
         self._at = (ctypes.addressof(self._c), self.S, heads, self.D, self.pages, self.page_size)
+
+    # Read only: calls take the addresses that were looked up above.
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    table = property(lambda self: self._tensors[2])
+    used = property(lambda self: self._tensors[3])
 
     @property
     def room(self):

@@ -160,3 +160,10 @@ def test_the_class_refuses():
     ):
         with pytest.raises(ValueError, match=match):
             sta.StaPagedCache(*args)
+
+
+@pytest.mark.parametrize("name", ["k", "v", "table", "used", "room"])
+def test_a_cache_keeps_its_tensors(name):
+    """Calls take addresses that were looked up when the cache was made: another tensor in an attribute's place would not be seen."""
+    with pytest.raises(AttributeError):
+        setattr(object.__new__(sta.StaPagedCache), name, None)
