@@ -788,7 +788,8 @@ struct PackedPlan {
 
 constexpr uint32_t kNoParts = 1u << 30;
 
-bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
+// at_once: tiles of 128 rows are cut into no more workgroups than are there at once, three a CU.
+bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan, bool at_once = false)
 {
     const int64_t g = Hq / Hkv, rows = g * max_q, cus = sta::compute_units(), subs = ((int64_t)max_k + kSub - 1) / kSub;
     auto tiles = [&](int64_t tile) { return tiles_of(tokens_q, g, S, max_q, tile); };
@@ -800,7 +801,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
         plan->waves = 2;
         if (halves < 2 * cus && cut && subs >= 256) {
             plan->waves = 4;
-            want = 6 * cus;
+            want = (at_once ? 3 : 6) * cus;
             least = 64;
         } else if (halves < cus / 4 && cut && subs >= 48) {
             want = 2 * cus;
@@ -816,7 +817,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     if (items > kMostWorkgroups) return false;
     plan->slots = (uint32_t)slots;
     if (items > 0 && items < want / 2) {
-        int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
+        int64_t parts = (at_once && !plan->few && plan->waves == 4 ? want : want + items - 1) / items, each = (subs + parts - 1) / parts;
         each = each < least ? least : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
         parts = (subs + each - 1) / each;
         if (parts > 1 && items * parts <= kMostWorkgroups) {

@@ -197,12 +197,16 @@ struct TileKeys<PagedParams, 128, 1> : KeysOf<PagedParams, 128> {
 //   16/16 x 64, 333, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578             67 | 49 | 55       12/4 x 128, 500, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578   87 | 68 | 74
 //   8/8 x 128, three of 512 on 512, 1000, 3000                               42 | 26 | 31
 // and where they stay: 40/8 x 128, 40 of 1 on 1000 and 300 on 1300  34 | 49 | 35; 32/8 x 128, four of 256 on 4096  80 | 124 | 117; 16 of 64 on 3000  64 | 128 | 97; 2048 on 4096  122 | 196 | 169.
+// Chunks of 128 channels and more alike lengths are cut into no more workgroups than are there at once, not into twice as many: us, 32 heads over 8, one chunk on 16,384 keys, of 416, 544, 640, 960 tokens
+//   129, 159, 186, 250 | 143, 169, 180, 271     15 heads over 5, 700 on 20,001  130 | 156     40 over 8, 300 and 200 on 12,000 and 9000  139 | 149
+// but 100, 60 and 350 on 9000, 16,000 and 30,000  258 | 242, and with 64 channels 256 each on 32,768 and 20,001  155 | 146.
 bool paged_plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
 {
-    if (!plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, cut, plan)) return false;
+    const bool alike = 4 * tokens_q > 3 * (int64_t)S * max_q;
+    if (!plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, cut, plan, D == 128 && alike)) return false;
     if (plan->few || plan->waves != 2 || plan->parts > 1) return true;
     const int64_t subs = ((int64_t)max_k + kSub - 1) / kSub, items = (int64_t)plan->slots * Hkv;
-    const bool uneven = subs >= 96 && 4 * tokens_q <= 3 * (int64_t)S * max_q, sparse = subs >= 64 && items < sta::compute_units();
+    const bool uneven = subs >= 96 && !alike, sparse = subs >= 64 && items < sta::compute_units();
     if (!uneven && !sparse) return true;
     const int64_t slots = tiles_of(tokens_q, Hq / Hkv, S, max_q, 32);
     if (slots * Hkv > kMostWorkgroups) return true;
@@ -217,7 +221,7 @@ extern "C" {
 
 size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
 {
-    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);       // what is not cut there is not cut here
+    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);       // what is not cut there is not cut here, nor into more parts
 }
 
 int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
