@@ -73,6 +73,30 @@ def test_walks_of_uneven_lengths():
         assert bool(((z[:, a].cpu().double() - want[1]).abs() <= b_lse).all()), s
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,used", [([100, 80], [9000, 8200]), ([200, 10, 1], [9001, 300, 9000]), ([130, 130, 130], [8200, 130, 100])])
+def test_chunks_that_are_cut_along_the_keys(new, used, D):
+    """Tiles of 128 rows in parts, of alike and of uneven lengths, sequences with fewer keys than a part and with fewer keys than rows among them."""
+    Hq, Hkv = 8, 2
+    assert sta.sta_paged_workspace_bytes(Hq, Hkv, D, len(new), sum(new), max(new), max(used)) > 0
+    cache = Cache(Hkv, D, 16, used, seed=7)
+    q = randn((sum(new), Hq, D), 8)
+    o, z = forward(q.to(DEV), cache, new, lse=True)
+    other = Cache(Hkv, D, 3, used, seed=9, layout="heads", keys=(cache.k, cache.v))
+    for a, b in zip((o, z), forward(q.to(DEV), other, new, lse=True)):
+        assert same(a, b)
+    cu = starts(new)
+    for s in range(len(new)):
+        a = slice(cu[s], cu[s] + new[s])
+        Q, K, V = q[a].double(), cache.k[s].double(), cache.v[s].double()
+        want = lu.attention(Q, K, V, True, D ** -0.5)
+        b_o, b_lse, _ = bounds(Q, K, V, True, D ** -0.5, want[1])
+        close(o[a], want[0], b_o, "sequence %d" % s)
+        seen = want[1] > -math.inf
+        assert torch.equal(seen, z[:, a].cpu() > -math.inf)
+        assert bool(((z[:, a].cpu().double() - want[1])[seen].abs() <= b_lse[seen]).all()), s
+
+
 @pytest.mark.parametrize("layout", ["tokens", "heads", "halves"])
 @pytest.mark.parametrize("page", [1, 4, 5, 8, 32, 33, 128])
 @pytest.mark.parametrize("D", [64, 128])
