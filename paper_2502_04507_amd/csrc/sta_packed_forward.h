@@ -296,15 +296,24 @@ __device__ __forceinline__ void limits_of(const PackedParams &p, const PackedSeq
 template <int D, int R>
 constexpr size_t part_floats() { return (size_t)R * D + 2 * R; }
 
-// How many parts a walk of n sub-blocks has, and where one ends: the last one takes what is left.
-__device__ __forceinline__ int parts_of(int n, const PackedParams &p)
+// The tile's rank of a launch's item, and which part it is; sub-blocks of a part of a tile of 128 rows.
+__device__ __forceinline__ uint32_t rank_of(uint32_t item, const PackedParams &p, uint32_t *part)
 {
-    const int want = (n + (int)p.part_subs - 1) / (int)p.part_subs;
+    const uint32_t rank = sta::fast_div(item, p.by_parts);
+    *part = item - rank * p.parts;
+    return rank;
+}
+__device__ __forceinline__ uint32_t part_subs_of(const PackedParams &p, int) { return p.part_subs; }
+
+// How many parts of `each` a walk of n sub-blocks has, and where one ends: the last one takes what is left.
+__device__ __forceinline__ int parts_of(int n, uint32_t each, const PackedParams &p)
+{
+    const int want = (n + (int)each - 1) / (int)each;
     return want < (int)p.parts ? want : (int)p.parts;
 }
-__device__ __forceinline__ int part_end(uint32_t part, int n, const PackedParams &p)
+__device__ __forceinline__ int part_end(uint32_t part, int n, uint32_t each, const PackedParams &p)
 {
-    const int end = (int)((part + 1) * p.part_subs);
+    const int end = (int)((part + 1) * each);
     return part + 1 == p.parts || end > n ? n : end;
 }
 
@@ -385,7 +394,8 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     const int kg = all_waves / RW, wave = all_waves % RW;
     // key heads next to each other: workgroup ids go to the 8 XCDs in turn, and a head's keys stay in one L2 where Hkv is a multiple of 8
     const uint32_t place = place_of_block(p), item = sta::fast_div(place, p.by_Hkv), kv = place - item * p.Hkv;
-    const uint32_t rank = sta::fast_div(item, p.by_parts), part = item - rank * p.parts;
+    uint32_t part;
+    const uint32_t rank = rank_of(item, p, &part);
     PackedTile tile;
     if (!find_tile<TILE, false>(rank, p, lane, &tile)) return;
     const PackedSeq seq = tile.seq;
@@ -393,8 +403,9 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     const uint32_t last_row = row0 + TILE < rows ? row0 + TILE - 1 : rows - 1;
     const int n_keys = uniform(seq.keys_of((int)sta::fast_div(last_row, p.by_g), p));
     const int n_all = (n_keys + kSub - 1) / kSub;
-    const int sub0 = (int)(part * p.part_subs);
-    const int sub1 = part_end(part, n_all, p);
+    const uint32_t each = RW == 4 ? part_subs_of(p, lane) : p.part_subs;
+    const int sub0 = (int)(part * each);
+    const int sub1 = part_end(part, n_all, each, p);
     if (part > 0 && sub0 >= n_all) return;                  // the first part of a tile without keys writes its zeros
 
     const uint32_t wave_row = row0 + 32 * wave;
@@ -546,7 +557,7 @@ __global__ __launch_bounds__(RW * KG * 64, KG > 2 && D == 128 ? 1 : KG > 2 ? 2 :
     }
     if (idle) return;
     const int last_lane = fresh_lane(), last_g4 = last_lane >> 4;
-    if (parts_of(n_all, p) > 1) {
+    if (parts_of(n_all, each, p) > 1) {
         float *ws = part_at(p, rank, kv, part, part_floats<D, TILE>());
 #pragma unroll
         for (int col = 0; col < NC; ++col) {
@@ -599,7 +610,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(Params p)
     const int n_keys = uniform(seq.keys_of((int)sta::fast_div(rows - 1, p.by_g), p));
     const int n_all = (n_keys + kSub - 1) / kSub;
     const int sub0 = (int)(part * p.part_subs);
-    const int sub1 = part_end(part, n_all, p);
+    const int sub1 = part_end(part, n_all, p.part_subs, p);
     if (part > 0 && sub0 >= n_all) return;
 
     int lim[NC];
@@ -674,7 +685,7 @@ __global__ __launch_bounds__(256) void sta_packed_few_kernel(Params p)
         if (g4 == 0) stats[wave][16 * col + c16] = make_float2(st.m[col], l);
     }
     __syncthreads();
-    const bool whole = parts_of(n_all, p) <= 1;
+    const bool whole = parts_of(n_all, p.part_subs, p) <= 1;
     float *ws = whole ? nullptr : part_at(p, s, kv, part, part_floats<D, R>());
 #pragma unroll
     for (int col = 0; col < NC; ++col) {
@@ -742,7 +753,7 @@ __global__ __launch_bounds__(256) void sta_packed_merge_kernel(Params p)
     if (rows == 0) return;
     const uint32_t r = blockIdx.y * ROWS + threadIdx.x / LPR;
     const int n_all = (seq.keys_of((int)sta::fast_div(row0 + in_tile - 1, p.by_g), p) + kSub - 1) / kSub;
-    const int n = parts_of(n_all, p), ch = 4 * (threadIdx.x % LPR);
+    const int n = parts_of(n_all, TILES && R == 128 ? part_subs_of(p, lane) : p.part_subs, p), ch = 4 * (threadIdx.x % LPR);
     if (r >= in_tile || n <= 1) return;
     const size_t floats = part_floats<D, R>();
     const float *ws = part_at(p, item, kv, 0, floats);
@@ -788,8 +799,7 @@ struct PackedPlan {
 
 constexpr uint32_t kNoParts = 1u << 30;
 
-// at_once: tiles of 128 rows are cut into no more workgroups than are there at once, three a CU.
-bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan, bool at_once = false)
+bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
 {
     const int64_t g = Hq / Hkv, rows = g * max_q, cus = sta::compute_units(), subs = ((int64_t)max_k + kSub - 1) / kSub;
     auto tiles = [&](int64_t tile) { return tiles_of(tokens_q, g, S, max_q, tile); };
@@ -801,7 +811,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
         plan->waves = 2;
         if (halves < 2 * cus && cut && subs >= 256) {
             plan->waves = 4;
-            want = (at_once ? 3 : 6) * cus;
+            want = 6 * cus;
             least = 64;
         } else if (halves < cus / 4 && cut && subs >= 48) {
             want = 2 * cus;
@@ -817,7 +827,7 @@ bool plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max
     if (items > kMostWorkgroups) return false;
     plan->slots = (uint32_t)slots;
     if (items > 0 && items < want / 2) {
-        int64_t parts = (at_once && !plan->few && plan->waves == 4 ? want : want + items - 1) / items, each = (subs + parts - 1) / parts;
+        int64_t parts = (want + items - 1) / items, each = (subs + parts - 1) / parts;
         each = each < least ? least : (each + 7) & ~(int64_t)7;          // whole stages of all groups end with a part
         parts = (subs + each - 1) / each;
         if (parts > 1 && items * parts <= kMostWorkgroups) {

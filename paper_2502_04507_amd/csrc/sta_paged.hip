@@ -17,6 +17,8 @@ namespace {
 struct PagedParams : PackedParams {     // k and v: the pool; k.token and k.head as there
     PagedCache c;
     uint32_t whole_groups;              // no page ends inside a group of rows
+    sta::FastDiv by_slots;
+    uint32_t at_once;                   // not 0: how many workgroups of tiles of 128 rows are there at once, where such are cut
 };
 
 // The keys of a sequence have no first row: its number stands in k0.
@@ -28,6 +30,36 @@ __device__ __forceinline__ PackedSeq seq_of(uint32_t s, const PagedParams &p)
     q.k0 = (int)s;
     q.lk = used_of(s, p.c);
     return q;
+}
+
+// Where tiles of 128 rows are cut, the size of the parts is chosen here, from the lengths: such that as many parts as there may be at once, three a CU, take all walks, or nearly so.  The launch has up to twice as many
+// workgroups.  Those that find nothing to do are the last ones, part after part: between the others they leave some CUs with three and others with none (544 tokens below 208 us).  us,
+// parts of the launch's size, about six a CU | this; 32 heads over 8 of 128 channels, one chunk of 416, 544, 640, 960 tokens on 16,384 keys 143, 170, 180, 271 | 126, 162, 188, 253; two of 256 on
+// 32,768 and 20,001  248 | 236; 100, 60 and 350 on 9000, 16,000 and 30,000  242 | 238; 15 heads over 5, 700 on 20,001  156 | 127; 40 over 8, 300 and 200 on 12,000 and 9000  149 | 129; of 64
+// channels, two of 256 as above 146 | 144, 24 heads, 333 on 20,000  74 | 73.
+__device__ __forceinline__ uint32_t rank_of(uint32_t item, const PagedParams &p, uint32_t *part)
+{
+    if (p.at_once == 0) return rank_of(item, static_cast<const PackedParams &>(p), part);
+    *part = sta::fast_div(item, p.by_slots);
+    return item - *part * p.by_slots.d;
+}
+__device__ __forceinline__ uint32_t part_subs_of(const PagedParams &p, int lane)
+{
+    constexpr uint32_t MOST = 1 << 19;          // products with a part's number stay in 32 bits, whatever the lengths are
+    if (p.at_once == 0) return p.part_subs;
+    uint32_t tiles = 0, subs = 0;
+    if (lane < (int)p.S) {
+        const PackedSeq seq = seq_of((uint32_t)lane, p);
+        tiles = ((uint32_t)seq.worked(p) * p.g + 127) / 128 * p.Hkv;
+        subs = ((uint32_t)seq.lk + kSub - 1) / kSub;
+        subs = subs < MOST ? subs : MOST;
+    }
+    uint32_t each = ((sum64(tiles * subs) + p.at_once - 1) / p.at_once + 1) & ~1u;      // (whole stages of two sub-blocks)
+    each = each < MOST ? each : MOST;
+    each = each > p.part_subs ? each : p.part_subs;
+#pragma unroll 1
+    for (int i = 0; i < 16 && sum64(tiles * ((subs + each - 1) / each)) > p.at_once; ++i) each += (each / 32 + 2) & ~1u;
+    return each;
 }
 
 template <int D>
@@ -197,16 +229,12 @@ struct TileKeys<PagedParams, 128, 1> : KeysOf<PagedParams, 128> {
 //   16/16 x 64, 333, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578             67 | 49 | 55       12/4 x 128, 500, 1, 65, 1, 578 on 6333, 7097, 6001, 77, 3578   87 | 68 | 74
 //   8/8 x 128, three of 512 on 512, 1000, 3000                               42 | 26 | 31
 // and where they stay: 40/8 x 128, 40 of 1 on 1000 and 300 on 1300  34 | 49 | 35; 32/8 x 128, four of 256 on 4096  80 | 124 | 117; 16 of 64 on 3000  64 | 128 | 97; 2048 on 4096  122 | 196 | 169.
-// Chunks of 128 channels and more alike lengths are cut into no more workgroups than are there at once, not into twice as many: us, 32 heads over 8, one chunk on 16,384 keys, of 416, 544, 640, 960 tokens
-//   129, 159, 186, 250 | 143, 169, 180, 271     15 heads over 5, 700 on 20,001  130 | 156     40 over 8, 300 and 200 on 12,000 and 9000  139 | 149
-// but 100, 60 and 350 on 9000, 16,000 and 30,000  258 | 242, and with 64 channels 256 each on 32,768 and 20,001  155 | 146.
 bool paged_plan_of(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k, bool cut, PackedPlan *plan)
 {
-    const bool alike = 4 * tokens_q > 3 * (int64_t)S * max_q;
-    if (!plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, cut, plan, D == 128 && alike)) return false;
+    if (!plan_of(Hq, Hkv, D, S, tokens_q, max_q, max_k, cut, plan)) return false;
     if (plan->few || plan->waves != 2 || plan->parts > 1) return true;
     const int64_t subs = ((int64_t)max_k + kSub - 1) / kSub, items = (int64_t)plan->slots * Hkv;
-    const bool uneven = subs >= 96 && !alike, sparse = subs >= 64 && items < sta::compute_units();
+    const bool uneven = subs >= 96 && 4 * tokens_q <= 3 * (int64_t)S * max_q, sparse = subs >= 64 && items < sta::compute_units();
     if (!uneven && !sparse) return true;
     const int64_t slots = tiles_of(tokens_q, Hq / Hkv, S, max_q, 32);
     if (slots * Hkv > kMostWorkgroups) return true;
@@ -221,7 +249,7 @@ extern "C" {
 
 size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k)
 {
-    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);       // what is not cut there is not cut here, nor into more parts
+    return sta_packed_workspace_bytes(Hq, Hkv, D, S, tokens_q, max_q, max_k);       // what is not cut there is not cut here
 }
 
 int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S,
@@ -270,6 +298,8 @@ int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse
     p.parts = plan.parts;
     p.part_subs = plan.part_subs;
     p.ws = static_cast<float *>(workspace);
+    p.at_once = plan.parts > 1 && !plan.few && plan.waves == 4 && S <= 64 ? 3 * (uint32_t)sta::compute_units() : 0;
+    p.by_slots = sta::fast_div_of(plan.slots > 0 ? plan.slots : 1);
     p.c = paged_cache_of(*cache);
     p.whole_groups = cache->page_size % (D == 128 ? Staged<128>::GroupRows : Staged<64>::GroupRows) == 0;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);

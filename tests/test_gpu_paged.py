@@ -74,9 +74,9 @@ def test_walks_of_uneven_lengths():
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("new,used", [([100, 80], [9000, 8200]), ([200, 10, 1], [9001, 300, 9000]), ([130, 130, 130], [8200, 130, 100])])
+@pytest.mark.parametrize("new,used", [([100, 80], [9000, 8200]), ([200, 10, 1], [9001, 300, 9000]), ([130, 130, 130], [8200, 130, 100]), ([9] * 66, [9000] + [20] * 65)])
 def test_chunks_that_are_cut_along_the_keys(new, used, D):
-    """Tiles of 128 rows in parts, of alike and of uneven lengths, sequences with fewer keys than a part and with fewer keys than rows among them."""
+    """Tiles of 128 rows in parts, of alike and of uneven lengths, more than 64 of them, sequences with fewer keys than a part and with fewer keys than rows among them."""
     Hq, Hkv = 8, 2
     assert sta.sta_paged_workspace_bytes(Hq, Hkv, D, len(new), sum(new), max(new), max(used)) > 0
     cache = Cache(Hkv, D, 16, used, seed=7)
