@@ -7,7 +7,9 @@
 // Roundings.  Products of bf16 numbers are exact, scores, exponents and sums fp32: four values of a lane are a tree, those of 512 rows go into one sum, and those into the key's.
 //
 // sta_paged_few_weights_kernel   at most 16 or 32 rows per sequence and key head: rows and keys straight from memory to registers, no LDS.  Bound by memory: 48 tokens of 32 heads over 8
-//                                on 1 to 16,384 keys 187 us, 4.7 TB/s (5.7 where nothing is written, though that is 12 of 870 MB).
+//                                on 1 to 16,384 keys 184 us, 4.7 TB/s (155 where nothing is written, though that is 12 of 870 MB).  Numbers before are asked for behind the keys'
+//                                rows and in a branch of their own: before them 190, inside the branch that finds their place 188, behind the sums 190.  Sums of 16 tiles held back and written
+//                                together by workgroups that stay: 180, but 53 in place of 45 with 64 channels.
 // sta_paged_weights_kernel       more: stages of 32 or 64 rows go through LDS, shared by the waves along the keys; small launches cut the rows among a workgroup's waves.  Bound by
 //                                vector and matrix instructions, which hardly overlap (per 64 rows and 64 keys of a wave 1024 cycles of the matrix pipe, 64 exponentials of 8 cycles, as
 //                                many multiply-adds and sums of 4): 2048 tokens of 32 heads over 8 of 128 channels on 16,384 keys 260 us, 990 TFLOP/s.  With stages of 32 rows 294 us, two stages
@@ -81,11 +83,9 @@ __device__ __forceinline__ OwnKey load_keys(const WeightsParams &p, uint32_t s, 
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks) K[col][ks] = *reinterpret_cast<const bf16x8 *>(head + at + 64 * ks);
     }
-    OwnKey own = {-1, 0.f};
-    if (lane < 16 * NC && mine < lk && mine < p.max_k && page >= 0 && page < (int)p.c.pages) {
-        own.at = ((int64_t)page * p.Hkv + kv) * p.c.by_page.d + slot;
-        if (p.before) own.before = p.before[own.at];
-    }
+    const bool there = lane < 16 * NC && mine < lk && mine < p.max_k && page >= 0 && page < (int)p.c.pages;
+    OwnKey own = {there ? ((int64_t)page * p.Hkv + kv) * p.c.by_page.d + slot : -1, 0.f};
+    if (own.at >= 0 && p.before) own.before = p.before[own.at];
     return own;
 }
 
