@@ -4,7 +4,7 @@
 //                          channels from float32 24.4 us, 6.2 TB/s.
 // sta_paged_select_kernel  a workgroup for each sequence and key head finds the smallest weight that stays, twelve, ten and ten bits of its place in the order of
 //                          numbers at a time, by counting how many have which; then writes down in order which keys stay.  Bound by the instructions and LDS of the one CU that a head has:
-//                          8 heads of 32,768 keys 23 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 4 the others, 2.5 to count and 5 to write down).
+//                          8 heads of 32,768 keys 22 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 3.5 the others, 2.5 to count and 5 to write down).
 // sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 78 us, 5.0 TB/s
 //                          (82 with stores through the caches).
 #include <hip/hip_runtime.h>
@@ -196,7 +196,7 @@ struct Run {
         weights = reinterpret_cast<const uint32_t *>(p.weights) + (uint64_t)head * p.from.by_page.d;
         own = numbers + wave * (64 * GROUPS) + lane;
         if (!kept) return;
-        constexpr int AT_ONCE = 4;
+        constexpr int AT_ONCE = GROUPS < 4 ? GROUPS : 8;
 #pragma unroll 1
         for (int j0 = begin; j0 < end; j0 += 256 * AT_ONCE) {
             u32x4 w[AT_ONCE];
@@ -258,6 +258,12 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
         else counts[tid] = 0;
         __syncthreads();
         run.each(p, lane, [&](int, u32x4 x) {
+            if (digit > 0) {                                        // most groups have none, of the last digit above all
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any = any || (x[e] ^ least) >> (shift + 10) == 0;
+                if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (digit == 0) atomicAdd(&counts[x[e] >> 20], 1u);
