@@ -297,3 +297,46 @@ def test_on_another_stream():
         torch.cuda.synchronize()
         for x, y in zip(a.results(), b.results()):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_cut_chunks_replayed_with_other_lengths(D):
+    """How long the parts of a walk are follows from the lengths on the device: a captured call replayed with others, parts of the replay before left in the workspace, against the same call made eagerly
+    and the definition."""
+    Hq, Hkv, page, S, T, max_k = 8, 2, 16, 3, 200, 12000
+    g = torch.Generator().manual_seed(11)
+    pages = S * (max_k // page)
+    pool = [torch.randn((pages, page, Hkv, D), generator=g).to(BF).to(DEV) for _ in range(2)]
+    table = torch.randperm(pages, generator=g).view(S, -1).to(torch.int32).to(DEV)
+    cache, cu = sta.StaPagedCache(*pool, table, ints([0] * S)), ints([0] * (S + 1))
+    q = randn((T, Hq, D), 12).to(DEV)
+    n = sta.sta_paged_workspace_bytes(Hq, Hkv, D, S, T, T, max_k)
+    assert n > 0
+    ws = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    out = [(torch.full_like(q, 7.0), torch.full((Hq, T), 7.0, device=DEV)) for _ in range(2)]
+
+    def call(i):
+        sta.sta_paged_forward(q, out[i][0], cu, cache, T, max_k, lse=out[i][1], workspace=ws[i])
+
+    call(0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(0)
+    for new, used in (([100, 60, 40], [12000, 9000, 40]), ([200, 0, 0], [11999, 0, 5]), ([1, 1, 198], [12000, 1, 198]), ([0, 200, 0], [12000, 3000, 12000]), ([70, 70, 60], [100, 100, 60])):
+        cu.copy_(torch.tensor(starts(new), dtype=torch.int32))
+        cache.used.copy_(torch.tensor(used, dtype=torch.int32))
+        graph.replay()
+        call(1)
+        torch.cuda.synchronize()
+        for a, b in zip(*out):
+            assert torch.equal(a, b), (new, used)
+        at = starts(new)
+        for s in range(S):
+            rows, keys = slice(at[s], at[s + 1]), [x[table[s].long()].view(-1, Hkv, D)[:used[s]].cpu().double() for x in pool]
+            Q = q[rows].cpu().double()
+            want = lu.attention(Q, *keys, True, D ** -0.5)
+            b_o, b_lse, _ = bounds(Q, *keys, True, D ** -0.5, want[1])
+            close(out[0][0][rows], want[0], b_o, "sequence %d of %s" % (s, used))
+            seen = want[1] > -math.inf
+            z = out[0][1][:, rows].cpu().double()
+            assert torch.equal(seen, z > -math.inf) and bool(((z - want[1])[seen].abs() <= b_lse[seen]).all()), (new, used)
