@@ -411,12 +411,17 @@ __global__ __launch_bounds__(256, 2) void sta_paged_weights_kernel(WeightsParams
 //   300 on 1300 and 1000 on 5000, 8/8 x 128 (320 | 640 | 1264)  25.6 | 23.5 | 27.9  four of 200 on 3000, 40/8 x 64 (384 | 768 | 1504)  37 | 31 | 35
 //   512 on 4000, 32/8 x 128 (128 | 256 | 504)  49 | 35 | 31       300 on 9000, 16/2 x 128 (72 | 142 | 282)  65 | 40 | 34
 //   eight of 64 on 1300, 40/5 x 128 (240 | 440 | 840)  18.8 | 18.1 | 24.6       50 on 30,000, 8/1 x 128 (118 | 235 | 469)  15.2 | 11.3 | 13.0
+// With 64 channels, where a stage is half the work, two waves by two groups with stages of 64 rows are the better ones for more than 512 rows, whatever the launch: us, four | two along the keys,
+//   512 on 20,001, 32/8  76 | 61       2048 on 8192, 16/16  58 | 50       2048 on 30,000, 8/8  90 | 83       four of 2048, 16/16  56 | 50       four of 1000 on 4000, 16/16  50 | 49
+//   and not for fewer: eight of 64 on 1300, 12/12  8.2 | 10.4; sixteen of 500 on 2048, 16/16  54.5 | 55.3       (stages of 32 rows: four of 200 on 3000, 40/8  29.5, 28.1 with 64; 1, 5 and 33 on 65 to 578, 16/16  4.3, 4.8;
+//   with 128 channels four of 200 38.6, 42)
 struct WeightsPlan {
     int few;                            // blocks of 16 rows, 0: stages
     int along;                          // waves of a workgroup along the keys
+    bool deep;                          // stages of 64 rows for two waves by two groups
     int64_t tiles, workgroups;
 };
-WeightsPlan weights_plan(int S, int Hkv, int64_t rows, int max_k)
+WeightsPlan weights_plan(int S, int Hkv, int D, int64_t rows, int max_k)
 {
     const int64_t cus = sta::compute_units(), heads = (int64_t)S * Hkv;
     auto tiles = [&](int64_t keys) { return (max_k + keys - 1) / keys; };
@@ -425,6 +430,8 @@ WeightsPlan weights_plan(int S, int Hkv, int64_t rows, int max_k)
     if (heads > kMostWorkgroups) return plan;               // too many whatever the tiles are
     plan.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     plan.along = plan.few || tiles(256) * heads >= 2 * cus ? 4 : tiles(128) * heads >= (rows <= 512 ? 3 * cus / 4 : 2 * cus) ? 2 : 1;
+    plan.deep = D == 64 && rows > 512;
+    if (plan.deep && plan.along == 4) plan.along = 2;
     plan.tiles = tiles(64 * plan.along);
     plan.workgroups = plan.tiles * heads;
     return plan;
@@ -442,6 +449,8 @@ hipError_t launch_weights(const WeightsParams &p, const WeightsPlan &plan, hipSt
     const uint32_t n = (uint32_t)plan.workgroups;
     if (plan.few == 1) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 1>, dim3(n), dim3(256), stream, p);
     if (plan.few == 2) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 2>, dim3(n), dim3(256), stream, p);
+    if constexpr (D == 64)
+        if (plan.deep && plan.along == 2) return launch_stages<D, 4, 2, 2>(p, n, stream);
     return plan.along == 4 ? launch_stages<D, 4, 4, 2>(p, n, stream) : plan.along == 2 ? launch_stages<D, 4, 2, 1>(p, n, stream) : launch_stages<D, 4, 1, 1>(p, n, stream);
 }
 
@@ -464,7 +473,7 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     if (S == 0 || max_k == 0) return STA_OK;
     if (!cu_q || !weights || (!lse && tokens_q > 0)) return STA_ERR_NULL;
     if (((uintptr_t)cu_q | (uintptr_t)lse | (uintptr_t)before | (uintptr_t)weights) & 3) return STA_ERR_SHAPE;
-    const WeightsPlan plan = weights_plan(S, Hkv, (int64_t)max_q * (q->heads / Hkv), max_k);
+    const WeightsPlan plan = weights_plan(S, Hkv, D, (int64_t)max_q * (q->heads / Hkv), max_k);
     if (plan.workgroups > kMostWorkgroups) return STA_ERR_SHAPE;
     const uint64_t w_bytes = (uint64_t)cache->pages * cache->page_size * Hkv * sizeof(float), lse_bytes = (uint64_t)tokens_q * q->heads * sizeof(float);
     if (rows_meet(*q, 1, tokens_q, D, weights, w_bytes) || meets_pages(*cache, D, weights, w_bytes) || meets_table(*cache, S, nullptr, 0, 0, D, weights, w_bytes) ||

@@ -93,6 +93,17 @@ WEIGHTS = [
 ]
 
 
+@pytest.mark.parametrize("case", [(16, 16, 64, [700, 30], [3000, 1500], True, 16, 0.5), (16, 16, 64, [600, 513, 0], [5000, 4000, 200], True, 1, 1.0),
+                                  (24, 8, 64, [300, 250], [7000, 6500], False, 20, 1.0), (24, 8, 64, [300, 1], [301, 7000], True, 64, 1.0)], ids=["0", "1", "2", "3"])
+def test_weights_of_many_rows_of_64_channels(case):
+    """More than 512 rows of a key head: two waves along the keys by two groups with stages of 64 rows."""
+    Hq, Hkv, D, new, used, causal, page, decay = case
+    cache = Cache(Hkv, D, page, used, seed=15)
+    q = randn((sum(new), Hq, D), 13)
+    _, lse = forward(q.to(DEV), cache, new, causal=causal, lse=True)
+    check_weights(cache, q, lse, new, causal, decay)
+
+
 @pytest.mark.parametrize("case", WEIGHTS, ids=[str(i) for i in range(len(WEIGHTS))])
 def test_weights(case):
     Hq, Hkv, D, new, used, causal, page, decay = case
