@@ -39,6 +39,7 @@ struct WeightsParams {
     int32_t max_q, max_k;
     sta::FastDiv by_g, by_Hkv, by_tiles;
     uint32_t causal;
+    uint32_t round;                     // tiles of a key head that are there at once, two a CU
     uint32_t even, g_shift;             // whether g is a power of two up to 32, and which
 };
 
@@ -259,29 +260,33 @@ __device__ __forceinline__ void add_rows(uint32_t q_addr, uint32_t row_addr, con
     for (int col = 0; col < NC; ++col) exponentials(BLOCKS - 1, col);
 }
 
-// Workgroup (sequence, KW * 64 keys, key head): KW waves next to each other along the keys, RG = 4 / KW groups of them that take the stages of 32 * U rows in turn.
+// A workgroup's LDS: KW waves next to each other along the keys, RG = 4 / KW groups of them that take the stages of 32 * U rows in turn.
 template <int D, int NC, int KW, int U>
-__global__ __launch_bounds__(256, 2) void sta_paged_weights_kernel(WeightsParams p)
+struct WeightsLds {
+    static constexpr int RG = 4 / KW, KEYS = KW * 16 * NC, ROWS = 32 * U;
+    static constexpr int ROWS_AT = U * StagedRows<D>::Tile, STAGE = ROWS_AT + 2 * ROWS * 4;        // rows, their offsets, how many keys they see
+    // stages: one that is read and two on their way, or one where the groups' stages would leave room for one workgroup a CU
+    static constexpr int RING = RG == 1 ? 3 : 2;
+    static constexpr int STAGES = RG * RING * STAGE, BYTES = STAGES + (RG > 1 ? RG * KEYS * 16 : 0);   // the groups' sums behind them
+};
+
+// The numbers of KW * 64 keys from tile0 on.
+template <int D, int NC, int KW, int U>
+__device__ __forceinline__ void weights_tile(const WeightsParams &p, uint32_t s, int tile0, uint32_t kv, char *smem)
 {
-    constexpr int RG = 4 / KW, OWN = 16 * NC, KEYS = KW * OWN, ROWS = 32 * U, FOLD = 16 / U;
+    using Lds = WeightsLds<D, NC, KW, U>;
+    constexpr int RG = Lds::RG, OWN = 16 * NC, KEYS = Lds::KEYS, ROWS = Lds::ROWS, FOLD = 16 / U, ROWS_AT = Lds::ROWS_AT, STAGE = Lds::STAGE, RING = Lds::RING;
     using L = StagedRows<D>;
     constexpr int PER_WAVE = U * L::Groups / KW;                            // DMA instructions of a wave for a stage
-    constexpr int ROWS_AT = U * L::Tile, STAGE = ROWS_AT + 2 * ROWS * 4;    // rows, their offsets, how many keys they see
-    // stages: one that is read and two on their way, or one where the groups' stages would leave room for one workgroup a CU
-    constexpr int RING = RG == 1 ? 3 : 2;
-    __shared__ __attribute__((aligned(1024))) char smem[RG * RING * STAGE];
-    __shared__ float joined[RG > 1 ? RG : 1][RG > 1 ? KEYS : 1][4];
+    float (*joined)[KEYS][4] = reinterpret_cast<float (*)[KEYS][4]>(smem + Lds::STAGES);
     const int lane = threadIdx.x & 63, all_waves = uniform(threadIdx.x >> 6), g4 = lane >> 4;
     const int rg = all_waves / KW, wave = all_waves % KW;
-    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
-    const uint32_t turn = sta::fast_div(item, p.by_tiles), tile = item - turn * p.by_tiles.d;
-    const uint32_t s = p.S <= 64 ? sequence_of_turn(turn, lane, p) : turn;
     WeightsSeq seq = weights_seq(s, p);
     seq.q0 = uniform(seq.q0);
     seq.lq = uniform(seq.lq);
     seq.lk = uniform(seq.lk);
     seq.rows = uniform(seq.rows);
-    const int tile0 = (int)tile * KEYS, key0 = tile0 + wave * OWN;
+    const int key0 = tile0 + wave * OWN;
     if (tile0 >= seq.lk) return;
     // the rows before token first_token see no key of the tile, those from whole_token on see all
     const int last = (tile0 + KEYS < seq.lk ? tile0 + KEYS : seq.lk) - 1, ahead = seq.lk - seq.lq;
@@ -405,6 +410,48 @@ __global__ __launch_bounds__(256, 2) void sta_paged_weights_kernel(WeightsParams
     if (key0 < seq.lk) store_weights(p, own_key, lane, sum);
 }
 
+// Workgroup (sequence, KW * 64 keys, key head).
+template <int D, int NC, int KW, int U>
+__global__ __launch_bounds__(256, 2) void sta_paged_weights_kernel(WeightsParams p)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[WeightsLds<D, NC, KW, U>::BYTES];
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    const uint32_t turn = sta::fast_div(item, p.by_tiles), tile = item - turn * p.by_tiles.d;
+    const uint32_t s = p.S <= 64 ? sequence_of_turn(turn, threadIdx.x & 63, p) : turn;
+    weights_tile<D, NC, KW, U>(p, s, (int)(tile * WeightsLds<D, NC, KW, U>::KEYS), kv, smem);
+}
+
+// Up to 64 sequences, a lane each: the tiles of 256 keys that there are, those of the sequences of many rows first.  What these leave behind whole rounds of workgroups over the chip, where it is a quarter of a
+// round at most, are two workgroups' of 128 keys each, so that every CU has one at most: us, 32 heads over 8, tiles alone | this, 512 tokens on 20,001 keys 97 | 81, 128 on 20,001  31 | 28, 2048 on 20,001  348 | 290;
+// and where more is left (always | this): 512 on 21,700  103 | 95, on 24,000  104 | 98.
+template <int D>
+__global__ __launch_bounds__(256, 2) void sta_paged_weights_rounds_kernel(WeightsParams p)
+{
+    constexpr int WHOLE = WeightsLds<D, 4, 4, 2>::BYTES, HALF = WeightsLds<D, 4, 2, 1>::BYTES;
+    __shared__ __attribute__((aligned(1024))) char smem[WHOLE > HALF ? WHOLE : HALF];
+    const int lane = threadIdx.x & 63;
+    const uint32_t item = sta::fast_div(blockIdx.x, p.by_Hkv), kv = blockIdx.x - item * p.Hkv;
+    uint32_t own = 0;
+    bool many = false;
+    if (lane < (int)p.S) {
+        const WeightsSeq seq = weights_seq((uint32_t)lane, p);
+        const uint32_t there = ((uint32_t)seq.lk + 255) / 256;
+        own = there < p.by_tiles.d ? there : p.by_tiles.d;
+        many = 2 * (int64_t)seq.lq >= p.max_q;
+    }
+    const uint32_t upto_many = scan64(many ? own : 0), all_many = (uint32_t)__builtin_amdgcn_readlane((int)upto_many, 63);
+    const uint32_t left = all_many % p.round, whole = 4 * left <= p.round ? all_many - left : all_many, with_halves = 2 * all_many - whole;
+    const bool few = item >= with_halves;
+    const uint32_t rank = few ? item - with_halves : item < whole ? item : whole + (item - whole) / 2;
+    const uint32_t upto = few ? scan64(many ? 0 : own) : upto_many;
+    const uint64_t at = __builtin_amdgcn_ballot_w64(upto > rank);
+    if (at == 0) return;
+    const int s = __builtin_ctzll(at);
+    const int tile0 = (int)((rank - (uint32_t)__builtin_amdgcn_readlane((int)(upto - own), s)) * 256);
+    if (!few && item >= whole) weights_tile<D, 4, 2, 1>(p, (uint32_t)s, tile0 + (int)((item - whole) % 2) * 128, kv, smem);
+    else weights_tile<D, 4, 4, 2>(p, (uint32_t)s, tile0, kv, smem);
+}
+
 // Four waves along the keys where that makes two workgroups a CU, two waves by two groups where that does, or where walks are of 512 rows at most and three quarters of the CUs
 // have one, else one wave by four groups.  us, four | two | one along the keys, new tokens on keys of heads / key heads x channels:
 //   512 on 20,001, 32/8 x 128 (632 | 1256 | 2504 workgroups)  107 | 105 | 142       2048 on 16,384, 32/8 x 128 (512 | 1024 | 2048)  259 | 287 | 353
@@ -449,6 +496,9 @@ hipError_t launch_weights(const WeightsParams &p, const WeightsPlan &plan, hipSt
     const uint32_t n = (uint32_t)plan.workgroups;
     if (plan.few == 1) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 1>, dim3(n), dim3(256), stream, p);
     if (plan.few == 2) return sta::launch_kernel(sta_paged_few_weights_kernel<D, 4, 2>, dim3(n), dim3(256), stream, p);
+    if constexpr (D == 128)
+        if (plan.along == 4 && p.S <= 64 && plan.workgroups + p.round * p.Hkv <= kMostWorkgroups)
+            return sta::launch_kernel(sta_paged_weights_rounds_kernel<D>, dim3(n + p.round * p.Hkv), dim3(256), stream, p);
     if constexpr (D == 64)
         if (plan.deep && plan.along == 2) return launch_stages<D, 4, 2, 2>(p, n, stream);
     return plan.along == 4 ? launch_stages<D, 4, 4, 2>(p, n, stream) : plan.along == 2 ? launch_stages<D, 4, 2, 1>(p, n, stream) : launch_stages<D, 4, 1, 1>(p, n, stream);
@@ -502,6 +552,7 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     p.even = (p.g & (p.g - 1)) == 0 && p.g <= 32 && q->head < (int64_t)1 << 25;
     p.g_shift = p.even ? (uint32_t)__builtin_ctz(p.g) : 0;
     p.by_tiles = sta::fast_div_of((uint32_t)plan.tiles);
+    p.round = (2 * (uint32_t)sta::compute_units() + Hkv - 1) / Hkv;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = D == 64 ? launch_weights<64>(p, plan, stream) : launch_weights<128>(p, plan, stream);
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;

@@ -104,6 +104,17 @@ def test_weights_of_many_rows_of_64_channels(case):
     check_weights(cache, q, lse, new, causal, decay)
 
 
+@pytest.mark.parametrize("case", [(16, 16, 128, [100, 40], [9500, 4000], True, 16, 0.5), (16, 16, 128, [100, 40, 0, 60], [8300, 4000, 129, 1], False, 5, 1.0),
+                                  (15, 5, 128, [50, 60, 1], [14000, 12900, 300], True, 64, 1.0), (15, 5, 128, [40, 1, 39], [14000, 12900, 12345], True, 1, 0.0)], ids=["0", "1", "2", "3"])
+def test_weights_of_rounds_of_tiles(case):
+    """Tiles of 256 keys of 128 channels, the last few of the many in halves, of which one may have no key."""
+    Hq, Hkv, D, new, used, causal, page, decay = case
+    cache = Cache(Hkv, D, page, used, seed=25)
+    q = randn((sum(new), Hq, D), 23)
+    _, lse = forward(q.to(DEV), cache, new, causal=causal, lse=True)
+    check_weights(cache, q, lse, new, causal, decay)
+
+
 @pytest.mark.parametrize("case", WEIGHTS, ids=[str(i) for i in range(len(WEIGHTS))])
 def test_weights(case):
     Hq, Hkv, D, new, used, causal, page, decay = case
