@@ -10,7 +10,8 @@
 //                                on 1 to 16,384 keys 184 us, 4.7 TB/s (155 where nothing is written, though that is 12 of 870 MB).  Numbers before are asked for behind the keys'
 //                                rows and in a branch of their own: before them 190, inside the branch that finds their place 188, behind the sums 190.  Sums of 16 tiles held back and written
 //                                together by workgroups that stay: 180, but 53 in place of 45 with 64 channels.
-// sta_paged_weights_kernel       more: stages of 32 or 64 rows go through LDS, shared by the waves along the keys; small launches cut the rows among a workgroup's waves.  Bound by
+// sta_paged_weights_kernel       (and sta_paged_weights_rounds_kernel, its tiles in another order, the last ones halved)
+//                                more: stages of 32 or 64 rows go through LDS, shared by the waves along the keys; small launches cut the rows among a workgroup's waves.  Bound by
 //                                vector and matrix instructions, which hardly overlap (per 64 rows and 64 keys of a wave 1024 cycles of the matrix pipe, 64 exponentials of 8 cycles, as
 //                                many multiply-adds and sums of 4): 2048 tokens of 32 heads over 8 of 128 channels on 16,384 keys 260 us, 990 TFLOP/s.  With stages of 32 rows 294 us, two stages
 //                                in place of three 265, 32 keys a wave 315, 128 keys a workgroup 274 to 296; the order of the instructions in a stage changes nothing.
