@@ -418,6 +418,9 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
  * from 1 on; multiples of 8 (head dimension 128: of 4) are read fastest.  A page may stand in the rows of several sequences (a common beginning).
  * table: device int32, S rows of table_pages entries; used: device int32 [S].  Lengths are cut to what a row of the table has places for.  Entries for keys that are
  * not used are not looked at; entries of used keys that are no pages are read as some page (of what is written there nothing is written).
+ * Numbers of keys (the attention weights that they have gathered, below), float32, key j of sequence s and key head n: with numbers_by_sequence 0 an array [pages, Hkv, page_size], where
+ * the key's row lies, at (page, n, slot); with 1 an array [S, Hkv, table_pages * page_size], at (s, n, j).  Pages that stand more than once in the table need the latter: the former has one
+ * number for all keys that a slot is, and what a call that writes numbers leaves there then depends on the order of its workgroups.
  * Supported: D in {64, 128}; rows at multiples of 16 bytes; pages and the slots of one page less than 2^32 bytes apart; table_pages * page_size counts up to
  * 2^31 - 4096.  Pages, tables and lengths must not overlap what a call writes, but for what it says.
  */
@@ -429,6 +432,7 @@ typedef struct {
     int64_t table_row;          /* entries from one sequence's row to the next */
     int table_pages;
     int32_t *used;
+    int numbers_by_sequence;    /* 0 or 1: where the keys' numbers stand */
 } sta_paged_cache;
 
 /*
@@ -436,7 +440,7 @@ typedef struct {
  * the new ones, as the attention behind it takes them.  k, v: [tokens, Hkv, D], strides as sta_head_rows says (batch is not looked at), both bf16 or both
  * float32 (rounded once).  cu: device int32 [S + 1].  max_new: host, an upper bound of the sequences' new tokens; tokens beyond it are not written, nor are those
  * whose key would be below 0 or beyond the table.  A key that two calls' sequences write at once holds one row or the other.
- * weights: NULL, or the keys' gathered attention weights, float32 [pages, Hkv, page_size]: 0 is written for every key that is.
+ * weights: NULL, or the keys' numbers: 0 is written for every key that is.
  * Supported: up to 65,535 sequences.
  */
 int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, int64_t tokens, const int32_t *cu, const sta_paged_cache *cache, int S, int max_new,
@@ -455,11 +459,11 @@ int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse
  * The attention weight that the keys of a cache in pages gather from the rows of a call: for every key j of a sequence and key head n
  *     weights_j = decay * before_j + sum over the query tokens i that see j, and the query heads of n, of exp(scale q_i . k_j - lse_i),
  * the sums of the columns of the attention's probabilities.  q, cu_q, causal, scale: as sta_paged_forward; lse: float32 [Hq, tokens_q] as it wrote it (a call on the
- * last rows of a prompt alone gives what those look at).  Rows without keys (lse -infinity) give nothing.  before, weights: float32 [pages, Hkv, page_size], key j's number where its
- * row lies; before may be weights itself, or NULL (nothing); decay 0: it is not looked at; decay has to be finite.  Written for every key j < max_k of a sequence, with
- * no query tokens too; the numbers of other slots are left as they are.  A page that several sequences share gets one sequence's numbers or the other's.
+ * last rows of a prompt alone gives what those look at).  Rows without keys (lse -infinity) give nothing.  before, weights: the keys' numbers;
+ * before may be weights itself, or NULL (nothing); decay 0: it is not looked at; decay has to be finite.  Written for every key j < max_k of a sequence, with
+ * no query tokens too; other numbers are left as they are.  Of pages that sequences share numbers by sequence alone mean something (sta_paged_cache).
  * max_q, max_k: host, upper bounds; query tokens beyond max_q give nothing.
- * Scores, exponents and sums in fp32; no atomics: repeated calls give identical bits.  NaN in a row or key that meet makes NaN of that key's number.
+ * Scores, exponents and sums in fp32; no atomics: repeated calls give identical bits (by page, of pages that stand once in the table).  NaN in a row or key that meet makes NaN of that key's number.
  * Supported: as sta_paged_forward; fewer than 2^24 workgroups, of which every sequence and key head has one for up to 256 keys of max_k (for 64 in small launches).
  */
 int sta_paged_weights(const sta_head_rows *q, const float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S, int max_q, int max_k,
@@ -469,9 +473,9 @@ int sta_paged_weights(const sta_head_rows *q, const float *lse, int64_t tokens_q
  * Takes what stays of the sequences of a cache to the pages of another table: of used[s] keys every key head keeps min(used[s], keep), the first `first`, the
  * last `recent`, and of those between the ones of the greatest weights, of equal ones the earlier (NaN counts as the greatest, -0 as 0).  Their order stays; what was the
  * row at index kept[s, n, j] is key j of head n in `into`, and so is its weight in into_weights (NULL: not taken).  Heads keep different keys, but equally many.
- * weights: float32 [pages, Hkv, page_size] of cache, into_weights of into.  kept: device int32 [S, Hkv, keep], written; -1 from min(used[s], keep) on.  into->used: written,
- * min(used[s], keep).  into's pool, page size and layout may be others, or the pool the same (then into_weights may be weights): the pages in into's table, which must be distinct, must then
- * be none that cache's rows have among their used ones.  So pages that sequences share can be evicted from, and a call that is made again gives the same.
+ * weights: the numbers of cache's keys, into_weights of into's, each as its cache has them.  kept: device int32 [S, Hkv, keep], written; -1 from min(used[s], keep) on.  into->used: written,
+ * min(used[s], keep).  into's pool, page size and layout may be others, or the pool the same (then into_weights may be weights where both are by page): the pages in into's table, which must be distinct, must then
+ * be none that cache's rows have among their used ones.  So pages that sequences share can be evicted from (by numbers by sequence), and a call that is made again gives the same.
  * first + recent may not exceed keep; into's rows of the table need places for keep keys (else STA_ERR_SHAPE).  One or two launches; fewer than 2^22 heads of all sequences, fewer than 2^24
  * blocks of 16 (head dimension 64: 32) kept rows of one head.
  */

@@ -511,10 +511,10 @@ struct PagedEntries {
     decltype(&sta_paged_evict) evict;
 } paged = {};
 
-// (address of a sta_paged_cache, sequences, key heads, channels, pages, slots of a page), as the cache's object keeps them
+// (address of a sta_paged_cache, sequences, key heads, channels, and what an array of its keys' numbers has before and behind the key heads), as the cache's object keeps them
 struct CacheArg {
     const sta_paged_cache *c;
-    int64_t S, Hkv, D, pages, page_size;
+    int64_t S, Hkv, D, outer, inner;
 };
 bool cache_of(PyObject *o, CacheArg &a)
 {
@@ -529,13 +529,13 @@ bool cache_of(PyObject *o, CacheArg &a)
     a = {a.c, x[0], x[1], x[2], x[3], x[4]};
     return a.c != nullptr && small(a.S) && small(a.Hkv) && small(a.D);
 }
-// Numbers of all keys of the pool, dense float32 [pages, Hkv, page_size]; None: null.
+// The keys' numbers, dense float32 [outer, Hkv, inner]; None: null.
 bool key_numbers(PyObject *o, const CacheArg &a, const void *&out)
 {
     out = nullptr;
     if (o == Py_None) return true;
     View v;
-    if (!dense(o, v) || v.t->dim() != 3 || v.t->size(0) != a.pages || v.t->size(1) != a.Hkv || v.t->size(2) != a.page_size || v.t->scalar_type() != at::kFloat)
+    if (!dense(o, v) || v.t->dim() != 3 || v.t->size(0) != a.outer || v.t->size(1) != a.Hkv || v.t->size(2) != a.inner || v.t->scalar_type() != at::kFloat)
         return false;
     out = v.ptr;
     return out != nullptr;

@@ -23,6 +23,12 @@ struct PagedCache {
     int32_t room;                   // keys that a row of the table has places for
 };
 
+// Where the numbers of a cache's keys stand.
+struct KeyNumbers {
+    uint32_t by_sequence;           // in rows, one for every sequence and key head; else beside the pages
+    int64_t row;
+};
+
 // Entries of the table that are no pages of the pool are cut to what is there: what is read for them means nothing, and is inside the pool.
 __device__ __forceinline__ uint32_t page_inside(int entry, const PagedCache &c) { return (uint32_t)bound_of(entry, 0, (int)c.pages - 1); }
 __device__ __forceinline__ int used_of(uint32_t s, const PagedCache &c) { return bound_of(c.used[s], 0, c.room); }
@@ -34,11 +40,19 @@ __device__ __forceinline__ uint32_t entry_of(uint32_t key, const PagedCache &c, 
     return n;
 }
 __device__ __forceinline__ uint64_t place_of(uint32_t page, uint32_t slot, const PagedCache &c) { return (uint64_t)page * c.page + slot * c.token; }
+// Where the number of a key stands, by floats: of key head h of Hkv, key `key` of sequence s, in a slot of a page.  Beside the pages one number is all keys' that a slot is, and so one sequence's
+// alone where the page stands once in the table.
+template <bool BY_SEQUENCE = true>          // false: by page in any case
+__device__ __forceinline__ int64_t number_at(uint32_t s, uint32_t h, uint32_t Hkv, uint32_t key, uint32_t page, uint32_t slot, const PagedCache &c, const KeyNumbers &n)
+{
+    return BY_SEQUENCE && n.by_sequence ? ((int64_t)s * Hkv + h) * n.row + key : ((int64_t)page * Hkv + h) * c.by_page.d + slot;
+}
 
 // Whether the kernels can take a cache; written: its rows are.  S sequences of heads of D channels.
 int paged_check(const sta_paged_cache *c, int S, int D, bool written)
 {
     if (!c) return STA_ERR_NULL;
+    if (c->numbers_by_sequence & ~1) return STA_ERR_UNSUPPORTED;
     if (c->pages < 0 || c->pages > 0x7fffffff || c->page_size < 1 || c->table_pages < 0 || c->table_row < 0 || c->table_row > kMostStride || S < 0) return STA_ERR_SHAPE;
     const sta_head_rows *rows[2] = {&c->k, &c->v};
     for (const sta_head_rows *r : rows) {
@@ -64,6 +78,16 @@ inline int64_t room_of(const sta_paged_cache &c)
     const int64_t room = (int64_t)c.table_pages * c.page_size;
     return c.pages == 0 ? 0 : room < kMostTokens ? room : kMostTokens;
 }
+
+// The keys' numbers of a cache of S sequences, all key heads; below 2^60 (else none of it is taken).
+inline __int128 numbers_of(const sta_paged_cache &c, int S)
+{
+    return (c.numbers_by_sequence ? (__int128)S * c.table_pages : (__int128)c.pages) * c.page_size * c.k.heads;
+}
+inline bool numbers_fit(const sta_paged_cache &c, int S) { return numbers_of(c, S) <= (__int128)1 << 60; }
+inline uint64_t number_bytes(const sta_paged_cache &c, int S) { return (uint64_t)numbers_of(c, S) * sizeof(float); }
+
+inline KeyNumbers key_numbers_of(const sta_paged_cache &c) { return {(uint32_t)c.numbers_by_sequence, (int64_t)c.table_pages * c.page_size}; }
 
 inline PagedCache paged_cache_of(const sta_paged_cache &c)
 {

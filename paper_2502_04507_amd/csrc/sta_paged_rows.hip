@@ -25,6 +25,7 @@ struct AppendParams {
     float *weights;                     // or null
     sta::FastDiv by_chunks;             // lanes of a token: 2 Hkv D / 8
     uint32_t tokens, max_new, Hkv, each, per_seq;      // tokens of a workgroup at a time, workgroups of a sequence
+    KeyNumbers numbers;
 };
 
 // Eight channels of a row as bf16, rounded to nearest where they are float32.
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(256) void sta_paged_append_kernel(AppendParams p)
                 const PackedRows &from = value ? p.v : p.k;
                 x[j] = eight_of<F32>(from.data + (int64_t)(first + (int)(t0 + t)) * from.token + (int64_t)h * from.head + c * (F32 ? 32 : 16));
                 to[j] = (value ? p.c.v : p.c.k) + place_of((uint32_t)page, slot, p.c) + (int64_t)h * p.c.head + 16 * c;
-                if (p.weights && !value && c == 0) p.weights[((int64_t)page * p.Hkv + h) * p.c.by_page.d + slot] = 0.f;
+                if (p.weights && !value && c == 0) p.weights[number_at(s, h, p.Hkv, (uint32_t)key, (uint32_t)page, slot, p.c, p.numbers)] = 0.f;
             }
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
@@ -102,11 +103,13 @@ struct EvictParams {
     sta::FastDiv by_Hkv, by_blocks;
     uint32_t page_weights;              // numbers of a page, of all key heads
     uint32_t row_lanes;                 // not 0: rows are moved by the kernel that selects them, so many lanes a row
-    uint32_t fours;                     // pages of a multiple of four slots, weights at a multiple of 16 bytes
+    uint32_t fours;                     // pages of a multiple of four slots (by sequence: such rows), weights at a multiple of 16 bytes
+    KeyNumbers from_numbers, to_numbers;
 };
 
-// Takes 16 bytes, chunk c, of key `key` of head h to key j of the other cache, and the weight with the first.
-template <bool STREAM>
+// Takes 16 bytes, chunk c, of key `key` of head h to key j of the other cache, and the weight with the first.  BY_SEQUENCE: the numbers of either cache may be by sequence (as a choice at every number
+// by itself it costs evictions that know no such caches 1 to 5 %: 8 heads of 32,768 keys 36.7 -> 38.3 us).
+template <bool STREAM, bool BY_SEQUENCE>
 __device__ __forceinline__ void move_chunk(const EvictParams &p, uint32_t s, uint32_t h, uint32_t j, uint32_t key, uint32_t c)
 {
     uint32_t slot, to_slot;
@@ -117,8 +120,7 @@ __device__ __forceinline__ void move_chunk(const EvictParams &p, uint32_t s, uin
     const u32x4 k = *reinterpret_cast<const u32x4 *>(p.from.k + at), v = *reinterpret_cast<const u32x4 *>(p.from.v + at);
     store_row<STREAM>(p.to.k + to, k);
     store_row<STREAM>(p.to.v + to, v);
-    if (c == 0 && p.to_weights)
-        p.to_weights[((uint64_t)to_page * p.Hkv + h) * p.to.by_page.d + to_slot] = p.weights[((uint64_t)page * p.Hkv + h) * p.from.by_page.d + slot];
+    if (c == 0 && p.to_weights) p.to_weights[number_at<BY_SEQUENCE>(s, h, p.Hkv, j, (uint32_t)to_page, to_slot, p.to, p.to_numbers)] = p.weights[number_at<BY_SEQUENCE>(s, h, p.Hkv, key, page, slot, p.from, p.from_numbers)];
 }
 
 // The bits of a number as a whole number in their order: NaN above all others, 0 and -0 the same.  On the bits throughout: comparisons of numbers are compiled as if
@@ -136,25 +138,30 @@ constexpr uint32_t kFewRows = 256;
 // What a wave looks at: a run of keys, four adjacent ones a lane and 256 at a time, as whole numbers in the order of their weights.  Keys that stay or go in any case (the first, the
 // recent ones, and places behind the last) count as 0, which no weight has, nor any up to 2^20.  A run of up to 256 * GROUPS keys stays in LDS from the first look on, of a longer one every
 // number is looked up every time.
-template <int GROUPS>
+template <int GROUPS, bool BY_SEQUENCE>
 struct Run {
     u32x4 *own;                         // of the wave and lane, in LDS
     int begin, end, length, lo, hi;     // length: of a run
     bool kept;
     const int32_t *row;
-    const uint32_t *weights;            // of the key head
+    const uint32_t *weights;            // of the key head, by sequence of the sequence
     __device__ __forceinline__ u32x4 look(const EvictParams &p, int j) const
     {
         u32x4 w = {0, 0, 0, 0};
         if (p.fours) {
             uint32_t slot;
             if (j >= end) return w;
+            if (BY_SEQUENCE && p.from_numbers.by_sequence) return *reinterpret_cast<const u32x4 *>(weights + j);
             const int entry = row[entry_of((uint32_t)j, p.from, &slot)];
             return *reinterpret_cast<const u32x4 *>(weights + ((uint64_t)page_inside(entry, p.from) * p.page_weights + slot));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (j + e >= end) return w;
+            if (BY_SEQUENCE && p.from_numbers.by_sequence) {
+                w[e] = weights[j + e];
+                continue;
+            }
             uint32_t slot;
             const uint32_t page = page_inside(row[entry_of((uint32_t)(j + e), p.from, &slot)], p.from);
             w[e] = weights[(uint64_t)page * p.page_weights + slot];
@@ -183,7 +190,7 @@ struct Run {
     }
     // whether no key of 256 stays or goes in any case
     __device__ __forceinline__ bool inside(int j0) const { return j0 >= lo && hi - j0 >= 256; }
-    __device__ __forceinline__ void start(const EvictParams &p, int n, int wave, int lane, const int32_t *table_row, uint32_t head, u32x4 *numbers)
+    __device__ __forceinline__ void start(const EvictParams &p, int n, int wave, int lane, uint32_t s, uint32_t h, u32x4 *numbers)
     {
         length = ((n + kSelectWaves - 1) / kSelectWaves + 255) & ~255;
         kept = length <= 256 * GROUPS;
@@ -192,8 +199,8 @@ struct Run {
         const int all = n - p.recent;
         lo = p.first > begin ? p.first : begin;
         hi = all < end ? all : end;
-        row = table_row;
-        weights = reinterpret_cast<const uint32_t *>(p.weights) + (uint64_t)head * p.from.by_page.d;
+        row = p.from.table + (int64_t)s * p.from.table_row;
+        weights = reinterpret_cast<const uint32_t *>(p.weights) + number_at<BY_SEQUENCE>(s, h, p.Hkv, 0, 0, 0, p.from, p.from_numbers);
         own = numbers + wave * (64 * GROUPS) + lane;
         if (!kept) return;
         constexpr int AT_ONCE = GROUPS < 4 ? GROUPS : 8;
@@ -222,7 +229,7 @@ struct Run {
 };
 
 // Workgroup: a sequence and key head, runs of up to 256 * GROUPS keys in LDS.
-template <int GROUPS>
+template <int GROUPS, bool BY_SEQUENCE>
 __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p)
 {
     __shared__ u32x4 numbers[kSelect * GROUPS];
@@ -238,7 +245,7 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
     if (n <= p.keep) {
         for (int j = tid; j < n; j += kSelect) kept[j] = j;
         if (lanes)
-            for (uint32_t i = tid; i < (uint32_t)n << shift; i += kSelect) move_chunk<false>(p, s, h, i >> shift, i >> shift, i & (lanes - 1));
+            for (uint32_t i = tid; i < (uint32_t)n << shift; i += kSelect) move_chunk<false, BY_SEQUENCE>(p, s, h, i >> shift, i >> shift, i & (lanes - 1));
         return;
     }
     auto stays = [&](uint32_t at, int j) __attribute__((always_inline)) {
@@ -246,8 +253,8 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
         kept[at] = j;
         if (lanes && at < kFewRows) few[at] = (uint32_t)j;
     };
-    Run<GROUPS> run;
-    run.start(p, n, wave, lane, p.from.table + (int64_t)s * p.from.table_row, h, numbers);
+    Run<GROUPS, BY_SEQUENCE> run;
+    run.start(p, n, wave, lane, s, h, numbers);
     uint32_t need = (uint32_t)(p.keep - p.first - p.recent);        // of those that may go so many stay
     uint32_t least = need > 0 ? 0 : 0xffffffffu;                    // the bits that are known of the least one that does
 #pragma unroll
@@ -364,11 +371,11 @@ __global__ __launch_bounds__(kSelect) void sta_paged_select_kernel(EvictParams p
     });
     if (!lanes) return;
     __syncthreads();
-    for (uint32_t i = tid; i < (uint32_t)p.keep << shift; i += kSelect) move_chunk<false>(p, s, h, i >> shift, (uint32_t)bound_of((int)few[i >> shift], 0, n - 1), i & (lanes - 1));
+    for (uint32_t i = tid; i < (uint32_t)p.keep << shift; i += kSelect) move_chunk<false, BY_SEQUENCE>(p, s, h, i >> shift, (uint32_t)bound_of((int)few[i >> shift], 0, n - 1), i & (lanes - 1));
 }
 
 // One row a lane: two and four at once, whose addresses and data leave room for fewer waves, took 86 and 96 us where one takes 81 (24 sequences, 8 heads, 2048 rows each).
-template <int D, bool STREAM>
+template <int D, bool STREAM, bool BY_SEQUENCE>
 __global__ __launch_bounds__(256) void sta_paged_move_kernel(EvictParams p)
 {
     constexpr int LPR = D / 8, ROWS = 256 / LPR;
@@ -376,7 +383,7 @@ __global__ __launch_bounds__(256) void sta_paged_move_kernel(EvictParams p)
     const uint32_t s = sta::fast_div(item, p.by_Hkv), h = item - s * p.Hkv;
     const int n = used_of(s, p.from), stay = n < p.keep ? n : p.keep, j = (int)block * ROWS + (int)(threadIdx.x / LPR);
     if (j >= stay) return;
-    move_chunk<STREAM>(p, s, h, (uint32_t)j, (uint32_t)bound_of(p.kept[(int64_t)item * p.keep + j], 0, n - 1), threadIdx.x % LPR);
+    move_chunk<STREAM, BY_SEQUENCE>(p, s, h, (uint32_t)j, (uint32_t)bound_of(p.kept[(int64_t)item * p.keep + j], 0, n - 1), threadIdx.x % LPR);
 }
 
 // Whether two pools share memory without being one and the same.
@@ -409,9 +416,6 @@ int new_rows_check(const sta_head_rows *r, int64_t tokens, int heads, int D)
     return STA_OK;
 }
 
-// Bytes of one number of 32 bits for every key of the pool and key head.
-uint64_t weight_bytes(const sta_paged_cache &c) { return (uint64_t)c.pages * c.page_size * c.k.heads * sizeof(float); }
-
 }  // namespace
 
 extern "C" int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, int64_t tokens, const int32_t *cu, const sta_paged_cache *cache, int S,
@@ -425,13 +429,13 @@ extern "C" int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, 
     if (int rc = new_rows_check(k, tokens, Hkv, D)) return rc;
     if (int rc = new_rows_check(v, tokens, Hkv, D)) return rc;
     if (k->dtype != v->dtype) return STA_ERR_UNSUPPORTED;
-    if ((__int128)cache->pages * cache->page_size * Hkv > (__int128)1 << 60) return STA_ERR_SHAPE;
+    if (!numbers_fit(*cache, S)) return STA_ERR_SHAPE;
     if (S == 0 || tokens == 0 || max_new == 0 || room_of(*cache) == 0) return STA_OK;
     if (!cu) return STA_ERR_NULL;
     if (((uintptr_t)cu | (uintptr_t)weights) & 3) return STA_ERR_SHAPE;
     if (S > 65535) return STA_ERR_SHAPE;
     if (rows_overlap(cache->k, cache->v, (int)cache->pages, cache->page_size, D)) return STA_ERR_ALIAS;
-    const uint64_t w_bytes = weight_bytes(*cache), cu_bytes = ((uint64_t)S + 1) * sizeof(int32_t);
+    const uint64_t w_bytes = number_bytes(*cache, S), cu_bytes = ((uint64_t)S + 1) * sizeof(int32_t);
     const sta_head_rows *rows[2] = {k, v}, *pool[2] = {&cache->k, &cache->v};
     for (int i = 0; i < 2; ++i) {
         if (rows_in_pages(*cache, D, *rows[i], tokens) || rows_meet(*rows[i], 1, tokens, D, weights, w_bytes)) return STA_ERR_ALIAS;
@@ -447,6 +451,7 @@ extern "C" int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, 
     p.v = {static_cast<char *>(v->data), v->token * size, v->head * size};
     p.cu = cu;
     p.c = paged_cache_of(*cache);
+    p.numbers = key_numbers_of(*cache);
     p.weights = weights;
     p.by_chunks = sta::fast_div_of(2 * Hkv * (D / 8));
     p.tokens = (uint32_t)tokens;
@@ -481,9 +486,9 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     const int Hkv = cache->k.heads;
     if (into->k.heads != Hkv || (int64_t)into->table_pages * into->page_size < keep || keep > kMostTokens) return STA_ERR_SHAPE;
     for (const sta_paged_cache *c : {cache, into})
-        if ((int64_t)c->page_size * Hkv > 0xffffffff || (__int128)c->pages * c->page_size * Hkv > (__int128)1 << 60) return STA_ERR_SHAPE;
+        if ((int64_t)c->page_size * Hkv > 0xffffffff || !numbers_fit(*c, S)) return STA_ERR_SHAPE;
     if (S == 0) return STA_OK;
-    const uint64_t w_bytes = weight_bytes(*cache), to_bytes = into_weights ? weight_bytes(*into) : 0;
+    const uint64_t w_bytes = number_bytes(*cache, S), to_bytes = into_weights ? number_bytes(*into, S) : 0;
     if ((!weights && w_bytes > 0) || (!kept && keep > 0)) return STA_ERR_NULL;
     if (((uintptr_t)weights | (uintptr_t)into_weights | (uintptr_t)kept) & 3) return STA_ERR_SHAPE;
     const int64_t rows = 2048 / D, blocks = (keep + rows - 1) / rows, items = (int64_t)S * Hkv;
@@ -491,7 +496,8 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     if (items > most_selects || items * blocks > kMostWorkgroups) return STA_ERR_SHAPE;
     const uint64_t kept_bytes = (uint64_t)items * keep * sizeof(int32_t);
     if (rows_overlap(into->k, into->v, (int)into->pages, into->page_size, D) || pools_meet(*cache, *into, D)) return STA_ERR_ALIAS;
-    const bool one = into_weights == weights && cache->pages == into->pages && cache->page_size == into->page_size;
+    // by page a number moves with its row, to where none is read; by sequence the numbers of a row of one array would move to where others are still to be read
+    const bool one = into_weights == weights && cache->pages == into->pages && cache->page_size == into->page_size && !cache->numbers_by_sequence && !into->numbers_by_sequence;
     if (!one && ranges_meet(weights, w_bytes, into_weights, to_bytes)) return STA_ERR_ALIAS;
     const struct { const void *at; uint64_t bytes; } written[3] = {{into_weights, to_bytes}, {kept, kept_bytes}, {into->used, used_bytes(S)}};
     for (int i = 0; i < 3; ++i) {
@@ -511,6 +517,8 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     EvictParams p = {};
     p.from = paged_cache_of(*cache);
     p.to = paged_cache_of(*into);
+    p.from_numbers = key_numbers_of(*cache);
+    p.to_numbers = key_numbers_of(*into);
     p.weights = weights;
     p.to_weights = into_weights;
     p.kept = kept;
@@ -524,18 +532,20 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     const bool pools = into->pages > 0 && cache->pages > 0, here = pools && (int64_t)keep * D <= 64 * (int64_t)kFewRows;
     p.row_lanes = here ? D / 8 : 0;
     p.page_weights = (uint32_t)cache->page_size * Hkv;
-    p.fours = cache->page_size % 4 == 0 && ((uintptr_t)weights & 15) == 0;
+    p.fours = (cache->numbers_by_sequence ? p.from_numbers.row : (int64_t)cache->page_size) % 4 == 0 && ((uintptr_t)weights & 15) == 0;
     p.by_blocks = sta::fast_div_of(blocks > 0 ? (uint32_t)blocks : 1);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    // up to 8192 keys two workgroups fit a CU, up to 32,768 one
-    hipError_t e = p.from.room <= 8 * kSelect ? sta::launch_kernel(sta_paged_select_kernel<2>, dim3((uint32_t)items), dim3(kSelect), stream, p)
-                                              : sta::launch_kernel(sta_paged_select_kernel<8>, dim3((uint32_t)items), dim3(kSelect), stream, p);
-    if (e == hipSuccess && keep > 0 && pools && !here) {
+    auto launch = [&](auto by) {
+        constexpr bool BY = decltype(by)::value;
+        // up to 8192 keys two workgroups fit a CU, up to 32,768 one
+        hipError_t e = p.from.room <= 8 * kSelect ? sta::launch_kernel(sta_paged_select_kernel<2, BY>, dim3((uint32_t)items), dim3(kSelect), stream, p)
+                                                  : sta::launch_kernel(sta_paged_select_kernel<8, BY>, dim3((uint32_t)items), dim3(kSelect), stream, p);
+        if (e != hipSuccess || keep == 0 || !pools || here) return e;
         const dim3 grid((uint32_t)(items * blocks)), block(256);
         const bool past = (__int128)4 * items * keep * D > kCaches;
-        e = D == 64 ? past ? sta::launch_kernel(sta_paged_move_kernel<64, true>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<64, false>, grid, block, stream, p)
-            : past  ? sta::launch_kernel(sta_paged_move_kernel<128, true>, grid, block, stream, p)
-                    : sta::launch_kernel(sta_paged_move_kernel<128, false>, grid, block, stream, p);
-    }
+        if (D == 64) return past ? sta::launch_kernel(sta_paged_move_kernel<64, true, BY>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<64, false, BY>, grid, block, stream, p);
+        return past ? sta::launch_kernel(sta_paged_move_kernel<128, true, BY>, grid, block, stream, p) : sta::launch_kernel(sta_paged_move_kernel<128, false, BY>, grid, block, stream, p);
+    };
+    const hipError_t e = cache->numbers_by_sequence || into->numbers_by_sequence ? launch(std::true_type{}) : launch(std::false_type{});
     return e == hipSuccess ? STA_OK : STA_ERR_HIP;
 }

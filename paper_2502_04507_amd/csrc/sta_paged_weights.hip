@@ -42,6 +42,7 @@ struct WeightsParams {
     uint32_t causal;
     uint32_t round;                     // tiles of a key head that are there at once, two a CU
     uint32_t even, g_shift;             // whether g is a power of two up to 32, and which
+    KeyNumbers numbers;
 };
 
 struct WeightsSeq {
@@ -86,7 +87,7 @@ __device__ __forceinline__ OwnKey load_keys(const WeightsParams &p, uint32_t s, 
         for (int ks = 0; ks < D / 32; ++ks) K[col][ks] = *reinterpret_cast<const bf16x8 *>(head + at + 64 * ks);
     }
     const bool there = lane < 16 * NC && mine < lk && mine < p.max_k && page >= 0 && page < (int)p.c.pages;
-    OwnKey own = {there ? ((int64_t)page * p.Hkv + kv) * p.c.by_page.d + slot : -1, 0.f};
+    OwnKey own = {there ? number_at(s, kv, p.Hkv, (uint32_t)mine, (uint32_t)page, slot, p.c, p.numbers) : -1, 0.f};
     if (own.at >= 0 && p.before) own.before = p.before[own.at];
     return own;
 }
@@ -518,7 +519,7 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     if (int rc = paged_check(cache, S, D, false)) return rc;
     const int Hkv = cache->k.heads;
     if (q->heads % Hkv || tokens_q * q->heads > kMostTokens) return STA_ERR_SHAPE;
-    if ((__int128)cache->pages * cache->page_size * Hkv > (__int128)1 << 60) return STA_ERR_SHAPE;
+    if (!numbers_fit(*cache, S)) return STA_ERR_SHAPE;
     const int64_t room = room_of(*cache);
     if (max_k > room) max_k = (int)room;
     if (S == 0 || max_k == 0) return STA_OK;
@@ -526,7 +527,7 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     if (((uintptr_t)cu_q | (uintptr_t)lse | (uintptr_t)before | (uintptr_t)weights) & 3) return STA_ERR_SHAPE;
     const WeightsPlan plan = weights_plan(S, Hkv, D, (int64_t)max_q * (q->heads / Hkv), max_k);
     if (plan.workgroups > kMostWorkgroups) return STA_ERR_SHAPE;
-    const uint64_t w_bytes = (uint64_t)cache->pages * cache->page_size * Hkv * sizeof(float), lse_bytes = (uint64_t)tokens_q * q->heads * sizeof(float);
+    const uint64_t w_bytes = number_bytes(*cache, S), lse_bytes = (uint64_t)tokens_q * q->heads * sizeof(float);
     if (rows_meet(*q, 1, tokens_q, D, weights, w_bytes) || meets_pages(*cache, D, weights, w_bytes) || meets_table(*cache, S, nullptr, 0, 0, D, weights, w_bytes) ||
         ranges_meet(weights, w_bytes, lse, lse_bytes) || ranges_meet(weights, w_bytes, cu_q, ((uint64_t)S + 1) * sizeof(int32_t)))
         return STA_ERR_ALIAS;
@@ -537,6 +538,7 @@ extern "C" int sta_paged_weights(const sta_head_rows *q, const float *lse, int64
     p.lse = lse;
     p.cu = cu_q;
     p.c = paged_cache_of(*cache);
+    p.numbers = key_numbers_of(*cache);
     p.before = before;
     p.weights = weights;
     p.decay = decay;

@@ -11,7 +11,8 @@ from .layer_ops import _HeadRows, _bounds, _int32, _lse_ptr, _packed_counts, _pa
 
 class _PagedCache(ctypes.Structure):
     _fields_ = [("k", _HeadRows), ("v", _HeadRows), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int), ("table", ctypes.c_void_p),
-                ("table_row", ctypes.c_int64), ("table_pages", ctypes.c_int), ("used", ctypes.c_void_p)]
+                ("table_row", ctypes.c_int64), ("table_pages", ctypes.c_int), ("used", ctypes.c_void_p),
+                ("numbers_by_sequence", ctypes.c_int)]
 
 
 def _bind(lib):
@@ -37,9 +38,11 @@ def _lib():
 class StaPagedCache:
     """A cache in pages: k, v (device bf16 [pages, page_size, Hkv, D], laid out alike, channels adjacent; strided views such as halves of one tensor or of
     [pages, Hkv, page_size, D] turned around), table (device int32 [S, n]: the pages of every sequence in the order of its keys), used (device int32 [S]: how many
-    keys it has).  The tensors are kept and used as they are: what they hold may change from call to call, other tensors need another cache."""
+    keys it has).  shared: the numbers of the keys (gathered weights, float32 of weights_shape) are every sequence's own, [S, Hkv, room], in place of [pages, Hkv, page_size],
+    beside the rows; pages that stand in the rows of several sequences need that, where numbers are gathered at all.  The tensors are kept and used as they are: what they hold may change from
+    call to call, other tensors need another cache."""
 
-    def __init__(self, k, v, table, used):
+    def __init__(self, k, v, table, used, shared=False):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
             raise ValueError("k and v must be bfloat16 [pages, page_size, Hkv, D]")
         if k.stride() != v.stride():
@@ -60,9 +63,10 @@ class StaPagedCache:
         # a tensor without elements has no address; nothing of it is touched
         self._c = _PagedCache(_HeadRows(k.data_ptr() or 16, page, token, head, heads, STA_BF16), _HeadRows(v.data_ptr() or 16, page, token, head, heads, STA_BF16),
                               self.pages, _int32(self.page_size, "the page size"), table.data_ptr() or 16, table.stride(0), _int32(table.shape[1], "the pages of a row"),
-                              _dev(used, "used") or 16)
+                              _dev(used, "used") or 16, int(bool(shared)))
         # for the extension: where the struct is, and what goes with it
-        self._at = (ctypes.addressof(self._c), self.S, heads, self.D, self.pages, self.page_size)
+        outer, _, inner = self.weights_shape
+        self._at = (ctypes.addressof(self._c), self.S, heads, self.D, outer, inner)
 
     # Read only: calls take the addresses that were looked up above.
     k = property(lambda self: self._tensors[0])
@@ -75,19 +79,28 @@ class StaPagedCache:
         """Keys that a sequence can have."""
         return self.table.shape[1] * self.page_size
 
+    @property
+    def shared(self):
+        return bool(self._c.numbers_by_sequence)
+
+    @property
+    def weights_shape(self):
+        """Of the keys' numbers."""
+        return (self.S, self.Hkv, self.room) if self.shared else (self.pages, self.Hkv, self.page_size)
+
 
 def _weights_ptr(w, cache, name):
-    """Numbers of all keys of the pool: [pages, Hkv, page_size]."""
+    """Numbers of the keys."""
     if w is None:
         return None
-    if w.dtype != torch.float32 or w.shape != (cache.pages, cache.Hkv, cache.page_size):
-        raise ValueError("%s must be float32 [pages, Hkv, page_size]" % name)
+    if w.dtype != torch.float32 or w.shape != cache.weights_shape:
+        raise ValueError("%s must be float32 [%s]" % (name, "S, Hkv, room" if cache.shared else "pages, Hkv, page_size"))
     return _dev(w, name) or 16
 
 
 def sta_paged_append(k, v, cu, cache, max_new, weights=None, stream=None):
     """New rows k, v (bf16 or float32 [tokens, Hkv, D], strided views with adjacent channels) into their pages: cu int32 [S + 1] where the sequences' tokens
-    begin; cache.used counts them already; weights float32 [pages, Hkv, page_size] or None, set to 0 for the new keys; max_new: upper bound of a sequence's tokens."""
+    begin; cache.used counts them already; weights: the keys' numbers, set to 0 for the new keys, or None; max_new: upper bound of a sequence's tokens."""
     if stream is None:
         status = _fast().paged_append(k, v, cu, cache._at, max_new, weights)
         if status is not None:
@@ -142,8 +155,9 @@ def sta_paged_forward(q, o, cu_q, cache, max_q, max_k, causal=True, scale=0.0, l
 
 
 def sta_paged_weights(q, lse, weights, cu_q, cache, max_q, max_k, before=None, decay=1.0, causal=True, scale=0.0, stream=None):
-    """What every key of the cache gathers from these rows, added to decay times before (None: nothing; may be weights): weights float32 [pages, Hkv, page_size];
-    q bf16 [tokens, Hq, D] and lse float32 [Hq, tokens] as sta_paged_forward had and wrote them."""
+    """What every key of the cache gathers from these rows, added to decay times before (None: nothing; may be weights): weights float32 of
+    cache.weights_shape (of pages that several sequences have, the numbers of a shared cache alone mean something); q bf16 [tokens, Hq, D] and lse float32 [Hq, tokens] as
+    sta_paged_forward had and wrote them."""
     if stream is None:
         status = _fast().paged_weights(q, lse, weights, cu_q, cache._at, max_q, max_k, before, decay, causal, scale)
         if status is not None:
@@ -160,7 +174,8 @@ def sta_paged_weights(q, lse, weights, cu_q, cache, max_q, max_k, before=None, d
 
 def sta_paged_evict(cache, weights, into, into_weights, kept, first=0, recent=0, stream=None):
     """Keeps of every sequence and key head kept.shape[2] keys: the first and recent ones, and of the others those of the greatest weights.  Their rows go to the pages of
-    into, another StaPagedCache whose used is written; their weights to into_weights (or None); kept int32 [S, Hkv, keep]: which they were, -1 where there are fewer."""
+    into, another StaPagedCache whose used is written; their weights, of cache.weights_shape, to into_weights, of into.weights_shape (or None); kept int32
+    [S, Hkv, keep]: which they were, -1 where there are fewer."""
     if stream is None:
         status = _fast().paged_evict(cache._at, weights, into._at, into_weights, kept, first, recent)
         if status is not None:
