@@ -194,7 +194,7 @@ struct Run {
     {
         length = ((n + kSelectWaves - 1) / kSelectWaves + 255) & ~255;
         kept = length <= 256 * GROUPS;
-        begin = wave < (n + length - 1) / length ? wave * length : n;
+        begin = (int64_t)wave * length < n ? wave * length : n;             // (n may be a few thousand below 2^31)
         end = n - begin < length ? n : begin + length;
         const int all = n - p.recent;
         lo = p.first > begin ? p.first : begin;
