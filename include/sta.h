@@ -464,7 +464,8 @@ int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse
  * no query tokens too; other numbers are left as they are.  Of pages that sequences share numbers by sequence alone mean something (sta_paged_cache).
  * max_q, max_k: host, upper bounds; query tokens beyond max_q give nothing.
  * Scores, exponents and sums in fp32; no atomics: repeated calls give identical bits (by page, of pages that stand once in the table).  NaN in a row or key that meet makes NaN of that key's number.
- * Supported: as sta_paged_forward; fewer than 2^24 workgroups, of which every sequence and key head has one for up to 256 keys of max_k (for 64 in small launches).
+ * Supported: as sta_paged_forward; fewer than 2^24 workgroups, of which every sequence and key head has one for up to 256 keys of max_k (for fewer only
+ * where the launch has room for that).
  */
 int sta_paged_weights(const sta_head_rows *q, const float *lse, int64_t tokens_q, const int32_t *cu_q, const sta_paged_cache *cache, int S, int max_q, int max_k,
                       int D, int causal, float scale, const float *before, float decay, float *weights, void *hip_stream);

@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256, 2) void sta_paged_weights_rounds_kernel(Weight
 //   eight of 64 on 1300, 40/5 x 128 (240 | 440 | 840)  18.8 | 18.1 | 24.6       50 on 30,000, 8/1 x 128 (118 | 235 | 469)  15.2 | 11.3 | 13.0
 // With 64 channels, where a stage is half the work, two waves by two groups with stages of 64 rows are the better ones for more than 512 rows, whatever the launch: us, four | two along the keys,
 //   512 on 20,001, 32/8  76 | 61       2048 on 8192, 16/16  58 | 50       2048 on 30,000, 8/8  90 | 83       four of 2048, 16/16  56 | 50       four of 1000 on 4000, 16/16  50 | 49
-//   and not for fewer: eight of 64 on 1300, 12/12  8.2 | 10.4; sixteen of 500 on 2048, 16/16  54.5 | 55.3       (stages of 32 rows: four of 200 on 3000, 40/8  29.5, 28.1 with 64; 1, 5 and 33 on 65 to 578, 16/16  4.3, 4.8;
+//   (as far as a launch has workgroups for tiles of 128 keys) and not for fewer: eight of 64 on 1300, 12/12  8.2 | 10.4; sixteen of 500 on 2048, 16/16  54.5 | 55.3       (stages of 32 rows: four of 200 on 3000, 40/8  29.5, 28.1 with 64; 1, 5 and 33 on 65 to 578, 16/16  4.3, 4.8;
 //   with 128 channels four of 200 38.6, 42)
 struct WeightsPlan {
     int few;                            // blocks of 16 rows, 0: stages
@@ -480,7 +480,7 @@ WeightsPlan weights_plan(int S, int Hkv, int D, int64_t rows, int max_k)
     plan.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     plan.along = plan.few || tiles(256) * heads >= 2 * cus ? 4 : tiles(128) * heads >= (rows <= 512 ? 3 * cus / 4 : 2 * cus) ? 2 : 1;
     plan.deep = D == 64 && rows > 512;
-    if (plan.deep && plan.along == 4) plan.along = 2;
+    if (plan.deep && plan.along == 4 && tiles(128) * heads <= kMostWorkgroups) plan.along = 2;
     plan.tiles = tiles(64 * plan.along);
     plan.workgroups = plan.tiles * heads;
     return plan;
