@@ -416,7 +416,9 @@ int sta_packed_backward(const sta_head_rows *q, const sta_head_rows *k, const st
  * A cache of keys and values in pages.  k and v: bf16 [pages, page_size, Hkv, D], laid out alike; of sta_head_rows `batch` is from page to page and
  * `token` from slot to slot.  Sequence s has used[s] keys; key j of it is slot j % page_size of page table[s * table_row + j / page_size].  Any page_size
  * from 1 on; multiples of 8 (head dimension 128: of 4) are read fastest.  A page may stand in the rows of several sequences (a common beginning).
- * table: device int32, S rows of table_pages entries; used: device int32 [S].  Lengths are cut to what a row of the table has places for.  Entries for keys that are
+ * table: device int32, S rows of table_pages entries; used: device int32 [S].  Lengths are to be at most what a row of the table has
+ * places for, table_pages * page_size.  Beyond that nothing is touched that is not there, but the calls disagree: sta_paged_append goes by the length as given and leaves out the tokens without a
+ * place, the others cut the length first, so that the same tokens count as the last ones of what is left and see keys as such.  Entries for keys that are
  * not used are not looked at; entries of used keys that are no pages are read as some page (of what is written there nothing is written).
  * Numbers of keys (the attention weights that they have gathered, below), float32, key j of sequence s and key head n: with numbers_by_sequence 0 an array [pages, Hkv, page_size], where
  * the key's row lies, at (page, n, slot); with 1 an array [S, Hkv, table_pages * page_size], at (s, n, j).  Pages that stand more than once in the table need the latter: the former has one

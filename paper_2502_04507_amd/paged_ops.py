@@ -38,7 +38,7 @@ def _lib():
 class StaPagedCache:
     """A cache in pages: k, v (device bf16 [pages, page_size, Hkv, D], laid out alike, channels adjacent; strided views such as halves of one tensor or of
     [pages, Hkv, page_size, D] turned around), table (device int32 [S, n]: the pages of every sequence in the order of its keys), used (device int32 [S]: how many
-    keys it has).  shared: the numbers of the keys (gathered weights, float32 of weights_shape) are every sequence's own, [S, Hkv, room], in place of [pages, Hkv, page_size],
+    keys it has, at most `room`).  shared: the numbers of the keys (gathered weights, float32 of weights_shape) are every sequence's own, [S, Hkv, room], in place of [pages, Hkv, page_size],
     beside the rows; pages that stand in the rows of several sequences need that, where numbers are gathered at all.  The tensors are kept and used as they are: what they hold may change from
     call to call, other tensors need another cache."""
 

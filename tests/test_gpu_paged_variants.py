@@ -71,3 +71,28 @@ def test_a_scale_of_the_callers(shape, D, scale):
     sta.sta_paged_forward(q.to(DEV), o2, *args, scale=scale, lse=lse.clone(), workspace=torch.empty(max(n, 16), dtype=torch.uint8, device=DEV), stream=stream)
     sta.sta_paged_weights(q.to(DEV), lse, w2, *args, scale=scale, stream=stream)
     assert same(o, o2) and same(w, w2)
+
+
+def test_a_step_beyond_the_table():
+    """Six tokens, two of which the table has no place for: the rows of the first four are keys, and the attention and the weights take the six for the last of the keys there are."""
+    Hq, Hkv, D, page, room = 4, 2, 64, 16, 48
+    cache = Cache(Hkv, D, page, [room], seed=41, room=3)
+    x, q = randn((6, 2 * Hkv, D), 42).to(DEV), randn((6, Hq, D), 43).to(DEV)
+    cache.lengths.fill_(room + 2)
+    sta.sta_paged_append(x[:, :Hkv], x[:, Hkv:], ints([0, 6]), cache.sta, 6)
+    for t, new in ((cache.k[0], x[:, :Hkv]), (cache.v[0], x[:, Hkv:])):
+        t[room - 4:] = new[:4].cpu()
+    at = [cache.place(0, j) for j in range(room)]
+    for t, rows in zip(cache.pool, (cache.k[0], cache.v[0])):
+        assert same(torch.stack([t[p, s] for p, s in at]).cpu(), rows)
+    beyond, within = [], []
+    for out in (beyond, within):
+        o, lse = forward(q, cache, [6], lse=True, max_k=room + 2)
+        w = torch.zeros((cache.pages, Hkv, page), device=DEV)
+        sta.sta_paged_weights(q, lse, w, ints([0, 6]), cache.sta, 6, room + 2)
+        out += [o, lse, w]
+        cache.lengths.fill_(room)
+    assert all(same(a, b) for a, b in zip(beyond, within))
+    want = lu.attention(q.cpu().double(), cache.k[0].double(), cache.v[0].double(), True, D ** -0.5)
+    b_o, _, _ = bounds(q.cpu().double(), cache.k[0].double(), cache.v[0].double(), True, D ** -0.5, want[1])
+    close(beyond[0], want[0], b_o, "beyond")
