@@ -450,7 +450,8 @@ int sta_paged_append(const sta_head_rows *k, const sta_head_rows *v, int64_t tok
 
 /*
  * sta_packed_forward with the keys in pages: chunks of new tokens (whose rows are in the cache by then) and single tokens against what is used.  With lq query
- * tokens and used[s] keys, causal tokens see the keys j <= i + used[s] - lq.  Everything else is as there (launches may be cut otherwise).  The same keys give the same
+ * tokens and used[s] keys, causal tokens see the keys j <= i + used[s] - lq.  Everything else is as there (launches may be cut otherwise; where
+ * they are cut along the keys, where a part ends follows from the lengths of all sequences, and so do the last bits of a sequence's result).  The same keys give the same
  * bits wherever their pages lie and however large they are.
  */
 size_t sta_paged_workspace_bytes(int Hq, int Hkv, int D, int S, int64_t tokens_q, int max_q, int max_k);

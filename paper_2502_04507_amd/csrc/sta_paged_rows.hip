@@ -4,8 +4,10 @@
 //                          channels from float32 24.4 us, 6.2 TB/s.
 // sta_paged_select_kernel  a workgroup for each sequence and key head finds the smallest weight that stays, twelve, ten and ten bits of its place in the order of
 //                          numbers at a time, by counting how many have which; then writes down in order which keys stay.  Bound by the instructions and LDS of the one CU that a head has:
-//                          8 heads of 32,768 keys 22 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 3.5 the others, 2.5 to count and 5 to write down).
-// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 78 us, 5.0 TB/s
+//                          8 heads of 32,768 keys 23 us (2.5 to begin, 5 to bring the numbers, 4.5 the first digit, 3.5 the others, 2.5 to count and 5 to write down).  The
+//                          counts of a thread's bins, 12 bytes, are in scratch, which is looked at by one thread for each digit.  More than 32,768 keys are looked up at every step:
+//                          32,769 keys 11 us more, 131,072 80.
+// sta_paged_move_kernel    takes the rows that stay, and their weights, to their new places.  Bound by memory: 24 sequences, 8 heads of 128 channels, 2048 rows each, 79 us, 5.0 TB/s
 //                          (82 with stores through the caches).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -537,7 +539,8 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     auto launch = [&](auto by) {
         constexpr bool BY = decltype(by)::value;
-        // up to 8192 keys two workgroups fit a CU, up to 32,768 one
+        // Up to 8192 keys two workgroups fit a CU, up to 32,768 one.  By the table's room, as the lengths stand on the device: short sequences in wide tables take 0 to 4 % longer (128 sequences
+        // of 500 keys, 8 heads of 64, to 100 keys 28.0 and 29.2 us; 24 of 8000 to 500 25.2 both).
         hipError_t e = p.from.room <= 8 * kSelect ? sta::launch_kernel(sta_paged_select_kernel<2, BY>, dim3((uint32_t)items), dim3(kSelect), stream, p)
                                                   : sta::launch_kernel(sta_paged_select_kernel<8, BY>, dim3((uint32_t)items), dim3(kSelect), stream, p);
         if (e != hipSuccess || keep == 0 || !pools || here) return e;
