@@ -462,7 +462,8 @@ int sta_paged_forward(const sta_head_rows *q, const sta_head_rows *o, float *lse
  * The attention weight that the keys of a cache in pages gather from the rows of a call: for every key j of a sequence and key head n
  *     weights_j = decay * before_j + sum over the query tokens i that see j, and the query heads of n, of exp(scale q_i . k_j - lse_i),
  * the sums of the columns of the attention's probabilities.  q, cu_q, causal, scale: as sta_paged_forward; lse: float32 [Hq, tokens_q] as it wrote it (a call on the
- * last rows of a prompt alone gives what those look at).  Rows without keys (lse -infinity) give nothing.  before, weights: the keys' numbers;
+ * last rows of a prompt alone gives what those look at).  Rows without keys give nothing, nor does a row whose
+ * lse is -infinity as far as its scores are numbers.  before, weights: the keys' numbers;
  * before may be weights itself, or NULL (nothing); decay 0: it is not looked at; decay has to be finite.  Written for every key j < max_k of a sequence, with
  * no query tokens too; other numbers are left as they are.  Of pages that sequences share numbers by sequence alone mean something (sta_paged_cache).
  * max_q, max_k: host, upper bounds; query tokens beyond max_q give nothing.

@@ -499,7 +499,8 @@ extern "C" int sta_paged_evict(const sta_paged_cache *cache, const float *weight
     const uint64_t kept_bytes = (uint64_t)items * keep * sizeof(int32_t);
     if (rows_overlap(into->k, into->v, (int)into->pages, into->page_size, D) || pools_meet(*cache, *into, D)) return STA_ERR_ALIAS;
     // by page a number moves with its row, to where none is read; by sequence the numbers of a row of one array would move to where others are still to be read
-    const bool one = into_weights == weights && cache->pages == into->pages && cache->page_size == into->page_size && !cache->numbers_by_sequence && !into->numbers_by_sequence;
+    const bool one = into_weights == weights && cache->pages == into->pages && cache->page_size == into->page_size && same_rows(cache->k, into->k) && same_rows(cache->v, into->v) &&
+                     !cache->numbers_by_sequence && !into->numbers_by_sequence;
     if (!one && ranges_meet(weights, w_bytes, into_weights, to_bytes)) return STA_ERR_ALIAS;
     const struct { const void *at; uint64_t bytes; } written[3] = {{into_weights, to_bytes}, {kept, kept_bytes}, {into->used, used_bytes(S)}};
     for (int i = 0; i < 3; ++i) {

@@ -1,7 +1,7 @@
 """Sizes at which launches of the operators on a cache in pages end: host side, nothing is launched (what is not refused for its size has an argument that is refused next)."""
 import pytest
 
-from tests.test_paged_refusals import ALIAS, M, SHAPE, both, rows, weights
+from tests.test_paged_refusals import ALIAS, M, SHAPE, both, evict, into, pool, rows, weights
 
 S20 = 1 << 20
 
@@ -26,3 +26,10 @@ def test_weights_of_up_to_2_to_the_24_groups_of_256_keys(D, max_q):
     assert many(S20 * 2, max_q, D) == SHAPE
     assert many(S20, max_q, D) == ALIAS
     assert many(S20 * 8 - 1, max_q, D, width=16) == ALIAS and many(S20 * 8, max_q, D, width=16) == SHAPE
+
+
+def test_numbers_beside_the_pages_of_two_pools():
+    """One array may be the numbers of both caches where the pool is the same; page 3 of another pool as large would write the number that is read of page 3 of this one."""
+    assert evict(into=into(pages=1000), into_weights=700 * M) == ALIAS
+    assert evict(into=into(k=pool(200 * M), pages=1000), into_weights=700 * M) == ALIAS                 # keys in the same, values in another
+    assert evict(into=into(k=pool(200 * M), v=pool(300 * M), pages=500), into_weights=700 * M) == ALIAS  # half of the same
