@@ -7,6 +7,7 @@ import paper_2502_04507_amd as sta
 from tests import paged_util as pu
 from tests.paged_util import BF, DEV, Cache, forward, ints, same, starts
 from tests.test_gpu_packed import randn
+from tests.test_gpu_paged_edges import Step
 from tests.test_gpu_paged_weights import gathered
 
 pytestmark = pytest.mark.gpu
@@ -147,3 +148,37 @@ def test_a_run_of_all_of_them(page):
             row = own[now].table[s].long()
             assert torch.equal(numbers[0][now][row].transpose(0, 1).flatten(1)[:, :n], numbers[1][now][s, :, :n]), (step, s)
     assert not torch.equal(numbers[1][0][0, :, :common * page], numbers[1][0][1, :, :common * page])       # of the shared pages, each its own
+
+
+class Shared(Step):
+    """The same step with the numbers by sequence."""
+
+    def __init__(self, seed):
+        super().__init__(seed)
+        self.cache, self.into = (sta.StaPagedCache(c.k, c.v, c.table, c.used, shared=True) for c in (self.cache, self.into))
+        self.w, self.to_w = (torch.zeros(c.weights_shape, device=DEV) for c in (self.cache, self.into))
+
+
+def test_steps_replayed_from_a_graph():
+    """Captured once and replayed with other lengths and rows, eager steps with the numbers by page and other work between: the same outputs, and the same numbers of the keys."""
+    a, b = Shared(1), Step(1)
+    for x in (a, b):
+        x.fill(3)
+        x.run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run()
+    b.run()                                                     # capturing runs nothing: as many steps of either from here on
+    graph.replay()
+    for seed in (4, 9, 5, 2, 9):
+        a.fill(seed)
+        b.fill(seed)
+        graph.replay()
+        b.run()
+        torch.cuda.synchronize()
+        for x, y in zip((*a.pools, a.o, a.lse, a.into.k, a.into.v, a.into.used, a.kept), (*b.pools, b.o, b.lse, b.into.k, b.into.v, b.into.used, b.kept)):
+            assert torch.equal(x, y), seed
+        for c, x, y in ((a.cache, a.w, b.w), (a.into, a.to_w, b.to_w)):
+            for s, n in enumerate(c.used.tolist()):
+                assert torch.equal(x[s, :, :n], y[c.table[s].long()].transpose(0, 1).flatten(1)[:, :n]), (seed, s)
+        assert bool(torch.isfinite(torch.randn((1 << 20,), device=DEV).sum()))
