@@ -7,7 +7,7 @@
 // Roundings.  Products of bf16 numbers are exact, scores, exponents and sums fp32: four values of a lane are a tree, those of 512 rows go into one sum, and those into the key's.
 //
 // sta_paged_few_weights_kernel   at most 16 or 32 rows per sequence and key head: rows and keys straight from memory to registers, no LDS.  Bound by memory: 48 tokens of 32 heads over 8
-//                                on 1 to 16,384 keys 184 us, 4.7 TB/s (155 where nothing is written, though that is 12 of 870 MB; a kernel that only reads as much 130).  Numbers before are asked for behind the keys'
+//                                on 1 to 16,384 keys 184 us, 4.7 TB/s (155 where nothing is written, though that is 12 of 870 MB; a kernel that only reads as much 125).  Numbers before are asked for behind the keys'
 //                                rows and in a branch of their own: before them 190, inside the branch that finds their place 188, behind the sums 190.  Sums of 16 tiles held back and written
 //                                together by workgroups that stay: 180, but 53 in place of 45 with 64 channels.
 // sta_paged_weights_kernel       (and sta_paged_weights_rounds_kernel, its tiles in another order, the last ones halved)
